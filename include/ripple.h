@@ -379,6 +379,178 @@ ripple_status ripple_decode_attn_noalloc(const ripple_decode_desc *desc, const v
                                          int32_t *dev_status, void *stream);
 
 /* ------------------------------------------------------------------------ */
+/* A paged cache: appending with the position rotation, decode attention, and */
+/* what the model answered. The paper decodes from contiguous caches (Sec.    */
+/* 4.1); these calls are for serving programs that batch sequences of         */
+/* different lengths and hand the cache out in pages.                         */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * One layer's paged cache. Row r (0-based) of sequence b, KV head h, lies in page
+ * block_table[b][r / page_size], slot r % page_size:
+ *   k_pages + page * page_stride + h * head_stride + slot * row_stride,
+ * d consecutive elements; v_pages likewise. Strides are in elements and multiples
+ * of 16 bytes; the three together must not make places overlap. All three 0 mean
+ * dense pools [n_pages][Hkv][page_size][d].
+ * block_table  device int32 [B][max_pages]. Only the entries of the pages that hold
+ *              a sequence's rows are read; the others may be anything. An entry
+ *              read that is outside [0, n_pages) is reported as RIPPLE_EBOUNDS.
+ * lens         device int32 [B]: cache rows of every sequence, the call's own new
+ *              tokens included. A sequence with lens[b] <= 0 is idle (a batch
+ *              padded to a captured size): nothing is stored for it, and it has
+ *              an empty attention. Lengths beyond max_pages * page_size are
+ *              reported as RIPPLE_EFULL.
+ */
+typedef struct {
+  int32_t batch;      /* B >= 1: sequences, rows of the block table */
+  int32_t n_kv_heads; /* Hkv >= 1 */
+  int32_t head_dim;   /* d: 64 or 128 */
+  int32_t page_size;  /* cache rows per page: a power of two, 1..1024 */
+  int32_t n_pages;    /* pages of each pool, >= 1 */
+  int32_t max_pages;  /* entries per sequence of the block table, >= 1 */
+  int32_t dtype;      /* ripple_dtype of the pages, q, k and v */
+  int64_t page_stride, head_stride, row_stride;
+} ripple_paged_desc;
+
+/* Where token i of sequence b, head h starts in a tensor of tokens, in elements
+ * (multiples of 16 bytes): b * seq_stride + i * token_stride + h * head_stride. */
+typedef struct {
+  int64_t seq_stride, token_stride, head_stride;
+} ripple_token_strides;
+
+/* The position rotation: with theta_j = pos * inv_freq_host[j], j < rot_dim / 2, the
+ * pair (x, y) of a head's elements (j, j + rot_dim / 2), or (2j, 2j + 1) where
+ * interleaved, becomes (x cos theta_j - y sin theta_j, y cos theta_j + x sin theta_j);
+ * elements rot_dim.. are kept. */
+typedef struct {
+  int32_t rot_dim;             /* a multiple of 16, 16..d */
+  int32_t interleaved;         /* 0 or 1 */
+  const double *inv_freq_host; /* host [rot_dim / 2], |.| <= 1024; read during the call */
+} ripple_rope;
+
+/*
+ * ripple_paged_append -- the keys and values of new tokens into a paged cache, the
+ * keys (and the tokens' queries, if given) rotated to their positions on the way.
+ *
+ * Tokens: with seq_starts == NULL every sequence has n_tokens / B tokens (n_tokens
+ * a multiple of B), token i of sequence b at (b, i) of the strides. Otherwise
+ * seq_starts is device int32 [B + 1], ascending: tokens seq_starts[b] ..
+ * seq_starts[b + 1] - 1 of the token dimension are sequence b's, token t lies at
+ * t * token_stride (seq_stride is not used), and tokens outside
+ * [seq_starts[0], seq_starts[B]), up to n_tokens, are left alone, their places in
+ * q_out too. With n_b tokens for sequence b, its token i goes to cache row
+ * lens[b] - n_b + i: lens counts them already, so that the same array serves the
+ * attention that follows. Rows are stored rounded to nearest (even) in dtype;
+ * rotated values are computed in fp32 from angles that are exact to 2^-32 turns at
+ * every int32 position.
+ *
+ * rope       NULL: nothing is rotated (for rows that are rotated already, such as
+ *            those ripple_compress_layer keeps).
+ * q, q_out   [tokens][n_q_heads][d] by their strides, or both NULL. q_out == q
+ *            with the same strides rotates in place. Queries of idle sequences are
+ *            rotated like the others.
+ * k, v       [tokens][Hkv][d] by their strides
+ * positions  device int32 [n_tokens] in token order, or NULL: a token's position is
+ *            its cache row. A compressed cache has fewer rows than positions.
+ * A page that receives tokens belongs to one sequence only (pages shared for
+ * reading are fine).
+ * Tokens whose row is negative while lens[b] > 0 (more tokens than rows) or whose
+ * page entry is out of range are not stored and reported as RIPPLE_EBOUNDS, rows at or
+ * behind max_pages * page_size as RIPPLE_EFULL.
+ * n_tokens == 0 does nothing. One launch. The call may be captured in a CUDA graph.
+ * Errors: RIPPLE_EINVAL (bad desc, strides or rope, NULL or not 16-byte aligned
+ * pointers), RIPPLE_ECUDA.
+ */
+ripple_status ripple_paged_append(const ripple_paged_desc *desc, const ripple_rope *rope,
+                                  int32_t n_tokens, const int32_t *seq_starts,
+                                  int32_t n_q_heads, const void *q,
+                                  const ripple_token_strides *q_strides, void *q_out,
+                                  const ripple_token_strides *q_out_strides, const void *k,
+                                  const ripple_token_strides *k_strides, const void *v,
+                                  const ripple_token_strides *v_strides,
+                                  const int32_t *positions, void *k_pages, void *v_pages,
+                                  const int32_t *block_table, const int32_t *lens,
+                                  int32_t *dev_status, void *stream);
+
+/* Device workspace bytes ripple_paged_decode_attn needs on the current device; the
+ * same for every length. Never fewer for a larger batch, more heads or a larger
+ * block table: a workspace made for a program's largest step serves all. */
+ripple_status ripple_paged_decode_workspace_bytes(const ripple_paged_desc *desc,
+                                                  int32_t n_q_heads, size_t *bytes_host);
+
+/*
+ * ripple_paged_decode_attn -- attention of one new token per sequence over a paged
+ * cache: for every sequence b and query head q, KV head h = q / G, G = n_q_heads / Hkv,
+ *   out[b][q] = sum over r < lens[b] of softmax_r(scale * q[b][q] . k[b][h][r]) * v[b][h][r],
+ *   lse[b][q] = log of the sum over r of exp(scale * q[b][q] . k[b][h][r]).
+ * The token's own row is appended before (ripple_paged_append). A sequence without
+ * rows, or whose scores are all -infinity, has out = 0 and lse = -infinity, so that the
+ * outputs of several caches can be joined by their lse.
+ *
+ * n_q_heads  a multiple of Hkv, G <= 16
+ * scale      logit scale; 0 means 1 / sqrt(d)
+ * q          [B][n_q_heads][d] by q_strides (its token_stride is not used; NULL: dense)
+ * out        device fp32 [B][n_q_heads][d]
+ * lse        device fp32 [B][n_q_heads], or NULL
+ * workspace  device scratch, 256-byte aligned; its contents need no initialisation.
+ *            Calls that share a workspace must be ordered on the GPU.
+ * Rows whose page entry is out of range are left out of the attention (and reported as
+ * RIPPLE_EBOUNDS), and so are rows behind max_pages * page_size (RIPPLE_EFULL).
+ * Arithmetic as in ripple_decode_attn (fp32; results do not depend on the run). The
+ * call may be captured in a CUDA graph: lengths and the table are read on the device.
+ * Errors: RIPPLE_EINVAL, RIPPLE_EWORKSPACE, RIPPLE_ECUDA.
+ */
+ripple_status ripple_paged_decode_attn(const ripple_paged_desc *desc, int32_t n_q_heads,
+                                       float scale, const void *q,
+                                       const ripple_token_strides *q_strides,
+                                       const void *k_pages, const void *v_pages,
+                                       const int32_t *block_table, const int32_t *lens,
+                                       float *out, float *lse, void *workspace,
+                                       size_t workspace_bytes, int32_t *dev_status,
+                                       void *stream);
+
+/* Largest number of alternatives ripple_token_logprobs gives. */
+#define RIPPLE_MAX_TOP 32
+
+/*
+ * ripple_token_logprobs -- log probabilities of given tokens, the entropy of their
+ * distributions and the most likely alternatives, from logits over the vocabulary.
+ *
+ * For every row i, with P_i = softmax of scale * logits[i]:
+ *   logprob_out[i] = log P_i(tokens[i]),   entropy_out[i] = - sum_v P_i(v) log P_i(v),
+ *   lse_out[i]     = log sum_v exp(scale * logits[i][v]),
+ *   top_idx_out[i], top_logprob_out[i]: the n_top largest logits in descending order
+ *   (equal ones: lower index first), and their log probabilities.
+ *
+ * n_rows      >= 0 (0 does nothing)
+ * vocab       1 .. 2^30, any; row_stride >= 0 elements from row to row
+ * dtype       ripple_dtype of the logits; -infinity masks a token. A row that holds a
+ *             NaN, +infinity or nothing but -infinity has no distribution: its outputs
+ *             are NaN (its lse is -infinity if every logit is), its indices any tokens, each once.
+ * scale       inverse temperature, > 0, finite; 0 means 1
+ * n_top       0 .. min(RIPPLE_MAX_TOP, vocab)
+ * tokens      device int32 [n_rows], or NULL (logprob_out NULL as well). A negative
+ *             token is padding: log probability 0. One >= vocab is reported as
+ *             RIPPLE_EBOUNDS and has NaN.
+ * logprob_out, entropy_out, lse_out  device fp32 [n_rows]; each may be NULL
+ * top_idx_out, top_logprob_out       device int32 and fp32 [n_rows][n_top], NULL where
+ *             n_top is 0; top_logprob_out may be NULL
+ * Logits are aligned to their element, outputs to 4 bytes. The logits are read from
+ * HBM once. Sums are fp32, of the terms relative to the row's largest logit, whose own
+ * term is left out: with S' the sum of the others, log P = scale (x - max) -
+ * log1p(S'), so that log probabilities near 0 and small entropies keep their relative
+ * precision. Results do not depend on the run. One launch, no workspace. The call may
+ * be captured in a CUDA graph.
+ * Errors: RIPPLE_EINVAL, RIPPLE_ECUDA.
+ */
+ripple_status ripple_token_logprobs(int32_t n_rows, int32_t vocab, int64_t row_stride,
+                                    int32_t dtype, float scale, int32_t n_top,
+                                    const void *logits, const int32_t *tokens,
+                                    float *logprob_out, float *entropy_out, float *lse_out,
+                                    int32_t *top_idx_out, float *top_logprob_out,
+                                    int32_t *dev_status, void *stream);
+
+/* ------------------------------------------------------------------------ */
 /* Sensitivity profiling (offline; Sec. 4.3, Algorithm 1 "Sensitivity        */
 /* Profiling"). The model forwards that turn a perturbed cache into output    */
 /* logits belong to the caller; these calls cover the perturbation (Eq. 6),   */

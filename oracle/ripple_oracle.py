@@ -332,3 +332,46 @@ def sensitivity_profile(d):
     for i in range(d.shape[0]):
         s = s + d[i]
     return s / d.shape[0]
+
+
+# ---------------------------------------------------------------------------
+# Around the decode step of a serving program (no paper counterpart): the position
+# rotation of queries and keys, and what the model answered.
+# ---------------------------------------------------------------------------
+
+
+def rotate(x, pos, inv_freq, interleaved=False):
+    """The rows x [n][..][d] turned to their positions pos [n]: with theta_j =
+    pos * inv_freq[j], the pair (j, j + rot/2), or (2j, 2j + 1) where interleaved, of
+    the first rot = 2 len(inv_freq) elements is rotated by theta_j; the rest is kept."""
+    x = np.array(x, np.float64)
+    half = len(inv_freq)
+    theta = np.multiply.outer(np.asarray(pos, np.float64), np.asarray(inv_freq, np.float64))
+    theta = theta.reshape(theta.shape[:1] + (1,) * (x.ndim - 2) + theta.shape[1:])
+    first = np.arange(half) * 2 if interleaved else np.arange(half)
+    second = first + (1 if interleaved else half)
+    a, b = x[..., first].copy(), x[..., second].copy()
+    x[..., first] = a * np.cos(theta) - b * np.sin(theta)
+    x[..., second] = b * np.cos(theta) + a * np.sin(theta)
+    return x
+
+
+def attention_lse(q, k_rows, scale):
+    """log sum_j exp(scale q_g . k_j) per query row g, [G]."""
+    x = (q @ k_rows.T) * scale
+    m = x.max(axis=1)
+    return m + np.log(np.exp(x - m[:, None]).sum(axis=1))
+
+
+def token_logprobs(logits, scale=1.0):
+    """(log probabilities [V], entropy) of softmax(scale * logits) of one row; -infinity
+    logits have probability 0 and take no part in the entropy."""
+    lp = log_softmax(np.asarray(logits, np.float64) * scale)
+    p = np.exp(lp)
+    return lp, float(-(p[p > 0] * lp[p > 0]).sum())
+
+
+def top_tokens(logits, n):
+    """Indices of the n largest logits, descending, equal ones by index."""
+    x = np.asarray(logits, np.float64)
+    return np.lexsort((np.arange(len(x)), -x))[:n]

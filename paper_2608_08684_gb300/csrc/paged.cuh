@@ -1,0 +1,75 @@
+// The paged cache as the kernels see it (ripple_paged_desc with its pointers),
+// and its host-side checks.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "ripple.h"
+
+namespace ripple {
+
+struct PagedGeom {
+  int B, Hkv, D, shift;        // page_size == 1 << shift
+  int n_pages, max_pages;
+  long long page_stride, head_stride, row_stride;  // elements
+};
+
+// Whether the places i * stride (i < count) of the dimensions, each `inner` long
+// elements at the innermost, are disjoint: sorted by stride, every stride reaches past
+// the dimensions within it.
+inline bool disjoint(int n, const long long *stride, const long long *count, long long inner) {
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + n, [&](int a, int b) { return stride[a] < stride[b]; });
+  long long extent = inner;
+  for (int i = 0; i < n; ++i) {
+    const int d = order[i];
+    if (count[d] <= 1) continue;
+    if (stride[d] < extent) return false;
+    extent += stride[d] * (count[d] - 1);
+  }
+  return true;
+}
+
+inline bool aligned16_host(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+// Elements of 16 bytes, or 0 for an unknown type.
+inline int vec_elems(int dtype) {
+  return dtype == RIPPLE_BF16 ? 8 : dtype == RIPPLE_F32 ? 4 : 0;
+}
+
+inline bool paged_geom(const ripple_paged_desc *d, PagedGeom *g) {
+  if (d == nullptr) return false;
+  const int vec = vec_elems(d->dtype);
+  if (vec == 0 || d->batch < 1 || d->n_kv_heads < 1 || d->n_pages < 1 || d->max_pages < 1)
+    return false;
+  if (d->head_dim != 64 && d->head_dim != 128) return false;
+  if (d->page_size < 1 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)) != 0)
+    return false;
+  if ((int64_t)d->batch * d->n_kv_heads > (1 << 24)) return false;
+  if ((int64_t)d->max_pages * d->page_size > 0x7fffffffLL) return false;
+  g->B = d->batch;
+  g->Hkv = d->n_kv_heads;
+  g->D = d->head_dim;
+  g->shift = 0;
+  while ((1 << g->shift) < d->page_size) ++g->shift;
+  g->n_pages = d->n_pages;
+  g->max_pages = d->max_pages;
+  g->row_stride = d->row_stride;
+  g->head_stride = d->head_stride;
+  g->page_stride = d->page_stride;
+  if (d->row_stride == 0 && d->head_stride == 0 && d->page_stride == 0) {
+    g->row_stride = d->head_dim;
+    g->head_stride = (long long)d->page_size * g->row_stride;
+    g->page_stride = d->n_kv_heads * g->head_stride;
+  }
+  const long long stride[3] = {g->row_stride, g->head_stride, g->page_stride};
+  const long long count[3] = {d->page_size, d->n_kv_heads, d->n_pages};
+  for (int i = 0; i < 3; ++i)
+    if (stride[i] < 0 || stride[i] > (1LL << 48) / count[i] || stride[i] % vec != 0) return false;
+  return disjoint(3, stride, count, d->head_dim);
+}
+
+}  // namespace ripple

@@ -58,6 +58,24 @@ class CacheDesc(ctypes.Structure):
                 ("dtype", ctypes.c_int32)]
 
 
+class PagedDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("page_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+class TokenStrides(ctypes.Structure):
+    _fields_ = [("seq_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("inv_freq_host", ctypes.POINTER(ctypes.c_double))]
+
+
 _p = ctypes.c_void_p
 _i32, _i64, _f64, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
 
@@ -105,6 +123,18 @@ _lib.ripple_decode_attn_noalloc.argtypes = [ctypes.POINTER(DecodeDesc), _p, _p, 
                                             ctypes.POINTER(_p), ctypes.POINTER(_p),
                                             ctypes.POINTER(_i32), _p, _p, _p, _p]
 _lib.ripple_decode_attn_noalloc.restype = _i32
+_lib.ripple_paged_append.argtypes = [_p, _p, _i32, _p, _i32, _p, _p, _p, _p, _p, _p, _p, _p, _p,
+                                     _p, _p, _p, _p, _p, _p]
+_lib.ripple_paged_append.restype = _i32
+_lib.ripple_paged_decode_workspace_bytes.argtypes = [ctypes.POINTER(PagedDesc), _i32,
+                                                     ctypes.POINTER(_sz)]
+_lib.ripple_paged_decode_workspace_bytes.restype = _i32
+_lib.ripple_paged_decode_attn.argtypes = [_p, _i32, ctypes.c_float, _p, _p, _p, _p, _p, _p, _p, _p,
+                                          _p, _sz, _p, _p]
+_lib.ripple_paged_decode_attn.restype = _i32
+_lib.ripple_token_logprobs.argtypes = [_i32, _i32, _i64, _i32, ctypes.c_float, _i32, _p, _p, _p, _p,
+                                       _p, _p, _p, _p, _p]
+_lib.ripple_token_logprobs.restype = _i32
 _lib.ripple_perturb_values.argtypes = [ctypes.POINTER(CacheDesc), _p, _p, ctypes.c_float, _i32,
                                        _i32, _p, _p]
 _lib.ripple_perturb_values.restype = _i32
@@ -147,9 +177,13 @@ def _ptr(t):
 try:
     from torch._C import _cuda_getCurrentRawStream, _cuda_getDevice
 except ImportError:
+    _current_device = torch.cuda.current_device
+
     def _current_stream():
         return torch.cuda.current_stream().cuda_stream
 else:
+    _current_device = _cuda_getDevice
+
     def _current_stream():
         return _cuda_getCurrentRawStream(_cuda_getDevice())
 
@@ -336,6 +370,190 @@ def ripple_decode_attn_noalloc(desc: DecodeDesc, q, k_new, v_new, tables: Decode
                                            tables.k, tables.v, tables.caps, _ptr(lens),
                                            _ptr(out), _ptr(dev_status), _stream(stream)),
            "ripple_decode_attn_noalloc")
+
+
+# ------------------------------------------------------------- paged caches
+
+MAX_TOP = 32
+
+
+def _here(device: int, *tensors):
+    """The call's tensors lie on `device`, and it is the current one (whose current
+    stream the call is given to)."""
+    if _current_device() != device:
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is another")
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"expected a tensor on cuda:{device}")
+
+
+class PagedCache:
+    """One layer's paged cache: pools k_pages, v_pages [n_pages][Hkv][page_size][d] (any
+    strides with the dims of a row consecutive, both alike: a pool laid out
+    [n_pages][page_size][Hkv][d] is passed transposed) and block_table int32
+    [B][max_pages]. Holds pointers and sizes; built once."""
+
+    def __init__(self, k_pages, v_pages, block_table):
+        if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or \
+                k_pages.stride() != v_pages.stride() or k_pages.dtype != v_pages.dtype:
+            raise ValueError("k_pages and v_pages must be [n_pages][Hkv][page_size][d], alike")
+        if k_pages.stride(3) != 1:
+            raise ValueError("the dims of a cache row must be consecutive")
+        if block_table.dim() != 2 or block_table.dtype != torch.int32:
+            raise ValueError("block_table must be int32 [B][max_pages]")
+        n_pages, H, ps, d = k_pages.shape
+        B, width = block_table.shape
+        self.table = _ptr(block_table)
+        self.device = k_pages.get_device()
+        if not k_pages.is_cuda or v_pages.get_device() != self.device or \
+                block_table.get_device() != self.device:
+            raise ValueError("expected CUDA tensors on one device")
+        self.batch, self.n_kv_heads, self.head_dim, self.dtype = B, H, d, k_pages.dtype
+        self.k, self.v = k_pages.data_ptr(), v_pages.data_ptr()
+        self.desc = PagedDesc(B, H, d, ps, n_pages, width, _DTYPES[k_pages.dtype],
+                              *k_pages.stride()[:3])
+        self._ref = ctypes.byref(self.desc)
+        self._keep = (k_pages, v_pages, block_table)
+
+
+class Rope:
+    """The position rotation of ripple_paged_append: inv_freq[j], the angle per position
+    of pair j (rot_dim / 2 of them); pairs (j, j + rot_dim / 2), or (2j, 2j + 1) if
+    interleaved."""
+
+    def __init__(self, inv_freq, interleaved: bool = False):
+        n = len(inv_freq)
+        self._freq = (_f64 * n)(*[float(x) for x in inv_freq])
+        self.desc = RopeDesc(2 * n, int(interleaved), self._freq)
+        self._ref = ctypes.byref(self.desc)
+
+
+def _tokens(t, heads, cache, ragged):
+    """(pointer, strides, leading sizes) of a tensor of tokens."""
+    shape, st = t.shape, t.stride()
+    if t.dtype != cache.dtype or shape[-2:] != (heads, cache.head_dim) or st[-1] != 1:
+        raise ValueError("tokens must be [..][heads][d] in the cache's dtype, dims consecutive")
+    if len(shape) == 3:
+        lead, strides = shape[:1], (0, st[0], st[1]) if ragged else (st[0], 0, st[1])
+    elif len(shape) == 4 and not ragged:
+        lead, strides = shape[:2], st[:3]
+    else:
+        raise ValueError("tokens must be [B][heads][d] or [B][n][heads][d]; with seq_starts "
+                         "[tokens][heads][d]")
+    if not ragged and lead[0] != cache.batch:
+        raise ValueError("one entry per sequence")
+    return t.data_ptr(), ctypes.byref(TokenStrides(*strides)), lead
+
+
+def ripple_paged_append(cache: PagedCache, lens, k, v, rope: Rope | None = None, positions=None,
+                        seq_starts=None, q=None, q_out=None, dev_status=None, stream=None):
+    """Store new tokens' keys and values in the cache's pages, the keys rotated, and rotate
+    their queries q into q_out (which may be q). k, v: [B][Hkv][d] (one token per sequence),
+    [B][n][Hkv][d], or with seq_starts (int32 [B + 1]) [tokens][Hkv][d]; q, q_out likewise
+    with the query heads; any strides with the dims consecutive. lens (int32 [B]) counts the
+    new tokens; positions: int32, k's leading sizes, or None (a token's cache row)."""
+    ragged = seq_starts is not None
+    kp, ks, lead = _tokens(k, cache.n_kv_heads, cache, ragged)
+    vp, vs, vlead = _tokens(v, cache.n_kv_heads, cache, ragged)
+    if vlead != lead:
+        raise ValueError("k and v must have the same tokens")
+    n = lead.numel()
+    qp = qs = op = os_ = None
+    heads = 0
+    if q is not None:
+        heads = q.shape[-2]
+        qp, qs, qlead = _tokens(q, heads, cache, ragged)
+        if q_out is None:
+            raise ValueError("q needs q_out")
+        op, os_, olead = _tokens(q_out, heads, cache, ragged)
+        if qlead != lead or olead != lead:
+            raise ValueError("q and q_out must have k's tokens")
+    elif q_out is not None:
+        raise ValueError("q_out needs q")
+    if positions is not None and (positions.dtype != torch.int32 or positions.shape != lead):
+        raise ValueError("positions must be int32 with k's leading sizes")
+    if lens.dtype != torch.int32 or lens.numel() != cache.batch:
+        raise ValueError("lens must be int32 [B]")
+    if ragged and (seq_starts.dtype != torch.int32 or seq_starts.numel() != cache.batch + 1):
+        raise ValueError("seq_starts must be int32 [B + 1]")
+    _here(cache.device, lens, k, v, positions, seq_starts, q, q_out, dev_status)
+    st = _lib.ripple_paged_append(cache._ref, rope._ref if rope is not None else None, n,
+                                  _ptr(seq_starts), heads, qp, qs, op, os_, kp, ks, vp, vs,
+                                  _ptr(positions), cache.k, cache.v, cache.table, _ptr(lens),
+                                  _ptr(dev_status), _stream(stream))
+    if st != OK:
+        raise RippleError(st, "ripple_paged_append")
+
+
+def ripple_paged_decode_workspace_bytes(cache: PagedCache, n_q_heads: int) -> int:
+    out = _sz()
+    _check(_lib.ripple_paged_decode_workspace_bytes(cache._ref, int(n_q_heads),
+                                                    ctypes.byref(out)),
+           "ripple_paged_decode_workspace_bytes")
+    return out.value
+
+
+def ripple_paged_decode_attn(cache: PagedCache, q, lens, out, workspace, lse=None,
+                             scale: float = 0.0, dev_status=None, stream=None):
+    """Attention of one token per sequence over the first lens[b] rows of the paged cache:
+    q [B][Hq][d] (any strides with the dims consecutive), out fp32 [B][Hq][d], lse fp32
+    [B][Hq] or None."""
+    shape, st = q.shape, q.stride()
+    if len(shape) != 3 or shape[0] != cache.batch or shape[2] != cache.head_dim or st[2] != 1 or \
+            q.dtype != cache.dtype:
+        raise ValueError("q must be [B][Hq][d] in the cache's dtype, dims consecutive")
+    if out.shape != shape or out.dtype != torch.float32:
+        raise ValueError("out must be fp32 [B][Hq][d]")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != shape[:2]):
+        raise ValueError("lse must be fp32 [B][Hq]")
+    if lens.dtype != torch.int32 or lens.numel() != cache.batch:
+        raise ValueError("lens must be int32 [B]")
+    _here(cache.device, q, lens, out, lse, workspace, dev_status)
+    s = _lib.ripple_paged_decode_attn(cache._ref, shape[1], scale, q.data_ptr(),
+                                      ctypes.byref(TokenStrides(st[0], 0, st[1])), cache.k,
+                                      cache.v, cache.table, _ptr(lens), _ptr(out), _ptr(lse),
+                                      _ptr(workspace),
+                                      workspace.numel() * workspace.element_size(),
+                                      _ptr(dev_status), _stream(stream))
+    if s != OK:
+        raise RippleError(s, "ripple_paged_decode_attn")
+
+
+def ripple_token_logprobs(logits, tokens=None, logprob_out=None, entropy_out=None, lse_out=None,
+                          top_idx=None, top_logprob=None, scale: float = 0.0, dev_status=None,
+                          stream=None):
+    """Log probabilities of tokens (int32 [n]; negative: padding) under softmax(scale *
+    logits), logits [n][V] (any row stride), with the entropy, the log of the sum of the
+    exponentials (fp32 [n] each) and the K largest logits' indices (int32 [n][K]) and log
+    probabilities (fp32 [n][K]); outputs left None are not written."""
+    if logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] > 1:
+        raise ValueError("logits must be [n][V], a row's logits consecutive")
+    n, vocab = logits.shape
+    if (tokens is None) != (logprob_out is None):
+        raise ValueError("tokens and logprob_out go together")
+    if tokens is not None and (tokens.dtype != torch.int32 or tokens.numel() != n):
+        raise ValueError("tokens must be int32 [n]")
+    for t in (logprob_out, entropy_out, lse_out):
+        if t is not None and (t.dtype != torch.float32 or t.numel() != n):
+            raise ValueError("outputs must be fp32 [n]")
+    k = 0
+    if top_idx is not None:
+        k = top_idx.shape[-1]
+        if top_idx.dtype != torch.int32 or top_idx.shape != (n, k):
+            raise ValueError("top_idx must be int32 [n][K]")
+    if top_logprob is not None and (top_logprob.dtype != torch.float32 or
+                                    top_idx is None or top_logprob.shape != top_idx.shape):
+        raise ValueError("top_logprob must be fp32, top_idx's shape")
+    if not logits.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    _here(logits.get_device(), tokens, logprob_out, entropy_out, lse_out, top_idx, top_logprob,
+          dev_status)
+    st = _lib.ripple_token_logprobs(n, vocab, logits.stride(0), _DTYPES[logits.dtype], scale, k,
+                                    logits.data_ptr(), _ptr(tokens), _ptr(logprob_out),
+                                    _ptr(entropy_out), _ptr(lse_out), _ptr(top_idx),
+                                    _ptr(top_logprob), _ptr(dev_status), _stream(stream))
+    if st != OK:
+        raise RippleError(st, "ripple_token_logprobs")
 
 
 # ----------------------------------------------------- sensitivity profiling
