@@ -522,7 +522,7 @@ ripple_status ripple_paged_decode_attn(const ripple_paged_desc *desc, int32_t n_
  *   top_idx_out[i], top_logprob_out[i]: the n_top largest logits in descending order
  *   (equal ones: lower index first), and their log probabilities.
  *
- * n_rows      >= 0 (0 does nothing)
+ * n_rows      0 .. 2^27 (0 does nothing)
  * vocab       1 .. 2^30, any; row_stride >= 0 elements from row to row
  * dtype       ripple_dtype of the logits; -infinity masks a token. A row that holds a
  *             NaN, +infinity or nothing but -infinity has no distribution: its outputs

@@ -129,7 +129,8 @@ def _logprobs(lib, n=4, vocab=100, stride=100, dtype=0, scale=1.0, top=2, logits
 
 def test_logprobs_refuses_bad_arguments(lib):
     E = lib.EINVAL
-    assert _logprobs(lib, n=-1) == E
+    for n in (-1, (1 << 27) + 1):
+        assert _logprobs(lib, n=n) == E
     for vocab in (0, -5, (1 << 30) + 1):
         assert _logprobs(lib, vocab=vocab) == E
     assert _logprobs(lib, stride=-1) == E
