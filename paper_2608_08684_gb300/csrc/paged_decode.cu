@@ -1,36 +1,36 @@
 // ripple_paged_decode_attn: attention of one new token per sequence over a paged cache.
 //
-// Work: the cache rows of every (sequence, KV head) group are cut into tiles of kTileRows
-// rows, and the tiles of all groups, in order, into one run of equal length per CTA (one
-// CTA per SM): whatever the lengths, every SM streams the same number of rows, and no
-// counter hands out work. Lengths are read on the device (graphs are replayed with new
-// ones); each CTA finds its run by a sum over the sequences.
+// Work: the cache rows of every (sequence, KV head) group are cut into blocks of 4 KB (K
+// and V each), and the blocks of all groups, in order, into runs, one CTA of one warp
+// each, eight per SM. Lengths are read on the device (graphs are replayed with new ones);
+// every CTA finds its run by a sum over the sequences. The first runs, one for every
+// place on the GPU, hold most of the blocks, later ones less and less (Runs): SMs differ
+// by a tenth in the bandwidth they get, and the later runs go where a place is free first.
+// (One run of equal length for every warp: 158 us for 64 sequences of 3800 rows, 979 MB,
+// of which the slowest SMs took 144 and the fastest 120.) What a run covers does not
+// depend on where it goes, so results do not either.
 //
-// A CTA's eight warps take the 4 KB blocks (K and V each) of a group's part in turn.
-// Every warp is on its own: it fetches its blocks with asynchronous 16-byte copies into a
-// ring of its own, two blocks ahead, whatever the page size and layout (a lane looks up
-// the page of one row of the block, one block before it is fetched), and keeps its own
-// running maximum and sum. Copies of 16 bytes and not bulk copies, because a block's rows
-// need a layout that ldmatrix reads without bank conflicts, and pages may be one row.
-// Rows behind a length and rows whose page is none are filled with zeros and left out by
-// their place, so that what lies there never counts.
+// A warp is on its own: it fetches its blocks with asynchronous 16-byte copies into a
+// ring, two blocks ahead, whatever the page size and layout (a lane looks up the page of
+// one row of the block, one block before it is fetched), and keeps a running maximum and
+// sum. Copies of 16 bytes and not bulk copies, because a block's rows need a layout that
+// ldmatrix reads without bank conflicts, and pages may be one row. Rows behind a length
+// and rows whose page is none are filled with zeros and left out by their place, so that
+// what lies there never counts.
 //
 // bf16: warp-level matrix instructions (mma.sync: a step is bound by its bytes, and its few
 // rows would leave tcgen05's 128-row tiles empty), probabilities in three bf16 parts so
 // that nothing is lost against fp32, short chains in the accumulators because matrix
 // instructions cut their sums off. fp32: the CUDA cores.
 //
-// At the end of a group's part the warps are merged through shared memory. A group that
-// lies in one CTA is written; otherwise each CTA leaves its partial in the workspace and
-// raises a flag, and the CTA with the group's last tiles joins them in order once it has
-// finished its own run. It waits for CTAs of lower index only, which have been given
-// their SMs before it, and the waits are bounded (RIPPLE_ETIMEOUT). A flag is the call's
-// 64-bit tag; the reader lowers it, so that a replay of the same launch starts from
-// lowered flags, and no workspace needs initialising.
+// A group that lies in one run is written there. Of the others every run leaves a partial
+// in the workspace (a run has two at most: of the group it begins within and of the one
+// it ends within), and the run with the group's first block a record of them; a second
+// launch, a programmatic dependent of the first that takes its place when the last runs
+// have begun, joins them in order.
 #include <math.h>
 
 #include <atomic>
-#include <chrono>
 
 #include "common.cuh"
 #include "kernels.cuh"
@@ -41,15 +41,23 @@ namespace ripple {
 namespace {
 
 constexpr int kMaxGroup = 16;
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
 constexpr int kBlockBytes = 4096;  // of K (and of V) a block
-constexpr int kStages = 3;         // blocks in a warp's ring
-constexpr int kTileRows = 64;
+constexpr int kStages = 3;         // blocks in the ring
+constexpr int kWarpsPerSm = 8;
 // A running maximum (log2 units) moves only when a score exceeds it by more than this.
 constexpr float kSlack = 8.f;
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kMaxDevices = 64;
+
+// The runs: kPhases times one for every place (warp) on the GPU, the phases' shares of the
+// blocks in 1/256. Few blocks, and few groups (of which each would be left in hundreds of
+// partials), are one phase.
+constexpr int kPhases = 3;
+__device__ __forceinline__ int share_before(int phase) {
+  return phase == 0 ? 0 : phase == 1 ? 190 : phase == 2 ? 236 : 256;
+}
+constexpr int kOnePhase = 32;   // blocks per place, at most
+constexpr int kFewGroups = 64;
 
 struct PagedDecParams {
   PagedGeom g;
@@ -61,12 +69,10 @@ struct PagedDecParams {
   const int32_t *table, *lens;
   float *out, *lse;
   int32_t *status;
-  unsigned long long *flags;  // [2 * CTAs] partials finished (the call's tag)
-  float *ws_o;                // [2 * CTAs][G][D] partial outputs
-  float2 *ws_ml;              // [2 * CTAs][G] their maximum and sum
-  unsigned long long tag;
-  long long wait_cycles;
-  int n_ctas;
+  int places, n_runs;
+  int2 *rec;      // [n_runs] the group that begins in the run and goes on, and its runs (0: none)
+  float *ws_o;    // [2 * n_runs][G][D] partial outputs: of the group begun before, begun here
+  float2 *ws_ml;  // [2 * n_runs][G] their maximum and sum
 };
 
 template <typename T, int D, int G>
@@ -82,9 +88,6 @@ struct Cfg {
   static constexpr int R = 32 / S;
   static constexpr int STEPS = RB / R;
   static constexpr int PPL = PIECES / S;  // 16-byte pieces of a row a lane has
-  // merge buffers of the warps; with many heads the warps share four
-  static constexpr int RED = G * D > 512 ? kWarps / 2 : kWarps;
-  static constexpr int PITCH = D + 8;     // floats per head in a merge buffer
   // where a piece of a row lies in the block: rows are multiples of 128 bytes, so eight rows
   // of ldmatrix, or the rows of a quarter warp, must differ in the piece
   static __device__ __forceinline__ int swizzle(int row) {
@@ -93,72 +96,79 @@ struct Cfg {
   static_assert(kMma || (S <= 32 && STEPS >= 1 && STEPS * R == RB && PPL >= 1), "lane layout");
 };
 
-template <typename T, int D, int G>
-struct Smem {
-  using C = Cfg<T, D, G>;
-  alignas(128) uint8_t ring[kWarps][kStages][2][kBlockBytes];  // [stage][K, V]
-  alignas(16) float red_o[C::RED][G][C::PITCH];
-  float red_m[C::RED][G], red_l[C::RED][G];
-  long long part[kWarps];
-  long long total, rest;
-  int first_seq;
-  int gave_up;
-};
-
 __device__ __forceinline__ int clamp_len(const PagedDecParams &p, int b) {
   const long long room = (long long)p.g.max_pages << p.g.shift;
   const int n = p.lens[b];
   return n <= 0 ? 0 : (int)(n < room ? n : room);
 }
-__device__ __forceinline__ int tiles_of(int len) {
-  return len / kTileRows + (len % kTileRows != 0);
-}
-
-// The first tile of CTA c's run, of `total` tiles over n CTAs; the CTA that has tile t.
-__device__ __forceinline__ long long run_start(int c, long long total, int n) {
-  return (long long)((unsigned long long)c * (unsigned long long)total / (unsigned)n);
-}
-__device__ __forceinline__ int cta_of(long long t, long long total, int n) {
-  return (int)((((unsigned long long)t + 1) * (unsigned)n - 1) / (unsigned long long)total);
-}
-
-// A walk over the parts of groups in a CTA's run.
-struct Walk {
-  int b, h;
-  int tiles, tile;     // of the group, and the part's first
-  int begin, end;      // the part's rows
-  long long left;      // tiles of the run, the part's included
-  __device__ __forceinline__ void set(int len) {
-    const long long n = min((long long)(tiles - tile), left);
-    begin = tile * kTileRows;
-    end = (int)min((long long)len, (tile + n) * kTileRows);
+// Where the runs of `total` blocks begin.
+struct Runs {
+  long long total;
+  int places, phases;
+  __device__ __forceinline__ Runs(long long total_, int places_, int n_runs) : total(total_) {
+    const bool one = total <= (long long)kOnePhase * places_ || n_runs < kPhases * places_;
+    places = one ? (int)min((long long)min(places_, n_runs), total) : places_;
+    phases = one ? 1 : kPhases;
   }
+  __device__ __forceinline__ int count() const { return places * phases; }
+  __device__ __forceinline__ long long phase_start(int i) const {
+    return phases == 1 ? (i == 0 ? 0 : total) : total * share_before(i) / 256;
+  }
+  __device__ __forceinline__ long long start(int run) const {
+    if (run >= count()) return total;
+    const int ph = run / places;
+    const long long a = phase_start(ph), n = phase_start(ph + 1) - a;
+    return a + n * (run - ph * places) / places;
+  }
+  // The run that has block t.
+  __device__ __forceinline__ int of(long long t) const {
+    int ph = 0;
+    while (ph + 1 < phases && t >= phase_start(ph + 1)) ++ph;
+    const long long a = phase_start(ph), n = phase_start(ph + 1) - a;
+    return ph * places + (int)(((t - a + 1) * places - 1) / n);
+  }
+};
+
+// A walk over the parts of groups in a warp's run. RB: rows of a block.
+template <int RB>
+struct Walk {
+  int b, h, len;
+  int block;           // the part's first in its group
+  int begin, end;      // the part's rows
+  long long left;      // blocks of the run, the part's included
+  static __device__ __forceinline__ int blocks_of(int len) { return len / RB + (len % RB != 0); }
+  __device__ __forceinline__ int blocks() const { return blocks_of(len); }
   __device__ __forceinline__ int count() const {
-    return (int)min((long long)(tiles - tile), left);
+    return (int)min((long long)(blocks() - block), left);
+  }
+  __device__ __forceinline__ void set() {
+    begin = block * RB;
+    end = (int)min((long long)len, (long long)(block + count()) * RB);
   }
   // To the next part; false at the end of the run.
   __device__ __forceinline__ bool next(const PagedDecParams &p) {
     left -= count();
     if (left <= 0) return false;
-    tile = 0;
-    if (++h < p.g.Hkv) {
-      set_len(p);
-      return true;
+    block = 0;
+    if (++h >= p.g.Hkv) {
+      h = 0;
+      do len = clamp_len(p, ++b);
+      while (len == 0);  // left > 0: there are more
     }
-    h = 0;
-    do {
-      ++b;
-      tiles = tiles_of(clamp_len(p, b));
-    } while (tiles == 0);  // left > 0: there are more
-    set_len(p);
+    set();
     return true;
   }
-  __device__ __forceinline__ void set_len(const PagedDecParams &p) { set(clamp_len(p, b)); }
 };
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
-               "r"(there ? 16 : 0)
+// The cache rows pass L2 once; what is read again (tables, partials) stays.
+__device__ __forceinline__ uint64_t evict_first() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst),
+               "l"(src), "r"(there ? 16 : 0), "l"(policy)
                : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -166,45 +176,29 @@ template <int N>
 __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-__device__ __forceinline__ unsigned long long ld_acquire64(const unsigned long long *p) {
-  unsigned long long v;
-  asm volatile("ld.acquire.gpu.global.b64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
-  return v;
-}
-__device__ __forceinline__ void st_release64(unsigned long long *p, unsigned long long v) {
-  asm volatile("st.release.gpu.global.b64 [%0], %1;" ::"l"(p), "l"(v) : "memory");
-}
-
 // A warp's fetching side: the walk, the next block of this warp in its part, and the page
 // of the lane's row in that block.
 template <typename T, int D, int G>
 struct Fetch {
   using C = Cfg<T, D, G>;
-  Walk w;
-  int blk;     // block of the part
+  Walk<C::RB> w;
+  int at;      // the next block's first row
   bool live;   // there is a next block
-  int entry;   // block-table entry of row begin + blk * RB + lane % RB
+  int entry;   // block-table entry of row at + lane % RB
+  uint64_t policy;
   __device__ __forceinline__ void look_up(const PagedDecParams &p, int lane) {
-    const int row = w.begin + blk * C::RB + lane % C::RB;
+    const int row = at + lane % C::RB;
     entry = -1;
     if (row < w.end)
       entry = p.table[guard((long long)w.b * p.g.max_pages + (row >> p.g.shift), 1,
                             (long long)p.g.B * p.g.max_pages, p.status)];
   }
-  // To a block of this warp at or after blk.
-  __device__ __forceinline__ void settle(const PagedDecParams &p, int warp, int lane) {
-    while (live && w.begin + blk * C::RB >= w.end) {
-      live = w.next(p);
-      blk = warp;
-    }
-    if (live) look_up(p, lane);
-  }
   // Copies the block into `stage` and goes on; returns its live rows as bits.
   __device__ __forceinline__ uint32_t issue(const PagedDecParams &p, uint8_t (*stage)[kBlockBytes],
-                                            int warp, int lane) {
+                                            int lane) {
     uint32_t rows = 0;
     if (live) {
-      const int row = w.begin + blk * C::RB + lane % C::RB;
+      const int row = at + lane % C::RB;
       const bool there = row < w.end, ok = there && (unsigned)entry < (unsigned)p.g.n_pages;
       if (there && !ok) report(p.status, RIPPLE_EBOUNDS);
       rows = __ballot_sync(kAll, ok) & (uint32_t)((1ull << C::RB) - 1);
@@ -219,11 +213,15 @@ struct Fetch {
         const long long o = __shfl_sync(kAll, off, r) + pc * (16 / (int)sizeof(T));
         const uint32_t dst = r * C::ROW_BYTES + (pc ^ C::swizzle(r)) * 16;
         const bool has = rows >> r & 1;
-        copy16(ks + dst, (const T *)p.k_pages + o, has);
-        copy16(vs + dst, (const T *)p.v_pages + o, has);
+        copy16(ks + dst, (const T *)p.k_pages + o, has, policy);
+        copy16(vs + dst, (const T *)p.v_pages + o, has, policy);
       }
-      blk += kWarps;
-      settle(p, warp, lane);
+      at += C::RB;
+      if (at >= w.end) {
+        live = w.next(p);
+        at = w.begin;
+      }
+      if (live) look_up(p, lane);
     }
     copy_commit();
     return rows;
@@ -247,7 +245,7 @@ struct Rows {
   float2 acc[NB][H];
   float m[H], l[H];
 
-  __device__ __forceinline__ void start(const PagedDecParams &p, const Walk &w, int lane) {
+  __device__ __forceinline__ void start(const PagedDecParams &p, const Walk<C::RB> &w, int lane) {
     const int g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int i = 0; i < H; ++i) {
@@ -402,6 +400,15 @@ struct Rows {
       }
     }
   }
+  // The outputs of a group that is done.
+  __device__ __forceinline__ void normalise() {
+#pragma unroll
+    for (int u = 0; u < H; ++u) {
+      const float inv = l[u] != 0.f ? 1.f / l[u] : 0.f;  // 0: no row counts
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b][u] = __fmul2_rn(acc[b][u], make_float2(inv, inv));
+    }
+  }
   // f(head, its maximum, its sum), once per head
   template <typename F>
   __device__ __forceinline__ void stats(int lane, F f) {
@@ -436,7 +443,7 @@ struct Rows<float, D, G> {
   float2 acc[G][2 * PPL];
   float m[1], l[1];                 // of head hq over this row group's rows
 
-  __device__ __forceinline__ void start(const PagedDecParams &p, const Walk &w, int lane) {
+  __device__ __forceinline__ void start(const PagedDecParams &p, const Walk<C::RB> &w, int lane) {
     const int sl = lane % S, hq = sl / HL;
 #pragma unroll
     for (int j = 0; j < G; ++j) {
@@ -548,6 +555,15 @@ struct Rows<float, D, G> {
         }
     }
   }
+  __device__ __forceinline__ void normalise() {
+    float inv[G];
+    spread_heads<S, G>(l[0] != 0.f ? 1.f / l[0] : 0.f, inv);  // 0: no row counts
+#pragma unroll
+    for (int j = 0; j < G; ++j)
+#pragma unroll
+      for (int e = 0; e < 2 * PPL; ++e)
+        acc[j][e] = __fmul2_rn(acc[j][e], make_float2(inv[j], inv[j]));
+  }
   template <typename F>
   __device__ __forceinline__ void stats(int lane, F f) {
     if (lane < S && lane % HL == 0) f(lane / HL, m[0], l[0]);
@@ -564,34 +580,27 @@ struct Rows<float, D, G> {
   }
 };
 
-// Writes a head's output element, or with lse its log of the sum.
-__device__ __forceinline__ void put(const PagedDecParams &p, long long row, int D, int d, float num,
-                                    float den, float M) {
-  p.out[guard(row * D + d, 1, (long long)p.g.B * p.Hq * D, p.status)] =
-      den != 0.f ? num / den : 0.f;  // no row counts: 0
-  // den >= 2^-kSlack of the largest score's 1
-  if (p.lse != nullptr && d == 0)
-    p.lse[guard(row, 1, (long long)p.g.B * p.Hq, p.status)] = (M + log2f(den)) * 0.6931471805599453f;
+__device__ __forceinline__ float lse_of(float m, float l) {  // of log2 units; no row: -infinity
+  return (m + log2f(l)) * 0.6931471805599453f;
 }
 
 template <typename T, int D, int G>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(32, kWarpsPerSm)
     paged_decode_kernel(const __grid_constant__ PagedDecParams p) {
   using C = Cfg<T, D, G>;
-  extern __shared__ __align__(128) uint8_t smem_raw[];
-  Smem<T, D, G> &s = *reinterpret_cast<Smem<T, D, G> *>(smem_raw);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int cta = blockIdx.x;
+  using W = Walk<C::RB>;
+  __shared__ __align__(128) uint8_t ring[kStages][2][kBlockBytes];  // [stage][K, V]
+  const int lane = threadIdx.x, run = blockIdx.x;
   pdl_launch_dependents();
   pdl_wait();
 
-  // The run of this CTA: tiles of all groups, thread by thread over the sequences.
-  const int per = (p.g.B + kThreads - 1) / kThreads;
-  const int b0 = min(tid * per, p.g.B), b1 = min(b0 + per, p.g.B);
+  // This run: blocks of all groups, lane by lane over the sequences.
+  const int per = (p.g.B + 31) / 32;
+  const int b0 = min(lane * per, p.g.B), b1 = min(b0 + per, p.g.B);
   long long mine = 0;
   for (int b = b0; b < b1; ++b) {
-    mine += (long long)tiles_of(clamp_len(p, b)) * p.g.Hkv;
-    if (cta == 0 && (long long)p.lens[b] > (long long)p.g.max_pages << p.g.shift)
+    mine += (long long)W::blocks_of(clamp_len(p, b)) * p.g.Hkv;
+    if (run == 0 && (long long)p.lens[b] > (long long)p.g.max_pages << p.g.shift)
       report(p.status, RIPPLE_EFULL);
   }
   long long incl = mine;
@@ -600,209 +609,214 @@ __global__ void __launch_bounds__(kThreads, 1)
     const long long y = __shfl_up_sync(kAll, incl, o);
     if (lane >= o) incl += y;
   }
-  if (lane == 31) s.part[warp] = incl;
-  __syncthreads();
-  long long total = 0, before = incl - mine;
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
-    if (i < warp) before += s.part[i];
-    total += s.part[i];
+  const Runs runs(__shfl_sync(kAll, incl, 31), p.places, p.n_runs);
+  const int rec_at = guard(run, 1, p.n_runs, p.status);
+  if (run >= runs.count()) {
+    if (lane == 0) p.rec[rec_at] = make_int2(0, 0);
+    return;
   }
-  const int n = (int)min((long long)p.n_ctas, total);
-  const bool busy = cta < n;
-  const long long t0 = busy ? run_start(cta, total, n) : 0;
-  const long long t1 = busy ? run_start(cta + 1, total, n) : 0;
-  if (busy && before <= t0 && t0 < before + mine) {
-    long long rest = t0 - before;
-    for (int b = b0;; ++b) {
-      const long long k = (long long)tiles_of(clamp_len(p, b)) * p.g.Hkv;
-      if (rest < k) {
-        s.first_seq = b;
-        s.rest = rest;
-        break;
-      }
+  const long long t0 = runs.start(run);
+  const int owner = __ffs(__ballot_sync(kAll, incl > t0)) - 1;
+  int seq = 0;
+  long long rest = t0 - (incl - mine);
+  if (lane == owner) {
+    for (seq = b0;; ++seq) {
+      const long long k = (long long)W::blocks_of(clamp_len(p, seq)) * p.g.Hkv;
+      if (rest < k) break;
       rest -= k;
     }
   }
-  if (tid == 0) s.gave_up = 0;
-  __syncthreads();
-
-  Fetch<T, D, G> fetch = {};
-  fetch.live = busy;
-  if (busy) {
-    Walk &w = fetch.w;
-    w.b = s.first_seq;
-    const int len = clamp_len(p, w.b);
-    w.tiles = tiles_of(len);
-    w.h = (int)(s.rest / w.tiles);
-    w.tile = (int)(s.rest % w.tiles);
-    w.left = t1 - t0;
-    w.set(len);
-  }
-  Walk at = fetch.w;
-  const int first_tile = at.tile;  // of the run's first part
-  fetch.blk = warp;
-  fetch.settle(p, warp, lane);
+  Fetch<T, D, G> fetch;
+  fetch.policy = evict_first();
+  W &w = fetch.w;
+  w.b = __shfl_sync(kAll, seq, owner);
+  rest = __shfl_sync(kAll, rest, owner);
+  w.len = clamp_len(p, w.b);
+  w.h = (int)(rest / w.blocks());
+  w.block = (int)(rest % w.blocks());
+  w.left = runs.start(run + 1) - t0;
+  w.set();
+  fetch.live = true;
+  fetch.at = w.begin;
+  fetch.look_up(p, lane);
+  W at = fetch.w;
   uint64_t coming = 0;  // live rows of the blocks on their way, 32 bits each
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i)
-    coming |= (uint64_t)fetch.issue(p, s.ring[warp][i], warp, lane) << (32 * i);
+    coming |= (uint64_t)fetch.issue(p, ring[i], lane) << (32 * i);
   static_assert(kStages == 3, "two blocks on their way");
 
-  // sequences without rows
-  for (int b = cta; b < p.g.B; b += gridDim.x) {
-    if (clamp_len(p, b) > 0) continue;
-    for (int e = tid; e < p.Hq * D; e += kThreads)
-      p.out[guard((long long)b * p.Hq * D + e, 1, (long long)p.g.B * p.Hq * D, p.status)] = 0.f;
-    for (int e = tid; p.lse != nullptr && e < p.Hq; e += kThreads)
-      p.lse[guard((long long)b * p.Hq + e, 1, (long long)p.g.B * p.Hq, p.status)] = -INFINITY;
-  }
-  if (!busy) return;
-
+  const long long n_rows = (long long)p.g.B * p.Hq;
+  int2 rec = make_int2(0, 0);
   int stage = 0;
-  bool joins = false;  // this CTA joins the partials of its first part's group
-  Walk first = at;
+  long long t = t0;  // the part's first block
   for (bool more = true; more;) {
     Rows<T, D, G> rows;
     rows.start(p, at, lane);
-    for (int blk = warp; at.begin + blk * C::RB < at.end; blk += kWarps) {
+    for (int row = at.begin; row < at.end; row += C::RB) {
       copy_wait<kStages - 2>();
       __syncwarp();  // the block has landed, and the stage before it has been read
       const uint32_t live = (uint32_t)coming;
-      const int fill = stage + kStages - 1 < kStages ? stage + kStages - 1 : stage - 1;
-      coming = coming >> 32 | (uint64_t)fetch.issue(p, s.ring[warp][fill], warp, lane) << 32;
-      rows.block(p, s.ring[warp][stage], live, lane);
+      const int fill = stage > 0 ? stage - 1 : kStages - 1;
+      coming = coming >> 32 | (uint64_t)fetch.issue(p, ring[fill], lane) << 32;
+      rows.block(p, ring[stage], live, lane);
       stage = stage + 1 < kStages ? stage + 1 : 0;
     }
     rows.finish();
-
-    // The warps of the part, through shared memory, as many at a time as there are buffers.
-    constexpr int NE = (G * D + kThreads - 1) / kThreads;
-    float M[NE], num[NE], den[NE];
-#pragma unroll
-    for (int i = 0; i < NE; ++i) {
-      M[i] = -INFINITY;
-      num[i] = den[i] = 0.f;
-    }
-#pragma unroll
-    for (int turn = 0; turn < kWarps / C::RED; ++turn) {
-      named_bar_sync(1, kThreads);  // the buffers have been read
-      if (warp / C::RED == turn) {
-        const int buf = warp % C::RED;
+    const bool ends = at.block + at.count() == at.blocks();
+    if (ends && at.block == 0) {
+      const long long row0 = guard((long long)at.b * p.Hq + at.h * p.G, p.G, n_rows, p.status);
+      rows.normalise();
+      rows.outputs(lane, [&](int head, int d, const float2 &o) {
+        if (head < p.G) *reinterpret_cast<float2 *>(&p.out[(row0 + head) * D + d]) = o;
+      });
+      if (p.lse != nullptr)
         rows.stats(lane, [&](int head, float m, float l) {
-          s.red_m[buf][head] = m;
-          s.red_l[buf][head] = l;
+          if (head < p.G) p.lse[row0 + head] = lse_of(m, l);
         });
-        rows.outputs(lane, [&](int head, int d, const float2 &o) {
-          *reinterpret_cast<float2 *>(&s.red_o[buf][head][d]) = o;
-        });
-      }
-      named_bar_sync(1, kThreads);
-#pragma unroll
-      for (int i = 0; i < NE; ++i) {
-        const int e = tid + i * kThreads, head = e / D;
-        if (e >= p.G * D) continue;
-        float top = M[i];
-#pragma unroll
-        for (int w = 0; w < C::RED; ++w) top = fmaxf(top, s.red_m[w][head]);
-        const float sub = top == -INFINITY ? 0.f : top;
-        const float old = fast_exp2(M[i] - sub);
-        num[i] *= old;
-        den[i] *= old;
-        M[i] = top;
-#pragma unroll
-        for (int w = 0; w < C::RED; ++w) {
-          const float a = fast_exp2(s.red_m[w][head] - sub);
-          num[i] += a * s.red_o[w][head][e % D];
-          den[i] += a * s.red_l[w][head];
-        }
-      }
+    } else {
+      const bool here = at.block == 0;  // the group begins in this run
+      const long long slot =
+          guard(2LL * run + (here ? 1 : 0), 1, 2LL * p.n_runs, p.status) * p.G;
+      rows.outputs(lane, [&](int head, int d, const float2 &o) {
+        if (head < p.G) *reinterpret_cast<float2 *>(&p.ws_o[(slot + head) * D + d]) = o;
+      });
+      rows.stats(lane, [&](int head, float m, float l) {
+        if (head < p.G) p.ws_ml[slot + head] = make_float2(m, l);
+      });
+      if (here)
+        rec = make_int2(at.b * p.g.Hkv + at.h, runs.of(t + at.blocks() - 1) - run + 1);
     }
-    const bool whole = at.tile == 0 && at.count() == at.tiles;
-    const int slot = 2 * cta + (at.tile == 0 ? 1 : 0);
-    const long long row0 = (long long)at.b * p.Hq + at.h * p.G;
-#pragma unroll
-    for (int i = 0; i < NE; ++i) {
-      const int e = tid + i * kThreads, head = e / D, d = e % D;
-      if (e >= p.G * D) continue;
-      if (whole) {
-        put(p, row0 + head, D, d, num[i], den[i], M[i]);
-      } else {
-        const long long at_slot =
-            guard((long long)slot * p.G + head, 1, 2LL * p.n_ctas * p.G, p.status);
-        p.ws_o[at_slot * D + d] = num[i];
-        if (d == 0) p.ws_ml[at_slot] = make_float2(M[i], den[i]);
-      }
-    }
-    if (!whole) {
-      const bool last = at.tile + at.count() == at.tiles;
-      if (last) {
-        joins = true;
-      } else {
-        __threadfence();
-        named_bar_sync(1, kThreads);
-        if (tid == 0) st_release64(&p.flags[slot], p.tag);
-      }
-    }
+    t += at.count();
     more = at.next(p);
   }
   copy_wait<0>();
+  if (lane == 0) p.rec[rec_at] = rec;
+}
 
-  if (!joins) return;
-  // The partials of the first part's group: of the CTA with its first tile (a part that
-  // begins the group), of those between, and this CTA's own.
-  const long long group_start = t0 - first_tile;
-  const int c0 = cta_of(group_start, total, n);
-  const int parts = cta - c0 + 1;
-  for (int i = tid; i < parts - 1; i += kThreads) {
-    unsigned long long *flag = &p.flags[2 * (c0 + i) + (i == 0 ? 1 : 0)];
-    const long long from = clock64();
-    bool up;
-    while (!(up = ld_acquire64(flag) == p.tag) && clock64() - from <= p.wait_cycles) __nanosleep(20);
-    if (up) {
-      *flag = 0;  // a replay of this launch starts from lowered flags
-    } else {
-      report(p.status, RIPPLE_ETIMEOUT);
-      s.gave_up = 1;
+// Joins the partials of the groups that begin in this CTA's kJoinRuns runs and go on, one
+// head of the group per blockIdx.y: a group of many partials by the whole CTA, the others
+// by as many warps each as there are for them. And the outputs of the sequences without
+// rows.
+constexpr int kJoinThreads = 256;
+constexpr int kJoinWarps = kJoinThreads / 32;
+constexpr int kJoinRuns = 32;
+constexpr int kMany = 32;  // partials
+
+struct Joined {
+  float m, den;
+  float4 sum;
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    den = 0.f;
+    sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __device__ __forceinline__ void scale_to(float mn) {  // a larger maximum
+    const float a = fast_exp2(m - (mn == -INFINITY ? 0.f : mn));
+    sum = make_float4(sum.x * a, sum.y * a, sum.z * a, sum.w * a);
+    den *= a;
+    m = mn;
+  }
+  __device__ __forceinline__ void add(float f, float l, const float4 &o) {
+    sum.x += f * o.x;
+    sum.y += f * o.y;
+    sum.z += f * o.z;
+    sum.w += f * o.w;
+    den += f * l;
+  }
+  __device__ __forceinline__ void add(const Joined &x) {
+    const float mn = fmaxf(m, x.m);
+    scale_to(mn);
+    add(fast_exp2(x.m - (mn == -INFINITY ? 0.f : mn)), x.den, x.sum);
+  }
+  // Partials first, first + step, .. of those of the group that begins in `run`.
+  __device__ __forceinline__ void add_partials(const PagedDecParams &p, int D, int run, int parts,
+                                               int first, int step, int head, int col) {
+    constexpr int kAt = 8;  // loaded at a time
+    for (int k0 = first; k0 < parts; k0 += kAt * step) {
+      float2 ml[kAt];
+      float4 o[kAt];
+#pragma unroll
+      for (int i = 0; i < kAt; ++i) {
+        const int k = min(k0 + i * step, parts - 1);
+        const long long slot =
+            guard(2LL * (run + k) + (k == 0 ? 1 : 0), 1, 2LL * p.n_runs, p.status) * p.G + head;
+        ml[i] = __ldcg(&p.ws_ml[slot]);
+        o[i] = __ldcg(reinterpret_cast<const float4 *>(p.ws_o + slot * D) + col);
+      }
+      float mn = m;
+#pragma unroll
+      for (int i = 0; i < kAt; ++i) mn = fmaxf(mn, ml[i].x);  // (repeats change no maximum)
+      scale_to(mn);
+      const float sub = mn == -INFINITY ? 0.f : mn;
+#pragma unroll
+      for (int i = 0; i < kAt; ++i)
+        if (k0 + i * step < parts) add(fast_exp2(ml[i].x - sub), ml[i].y, o[i]);
     }
   }
-  __threadfence();
+  __device__ __forceinline__ void write(const PagedDecParams &p, int D, int group, int head,
+                                        int col) const {
+    const long long row =
+        guard((long long)(group / p.g.Hkv) * p.Hq + group % p.g.Hkv * p.G + head, 1,
+              (long long)p.g.B * p.Hq, p.status);
+    const float inv = den != 0.f ? 1.f / den : 0.f;  // 0: no row counts
+    reinterpret_cast<float4 *>(p.out + row * D)[col] =
+        make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+    if (p.lse != nullptr && col == 0) p.lse[row] = lse_of(m, den);
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads, 3)
+    paged_join_kernel(const __grid_constant__ PagedDecParams p) {
+  constexpr int kCols = D / 4;
+  __shared__ Joined part[kJoinThreads];
+  __shared__ int3 few[kJoinRuns], many[kJoinRuns];  // run, group, partials
+  __shared__ int n_few, n_many;
+  const int tid = threadIdx.x, warp = tid >> 5, head = blockIdx.y;
+  if (tid == 0) n_few = n_many = 0;
   __syncthreads();
-  if (s.gave_up) return;
-  const long long row0 = (long long)first.b * p.Hq + first.h * p.G;
-  constexpr int kAt = 8;  // partials loaded at a time
-  for (int e = tid; e < p.G * D; e += kThreads) {
-    const int head = e / D, d = e % D;
-    float M = -INFINITY, num = 0.f, den = 0.f;
-    for (int i0 = 0; i0 < parts; i0 += kAt) {
-      float2 ml[kAt];
-      float o[kAt];
-#pragma unroll
-      for (int i = 0; i < kAt; ++i) {
-        const int c = min(i0 + i, parts - 1);
-        const long long slot = 2 * (c0 + c) + (c == 0 ? 1 : 0);
-        ml[i] = __ldcg(&p.ws_ml[slot * p.G + head]);
-        o[i] = __ldcg(&p.ws_o[(slot * p.G + head) * D + d]);
-        if (i0 + i >= parts) {
-          ml[i] = make_float2(-INFINITY, 0.f);
-          o[i] = 0.f;
-        }
+  pdl_launch_dependents();
+  pdl_wait();
+  const int run = blockIdx.x * kJoinRuns + tid;
+  if (tid < kJoinRuns && run < p.n_runs) {
+    const int2 r = __ldcg(&p.rec[run]);
+    // (listed in any order: each group is joined by itself)
+    if (r.y > kMany)
+      many[atomicAdd(&n_many, 1)] = make_int3(run, r.x, r.y);
+    else if (r.y > 0)
+      few[atomicAdd(&n_few, 1)] = make_int3(run, r.x, r.y);
+  }
+  __syncthreads();
+  // `warps` warps a group, each stripe of D / 4 threads of them taking every stripes-th partial
+  auto join = [&](const int3 *groups, int n, int warps) {
+    const int stripes = warps * 32 / kCols, at_once = kJoinWarps / warps;
+    const int in = tid % (warps * 32), col = in % kCols, stripe = in / kCols;
+    for (int i0 = 0; i0 < n; i0 += at_once) {
+      const int i = i0 + warp / warps;
+      Joined j;
+      j.clear();
+      if (i < n) j.add_partials(p, D, groups[i].x, groups[i].z, stripe, stripes, head, col);
+      if (stripes > 1) {
+        part[tid] = j;
+        __syncthreads();
+        if (stripe == 0)
+          for (int k = 1; k < stripes; ++k) j.add(part[tid + k * kCols]);
+        __syncthreads();
       }
-      float Mn = M;
-#pragma unroll
-      for (int i = 0; i < kAt; ++i) Mn = fmaxf(Mn, ml[i].x);
-      const float sub = Mn == -INFINITY ? 0.f : Mn, a = fast_exp2(M - sub);
-      num *= a;
-      den *= a;
-      M = Mn;
-#pragma unroll
-      for (int i = 0; i < kAt; ++i) {
-        const float w = fast_exp2(ml[i].x - sub);
-        den += w * ml[i].y;
-        num += w * o[i];
-      }
+      if (i < n && stripe == 0) j.write(p, D, groups[i].y, head, col);
     }
-    put(p, row0 + head, D, d, num, den, M);
+  };
+  join(many, n_many, kJoinWarps);
+  join(few, n_few, n_few <= 1 ? kJoinWarps : n_few <= 2 ? 4 : n_few <= 4 ? 2 : 1);
+  for (int b = blockIdx.x; b < p.g.B; b += gridDim.x) {
+    if (clamp_len(p, b) > 0) continue;
+    for (int e = tid; e < p.g.Hkv * D; e += kJoinThreads) {
+      const long long row = guard((long long)b * p.Hq + e / D * p.G + head, 1,
+                                  (long long)p.g.B * p.Hq, p.status);
+      p.out[row * D + e % D] = 0.f;
+      if (p.lse != nullptr && e % D == 0) p.lse[row] = -INFINITY;
+    }
   }
 }
 
@@ -820,18 +834,6 @@ int sm_count(int dev) {
   return v;
 }
 
-// Tag of a call: a sequence, never 0, from a start taken from the clock, so that a flag
-// left in reused memory by an earlier call or process does not match.
-unsigned long long next_tag() {
-  static std::atomic<unsigned long long> seq{
-      (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() *
-      0x9e3779b97f4a7c15ULL};
-  unsigned long long t;
-  do t = seq.fetch_add(1, std::memory_order_relaxed) + 1;
-  while (t == 0);
-  return t;
-}
-
 size_t round_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
 bool decode_args(const ripple_paged_desc *d, int n_q_heads, PagedDecParams *p) {
@@ -842,60 +844,63 @@ bool decode_args(const ripple_paged_desc *d, int n_q_heads, PagedDecParams *p) {
   return p->G <= kMaxGroup;
 }
 
-// Workspace layout: flags, (max, sum), outputs, two partials per CTA at most (the first
-// and the last part of its run). Returns the bytes; fills p's pointers if given a base.
-size_t plan(PagedDecParams *p, int sms, void *ws) {
-  const size_t slots = 2 * (size_t)sms;
-  const size_t flags = round_up(slots * sizeof(unsigned long long));
+// Runs of a call and the workspace: records, (max, sum), outputs of the partials. The runs are bounded by the blocks that the table has room for, so that small caches
+// take few CTAs; everything grows with the call. Returns the bytes; fills p's pointers if
+// given a base.
+size_t plan(PagedDecParams *p, int dtype, int sms, void *ws) {
+  const int rows = kBlockBytes / (p->g.D * (dtype == RIPPLE_BF16 ? 2 : 4));
+  const long long room = (((long long)p->g.max_pages << p->g.shift) + rows - 1) / rows * p->g.B * p->g.Hkv;
+  p->places = sms * kWarpsPerSm;
+  const int phases = (long long)p->g.B * p->g.Hkv <= kFewGroups ? 1 : kPhases;
+  p->n_runs = (int)std::min<long long>(phases * p->places, room);
+  const size_t slots = 2 * (size_t)p->n_runs;
+  const size_t rec = round_up(p->n_runs * sizeof(int2));
   const size_t ml = round_up(slots * p->G * sizeof(float2));
   uint8_t *base = (uint8_t *)ws;
-  p->n_ctas = sms;
-  p->flags = (unsigned long long *)base;
-  p->ws_ml = (float2 *)(base + flags);
-  p->ws_o = (float *)(base + flags + ml);
-  return flags + ml + round_up(slots * p->G * p->g.D * sizeof(float));
+  p->rec = (int2 *)base;
+  p->ws_ml = (float2 *)(base + rec);
+  p->ws_o = (float *)(base + rec + ml);
+  return rec + ml + round_up(slots * p->G * p->g.D * sizeof(float));
 }
 
-template <typename T, int D, int G>
-cudaError_t launch(const PagedDecParams &p, int dev, cudaStream_t st) {
-  static std::atomic<bool> attr_set[kMaxDevices];
-  constexpr int smem = (int)sizeof(Smem<T, D, G>);
-  static_assert(smem <= 227 * 1024, "shared memory per CTA");
-  if (!attr_set[dev].load(std::memory_order_acquire)) {
-    const cudaError_t e = cudaFuncSetAttribute(paged_decode_kernel<T, D, G>,
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-    attr_set[dev].store(true, std::memory_order_release);
-  }
+cudaError_t launch_pdl(void (*kernel)(PagedDecParams), dim3 grid, int threads,
+                       const PagedDecParams &p, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.n_ctas);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, paged_decode_kernel<T, D, G>, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
   count_launches(1);
   return e;
+}
+
+template <typename T, int D, int G>
+cudaError_t launch(const PagedDecParams &p, cudaStream_t st) {
+  const cudaError_t e = launch_pdl(paged_decode_kernel<T, D, G>, dim3(p.n_runs), 32, p, st);
+  if (e != cudaSuccess) return e;
+  const int ctas = (p.n_runs + kJoinRuns - 1) / kJoinRuns;
+  return launch_pdl(paged_join_kernel<D>, dim3(ctas, p.G), kJoinThreads, p, st);
 }
 
 // Heads of a group, padded: for the matrix instructions to 4, 8 or 16, on the CUDA
 // cores to a power of two.
 template <int D>
-cudaError_t launch_d(const PagedDecParams &p, int dtype, int dev, cudaStream_t st) {
+cudaError_t launch_d(const PagedDecParams &p, int dtype, cudaStream_t st) {
   if (dtype == RIPPLE_BF16) {
-    if (p.G <= 4) return launch<__nv_bfloat16, D, 4>(p, dev, st);
-    if (p.G <= 8) return launch<__nv_bfloat16, D, 8>(p, dev, st);
-    return launch<__nv_bfloat16, D, 16>(p, dev, st);
+    if (p.G <= 4) return launch<__nv_bfloat16, D, 4>(p, st);
+    if (p.G <= 8) return launch<__nv_bfloat16, D, 8>(p, st);
+    return launch<__nv_bfloat16, D, 16>(p, st);
   }
-  if (p.G == 1) return launch<float, D, 1>(p, dev, st);
-  if (p.G == 2) return launch<float, D, 2>(p, dev, st);
-  if (p.G <= 4) return launch<float, D, 4>(p, dev, st);
-  if (p.G <= 8) return launch<float, D, 8>(p, dev, st);
-  return launch<float, D, 16>(p, dev, st);
+  if (p.G == 1) return launch<float, D, 1>(p, st);
+  if (p.G == 2) return launch<float, D, 2>(p, st);
+  if (p.G <= 4) return launch<float, D, 4>(p, st);
+  if (p.G <= 8) return launch<float, D, 8>(p, st);
+  return launch<float, D, 16>(p, st);
 }
 
 }  // namespace
@@ -910,7 +915,7 @@ extern "C" ripple_status ripple_paged_decode_workspace_bytes(const ripple_paged_
   if (!decode_args(desc, n_q_heads, &p) || bytes_host == nullptr) return RIPPLE_EINVAL;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
-  *bytes_host = plan(&p, sm_count(dev), nullptr);
+  *bytes_host = plan(&p, desc->dtype, sm_count(dev), nullptr);
   return RIPPLE_OK;
 }
 
@@ -941,7 +946,7 @@ extern "C" ripple_status ripple_paged_decode_attn(
   int dev = 0;
   const cudaError_t got = cudaGetDevice(&dev);
   if (got != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
-  if (workspace_bytes < plan(&p, sm_count(dev), workspace)) return RIPPLE_EWORKSPACE;
+  if (workspace_bytes < plan(&p, desc->dtype, sm_count(dev), workspace)) return RIPPLE_EWORKSPACE;
   if (got != cudaSuccess) return RIPPLE_ECUDA;
   p.scale2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)desc->head_dim)) * kLog2e;
   p.q = q;
@@ -952,10 +957,8 @@ extern "C" ripple_status ripple_paged_decode_attn(
   p.out = out;
   p.lse = lse;
   p.status = dev_status;
-  p.tag = next_tag();
-  p.wait_cycles = wait_limit_cycles();
   cudaStream_t st = (cudaStream_t)stream;
-  RIPPLE_CUDA_TRY(desc->head_dim == 128 ? launch_d<128>(p, desc->dtype, dev, st)
-                                        : launch_d<64>(p, desc->dtype, dev, st));
+  RIPPLE_CUDA_TRY(desc->head_dim == 128 ? launch_d<128>(p, desc->dtype, st)
+                                        : launch_d<64>(p, desc->dtype, st));
   return RIPPLE_OK;
 }
