@@ -541,7 +541,7 @@ ripple_status ripple_paged_decode_attn(const ripple_paged_desc *desc, int32_t n_
  * log1p(S'), so that log probabilities near 0 and small entropies keep their relative
  * precision. Results do not depend on the run. One launch, no workspace. The call may
  * be captured in a CUDA graph.
- * Errors: RIPPLE_EINVAL, RIPPLE_ECUDA.
+ * Errors: RIPPLE_EINVAL, RIPPLE_ECUDA. Device status: RIPPLE_EBOUNDS.
  */
 ripple_status ripple_token_logprobs(int32_t n_rows, int32_t vocab, int64_t row_stride,
                                     int32_t dtype, float scale, int32_t n_top,

@@ -6,21 +6,28 @@
 //   log P(x) = scale d - log1p(S'),   entropy = log1p(S') - scale T / (1 + S').
 // Leaving the 1 out of the sum keeps the relative precision of log probabilities near 0.
 //
-// Work: a row is cut into C slices, one CTA each, the C CTAs of a row being a cluster
-// (slices_of). A warp streams its share of the slice with 16-byte loads, several in
-// flight, and keeps a running maximum for the warp (a vote per 8 logits of a lane, moved
-// and rescaled when one is larger, which soon gets rare), sums per lane, and each lane's
-// largest logit. The warps are merged through shared memory, the slices through the
-// shared memory of the cluster's first CTA.
+// Work: one CTA per row, or with few rows one per slice of a row, the slices of a row being
+// a cluster (slices_of). Every thread copies its 16-byte vectors of the row into places of
+// its own in shared memory, kStages chunks ahead (asynchronous copies, waited for by the
+// thread alone), so that the loads in flight cost no registers and no barrier. A warp
+// keeps a maximum, which begins as the largest logit of the CTA's first chunk and so
+// rarely moves (a vote per chunk), and sums per lane. The warps are merged through shared
+// memory, the slices through the shared memory of the cluster's first CTA.
 //
 // Alternatives: keys order logits descending, equal ones by index. The n-th largest of the
-// 32 largest logits of 8 lanes each bounds the slice's n-th largest key from below, so
-// only lanes whose largest logit reaches it hold candidates; their logits are read once
-// more (L2), and the candidates, a few more than n, are ranked by counting. Where there
-// are more than fit (many ties, sorted rows), the n-th largest of those found is a
-// higher bound, and the reading is repeated with it; every turn drops some.
+// 32 largest logits of kGroup lanes each bounds the slice's n-th largest key from below.
+// The largest logit of every lane and segment of the slice (a few chunks) has been kept,
+// so only the segments that reach the bound are read once more (from L2, mostly), and the
+// candidates, a few more than n, are ranked by counting. Where there are more than fit
+// (many ties, sorted rows), the n-th largest of those found is a higher bound, and the
+// reading is repeated with it; every turn drops some.
+//
+// Bound: the special-function units, 16 exponentials a clock and SM: 57 us for 2048 rows of
+// 128256, with HBM (77 us for bf16) close behind.
 #include <float.h>
 #include <math.h>
+
+#include <atomic>
 
 #include "common.cuh"
 #include "kernels.cuh"
@@ -28,13 +35,19 @@
 namespace ripple {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kCtasPerSm = 4;
+constexpr int kWarps = 8;
+constexpr int kThreads = kWarps * 32;
+constexpr int kCtasPerSm = 3;
+constexpr int kPlaces = 152 * kCtasPerSm;
 constexpr int kMaxSlices = 8;
-constexpr int kVecs = 4;      // 16-byte loads a thread has in flight
-constexpr int kCands = 512;   // candidates ranked at a time
+constexpr int kVecs = 4;               // 16-byte vectors of a thread in a chunk
+constexpr int kChunkVecs = kThreads * kVecs;
+constexpr int kStages = 3;
+constexpr int kSegments = 8;
+constexpr int kGroup = kThreads / 32;  // lanes whose largest logit bounds the alternatives
+constexpr int kCands = 512;            // candidates ranked at a time
 constexpr unsigned kAll = 0xffffffffu;
+constexpr int kMaxDevices = 64;
 typedef unsigned long long Key;
 
 struct LogprobParams {
@@ -60,10 +73,10 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 }
 __device__ __forceinline__ Key key_of(float x, int i) { return (Key)order_of(x) << 32 | (uint32_t)~i; }
 
-// Part of a row: its largest logit m, S' (the sum without that logit, so -1 for a part
-// with nothing but -infinity) and T, relative to m.
+// Part of a row: a logit m at least as large as all of its logits, the sum of the terms
+// relative to it, 1 for one logit m if it is in the part (one) and s for all others, and T.
 struct Sums {
-  float m, s, t;
+  float m, s, t, one;
 };
 // A sum n of terms relative to m_from, and its t, to a larger m.
 __device__ __forceinline__ void rebase(float n, float &t, float &s, float m_from, float m,
@@ -74,13 +87,22 @@ __device__ __forceinline__ void rebase(float n, float &t, float &s, float m_from
   s = n * e;
 }
 __device__ __forceinline__ Sums merge(const Sums &a, const Sums &b, float scale2) {
-  const bool first = a.m >= b.m;
+  const bool first = a.m > b.m || (a.m == b.m && a.one >= b.one);
   const Sums &hi = first ? a : b, &lo = first ? b : a;
   float s, t = lo.t;
-  rebase(1.f + lo.s, t, s, lo.m, hi.m, scale2);
-  return Sums{hi.m, hi.s + s, hi.t + t};
+  rebase(lo.one + lo.s, t, s, lo.m, hi.m, scale2);
+  return Sums{hi.m, hi.s + s, hi.t + t, hi.one};
 }
 
+// The largest of the warp's values (the others if some are no numbers).
+__device__ __forceinline__ float warp_max(float v) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// The logits of a 16-byte vector: as floats, their largest, and with the first that equals
+// `v` made -infinity (true if there is one).
 __device__ __forceinline__ void unpack16(const uint4 &u, const float *, float *x) {
   x[0] = __uint_as_float(u.x);
   x[1] = __uint_as_float(u.y);
@@ -94,6 +116,41 @@ __device__ __forceinline__ void unpack16(const uint4 &u, const __nv_bfloat16 *, 
     x[2 * i] = __uint_as_float(w[i] << 16);
     x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
   }
+}
+__device__ __forceinline__ float max16(const uint4 &u, const float *) {
+  return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)),
+               fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+}
+__device__ __forceinline__ uint32_t max_pairs(uint32_t a, uint32_t b) {  // of two bf16 each
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ float max16(const uint4 &u, const __nv_bfloat16 *) {
+  const uint32_t m = max_pairs(max_pairs(u.x, u.y), max_pairs(u.z, u.w));
+  return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+}
+__device__ __forceinline__ bool take(uint32_t &w, float v, const float *) {
+  const bool is = __uint_as_float(w) == v;
+  if (is) w = 0xff800000u;
+  return is;
+}
+__device__ __forceinline__ bool take(uint32_t &w, float v, const __nv_bfloat16 *) {
+  const bool low = __uint_as_float(w << 16) == v;
+  const bool high = !low && __uint_as_float(w & 0xffff0000u) == v;
+  if (low) w = (w & 0xffff0000u) | 0xff80u;
+  if (high) w = (w & 0xffffu) | 0xff800000u;
+  return low || high;
+}
+template <typename T>
+__device__ __forceinline__ bool take16(uint4 &u, float v, const T *type) {
+  return take(u.x, v, type) || take(u.y, v, type) || take(u.z, v, type) || take(u.w, v, type);
+}
+__device__ __forceinline__ uint4 none16(const float *) {  // a vector of -infinity
+  return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
+}
+__device__ __forceinline__ uint4 none16(const __nv_bfloat16 *) {
+  return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
 }
 
 // A row as vectors of 16 bytes: vector v holds elements v * E - lead .. , of which only
@@ -116,6 +173,24 @@ struct Row {
   __device__ __forceinline__ uint4 load(int v) const {
     return __ldcg(reinterpret_cast<const uint4 *>(x + first(v)));
   }
+  // A partial vector as it would lie there, -infinity where the row has no element.
+  __device__ __forceinline__ uint4 get_raw(int v) const {
+    return make_uint4(word(v, 0), word(v, 1), word(v, 2), word(v, 3));
+  }
+  __device__ __forceinline__ uint32_t word(int v, int w) const {
+    uint32_t r = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+#pragma unroll
+    for (int e = 0; e < E / 4; ++e) {
+      const int i = first(v) + w * (E / 4) + e;
+      if (i < 0 || i >= vocab) continue;
+      if (sizeof(T) == 4)
+        r = reinterpret_cast<const uint32_t *>(x)[i];
+      else
+        r = e == 0 ? (r & 0xffff0000u) | reinterpret_cast<const uint16_t *>(x)[i]
+                   : (r & 0xffffu) | (uint32_t)reinterpret_cast<const uint16_t *>(x)[i] << 16;
+    }
+    return r;
+  }
   // Elements of any vector; -infinity where the row has none.
   __device__ __forceinline__ void get(int v, float (&y)[E]) const {
     if (whole(v)) {
@@ -130,67 +205,90 @@ struct Row {
   }
 };
 
-// A lane's part of the warp's running sums. The warp's m is the same on every lane; the
-// lane that `owns` the logit m has left it out of its s.
+// A lane's part of the warp's running sums. m is the same on every lane; the lane that
+// `owns` a logit m has left it out of its s. m begins as the largest logit of the CTA's
+// first chunk, so that it rarely moves.
+template <typename T>
 struct Lane {
-  float m = -INFINITY, top = -INFINITY;  // the warp's largest, this lane's own
+  float m, top = -INFINITY;  // of the warp, and this lane's own largest
   float2 s = make_float2(0.f, 0.f), t = make_float2(0.f, 0.f);
   bool owns = false;
 
-  // N logits of every lane (-infinity for none).
   template <int N>
-  __device__ __forceinline__ void add(const float (&x)[N], float scale2, int lane) {
-    float g = x[0];
+  static __device__ __forceinline__ float largest(const uint4 (&u)[N]) {
+    const T *type = nullptr;
+    float g = max16(u[0], type);
 #pragma unroll
-    for (int e = 1; e < N; ++e) g = fmaxf(g, x[e]);
-    top = fmaxf(top, g);
-    int skip = -1;
+    for (int i = 1; i < N; ++i) g = fmaxf(g, max16(u[i], type));
+    return g;
+  }
+  // The first lane that has a logit m takes it out of u, its largest being g.
+  template <int N>
+  __device__ __forceinline__ void own(uint4 (&u)[N], float g, int lane) {
+    owns = lane == __ffs(__ballot_sync(kAll, g == m)) - 1;
+    if (owns) {
+      const T *type = nullptr;
+      bool taken = false;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (!taken) taken = take16(u[i], m, type);
+    }
+  }
+  // N vectors of every lane, this lane's largest being g.
+  template <int N>
+  __device__ __forceinline__ void add(uint4 (&u)[N], float g, float scale2, int lane) {
+    constexpr int E = 16 / (int)sizeof(T);
+    const T *type = nullptr;
     if (__any_sync(kAll, g > m)) {
-      float mn = g;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) mn = fmaxf(mn, __shfl_xor_sync(kAll, mn, o));
-      const float n = s.x + s.y + (owns ? 1.f : 0.f);
+      const float mn = warp_max(g);
       float ss, tt = t.x + t.y;
-      rebase(n, tt, ss, m, mn, scale2);
+      rebase(s.x + s.y + (owns ? 1.f : 0.f), tt, ss, m, mn, scale2);
       s = make_float2(ss, 0.f);
       t = make_float2(tt, 0.f);
       m = mn;
-      owns = lane == __ffs(__ballot_sync(kAll, g == mn)) - 1;
-      if (owns) {
-#pragma unroll
-        for (int e = N - 1; e >= 0; --e)
-          if (x[e] == mn) skip = e;
-      }
+      own(u, g, lane);
     }
-    const float m0 = fmaxf(m, -FLT_MAX);  // a warp with nothing but -infinity so far: w = 0
+    const float m0 = fmaxf(m, -FLT_MAX);  // nothing but -infinity so far: w = 0
     const float2 minus = make_float2(-m0, -m0), c = make_float2(scale2, scale2);
 #pragma unroll
-    for (int e = 0; e < N; e += 2) {
-      float2 d = __fadd2_rn(make_float2(x[e], x[e + 1]), minus);
-      const float2 y = __fmul2_rn(d, c);
-      float2 w = make_float2(fast_exp2(y.x), fast_exp2(y.y));
-      if (skip >= 0) {
-        if (skip == e) w.x = 0.f;
-        if (skip == e + 1) w.y = 0.f;
+    for (int i = 0; i < N; ++i) {
+      float x[E];
+      unpack16(u[i], type, x);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        float2 d = __fadd2_rn(make_float2(x[e], x[e + 1]), minus);
+        const float2 y = __fmul2_rn(d, c);
+        const float2 w = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+        s = __fadd2_rn(s, w);
+        d.x = fmaxf(d.x, -FLT_MAX);  // 0 times -infinity is no term
+        d.y = fmaxf(d.y, -FLT_MAX);
+        t = __ffma2_rn(w, d, t);
       }
-      s = __fadd2_rn(s, w);
-      d.x = fmaxf(d.x, -FLT_MAX);  // 0 times -infinity is no term
-      d.y = fmaxf(d.y, -FLT_MAX);
-      t = __ffma2_rn(w, d, t);
     }
   }
 };
 
 struct Smem {
+  uint4 ring[kStages][kVecs][kThreads];
+  float seg[kSegments][kThreads];  // largest logit of a segment's lane
   Key cand[kCands];
-  Key best[kMaxSlices][RIPPLE_MAX_TOP];  // of the slices, in the cluster's first CTA
-  Sums sums[kMaxSlices];
-  Sums warp[kWarps];
-  float group[32];
-  Key bound, kth;
-  int n_hot, n_cand;
-  uint16_t hot[kThreads];
+  Key best[kMaxSlices * RIPPLE_MAX_TOP];  // n_top of every slice, in the cluster's first CTA
+  Sums sums[kMaxSlices], warp[kWarps];
+  float first[kWarps], group[32];
+  uint16_t hot[kWarps][kSegments * 32];   // segment * 32 + lane
+  Key kth;
+  int n_cand;
 };
+
+__device__ __forceinline__ void copy16(void *dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src)
+               : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 
 // Ranks `n` keys by counting: f(rank, key) for each; equal keys (0: none) share a rank.
 template <typename F>
@@ -228,83 +326,150 @@ __device__ __forceinline__ void st_cluster(uint32_t at, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
 }
 
+// A CTA's slice of a row: vectors [v0, v1), of which [w0, w1) are whole and come through
+// the ring, chunk by chunk.
+template <typename T>
+struct Slice {
+  int v0, v1, w0, w1;
+  __device__ __forceinline__ Slice(const Row<T> &row, int slice, int slices) {
+    v0 = row.n_vec / slices * slice;  // the last slice has the rest
+    v1 = slice + 1 < slices ? v0 + row.n_vec / slices : row.n_vec;
+    w0 = v0 + (v0 < v1 && !row.whole(v0) ? 1 : 0);
+    w1 = max(w0, v1 - (v0 < v1 && !row.whole(v1 - 1) ? 1 : 0));
+  }
+  __device__ __forceinline__ int chunks() const { return (w1 - w0 + kChunkVecs - 1) / kChunkVecs; }
+  // The partial vectors: the first, the last, or -1.
+  __device__ __forceinline__ int partial(int which) const {
+    return which == 0 ? (w0 > v0 ? v0 : -1) : (v1 > w1 ? v1 - 1 : -1);
+  }
+};
+
+// The Sums of lanes 0 .. n - 1, n <= 8, merged in a fixed order; on every lane.
+__device__ __forceinline__ Sums merge_lanes(Sums a, int n, int lane, float scale2) {
+  if (lane >= n) a = Sums{-INFINITY, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int o = 1; o < 8; o *= 2) {
+    const Sums b{__shfl_xor_sync(kAll, a.m, o), __shfl_xor_sync(kAll, a.s, o),
+                 __shfl_xor_sync(kAll, a.t, o), __shfl_xor_sync(kAll, a.one, o)};
+    a = lane & o ? merge(b, a, scale2) : merge(a, b, scale2);
+  }
+  return Sums{__shfl_sync(kAll, a.m, 0), __shfl_sync(kAll, a.s, 0), __shfl_sync(kAll, a.t, 0),
+              __shfl_sync(kAll, a.one, 0)};
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     logprob_kernel(const __grid_constant__ LogprobParams p) {
-  __shared__ Smem s;
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  Smem &s = *reinterpret_cast<Smem *>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int row_i = blockIdx.x / p.slices;
-  const int slice = p.slices > 1 ? (int)cluster_rank() : 0;
+  const bool many = p.slices > 1;
+  const int slice = many ? (int)cluster_rank() : 0, r = blockIdx.x / p.slices;
+  const int n_top = p.n_top;
   pdl_launch_dependents();
   pdl_wait();
-  if (p.slices > 1) cluster_arrive();  // waited for before the first CTA's memory is written
+  if (many) cluster_arrive();  // waited for before the first CTA's memory is written
 
-  const Row<T> row(p, row_i);
-  constexpr int E = Row<T>::E;
-  const int v0 = (int)((long long)row.n_vec * slice / p.slices);
-  const int v1 = (int)((long long)row.n_vec * (slice + 1) / p.slices);
-
-  // the given token's logit, on its way while the row is read
+  const Row<T> row(p, r);
+  const Slice<T> part(row, slice, p.slices);
+  const int chunks = part.chunks();
+  auto fetch = [&](int c) {  // chunk c into its stage; the thread's vectors behind w1 are none
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int v = part.w0 + c * kChunkVecs + i * kThreads + tid;
+      if (v < part.w1) copy16(&s.ring[c % kStages][i][tid], row.x + row.first(v));
+    }
+  };
+#pragma unroll
+  for (int c = 0; c < kStages - 1; ++c) {
+    if (c < chunks) fetch(c);
+    copy_commit();
+  }
+  // the given token's logit, on its way while the row is read (the warp that writes it)
   float given = 0.f;
   int token = -1;
-  if (slice == 0 && tid == 0 && p.tokens != nullptr) {
-    token = p.tokens[row_i];
+  if (slice == 0 && warp == kWarps - 1 && p.tokens != nullptr) {
+    token = p.tokens[r];
     if (token >= 0 && token < p.vocab) given = to_f32(row.x[token]);
   }
+  if (tid == 0) s.n_cand = 0;
 
-  // Thread t has vectors v0 + t, v0 + t + kThreads, ..
-  Lane sum;
-  auto some = [&](int at) {  // one vector of every lane, partial ones and none among them
-    float x[E];
-    if (at < v1) {
-      row.get(at, x);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = -INFINITY;
-    }
-    sum.add(x, p.scale2, lane);
-  };
-  int at = v0 + warp * 32;  // the warp's next
-  if (v0 == 0 && row.lead != 0 && at < v1) {  // the row's first vector is partial
-    some(at + lane);
-    at += kThreads;
-  }
-  const int end = v1 - (v1 == row.n_vec && !row.whole(v1 - 1) ? 1 : 0);  // of whole vectors
-  for (; at + 31 + (kVecs - 1) * kThreads < end; at += kVecs * kThreads) {
+  Lane<T> sum;
+  sum.m = -INFINITY;
+  float largest = -INFINITY;                                 // of this lane
+  const int per_seg = (chunks + kSegments - 1) / kSegments;  // chunks of a segment
+  int seg = 0, in_seg = 0, stage = 0;
+  for (int c = 0; c < chunks; ++c) {
+    copy_wait<kStages - 2>();
     uint4 u[kVecs];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) u[i] = row.load(at + lane + i * kThreads);
+    for (int i = 0; i < kVecs; ++i) u[i] = s.ring[stage][i][tid];
+    if (part.w1 - part.w0 - c * kChunkVecs < kChunkVecs) {  // the last chunk
 #pragma unroll
-    for (int i = 0; i < kVecs; i += 8 / E) {
-      float x[8];
+      for (int i = 0; i < kVecs; ++i)
+        if (part.w0 + c * kChunkVecs + i * kThreads + tid >= part.w1) u[i] = none16(row.x);
+    }
+    // (the stage read in the turn before, by this thread alone)
+    const int ahead = c + kStages - 1;
+    if (ahead < chunks) {
+      const int to = stage > 0 ? stage - 1 : kStages - 1;
 #pragma unroll
-      for (int k = 0; k < 8 / E; ++k) unpack16(u[i + k], row.x, x + k * E);
-      sum.add(x, p.scale2, lane);
+      for (int i = 0; i < kVecs; ++i) {
+        const int v = part.w0 + ahead * kChunkVecs + i * kThreads + tid;
+        if (v < part.w1) copy16(&s.ring[to][i][tid], row.x + row.first(v));
+      }
+    }
+    copy_commit();
+    stage = stage + 1 < kStages ? stage + 1 : 0;
+    const float g = Lane<T>::largest(u);
+    sum.top = fmaxf(sum.top, g);
+    if (c == 0) {
+      const float mine = warp_max(g);
+      if (lane == 0) s.first[warp] = mine;
+      __syncthreads();
+      const float of = lane < kWarps ? s.first[lane] : -INFINITY;
+      sum.m = warp_max(of);
+      // the first warp that has it owns a logit
+      const int owner = __ffs(__ballot_sync(kAll, lane < kWarps && of == sum.m)) - 1;
+      if (sum.m > -INFINITY && warp == owner) sum.own(u, g, lane);
+    }
+    sum.add(u, g, p.scale2, lane);
+    if (++in_seg == per_seg || c == chunks - 1) {  // the segment's end
+      s.seg[seg++][tid] = sum.top;
+      largest = fmaxf(largest, sum.top);
+      sum.top = -INFINITY;
+      in_seg = 0;
     }
   }
-  for (; at < v1; at += kThreads) some(at + lane);
+  if (warp == 0 && (part.partial(0) >= 0 || part.partial(1) >= 0)) {
+    uint4 x[1] = {none16(row.x)};
+    if (lane < 2 && part.partial(lane) >= 0) x[0] = row.get_raw(part.partial(lane));
+    const float g = Lane<T>::largest(x);
+    largest = fmaxf(largest, g);  // (looked at apart from the segments)
+    sum.add(x, g, p.scale2, lane);
+  }
 
   // the warp, the slice
   {
     float ss = sum.s.x + sum.s.y, tt = sum.t.x + sum.t.y;
+    const bool one = __any_sync(kAll, sum.owns);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       ss += __shfl_xor_sync(kAll, ss, o);
       tt += __shfl_xor_sync(kAll, tt, o);
     }
-    if (lane == 0) s.warp[warp] = Sums{sum.m, sum.m == -INFINITY ? ss - 1.f : ss, tt};
+    if (lane == 0) s.warp[warp] = Sums{sum.m, ss, tt, one ? 1.f : 0.f};
   }
-  float g = sum.top;
+  float g = largest;
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(kAll, g, o));
-  if ((lane & 7) == 0) s.group[tid >> 3] = g;
-  if (tid == 0) s.n_hot = s.n_cand = 0;
+  for (int o = kGroup / 2; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(kAll, g, o));
+  if (lane % kGroup == 0) s.group[tid / kGroup] = g;
   __syncthreads();
 
-  const int n_top = p.n_top;
   if (n_top > 0) {
     // the n-th largest of the 32 groups' largest logits
-    if (warp == 0) {
+    Key bound;
+    {
       const uint32_t o = order_of(s.group[lane]);
       int above = 0;  // groups before this one, by value and then by lane
 #pragma unroll
@@ -312,33 +477,42 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
         const uint32_t other = __shfl_sync(kAll, o, i);
         above += other > o || (other == o && i < lane);
       }
-      if (above == n_top - 1) s.bound = (Key)o << 32;
+      const int at = __ffs(__ballot_sync(kAll, above == n_top - 1)) - 1;
+      bound = (Key)__shfl_sync(kAll, o, at) << 32;
     }
-    __syncthreads();
-    Key bound = s.bound;
-    // threads with candidates
-    const bool has = v0 + tid < v1;
-    if (has && (Key)order_of(sum.top) << 32 >= bound) s.hot[atomicAdd(&s.n_hot, 1)] = tid;
-    __syncthreads();
-    const int n_hot = s.n_hot;
+    // the warp's lanes' segments with candidates
+    int n_hot = 0;
+    if (__any_sync(kAll, (Key)order_of(largest) << 32 >= bound))
+      for (int i = 0; i < seg; ++i) {
+        const bool is = (Key)order_of(s.seg[i][tid]) << 32 >= bound;
+        const unsigned all = __ballot_sync(kAll, is);
+        if (is) s.hot[warp][n_hot + __popc(all & ((1u << lane) - 1))] = (uint16_t)(i * 32 + lane);
+        n_hot += __popc(all);
+      }
+    __syncwarp();
+    const int per = per_seg * kVecs;  // vectors of one, at most
     for (;;) {
-      for (int i = warp; i < n_hot; i += kWarps)
-        for (int u = v0 + s.hot[i] + lane * kThreads; u < v1; u += 32 * kThreads) {
-          float x[E];
-          row.get(u, x);
+      auto look = [&](int v) {
+        float x[Row<T>::E];
+        row.get(v, x);
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int idx = row.first(u) + e;
-            const Key k = key_of(x[e], idx);
-            if (k >= bound && idx >= 0 && idx < p.vocab) {
-              const int n = atomicAdd(&s.n_cand, 1);
-              if (n < kCands) s.cand[n] = k;
-            }
+        for (int e = 0; e < Row<T>::E; ++e) {
+          const int idx = row.first(v) + e;
+          const Key k = key_of(x[e], idx);
+          if (k >= bound && idx >= 0 && idx < p.vocab) {
+            const int at = atomicAdd(&s.n_cand, 1);
+            if (at < kCands) s.cand[at] = k;
           }
         }
+      };
+      for (int i = lane; i < n_hot * per; i += 32) {
+        const int hot = s.hot[warp][i / per];
+        const int v = part.w0 + (hot / 32 * per + i % per) * kThreads + warp * 32 + hot % 32;
+        if (v < part.w1) look(v);
+      }
+      if (tid < 2 && part.partial(tid) >= 0) look(part.partial(tid));
       __syncthreads();
-      const int n = s.n_cand;
-      if (n <= kCands) break;
+      if (s.n_cand <= kCands) break;
       // too many: a higher bound from those found
       rank_keys(s.cand, kCands, [&](int rank, Key k) {
         if (rank == n_top - 1) s.kth = k;
@@ -349,55 +523,39 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
       __syncthreads();
     }
   }
-  Key *best = s.best[0];  // the slice's n_top largest, descending (0: none)
-  if (p.slices > 1) cluster_wait();  // the first CTA runs
-  if (n_top > 0) {
-    const int n = s.n_cand;
-    const uint32_t to = p.slices > 1 ? in_first(s.best[slice]) : 0;
-    auto store = [&](int rank, Key k) {
-      if (rank >= n_top) return;
-      if (p.slices > 1)
-        st_cluster(to + rank * 8, k);
-      else
-        best[rank] = k;
-    };
-    rank_keys(s.cand, n, store);
-    if (tid >= n && tid < n_top) store(tid, 0);
-  }
-  Sums all = s.warp[0];
-  if (tid == 0) {
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) all = merge(all, s.warp[w], p.scale2);
-    if (p.slices > 1) {
+  Sums all = merge_lanes(s.warp[lane % kWarps], kWarps, lane, p.scale2);
+  const Key *keys = s.cand;
+  int n_keys = n_top > 0 ? s.n_cand : 0;
+  if (many) {
+    cluster_wait();  // the first CTA runs
+    if (n_top > 0) {
+      const uint32_t to = in_first(s.best + slice * n_top);
+      rank_keys(keys, n_keys, [&](int rank, Key k) {
+        if (rank < n_top) st_cluster(to + rank * 8, k);
+      });
+      if (tid >= n_keys && tid < n_top) st_cluster(to + tid * 8, (Key)0);
+    }
+    if (tid == 0) {
       const uint32_t to = in_first(&s.sums[slice]);
       st_cluster(to, all.m);
       st_cluster(to + 4, all.s);
       st_cluster(to + 8, all.t);
+      st_cluster(to + 12, all.one);
     }
-  }
-  if (p.slices > 1) {
     cluster_arrive();
     cluster_wait();
     if (slice != 0) return;
-    if (tid == 0) {
-      all = s.sums[0];
-      for (int i = 1; i < p.slices; ++i) all = merge(all, s.sums[i], p.scale2);
-    }
-    // the slices' alternatives, packed, and ranked again
-    if (n_top > 0) {
-      for (int i = tid; i < p.slices * n_top; i += kThreads)
-        s.cand[i] = s.best[i / n_top][i % n_top];
-      __syncthreads();
-      rank_keys(s.cand, p.slices * n_top, [&](int rank, Key k) {
-        if (rank < n_top) best[rank] = k;
-      });
-    }
+    all = merge_lanes(s.sums[lane % kMaxSlices], p.slices, lane, p.scale2);
+    keys = s.best;
+    n_keys = p.slices * n_top;
   }
-  if (tid == 0) {
-    if (all.m == INFINITY) all.s = NAN;
-    const float ls = log1pf(all.s);
-    if (p.lse != nullptr) p.lse[row_i] = all.m == -INFINITY ? all.m + 0.f * all.s : p.scale * all.m + ls;
-    if (p.entropy != nullptr) p.entropy[row_i] = ls - p.scale * all.t / (1.f + all.s);
+  if (all.m == INFINITY) all.s = NAN;
+  all.s -= 1.f - all.one;  // S' (no logit but -infinity: -1)
+  const float ls = log1pf(all.s);
+  if (warp == kWarps - 1 && lane == 0) {
+    if (p.lse != nullptr)
+      p.lse[r] = all.m == -INFINITY ? all.m + 0.f * all.s : p.scale * all.m + ls;
+    if (p.entropy != nullptr) p.entropy[r] = ls - p.scale * all.t / (1.f + all.s);
     if (p.logprob != nullptr) {
       float y = 0.f;
       if (token >= p.vocab) {
@@ -406,36 +564,41 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
       } else if (token >= 0) {
         y = p.scale * (given - all.m) - ls;
       }
-      p.logprob[row_i] = y;
+      p.logprob[r] = y;
     }
-    s.sums[0] = Sums{all.m, ls, 0.f};
   }
-  __syncthreads();
-  if (tid < n_top) {
-    const long long to = (long long)row_i * n_top + tid;
-    const Key k = best[tid];
+  rank_keys(keys, n_keys, [&](int rank, Key k) {
+    if (rank >= n_top) return;
+    const long long to = (long long)r * n_top + rank;
     p.top_idx[to] = (int)~(uint32_t)k;
     if (p.top_logprob != nullptr)
-      p.top_logprob[to] = p.scale * (value_of((uint32_t)(k >> 32)) - s.sums[0].m) - s.sums[0].s;
-  }
+      p.top_logprob[to] = p.scale * (value_of((uint32_t)(k >> 32)) - all.m) - ls;
+  });
 }
 
-// Slices of a row: enough CTAs for every place on the GPU, of at least kVecs vectors a
-// thread.
+// Slices of a row: as many CTAs as find a place at once, of two chunks at least.
 int slices_of(int n_rows, long long row_bytes) {
-  constexpr int kPlaces = 152 * kCtasPerSm;
   int c = 1;
-  while (c < kMaxSlices && (long long)n_rows * c < kPlaces &&
-         row_bytes >= 2LL * c * kThreads * 16 * kVecs)
+  while (c < kMaxSlices && (long long)n_rows * 2 * c <= kPlaces &&
+         row_bytes >= 2LL * c * kChunkVecs * 16)
     c *= 2;
   return c;
 }
 
 template <typename T>
-cudaError_t launch(const LogprobParams &p, cudaStream_t st) {
+cudaError_t launch(const LogprobParams &p, int dev, cudaStream_t st) {
+  static std::atomic<bool> attr_set[kMaxDevices];
+  static_assert(kCtasPerSm * (sizeof(Smem) + 1024) <= 228 * 1024, "shared memory per SM");
+  if (!attr_set[dev].load(std::memory_order_acquire)) {
+    const cudaError_t e = cudaFuncSetAttribute(
+        logprob_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+    if (e != cudaSuccess) return e;
+    attr_set[dev].store(true, std::memory_order_release);
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.n_rows * p.slices);
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = sizeof(Smem);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -483,6 +646,9 @@ extern "C" ripple_status ripple_token_logprobs(
                         logprob_out, entropy_out, lse_out, top_idx_out, top_logprob_out,
                         dev_status};
   cudaStream_t st = (cudaStream_t)stream;
-  RIPPLE_CUDA_TRY(dtype == RIPPLE_BF16 ? launch<__nv_bfloat16>(p, st) : launch<float>(p, st));
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return RIPPLE_ECUDA;
+  RIPPLE_CUDA_TRY(dtype == RIPPLE_BF16 ? launch<__nv_bfloat16>(p, dev, st)
+                                       : launch<float>(p, dev, st));
   return RIPPLE_OK;
 }

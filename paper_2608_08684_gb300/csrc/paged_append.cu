@@ -11,8 +11,10 @@
 //
 // Work: a head's d elements are spread over d / 16 lanes, each with the two 16-byte
 // (fp32: 32-byte) pieces that hold eight pairs, so that the eight sines and cosines
-// of a lane serve every head of the token that its warp takes. A token's
-// Hq + 2 Hkv head rows are cut into groups of 32 / (d / 16) rows, one per warp step.
+// of a lane serve every head of the token that its warp takes (the lanes that need the
+// same eight compute them together). A token's Hq + 2 Hkv head rows are cut into groups
+// of 32 / (d / 16) rows, one per warp step; with few tokens every warp takes one group,
+// with many a warp takes several, the loads of kAhead of them in flight at a time.
 #include <math.h>
 
 #include "common.cuh"
@@ -121,23 +123,53 @@ __device__ __forceinline__ int find_seq(const int32_t *starts, int B, int t, int
   }
 }
 
-template <typename T, int D, bool kInter>
+// kAhead: groups whose loads are in flight at a time.
+template <typename T, int D, bool kInter, int kAhead>
 __global__ void __launch_bounds__(kAppendWarps * 32)
     append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int kLanes = D / 16;       // lanes per head row
   constexpr int kRows = 32 / kLanes;   // head rows per warp step
+  pdl_launch_dependents();
+  pdl_wait();
   const int lane = threadIdx.x & 31;
-  const long long w = (long long)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
-  const int t = (int)(w / p.warps), part = (int)(w % p.warps);
+  const unsigned w = blockIdx.x * (unsigned)kAppendWarps + (threadIdx.x >> 5);
+  const int t = (int)(w / (unsigned)p.warps), part = (int)(w % (unsigned)p.warps);
   if (t >= p.n_tokens) return;
+  const int l = lane % kLanes, sub = lane / kLanes;
+  const bool turns = l < p.rot / 16;
+  const int o0 = turns && !kInter ? 8 * l : 16 * l;
+  const int o1 = turns && !kInter ? p.rot / 2 + 8 * l : 16 * l + 8;
+  const int n_rows = p.Hq + 2 * p.g.Hkv;
+  int b = 0, i = t;  // of seq_starts: found below
+  if (p.per_seq > 0) {
+    b = t / p.per_seq;
+    i = t - b * p.per_seq;
+  }
+
+  // The rows of kAhead groups from g on, as they are.
+  const int g_end = min(p.groups, (part + 1) * p.per_warp);
+  Raw8<T> x[kAhead], y[kAhead];
+  auto load = [&](int g, int b, int i) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int r = (g + u) * kRows + sub;
+      if (g + u >= g_end || r >= n_rows) continue;
+      const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.g.Hkv;
+      const TokenRows &src = is_q ? p.q : is_v ? p.v : p.k;
+      const int h = is_q ? r : is_v ? r - p.Hq - p.g.Hkv : r - p.Hq;
+      const T *from = (const T *)src.data + b * src.seq + i * src.token + h * src.head;
+      x[u] = load_raw(from + o0);
+      y[u] = load_raw(from + o1);
+    }
+  };
+  // where a token lies does not depend on its sequence with seq_starts (strides by t alone)
+  const int src_b = b, src_i = i;
+  int g = part * p.per_warp;
+  load(g, src_b, src_i);
 
   // the token's sequence, cache row and position
-  int b, i, n_b;
-  if (p.per_seq > 0) {
-    n_b = p.per_seq;
-    b = t / n_b;
-    i = t - b * n_b;
-  } else {
+  int n_b = p.per_seq;
+  if (p.per_seq == 0) {
     b = find_seq(p.starts, p.g.B, t, lane);
     if (b < 0) return;
     const int s0 = p.starts[b], s1 = p.starts[b + 1];
@@ -147,6 +179,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32)
   }
   const int len = p.lens[b];
   const long long row = (long long)len - n_b + i;
+  const long long pos = p.positions != nullptr ? (long long)p.positions[t] : row;
   int32_t bad = 0;
   long long place = -1;  // element offset of the row, head 0
   if (len > 0) {
@@ -164,60 +197,67 @@ __global__ void __launch_bounds__(kAppendWarps * 32)
     }
   }
   if (bad != 0 && part == 0 && lane == 0) report(p.status, bad);
-  const long long pos = p.positions != nullptr ? (long long)p.positions[t] : row;
 
-  const int l = lane % kLanes, sub = lane / kLanes;
-  const bool turns = l < p.rot / 16;
-  const int o0 = turns && !kInter ? 8 * l : 16 * l;
-  const int o1 = turns && !kInter ? p.rot / 2 + 8 * l : 16 * l + 8;
+  // Eight sines and cosines for every lane of the same l: each of the kRows lanes of that
+  // l computes its share.
   float c[8], s[8];
+  {
+    constexpr int kShare = 8 / kRows;  // 2 (d = 128) or 1 (d = 64)
+    float cs[kShare], sn[kShare];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    c[j] = 1.f;
-    s[j] = 0.f;
-    if (turns) cos_sin((unsigned long long)pos * p.freq[8 * l + j], c[j], s[j]);
+    for (int j = 0; j < kShare; ++j) {
+      cs[j] = 1.f;
+      sn[j] = 0.f;
+      if (turns) cos_sin((unsigned long long)pos * p.freq[8 * l + sub * kShare + j], cs[j], sn[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      c[j] = __shfl_sync(0xffffffffu, cs[j % kShare], j / kShare * kLanes + l);
+      s[j] = __shfl_sync(0xffffffffu, sn[j % kShare], j / kShare * kLanes + l);
+    }
   }
 
-  const int n_rows = p.Hq + 2 * p.g.Hkv;
-  const long long bs = p.per_seq > 0 ? b : 0, ts = p.per_seq > 0 ? i : t;
-  const int g_end = min(p.groups, (part + 1) * p.per_warp);
-  for (int g = part * p.per_warp; g < g_end; ++g) {
-    const int r = g * kRows + sub;
-    if (r >= n_rows) continue;
-    const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.g.Hkv;
-    const int h = is_q ? r : is_v ? r - p.Hq - p.g.Hkv : r - p.Hq;
-    const TokenRows &src = is_q ? p.q : is_v ? p.v : p.k;
-    if (!is_q && place < 0) continue;
-    const T *from = (const T *)src.data + bs * src.seq + ts * src.token + h * src.head;
-    T *to = is_q ? (T *)p.q_out.data + bs * p.q_out.seq + ts * p.q_out.token + h * p.q_out.head
-                 : (T *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
-    Raw8<T> x = load_raw(from + o0), y = load_raw(from + o1);
-    if (turns && !is_v) {
-      float a[8], d[8];
-      unpack(x, a);
-      unpack(y, d);
-      if (kInter) {  // pairs (0, 1), (2, 3), .. of the 16 elements a, d
+  for (;;) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float a0 = a[2 * j], a1 = a[2 * j + 1], d0 = d[2 * j], d1 = d[2 * j + 1];
-          a[2 * j] = a0 * c[j] - a1 * s[j];
-          a[2 * j + 1] = a1 * c[j] + a0 * s[j];
-          d[2 * j] = d0 * c[4 + j] - d1 * s[4 + j];
-          d[2 * j + 1] = d1 * c[4 + j] + d0 * s[4 + j];
-        }
-      } else {  // pairs (a_j, d_j)
+    for (int u = 0; u < kAhead; ++u) {
+      const int r = (g + u) * kRows + sub;
+      if (g + u >= g_end || r >= n_rows) continue;
+      const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.g.Hkv;
+      if (!is_q && place < 0) continue;
+      const int h = is_q ? r : is_v ? r - p.Hq - p.g.Hkv : r - p.Hq;
+      T *to = is_q ? (T *)p.q_out.data + src_b * p.q_out.seq + src_i * p.q_out.token +
+                         h * p.q_out.head
+                   : (T *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
+      if (turns && !is_v) {
+        float a[8], d[8];
+        unpack(x[u], a);
+        unpack(y[u], d);
+        if (kInter) {  // pairs (0, 1), (2, 3), .. of the 16 elements a, d
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float a0 = a[j], d0 = d[j];
-          a[j] = a0 * c[j] - d0 * s[j];
-          d[j] = d0 * c[j] + a0 * s[j];
+          for (int j = 0; j < 4; ++j) {
+            const float a0 = a[2 * j], a1 = a[2 * j + 1], d0 = d[2 * j], d1 = d[2 * j + 1];
+            a[2 * j] = a0 * c[j] - a1 * s[j];
+            a[2 * j + 1] = a1 * c[j] + a0 * s[j];
+            d[2 * j] = d0 * c[4 + j] - d1 * s[4 + j];
+            d[2 * j + 1] = d1 * c[4 + j] + d0 * s[4 + j];
+          }
+        } else {  // pairs (a_j, d_j)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float a0 = a[j], d0 = d[j];
+            a[j] = a0 * c[j] - d0 * s[j];
+            d[j] = d0 * c[j] + a0 * s[j];
+          }
         }
+        pack(a, x[u]);
+        pack(d, y[u]);
       }
-      pack(a, x);
-      pack(d, y);
+      store_raw(to + o0, x[u]);
+      store_raw(to + o1, y[u]);
     }
-    store_raw(to + o0, x);
-    store_raw(to + o1, y);
+    g += kAhead;
+    if (g >= g_end) break;
+    load(g, src_b, src_i);
   }
 }
 
@@ -238,14 +278,29 @@ unsigned long long to_turns(double inv_freq) {
   return inv_freq < 0 ? 0ULL - turns : turns;
 }
 
+template <typename T, int D, bool kInter, int kAhead>
+cudaError_t launch_as(const AppendParams &p, int grid, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kAppendWarps * 32);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, append_kernel<T, D, kInter, kAhead>, p);
+  count_launches(1);
+  return e;
+}
+
 template <typename T, int D>
 cudaError_t launch(const AppendParams &p, bool inter, int grid, cudaStream_t st) {
-  if (inter)
-    append_kernel<T, D, true><<<grid, kAppendWarps * 32, 0, st>>>(p);
-  else
-    append_kernel<T, D, false><<<grid, kAppendWarps * 32, 0, st>>>(p);
-  count_launches(1);
-  return cudaGetLastError();
+  constexpr int kMany = sizeof(T) == 2 ? 4 : 2;  // 8 loads of a lane in flight
+  if (p.per_warp == 1)
+    return inter ? launch_as<T, D, true, 1>(p, grid, st) : launch_as<T, D, false, 1>(p, grid, st);
+  return inter ? launch_as<T, D, true, kMany>(p, grid, st)
+               : launch_as<T, D, false, kMany>(p, grid, st);
 }
 
 // A tensor of tokens: pointer and strides in place, and for outputs disjoint places.
@@ -319,10 +374,14 @@ extern "C" ripple_status ripple_paged_append(
   p.status = dev_status;
   const int rows = 32 / (desc->head_dim / 16);
   p.groups = (p.Hq + 2 * p.g.Hkv + rows - 1) / rows;
-  p.per_warp = 1;
-  p.warps = p.groups;
+  // one group a warp while all warps find a place at once, then more
+  constexpr int kPlaces = 152 * 32;
+  const long long steps = (long long)n_tokens * p.groups;
+  p.warps = (int)std::max<long long>(1, std::min<long long>(p.groups, kPlaces * (long long)p.groups / steps));
+  p.per_warp = (p.groups + p.warps - 1) / p.warps;
+  p.warps = (p.groups + p.per_warp - 1) / p.per_warp;
   const long long ctas = ((long long)n_tokens * p.warps + kAppendWarps - 1) / kAppendWarps;
-  if (ctas > 0x7fffffffLL) return RIPPLE_EINVAL;
+  if (ctas > 0x7fffffffLL / kAppendWarps) return RIPPLE_EINVAL;
   cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e;
   if (desc->dtype == RIPPLE_BF16)

@@ -9,6 +9,7 @@ module fails loudly if the library has not been built.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -377,14 +378,33 @@ def ripple_decode_attn_noalloc(desc: DecodeDesc, q, k_new, v_new, tables: Decode
 MAX_TOP = 32
 
 
-def _here(device: int, *tensors):
-    """The call's tensors lie on `device`, and it is the current one (whose current
-    stream the call is given to)."""
+# A decode step makes these calls once per layer, so that the time of their checks counts:
+# a layout (shape and strides) is looked over once.
+
+
+def _wrong_device(device, *tensors):
+    """Raises for a call whose tensors do not all lie on the current device."""
     if _current_device() != device:
-        raise ValueError(f"the tensors are on cuda:{device}, the current device is another")
+        raise ValueError(f"the tensors are on device {device}, the current one is another")
     for t in tensors:
         if t is not None and t.get_device() != device:
             raise ValueError(f"expected a tensor on cuda:{device}")
+    raise ValueError("expected contiguous tensors")
+
+
+@functools.lru_cache(maxsize=256)
+def _token_layout(shape, st, ragged: bool, head_dim: int):
+    """(strides, leading sizes, heads) of a tensor of tokens of that shape and stride."""
+    if len(shape) == 3:
+        lead, strides = shape[:1], (0, st[0], st[1]) if ragged else (st[0], 0, st[1])
+    elif len(shape) == 4 and not ragged:
+        lead, strides = shape[:2], st[:3]
+    else:
+        raise ValueError("tokens must be [B][heads][d] or [B][n][heads][d]; with seq_starts "
+                         "[tokens][heads][d]")
+    if shape[-1] != head_dim or st[-1] != 1:
+        raise ValueError("tokens must be [..][heads][d], the dims consecutive")
+    return ctypes.byref(TokenStrides(*strides)), lead, shape[-2]
 
 
 class PagedCache:
@@ -405,7 +425,7 @@ class PagedCache:
         B, width = block_table.shape
         self.table = _ptr(block_table)
         self.device = k_pages.get_device()
-        if not k_pages.is_cuda or v_pages.get_device() != self.device or \
+        if self.device < 0 or v_pages.get_device() != self.device or \
                 block_table.get_device() != self.device:
             raise ValueError("expected CUDA tensors on one device")
         self.batch, self.n_kv_heads, self.head_dim, self.dtype = B, H, d, k_pages.dtype
@@ -428,23 +448,6 @@ class Rope:
         self._ref = ctypes.byref(self.desc)
 
 
-def _tokens(t, heads, cache, ragged):
-    """(pointer, strides, leading sizes) of a tensor of tokens."""
-    shape, st = t.shape, t.stride()
-    if t.dtype != cache.dtype or shape[-2:] != (heads, cache.head_dim) or st[-1] != 1:
-        raise ValueError("tokens must be [..][heads][d] in the cache's dtype, dims consecutive")
-    if len(shape) == 3:
-        lead, strides = shape[:1], (0, st[0], st[1]) if ragged else (st[0], 0, st[1])
-    elif len(shape) == 4 and not ragged:
-        lead, strides = shape[:2], st[:3]
-    else:
-        raise ValueError("tokens must be [B][heads][d] or [B][n][heads][d]; with seq_starts "
-                         "[tokens][heads][d]")
-    if not ragged and lead[0] != cache.batch:
-        raise ValueError("one entry per sequence")
-    return t.data_ptr(), ctypes.byref(TokenStrides(*strides)), lead
-
-
 def ripple_paged_append(cache: PagedCache, lens, k, v, rope: Rope | None = None, positions=None,
                         seq_starts=None, q=None, q_out=None, dev_status=None, stream=None):
     """Store new tokens' keys and values in the cache's pages, the keys rotated, and rotate
@@ -453,34 +456,53 @@ def ripple_paged_append(cache: PagedCache, lens, k, v, rope: Rope | None = None,
     with the query heads; any strides with the dims consecutive. lens (int32 [B]) counts the
     new tokens; positions: int32, k's leading sizes, or None (a token's cache row)."""
     ragged = seq_starts is not None
-    kp, ks, lead = _tokens(k, cache.n_kv_heads, cache, ragged)
-    vp, vs, vlead = _tokens(v, cache.n_kv_heads, cache, ragged)
-    if vlead != lead:
-        raise ValueError("k and v must have the same tokens")
-    n = lead.numel()
-    qp = qs = op = os_ = None
+    d, device, dtype = cache.head_dim, cache.device, cache.dtype
+    ks, lead, heads = _token_layout(k.shape, k.stride(), ragged, d)
+    vs, vlead, vheads = _token_layout(v.shape, v.stride(), ragged, d)
+    if vlead != lead or heads != cache.n_kv_heads or vheads != heads:
+        raise ValueError("k and v must have the same tokens and the cache's heads")
+    if not ragged and lead[0] != cache.batch:
+        raise ValueError("one entry per sequence")
+    same = k.dtype is dtype and v.dtype is dtype
+    fine = (_current_device() == device and k.get_device() == device and
+            v.get_device() == device and lens.get_device() == device and lens.is_contiguous())
+    qp = qs = op = os_ = pp = sp = None
     heads = 0
     if q is not None:
-        heads = q.shape[-2]
-        qp, qs, qlead = _tokens(q, heads, cache, ragged)
         if q_out is None:
             raise ValueError("q needs q_out")
-        op, os_, olead = _tokens(q_out, heads, cache, ragged)
-        if qlead != lead or olead != lead:
-            raise ValueError("q and q_out must have k's tokens")
+        qs, qlead, heads = _token_layout(q.shape, q.stride(), ragged, d)
+        os_, olead, oheads = _token_layout(q_out.shape, q_out.stride(), ragged, d)
+        if qlead != lead or olead != lead or oheads != heads:
+            raise ValueError("q and q_out must have k's tokens, and the same heads")
+        same = same and q.dtype is dtype and q_out.dtype is dtype
+        fine = fine and q.get_device() == device and q_out.get_device() == device
+        qp, op = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out needs q")
-    if positions is not None and (positions.dtype != torch.int32 or positions.shape != lead):
-        raise ValueError("positions must be int32 with k's leading sizes")
-    if lens.dtype != torch.int32 or lens.numel() != cache.batch:
+    if not same:
+        raise ValueError("tokens must be in the cache's dtype")
+    if positions is not None:
+        if positions.dtype is not torch.int32 or positions.shape != lead:
+            raise ValueError("positions must be int32 with k's leading sizes")
+        fine = fine and positions.get_device() == device and positions.is_contiguous()
+        pp = positions.data_ptr()
+    if ragged:
+        if seq_starts.dtype is not torch.int32 or seq_starts.numel() != cache.batch + 1:
+            raise ValueError("seq_starts must be int32 [B + 1]")
+        fine = fine and seq_starts.get_device() == device and seq_starts.is_contiguous()
+        sp = seq_starts.data_ptr()
+    if lens.dtype is not torch.int32 or lens.numel() != cache.batch:
         raise ValueError("lens must be int32 [B]")
-    if ragged and (seq_starts.dtype != torch.int32 or seq_starts.numel() != cache.batch + 1):
-        raise ValueError("seq_starts must be int32 [B + 1]")
-    _here(cache.device, lens, k, v, positions, seq_starts, q, q_out, dev_status)
-    st = _lib.ripple_paged_append(cache._ref, rope._ref if rope is not None else None, n,
-                                  _ptr(seq_starts), heads, qp, qs, op, os_, kp, ks, vp, vs,
-                                  _ptr(positions), cache.k, cache.v, cache.table, _ptr(lens),
-                                  _ptr(dev_status), _stream(stream))
+    if dev_status is not None:
+        fine = fine and dev_status.get_device() == device
+    if not fine:
+        _wrong_device(device, k, v, q, q_out, lens, positions, seq_starts, dev_status)
+    st = _lib.ripple_paged_append(cache._ref, None if rope is None else rope._ref, lead.numel(),
+                                  sp, heads, qp, qs, op, os_, k.data_ptr(), ks, v.data_ptr(), vs,
+                                  pp, cache.k, cache.v, cache.table, lens.data_ptr(),
+                                  None if dev_status is None else dev_status.data_ptr(),
+                                  _current_stream() if stream is None else _stream(stream))
     if st != OK:
         raise RippleError(st, "ripple_paged_append")
 
@@ -498,23 +520,35 @@ def ripple_paged_decode_attn(cache: PagedCache, q, lens, out, workspace, lse=Non
     """Attention of one token per sequence over the first lens[b] rows of the paged cache:
     q [B][Hq][d] (any strides with the dims consecutive), out fp32 [B][Hq][d], lse fp32
     [B][Hq] or None."""
-    shape, st = q.shape, q.stride()
-    if len(shape) != 3 or shape[0] != cache.batch or shape[2] != cache.head_dim or st[2] != 1 or \
-            q.dtype != cache.dtype:
-        raise ValueError("q must be [B][Hq][d] in the cache's dtype, dims consecutive")
-    if out.shape != shape or out.dtype != torch.float32:
+    shape = q.shape
+    strides, lead, heads = _token_layout(shape, q.stride(), False, cache.head_dim)
+    if len(shape) != 3 or lead[0] != cache.batch or q.dtype is not cache.dtype:
+        raise ValueError("q must be [B][Hq][d] in the cache's dtype")
+    if out.shape != shape or out.dtype is not torch.float32:
         raise ValueError("out must be fp32 [B][Hq][d]")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != shape[:2]):
-        raise ValueError("lse must be fp32 [B][Hq]")
-    if lens.dtype != torch.int32 or lens.numel() != cache.batch:
+    if lens.dtype is not torch.int32 or lens.numel() != cache.batch:
         raise ValueError("lens must be int32 [B]")
-    _here(cache.device, q, lens, out, lse, workspace, dev_status)
-    s = _lib.ripple_paged_decode_attn(cache._ref, shape[1], scale, q.data_ptr(),
-                                      ctypes.byref(TokenStrides(st[0], 0, st[1])), cache.k,
-                                      cache.v, cache.table, _ptr(lens), _ptr(out), _ptr(lse),
-                                      _ptr(workspace),
-                                      workspace.numel() * workspace.element_size(),
-                                      _ptr(dev_status), _stream(stream))
+    device = cache.device
+    fine = (_current_device() == device and q.get_device() == device and
+            lens.get_device() == device and out.get_device() == device and
+            workspace.get_device() == device and lens.is_contiguous() and out.is_contiguous() and
+            workspace.is_contiguous())
+    lp = None
+    if lse is not None:
+        if lse.dtype is not torch.float32 or lse.shape != shape[:2]:
+            raise ValueError("lse must be fp32 [B][Hq]")
+        fine = fine and lse.get_device() == device and lse.is_contiguous()
+        lp = lse.data_ptr()
+    if dev_status is not None:
+        fine = fine and dev_status.get_device() == device
+    if not fine:
+        _wrong_device(device, q, lens, out, workspace, lse, dev_status)
+    s = _lib.ripple_paged_decode_attn(cache._ref, heads, scale, q.data_ptr(),
+                                      strides, cache.k, cache.v,
+                                      cache.table, lens.data_ptr(), out.data_ptr(), lp,
+                                      workspace.data_ptr(), workspace.nbytes,
+                                      None if dev_status is None else dev_status.data_ptr(),
+                                      _current_stream() if stream is None else _stream(stream))
     if s != OK:
         raise RippleError(s, "ripple_paged_decode_attn")
 
@@ -526,34 +560,51 @@ def ripple_token_logprobs(logits, tokens=None, logprob_out=None, entropy_out=Non
     logits), logits [n][V] (any row stride), with the entropy, the log of the sum of the
     exponentials (fp32 [n] each) and the K largest logits' indices (int32 [n][K]) and log
     probabilities (fp32 [n][K]); outputs left None are not written."""
-    if logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] > 1:
+    shape, st = logits.shape, logits.stride()
+    if len(shape) != 2 or (st[1] != 1 and shape[1] > 1):
         raise ValueError("logits must be [n][V], a row's logits consecutive")
-    n, vocab = logits.shape
+    n, vocab = shape
+    device = logits.get_device()
+    if device < 0:
+        raise ValueError("expected a CUDA tensor")
+    fine = _current_device() == device
     if (tokens is None) != (logprob_out is None):
         raise ValueError("tokens and logprob_out go together")
-    if tokens is not None and (tokens.dtype != torch.int32 or tokens.numel() != n):
-        raise ValueError("tokens must be int32 [n]")
-    for t in (logprob_out, entropy_out, lse_out):
-        if t is not None and (t.dtype != torch.float32 or t.numel() != n):
-            raise ValueError("outputs must be fp32 [n]")
-    k = 0
+    ptrs = []
+    for t, dtype in ((tokens, torch.int32), (logprob_out, torch.float32),
+                     (entropy_out, torch.float32), (lse_out, torch.float32)):
+        if t is None:
+            ptrs.append(None)
+            continue
+        if t.dtype is not dtype or t.numel() != n:
+            raise ValueError("tokens must be int32 [n], outputs fp32 [n]")
+        fine = fine and t.get_device() == device and t.is_contiguous()
+        ptrs.append(t.data_ptr())
+    k, ip, lp = 0, None, None
     if top_idx is not None:
-        k = top_idx.shape[-1]
-        if top_idx.dtype != torch.int32 or top_idx.shape != (n, k):
+        tops = top_idx.shape
+        if top_idx.dtype is not torch.int32 or len(tops) != 2 or tops[0] != n:
             raise ValueError("top_idx must be int32 [n][K]")
-    if top_logprob is not None and (top_logprob.dtype != torch.float32 or
-                                    top_idx is None or top_logprob.shape != top_idx.shape):
-        raise ValueError("top_logprob must be fp32, top_idx's shape")
-    if not logits.is_cuda:
-        raise ValueError("expected a CUDA tensor")
-    _here(logits.get_device(), tokens, logprob_out, entropy_out, lse_out, top_idx, top_logprob,
-          dev_status)
-    st = _lib.ripple_token_logprobs(n, vocab, logits.stride(0), _DTYPES[logits.dtype], scale, k,
-                                    logits.data_ptr(), _ptr(tokens), _ptr(logprob_out),
-                                    _ptr(entropy_out), _ptr(lse_out), _ptr(top_idx),
-                                    _ptr(top_logprob), _ptr(dev_status), _stream(stream))
-    if st != OK:
-        raise RippleError(st, "ripple_token_logprobs")
+        k = tops[1]
+        fine = fine and top_idx.get_device() == device and top_idx.is_contiguous()
+        ip = top_idx.data_ptr()
+    if top_logprob is not None:
+        if top_idx is None or top_logprob.dtype is not torch.float32 or \
+                top_logprob.shape != top_idx.shape:
+            raise ValueError("top_logprob must be fp32, top_idx's shape")
+        fine = fine and top_logprob.get_device() == device and top_logprob.is_contiguous()
+        lp = top_logprob.data_ptr()
+    if dev_status is not None:
+        fine = fine and dev_status.get_device() == device
+    if not fine:
+        _wrong_device(device, tokens, logprob_out, entropy_out, lse_out, top_idx, top_logprob,
+                      dev_status)
+    s = _lib.ripple_token_logprobs(n, vocab, st[0], _DTYPES[logits.dtype], scale, k,
+                                   logits.data_ptr(), *ptrs, ip, lp,
+                                   None if dev_status is None else dev_status.data_ptr(),
+                                   _current_stream() if stream is None else _stream(stream))
+    if s != OK:
+        raise RippleError(s, "ripple_token_logprobs")
 
 
 # ----------------------------------------------------- sensitivity profiling
