@@ -1,4 +1,6 @@
-"""In-tree build of libripple.so (CUDA kernels for sm_103a + the host C allocator).
+"""In-tree build of libripple.so (CUDA kernels for sm_103a + the host C allocator) and of
+the extension module _binding.so (argument marshalling of the per-layer calls, against the
+installed Python and PyTorch).
 
 Each translation unit is compiled in parallel with nvcc (CUDA) or gcc (C), then
 linked with nvcc into paper_2608_08684_gb300/libripple.so. The build is skipped
@@ -16,6 +18,7 @@ from __future__ import annotations
 import concurrent.futures as cf
 import glob
 import os
+import shutil
 import subprocess
 import sys
 
@@ -26,6 +29,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libripple.so")
 BUILD_CHECKED = os.path.join(PKG, "_build_checked")
+BINDING_SRC = os.path.join(CSRC, "binding.cpp")
+BINDING = os.path.join(PKG, "_binding.so")
 LIB_CHECKED = os.path.join(PKG, "libripple_checked.so")
 
 NVCC = os.environ.get("NVCC", "nvcc")
@@ -43,11 +48,11 @@ def _deps():
     return _sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(INCLUDE, "*.h"))
 
 
-def _stale(lib: str) -> bool:
+def _stale(lib: str, deps=None) -> bool:
     if not os.path.exists(lib):
         return True
     t = os.path.getmtime(lib)
-    return any(os.path.getmtime(p) > t for p in _deps())
+    return any(os.path.getmtime(p) > t for p in deps or _deps())
 
 
 def _compile(src: str, extra: list, build_dir: str) -> str:
@@ -62,10 +67,40 @@ def _compile(src: str, extra: list, build_dir: str) -> str:
     return obj
 
 
+def build_binding(force: bool = False, verbose: bool = False) -> str:
+    """Build _binding.so if it is missing or older than its sources; return its path."""
+    if not force and not _stale(BINDING, [BINDING_SRC, os.path.join(INCLUDE, "ripple.h")]):
+        return BINDING
+    import sysconfig
+
+    import torch
+
+    at = os.path.join(os.path.dirname(torch.__file__), "")
+    nvcc = shutil.which(NVCC)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc))) if nvcc else "/usr/local/cuda"
+    tmp = BINDING + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", BINDING_SRC,
+           "-o", tmp, "-I", INCLUDE, "-I", at + "include",
+           "-I", at + "include/torch/csrc/api/include", "-I", os.path.join(cuda, "include"),
+           "-I", sysconfig.get_paths()["include"],
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-L", at + "lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+           f"-Wl,-rpath,{at}lib"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, BINDING)
+    if verbose:
+        print(f"built {BINDING}", file=sys.stderr)
+    return BINDING
+
+
 def build_library(force: bool = False, verbose: bool = False, extra_nvcc=(),
                   checked: bool = False) -> str:
     """Build libripple.so (libripple_checked.so with checked=True) if it is
-    missing or older than its sources; return its path."""
+    missing or older than its sources, and the binding's extension module; return the
+    library's path."""
+    build_binding(force, verbose)
     lib, build_dir = (LIB_CHECKED, BUILD_CHECKED) if checked else (LIB, BUILD)
     extra = list(extra_nvcc) + (["-DRIPPLE_CHECKED"] if checked else [])
     if not force and not _stale(lib):

@@ -366,7 +366,6 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
   const bool many = p.slices > 1;
   const int slice = many ? (int)cluster_rank() : 0, r = blockIdx.x / p.slices;
   const int n_top = p.n_top;
-  pdl_launch_dependents();
   pdl_wait();
   if (many) cluster_arrive();  // waited for before the first CTA's memory is written
 

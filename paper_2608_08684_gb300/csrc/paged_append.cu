@@ -24,7 +24,7 @@
 namespace ripple {
 namespace {
 
-constexpr int kAppendWarps = 8;  // per CTA
+constexpr int kAppendWarps = 4;  // per CTA (8: 142 us for 63k tokens of 48 head rows; 4: 131)
 constexpr int kMaxPairs = 64;
 
 struct TokenRows {
@@ -129,7 +129,6 @@ __global__ void __launch_bounds__(kAppendWarps * 32)
     append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int kLanes = D / 16;       // lanes per head row
   constexpr int kRows = 32 / kLanes;   // head rows per warp step
-  pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31;
   const unsigned w = blockIdx.x * (unsigned)kAppendWarps + (threadIdx.x >> 5);
@@ -278,6 +277,9 @@ unsigned long long to_turns(double inv_freq) {
   return inv_freq < 0 ? 0ULL - turns : turns;
 }
 
+// A programmatic dependent of the kernel before it, as that one ends: without a trigger in
+// it, since CTAs that wait in its SMs cost more (a batch of 108 tokens 5.2 us from a graph,
+// 3.7 without) than an earlier start gains (one token 2.9, 3.0).
 template <typename T, int D, bool kInter, int kAhead>
 cudaError_t launch_as(const AppendParams &p, int grid, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
@@ -296,7 +298,7 @@ cudaError_t launch_as(const AppendParams &p, int grid, cudaStream_t st) {
 
 template <typename T, int D>
 cudaError_t launch(const AppendParams &p, bool inter, int grid, cudaStream_t st) {
-  constexpr int kMany = sizeof(T) == 2 ? 4 : 2;  // 8 loads of a lane in flight
+  constexpr int kMany = sizeof(T) == 2 && D == 64 ? 4 : 2;  // 4 to 8 loads of a lane in flight
   if (p.per_warp == 1)
     return inter ? launch_as<T, D, true, 1>(p, grid, st) : launch_as<T, D, false, 1>(p, grid, st);
   return inter ? launch_as<T, D, true, kMany>(p, grid, st)

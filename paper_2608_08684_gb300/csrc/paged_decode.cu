@@ -26,8 +26,7 @@
 // A group that lies in one run is written there. Of the others every run leaves a partial
 // in the workspace (a run has two at most: of the group it begins within and of the one
 // it ends within), and the run with the group's first block a record of them; a second
-// launch, a programmatic dependent of the first that takes its place when the last runs
-// have begun, joins them in order.
+// launch, a programmatic dependent of the first, joins them in order.
 #include <math.h>
 
 #include <atomic>
@@ -591,7 +590,6 @@ __global__ void __launch_bounds__(32, kWarpsPerSm)
   using W = Walk<C::RB>;
   __shared__ __align__(128) uint8_t ring[kStages][2][kBlockBytes];  // [stage][K, V]
   const int lane = threadIdx.x, run = blockIdx.x;
-  pdl_launch_dependents();
   pdl_wait();
 
   // This run: blocks of all groups, lane by lane over the sequences.
@@ -776,7 +774,6 @@ __global__ void __launch_bounds__(kJoinThreads, 3)
   const int tid = threadIdx.x, warp = tid >> 5, head = blockIdx.y;
   if (tid == 0) n_few = n_many = 0;
   __syncthreads();
-  pdl_launch_dependents();
   pdl_wait();
   const int run = blockIdx.x * kJoinRuns + tid;
   if (tid < kJoinRuns && run < p.n_runs) {

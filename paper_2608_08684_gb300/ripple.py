@@ -1,6 +1,7 @@
 """Python binding of libripple.so (the C ABI declared in include/ripple.h).
 
-Argument marshalling only: every function here passes raw pointers, sizes and
+Argument marshalling only (ctypes; for the calls of every layer and token an extension
+module): every function here passes raw pointers, sizes and
 the current CUDA stream to the entry point of the same name, and raises
 RippleError on a non-zero status. All computation happens in the library's
 kernels (or, for ripple_alloc_budgets, in its host C code). Importing this
@@ -9,7 +10,7 @@ module fails loudly if the library has not been built.
 from __future__ import annotations
 
 import ctypes
-import functools
+import importlib.util
 import os
 
 import torch
@@ -22,6 +23,19 @@ if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built: call paper_2608_08684_gb300.build."
                       f"build_library(checked={CHECKED})")
 _lib = ctypes.CDLL(LIB_PATH)
+
+
+def _load_binding():
+    path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_binding.so")
+    if not os.path.exists(path):
+        raise ImportError(f"{path} is not built: call paper_2608_08684_gb300.build.build_library()")
+    spec = importlib.util.spec_from_file_location("_binding", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+_binding = _load_binding()
 
 F32, BF16 = 0, 1
 POOL_MAX, POOL_AVG, POOL_NONE = 0, 1, 2
@@ -178,13 +192,9 @@ def _ptr(t):
 try:
     from torch._C import _cuda_getCurrentRawStream, _cuda_getDevice
 except ImportError:
-    _current_device = torch.cuda.current_device
-
     def _current_stream():
         return torch.cuda.current_stream().cuda_stream
 else:
-    _current_device = _cuda_getDevice
-
     def _current_stream():
         return _cuda_getCurrentRawStream(_cuda_getDevice())
 
@@ -378,33 +388,11 @@ def ripple_decode_attn_noalloc(desc: DecodeDesc, q, k_new, v_new, tables: Decode
 MAX_TOP = 32
 
 
-# A decode step makes these calls once per layer, so that the time of their checks counts:
-# a layout (shape and strides) is looked over once.
-
-
-def _wrong_device(device, *tensors):
-    """Raises for a call whose tensors do not all lie on the current device."""
-    if _current_device() != device:
-        raise ValueError(f"the tensors are on device {device}, the current one is another")
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"expected a tensor on cuda:{device}")
-    raise ValueError("expected contiguous tensors")
-
-
-@functools.lru_cache(maxsize=256)
-def _token_layout(shape, st, ragged: bool, head_dim: int):
-    """(strides, leading sizes, heads) of a tensor of tokens of that shape and stride."""
-    if len(shape) == 3:
-        lead, strides = shape[:1], (0, st[0], st[1]) if ragged else (st[0], 0, st[1])
-    elif len(shape) == 4 and not ragged:
-        lead, strides = shape[:2], st[:3]
-    else:
-        raise ValueError("tokens must be [B][heads][d] or [B][n][heads][d]; with seq_starts "
-                         "[tokens][heads][d]")
-    if shape[-1] != head_dim or st[-1] != 1:
-        raise ValueError("tokens must be [..][heads][d], the dims consecutive")
-    return ctypes.byref(TokenStrides(*strides)), lead, shape[-2]
+# A decode step makes these calls once per layer, so that their host time counts: the
+# checks and the marshalling are those of the extension module (csrc/binding.cpp).
+_paged_append, _paged_decode_attn, _token_logprobs = (
+    ctypes.cast(f, _p).value for f in (_lib.ripple_paged_append, _lib.ripple_paged_decode_attn,
+                                       _lib.ripple_token_logprobs))
 
 
 class PagedCache:
@@ -423,16 +411,15 @@ class PagedCache:
             raise ValueError("block_table must be int32 [B][max_pages]")
         n_pages, H, ps, d = k_pages.shape
         B, width = block_table.shape
-        self.table = _ptr(block_table)
         self.device = k_pages.get_device()
         if self.device < 0 or v_pages.get_device() != self.device or \
                 block_table.get_device() != self.device:
             raise ValueError("expected CUDA tensors on one device")
-        self.batch, self.n_kv_heads, self.head_dim, self.dtype = B, H, d, k_pages.dtype
-        self.k, self.v = k_pages.data_ptr(), v_pages.data_ptr()
         self.desc = PagedDesc(B, H, d, ps, n_pages, width, _DTYPES[k_pages.dtype],
                               *k_pages.stride()[:3])
-        self._ref = ctypes.byref(self.desc)
+        self._handle = _binding.cache(ctypes.addressof(self.desc), k_pages.data_ptr(),
+                                      v_pages.data_ptr(), _ptr(block_table), self.device,
+                                      k_pages.dtype is torch.bfloat16)
         self._keep = (k_pages, v_pages, block_table)
 
 
@@ -445,7 +432,7 @@ class Rope:
         n = len(inv_freq)
         self._freq = (_f64 * n)(*[float(x) for x in inv_freq])
         self.desc = RopeDesc(2 * n, int(interleaved), self._freq)
-        self._ref = ctypes.byref(self.desc)
+        self._addr = ctypes.addressof(self.desc)
 
 
 def ripple_paged_append(cache: PagedCache, lens, k, v, rope: Rope | None = None, positions=None,
@@ -455,61 +442,16 @@ def ripple_paged_append(cache: PagedCache, lens, k, v, rope: Rope | None = None,
     [B][n][Hkv][d], or with seq_starts (int32 [B + 1]) [tokens][Hkv][d]; q, q_out likewise
     with the query heads; any strides with the dims consecutive. lens (int32 [B]) counts the
     new tokens; positions: int32, k's leading sizes, or None (a token's cache row)."""
-    ragged = seq_starts is not None
-    d, device, dtype = cache.head_dim, cache.device, cache.dtype
-    ks, lead, heads = _token_layout(k.shape, k.stride(), ragged, d)
-    vs, vlead, vheads = _token_layout(v.shape, v.stride(), ragged, d)
-    if vlead != lead or heads != cache.n_kv_heads or vheads != heads:
-        raise ValueError("k and v must have the same tokens and the cache's heads")
-    if not ragged and lead[0] != cache.batch:
-        raise ValueError("one entry per sequence")
-    same = k.dtype is dtype and v.dtype is dtype
-    fine = (_current_device() == device and k.get_device() == device and
-            v.get_device() == device and lens.get_device() == device and lens.is_contiguous())
-    qp = qs = op = os_ = pp = sp = None
-    heads = 0
-    if q is not None:
-        if q_out is None:
-            raise ValueError("q needs q_out")
-        qs, qlead, heads = _token_layout(q.shape, q.stride(), ragged, d)
-        os_, olead, oheads = _token_layout(q_out.shape, q_out.stride(), ragged, d)
-        if qlead != lead or olead != lead or oheads != heads:
-            raise ValueError("q and q_out must have k's tokens, and the same heads")
-        same = same and q.dtype is dtype and q_out.dtype is dtype
-        fine = fine and q.get_device() == device and q_out.get_device() == device
-        qp, op = q.data_ptr(), q_out.data_ptr()
-    elif q_out is not None:
-        raise ValueError("q_out needs q")
-    if not same:
-        raise ValueError("tokens must be in the cache's dtype")
-    if positions is not None:
-        if positions.dtype is not torch.int32 or positions.shape != lead:
-            raise ValueError("positions must be int32 with k's leading sizes")
-        fine = fine and positions.get_device() == device and positions.is_contiguous()
-        pp = positions.data_ptr()
-    if ragged:
-        if seq_starts.dtype is not torch.int32 or seq_starts.numel() != cache.batch + 1:
-            raise ValueError("seq_starts must be int32 [B + 1]")
-        fine = fine and seq_starts.get_device() == device and seq_starts.is_contiguous()
-        sp = seq_starts.data_ptr()
-    if lens.dtype is not torch.int32 or lens.numel() != cache.batch:
-        raise ValueError("lens must be int32 [B]")
-    if dev_status is not None:
-        fine = fine and dev_status.get_device() == device
-    if not fine:
-        _wrong_device(device, k, v, q, q_out, lens, positions, seq_starts, dev_status)
-    st = _lib.ripple_paged_append(cache._ref, None if rope is None else rope._ref, lead.numel(),
-                                  sp, heads, qp, qs, op, os_, k.data_ptr(), ks, v.data_ptr(), vs,
-                                  pp, cache.k, cache.v, cache.table, lens.data_ptr(),
-                                  None if dev_status is None else dev_status.data_ptr(),
-                                  _current_stream() if stream is None else _stream(stream))
+    st = _binding.paged_append(_paged_append, cache._handle, None if rope is None else rope._addr,
+                               lens, k, v, positions, seq_starts, q, q_out, dev_status,
+                               None if stream is None else _stream(stream))
     if st != OK:
         raise RippleError(st, "ripple_paged_append")
 
 
 def ripple_paged_decode_workspace_bytes(cache: PagedCache, n_q_heads: int) -> int:
     out = _sz()
-    _check(_lib.ripple_paged_decode_workspace_bytes(cache._ref, int(n_q_heads),
+    _check(_lib.ripple_paged_decode_workspace_bytes(ctypes.byref(cache.desc), int(n_q_heads),
                                                     ctypes.byref(out)),
            "ripple_paged_decode_workspace_bytes")
     return out.value
@@ -520,37 +462,11 @@ def ripple_paged_decode_attn(cache: PagedCache, q, lens, out, workspace, lse=Non
     """Attention of one token per sequence over the first lens[b] rows of the paged cache:
     q [B][Hq][d] (any strides with the dims consecutive), out fp32 [B][Hq][d], lse fp32
     [B][Hq] or None."""
-    shape = q.shape
-    strides, lead, heads = _token_layout(shape, q.stride(), False, cache.head_dim)
-    if len(shape) != 3 or lead[0] != cache.batch or q.dtype is not cache.dtype:
-        raise ValueError("q must be [B][Hq][d] in the cache's dtype")
-    if out.shape != shape or out.dtype is not torch.float32:
-        raise ValueError("out must be fp32 [B][Hq][d]")
-    if lens.dtype is not torch.int32 or lens.numel() != cache.batch:
-        raise ValueError("lens must be int32 [B]")
-    device = cache.device
-    fine = (_current_device() == device and q.get_device() == device and
-            lens.get_device() == device and out.get_device() == device and
-            workspace.get_device() == device and lens.is_contiguous() and out.is_contiguous() and
-            workspace.is_contiguous())
-    lp = None
-    if lse is not None:
-        if lse.dtype is not torch.float32 or lse.shape != shape[:2]:
-            raise ValueError("lse must be fp32 [B][Hq]")
-        fine = fine and lse.get_device() == device and lse.is_contiguous()
-        lp = lse.data_ptr()
-    if dev_status is not None:
-        fine = fine and dev_status.get_device() == device
-    if not fine:
-        _wrong_device(device, q, lens, out, workspace, lse, dev_status)
-    s = _lib.ripple_paged_decode_attn(cache._ref, heads, scale, q.data_ptr(),
-                                      strides, cache.k, cache.v,
-                                      cache.table, lens.data_ptr(), out.data_ptr(), lp,
-                                      workspace.data_ptr(), workspace.nbytes,
-                                      None if dev_status is None else dev_status.data_ptr(),
-                                      _current_stream() if stream is None else _stream(stream))
-    if s != OK:
-        raise RippleError(s, "ripple_paged_decode_attn")
+    st = _binding.paged_decode_attn(_paged_decode_attn, cache._handle, q, lens, out, workspace,
+                                    lse, scale, dev_status,
+                                    None if stream is None else _stream(stream))
+    if st != OK:
+        raise RippleError(st, "ripple_paged_decode_attn")
 
 
 def ripple_token_logprobs(logits, tokens=None, logprob_out=None, entropy_out=None, lse_out=None,
@@ -560,51 +476,11 @@ def ripple_token_logprobs(logits, tokens=None, logprob_out=None, entropy_out=Non
     logits), logits [n][V] (any row stride), with the entropy, the log of the sum of the
     exponentials (fp32 [n] each) and the K largest logits' indices (int32 [n][K]) and log
     probabilities (fp32 [n][K]); outputs left None are not written."""
-    shape, st = logits.shape, logits.stride()
-    if len(shape) != 2 or (st[1] != 1 and shape[1] > 1):
-        raise ValueError("logits must be [n][V], a row's logits consecutive")
-    n, vocab = shape
-    device = logits.get_device()
-    if device < 0:
-        raise ValueError("expected a CUDA tensor")
-    fine = _current_device() == device
-    if (tokens is None) != (logprob_out is None):
-        raise ValueError("tokens and logprob_out go together")
-    ptrs = []
-    for t, dtype in ((tokens, torch.int32), (logprob_out, torch.float32),
-                     (entropy_out, torch.float32), (lse_out, torch.float32)):
-        if t is None:
-            ptrs.append(None)
-            continue
-        if t.dtype is not dtype or t.numel() != n:
-            raise ValueError("tokens must be int32 [n], outputs fp32 [n]")
-        fine = fine and t.get_device() == device and t.is_contiguous()
-        ptrs.append(t.data_ptr())
-    k, ip, lp = 0, None, None
-    if top_idx is not None:
-        tops = top_idx.shape
-        if top_idx.dtype is not torch.int32 or len(tops) != 2 or tops[0] != n:
-            raise ValueError("top_idx must be int32 [n][K]")
-        k = tops[1]
-        fine = fine and top_idx.get_device() == device and top_idx.is_contiguous()
-        ip = top_idx.data_ptr()
-    if top_logprob is not None:
-        if top_idx is None or top_logprob.dtype is not torch.float32 or \
-                top_logprob.shape != top_idx.shape:
-            raise ValueError("top_logprob must be fp32, top_idx's shape")
-        fine = fine and top_logprob.get_device() == device and top_logprob.is_contiguous()
-        lp = top_logprob.data_ptr()
-    if dev_status is not None:
-        fine = fine and dev_status.get_device() == device
-    if not fine:
-        _wrong_device(device, tokens, logprob_out, entropy_out, lse_out, top_idx, top_logprob,
-                      dev_status)
-    s = _lib.ripple_token_logprobs(n, vocab, st[0], _DTYPES[logits.dtype], scale, k,
-                                   logits.data_ptr(), *ptrs, ip, lp,
-                                   None if dev_status is None else dev_status.data_ptr(),
-                                   _current_stream() if stream is None else _stream(stream))
-    if s != OK:
-        raise RippleError(s, "ripple_token_logprobs")
+    st = _binding.token_logprobs(_token_logprobs, logits, tokens, logprob_out, entropy_out,
+                                 lse_out, top_idx, top_logprob, scale, dev_status,
+                                 None if stream is None else _stream(stream))
+    if st != OK:
+        raise RippleError(st, "ripple_token_logprobs")
 
 
 # ----------------------------------------------------- sensitivity profiling
