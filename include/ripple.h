@@ -402,12 +402,13 @@ ripple_status ripple_decode_attn_noalloc(const ripple_decode_desc *desc, const v
  *              reported as RIPPLE_EFULL.
  */
 typedef struct {
-  int32_t batch;      /* B >= 1: sequences, rows of the block table */
+  int32_t batch;      /* B: sequences, rows of the block table, 1..65536 */
   int32_t n_kv_heads; /* Hkv >= 1 */
   int32_t head_dim;   /* d: 64 or 128 */
   int32_t page_size;  /* cache rows per page: a power of two, 1..1024 */
   int32_t n_pages;    /* pages of each pool, >= 1 */
-  int32_t max_pages;  /* entries per sequence of the block table, >= 1 */
+  int32_t max_pages;  /* entries per sequence of the block table, >= 1; with page_size
+                         fewer than 2^31 - 1024 rows */
   int32_t dtype;      /* ripple_dtype of the pages, q, k and v */
   int64_t page_stride, head_stride, row_stride;
 } ripple_paged_desc;

@@ -372,16 +372,18 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
   const Row<T> row(p, r);
   const Slice<T> part(row, slice, p.slices);
   const int chunks = part.chunks();
-  auto fetch = [&](int c) {  // chunk c into its stage; the thread's vectors behind w1 are none
+  auto fetch = [&](int c, int stage) {  // chunk c; the thread's vectors behind w1 are none
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
       const int v = part.w0 + c * kChunkVecs + i * kThreads + tid;
-      if (v < part.w1) copy16(&s.ring[c % kStages][i][tid], row.x + row.first(v));
+      if (v < part.w1)
+        copy16(&s.ring[stage][i][tid],
+               row.x + row.first((int)guard(v, 1, row.n_vec, p.status)));
     }
   };
 #pragma unroll
   for (int c = 0; c < kStages - 1; ++c) {
-    if (c < chunks) fetch(c);
+    if (c < chunks) fetch(c, c);
     copy_commit();
   }
   // the given token's logit, on its way while the row is read (the warp that writes it)
@@ -408,16 +410,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
       for (int i = 0; i < kVecs; ++i)
         if (part.w0 + c * kChunkVecs + i * kThreads + tid >= part.w1) u[i] = none16(row.x);
     }
-    // (the stage read in the turn before, by this thread alone)
-    const int ahead = c + kStages - 1;
-    if (ahead < chunks) {
-      const int to = stage > 0 ? stage - 1 : kStages - 1;
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i) {
-        const int v = part.w0 + ahead * kChunkVecs + i * kThreads + tid;
-        if (v < part.w1) copy16(&s.ring[to][i][tid], row.x + row.first(v));
-      }
-    }
+    // (into the stage read in the turn before, by this thread alone)
+    if (c + kStages - 1 < chunks) fetch(c + kStages - 1, stage > 0 ? stage - 1 : kStages - 1);
     copy_commit();
     stage = stage + 1 < kStages ? stage + 1 : 0;
     const float g = Lane<T>::largest(u);
@@ -507,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
       for (int i = lane; i < n_hot * per; i += 32) {
         const int hot = s.hot[warp][i / per];
         const int v = part.w0 + (hot / 32 * per + i % per) * kThreads + warp * 32 + hot % 32;
-        if (v < part.w1) look(v);
+        if (v < part.w1) look((int)guard(v, 1, row.n_vec, p.status));
       }
       if (tid < 2 && part.partial(tid) >= 0) look(part.partial(tid));
       __syncthreads();
@@ -568,7 +562,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
   }
   rank_keys(keys, n_keys, [&](int rank, Key k) {
     if (rank >= n_top) return;
-    const long long to = (long long)r * n_top + rank;
+    const long long to =
+        guard((long long)r * n_top + rank, 1, (long long)p.n_rows * n_top, p.status);
     p.top_idx[to] = (int)~(uint32_t)k;
     if (p.top_logprob != nullptr)
       p.top_logprob[to] = p.scale * (value_of((uint32_t)(k >> 32)) - all.m) - ls;

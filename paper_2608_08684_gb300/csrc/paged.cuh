@@ -48,8 +48,10 @@ inline bool paged_geom(const ripple_paged_desc *d, PagedGeom *g) {
   if (d->head_dim != 64 && d->head_dim != 128) return false;
   if (d->page_size < 1 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)) != 0)
     return false;
-  if ((int64_t)d->batch * d->n_kv_heads > (1 << 24)) return false;
-  if ((int64_t)d->max_pages * d->page_size > 0x7fffffffLL) return false;
+  // every CTA of the decode sums over the sequences
+  if (d->batch > (1 << 16) || (int64_t)d->batch * d->n_kv_heads > (1 << 24)) return false;
+  // row numbers are int32, a block's end behind the last one included
+  if ((int64_t)d->max_pages * d->page_size > 0x7fffffffLL - 1024) return false;
   g->B = d->batch;
   g->Hkv = d->n_kv_heads;
   g->D = d->head_dim;

@@ -188,11 +188,13 @@ __global__ void __launch_bounds__(kAppendWarps * 32)
     } else if (pg >= p.g.max_pages) {
       bad = RIPPLE_EFULL;
     } else {
-      const int page = p.table[(long long)b * p.g.max_pages + pg];
+      const int page = p.table[guard((long long)b * p.g.max_pages + pg, 1,
+                                     (long long)p.g.B * p.g.max_pages, p.status)];
       if ((unsigned)page >= (unsigned)p.g.n_pages)
         bad = RIPPLE_EBOUNDS;
       else
-        place = page * p.g.page_stride + (row & ((1 << p.g.shift) - 1)) * p.g.row_stride;
+        place = guard(page, 1, p.g.n_pages, p.status) * p.g.page_stride +
+                (row & ((1 << p.g.shift) - 1)) * p.g.row_stride;
     }
   }
   if (bad != 0 && part == 0 && lane == 0) report(p.status, bad);

@@ -1,4 +1,5 @@
-"""Per-layer decode loop over the ragged compressed caches, captured in a CUDA graph.
+"""Per-layer decode loops over the compressed caches, contiguous or in pages, captured in a
+CUDA graph.
 
 Sec. 4.1: during decoding each new query attends to the cached states, layer
 after layer; the paper's end-to-end decode throughput (Table 3) is measured
@@ -62,6 +63,71 @@ class LayerDecodeLoop:
         """Capture one step in a CUDA graph. Run issue_step() once outside the
         capture first (the library's first call on a device sets the decode
         kernel's attributes); that step appends like any other."""
+        self.graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(self.graph):
+            self.issue_step()
+        return self.graph
+
+    def replay(self):
+        self.graph.replay()
+
+
+class PagedDecodeLoop:
+    """One decode step of L layers over paged caches, for a batch whose sequences come and
+    go: per layer ripple_paged_append (the new token's keys rotated into their page, its
+    queries rotated) and ripple_paged_decode_attn.
+
+    caches: per layer a ripple.PagedCache (block tables for B sequences). Compressed rows
+        get into the pages by ripple_paged_append without a rotation, from
+        k_out[:, :, :n].transpose(1, 2) of ripple_compress_layer.
+    lens: device int32 [L][B], cache rows per layer and sequence; advanced by every step
+        (a compressed cache has its own length in every layer).
+    positions: device int32 [B], the next token's position; advanced by every step.
+    active: device int32 [B], 1 for the sequences of the step, 0 for idle places of the
+        batch, whose lens are 0.
+    rope: ripple.Rope, or None where queries and keys come rotated.
+    before(l): returns (q [B][Hq][d], k [B][Hkv][d], v [B][Hkv][d]) of layer l's new token,
+        not rotated, in the caches' dtype, any strides with the dims consecutive (views of
+        a fused projection's output); called while the step is issued (and captured).
+    after(l, out): consumes layer l's attention output out [B][Hq][d] fp32.
+
+    Pages are the caller's: before a step, every active sequence's table has an entry for
+    its next row. status holds RIPPLE_EFULL or RIPPLE_EBOUNDS where it had not.
+    """
+
+    def __init__(self, caches, lens, positions, active, n_q_heads, rope, before, after, scale=0.0):
+        if tuple(lens.shape) != (len(caches), positions.numel()):
+            raise ValueError("lens must be [layers][sequences]")
+        self.caches, self.before, self.after = list(caches), before, after
+        self.lens, self.positions, self.active = lens, positions, active
+        self.rope, self.scale = rope, scale
+        k = caches[0]._keep[0]
+        B, d = positions.numel(), k.shape[-1]
+        # calls are ordered on one stream, so every layer shares the scratch buffers
+        ws = max(R.ripple_paged_decode_workspace_bytes(c, n_q_heads) for c in caches)
+        self.ws = torch.empty(ws, dtype=torch.uint8, device=k.device)
+        self.q = torch.empty(B, n_q_heads, d, dtype=k.dtype, device=k.device)
+        self.out = [torch.empty(B, n_q_heads, d, dtype=torch.float32, device=k.device)
+                    for _ in caches]
+        self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self.graph = None
+
+    def issue_step(self):
+        """Enqueue one decode step of every layer on the current stream."""
+        self.lens.add_(self.active)  # the step's tokens count from here on
+        for l, cache in enumerate(self.caches):
+            q, k, v = self.before(l)
+            R.ripple_paged_append(cache, self.lens[l], k, v, rope=self.rope,
+                                  positions=self.positions, q=q, q_out=self.q,
+                                  dev_status=self.status)
+            R.ripple_paged_decode_attn(cache, self.q, self.lens[l], self.out[l], self.ws,
+                                       scale=self.scale, dev_status=self.status)
+            self.after(l, self.out[l])
+        self.positions.add_(self.active)
+
+    def capture(self):
+        """Capture one step in a CUDA graph. Run issue_step() once outside the capture
+        first; that step appends like any other."""
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(self.graph):
             self.issue_step()

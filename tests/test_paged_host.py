@@ -19,7 +19,8 @@ def _desc(lib, **over):
 BAD_DESCS = [
     dict(batch=0), dict(n_kv_heads=0), dict(head_dim=96), dict(page_size=0), dict(page_size=24),
     dict(page_size=2048), dict(n_pages=0), dict(max_pages=0), dict(dtype=2),
-    dict(max_pages=1 << 28),                                       # rows past int32
+    dict(max_pages=1 << 28), dict(max_pages=1 << 27),              # rows past int32
+    dict(batch=(1 << 16) + 1), dict(batch=1 << 16, n_kv_heads=257),
     dict(page_stride=-4096, head_stride=2048, row_stride=128),
     dict(page_stride=4096, head_stride=2048, row_stride=132),      # not 16 bytes
     dict(page_stride=4096, head_stride=2048, row_stride=64),       # rows overlap
