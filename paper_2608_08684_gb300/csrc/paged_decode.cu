@@ -27,6 +27,11 @@
 // in the workspace (a run has two at most: of the group it begins within and of the one
 // it ends within), and the run with the group's first block a record of them; a second
 // launch, a programmatic dependent of the first, joins them in order.
+//
+// Short caches (tables with room for few blocks a warp, as compressed caches have): a
+// cluster of up to eight CTAs of four warps takes a group, the warps equal parts of it,
+// and joins them through shared memory: one launch, no sums over the sequences and no
+// workspace (short_cluster).
 #include <math.h>
 
 #include <atomic>
@@ -68,7 +73,7 @@ struct PagedDecParams {
   const int32_t *table, *lens;
   float *out, *lse;
   int32_t *status;
-  int places, n_runs;
+  int places, n_runs;  // warps that find a place at once (short caches: CTAs of a cluster), runs
   int2 *rec;      // [n_runs] the group that begins in the run and goes on, and its runs (0: none)
   float *ws_o;    // [2 * n_runs][G][D] partial outputs: of the group begun before, begun here
   float2 *ws_ml;  // [2 * n_runs][G] their maximum and sum
@@ -183,37 +188,70 @@ struct Fetch {
   Walk<C::RB> w;
   int at;      // the next block's first row
   bool live;   // there is a next block
-  int entry;   // block-table entry of row at + lane % RB
+  int entry;   // block-table entry of the block, or of row at + lane % RB where it has several
   uint64_t policy;
   __device__ __forceinline__ void look_up(const PagedDecParams &p, int lane) {
-    const int row = at + lane % C::RB;
+    const int row = (1 << p.g.shift) >= C::RB ? at : at + lane % C::RB;
     entry = -1;
     if (row < w.end)
       entry = p.table[guard((long long)w.b * p.g.max_pages + (row >> p.g.shift), 1,
                             (long long)p.g.B * p.g.max_pages, p.status)];
   }
-  // Copies the block into `stage` and goes on; returns its live rows as bits.
+  // Copies the block into `stage` and goes on; returns its live rows as bits. A lane copies
+  // piece lane % PIECES of every kRowsPer-th row.
   __device__ __forceinline__ uint32_t issue(const PagedDecParams &p, uint8_t (*stage)[kBlockBytes],
                                             int lane) {
+    constexpr int kCopies = kBlockBytes / 512, kRowsPer = 32 / C::PIECES;
+    const int r0 = lane / C::PIECES, pc = lane % C::PIECES;
     uint32_t rows = 0;
     if (live) {
-      const int row = at + lane % C::RB;
-      const bool there = row < w.end, ok = there && (unsigned)entry < (unsigned)p.g.n_pages;
-      if (there && !ok) report(p.status, RIPPLE_EBOUNDS);
-      rows = __ballot_sync(kAll, ok) & (uint32_t)((1ull << C::RB) - 1);
-      const long long off = ok ? entry * p.g.page_stride +
-                                     (row & ((1 << p.g.shift) - 1)) * p.g.row_stride +
-                                     w.h * p.g.head_stride
-                               : 0;
-      const uint32_t ks = smem_u32(stage[0]), vs = smem_u32(stage[1]);
+      const uint32_t ks = smem_u32(stage[0]) + r0 * C::ROW_BYTES;
+      const uint32_t vs = smem_u32(stage[1]) + r0 * C::ROW_BYTES;
+      auto place = [&](int j) {  // in a stage, of the lane's copy j
+        return j * 512u + ((pc ^ C::swizzle(j * kRowsPer + r0)) << 4);
+      };
+      const long long in_page = (at & ((1 << p.g.shift) - 1)) * p.g.row_stride + w.h * p.g.head_stride;
+      if ((1 << p.g.shift) >= C::RB) {  // the block lies in one page
+        const int n = min(C::RB, w.end - at);
+        const bool ok = (unsigned)entry < (unsigned)p.g.n_pages;
+        if (!ok && lane == 0) report(p.status, RIPPLE_EBOUNDS);
+        rows = ok ? 0xffffffffu >> (32 - n) : 0u;
+        const long long off =
+            ok ? entry * p.g.page_stride + in_page + r0 * p.g.row_stride + pc * (16 / (int)sizeof(T))
+               : 0;
+        const T *k = (const T *)p.k_pages + off, *v = (const T *)p.v_pages + off;
+        const long long step = kRowsPer * p.g.row_stride;
+        if (rows == 0xffffffffu >> (32 - C::RB)) {
 #pragma unroll
-      for (int j = 0; j < kBlockBytes / 512; ++j) {
-        const int r = (j * 32 + lane) / C::PIECES, pc = (j * 32 + lane) % C::PIECES;
-        const long long o = __shfl_sync(kAll, off, r) + pc * (16 / (int)sizeof(T));
-        const uint32_t dst = r * C::ROW_BYTES + (pc ^ C::swizzle(r)) * 16;
-        const bool has = rows >> r & 1;
-        copy16(ks + dst, (const T *)p.k_pages + o, has, policy);
-        copy16(vs + dst, (const T *)p.v_pages + o, has, policy);
+          for (int j = 0; j < kCopies; ++j, k += step, v += step) {
+            copy16(ks + place(j), k, true, policy);
+            copy16(vs + place(j), v, true, policy);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < kCopies; ++j, k += step, v += step) {
+            const bool has = rows >> (j * kRowsPer + r0) & 1;
+            copy16(ks + place(j), has ? k : (const T *)p.k_pages, has, policy);
+            copy16(vs + place(j), has ? v : (const T *)p.v_pages, has, policy);
+          }
+        }
+      } else {  // a page for each lane's row
+        const int row = at + lane % C::RB;
+        const bool there = row < w.end, ok = there && (unsigned)entry < (unsigned)p.g.n_pages;
+        if (there && !ok) report(p.status, RIPPLE_EBOUNDS);
+        rows = __ballot_sync(kAll, ok) & (0xffffffffu >> (32 - C::RB));
+        const long long off = ok ? entry * p.g.page_stride +
+                                       (row & ((1 << p.g.shift) - 1)) * p.g.row_stride +
+                                       w.h * p.g.head_stride
+                                 : 0;
+#pragma unroll
+        for (int j = 0; j < kCopies; ++j) {
+          const int r = j * kRowsPer + r0;
+          const long long o = __shfl_sync(kAll, off, r) + pc * (16 / (int)sizeof(T));
+          const bool has = rows >> r & 1;
+          copy16(ks + place(j), (const T *)p.k_pages + o, has, policy);
+          copy16(vs + place(j), (const T *)p.v_pages + o, has, policy);
+        }
       }
       at += C::RB;
       if (at >= w.end) {
@@ -642,7 +680,7 @@ __global__ void __launch_bounds__(32, kWarpsPerSm)
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i)
     coming |= (uint64_t)fetch.issue(p, ring[i], lane) << (32 * i);
-  static_assert(kStages == 3, "two blocks on their way");
+  static_assert(kStages <= 3, "two blocks on their way at most");
 
   const long long n_rows = (long long)p.g.B * p.Hq;
   int2 rec = make_int2(0, 0);
@@ -656,7 +694,7 @@ __global__ void __launch_bounds__(32, kWarpsPerSm)
       __syncwarp();  // the block has landed, and the stage before it has been read
       const uint32_t live = (uint32_t)coming;
       const int fill = stage > 0 ? stage - 1 : kStages - 1;
-      coming = coming >> 32 | (uint64_t)fetch.issue(p, ring[fill], lane) << 32;
+      coming = coming >> 32 | (uint64_t)fetch.issue(p, ring[fill], lane) << (32 * (kStages - 2));
       rows.block(p, ring[stage], live, lane);
       stage = stage + 1 < kStages ? stage + 1 : 0;
     }
@@ -690,6 +728,169 @@ __global__ void __launch_bounds__(32, kWarpsPerSm)
   }
   copy_wait<0>();
   if (lane == 0) p.rec[rec_at] = rec;
+}
+
+// ------------------------------------------------------------ short caches
+constexpr int kShortWarps = 4;
+constexpr int kShortThreads = kShortWarps * 32;
+constexpr int kMaxCluster = 8;
+// Blocks that a warp gets at most, where the clusters leave SMs idle that runs would use, and
+// where they do not. Measured (bf16, D 128, 8 KV heads, us, clusters and runs): 1 sequence with
+// 4 heads a group: 470 rows 4.2 and 7.0, 2000 rows 6.6 and 8.0, 4000 rows 9.8 and 9.6, 8000 rows
+// 15.8 and 11.8; 16 sequences of up to 1000 rows 10.2 and 14.0, up to 4000 rows 30.4 and 33.5;
+// 64 of up to 1000 rows 32.3 and 37.5, with 8 heads a group 35.4 and 41.3, 16 heads 43.7 and 53.5.
+// The clusters lose where lengths are far apart (64 of 20 to 2000 rows: 27.8 and 26.4) and where
+// most warps have nothing to do (256 of up to 30 rows: 18.9 and 16.6).
+constexpr int kShortFew = 8, kShortMany = 32;
+
+template <typename T, int D, int G>
+struct ShortSmem {
+  struct alignas(16) Partial {  // read and written four outputs at a time
+    float o[G][D];
+    float2 ml[G];
+  };
+  static_assert(sizeof(Partial) % 16 == 0, "");
+  union Ring {
+    alignas(128) uint8_t stage[kStages][2][kBlockBytes];
+    Partial part;  // of the warp, when its blocks are done
+  };
+  Ring ring[kShortWarps];
+  int has[kShortWarps];  // the warp has blocks
+  Partial parts[1];      // of each of the cluster's CTAs, if there are several: this one's share
+  static constexpr int bytes(int ctas) {
+    return (int)(sizeof(ShortSmem) - sizeof(Partial) + (ctas > 1 ? ctas * sizeof(Partial) : 0));
+  }
+};
+
+__device__ __forceinline__ void axpy(float f, const float4 &x, float4 &y) {
+  y.x += f * x.x;
+  y.y += f * x.y;
+  y.z += f * x.z;
+  y.w += f * x.w;
+}
+// To the shared memory of a CTA of the cluster, at the place that `at` has in this one's.
+__device__ __forceinline__ uint32_t in_cta(const void *at, int cta) {
+  uint32_t to;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_u32(at)), "r"(cta));
+  return to;
+}
+__device__ __forceinline__ void st_cluster(uint32_t to, const float4 &v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(v.x), "f"(v.y),
+               "f"(v.z), "f"(v.w)
+               : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t to, const float2 &v) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(v.x), "f"(v.y) : "memory");
+}
+
+template <typename T, int D, int G>
+__global__ void __launch_bounds__(kShortThreads)
+    paged_short_kernel(const __grid_constant__ PagedDecParams p) {
+  using C = Cfg<T, D, G>;
+  using W = Walk<C::RB>;
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  ShortSmem<T, D, G> &s = *reinterpret_cast<ShortSmem<T, D, G> *>(smem_raw);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int ctas = p.places, shift = __ffs(ctas) - 1;  // of the cluster, a power of two
+  const int group = blockIdx.x >> shift, rank = blockIdx.x & (ctas - 1);
+  pdl_wait();
+  if (ctas > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  const int b = group / p.g.Hkv, h = group % p.g.Hkv;
+  if (h == 0 && rank == 0 && tid == 0 && (long long)p.lens[b] > (long long)p.g.max_pages << p.g.shift)
+    report(p.status, RIPPLE_EFULL);
+  const int len = clamp_len(p, b), blocks = W::blocks_of(len);
+  const int worker = rank * kShortWarps + warp, workers = ctas * kShortWarps;
+  const int first = blocks * worker / workers, last = blocks * (worker + 1) / workers;
+  if (first < last) {
+    Fetch<T, D, G> fetch;
+    fetch.policy = evict_first();
+    fetch.w.b = b;
+    fetch.w.h = h;
+    fetch.w.len = len;
+    fetch.w.block = first;
+    fetch.w.left = last - first;
+    fetch.w.set();
+    fetch.live = true;
+    fetch.at = fetch.w.begin;
+    fetch.look_up(p, lane);
+    const W at = fetch.w;
+    uint8_t(*ring)[2][kBlockBytes] = s.ring[warp].stage;
+    uint64_t coming = 0;
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i)
+      coming |= (uint64_t)fetch.issue(p, ring[i], lane) << (32 * i);
+    Rows<T, D, G> rows;
+    rows.start(p, at, lane);
+    int stage = 0;
+    for (int row = at.begin; row < at.end; row += C::RB) {
+      copy_wait<kStages - 2>();
+      __syncwarp();
+      const uint32_t live = (uint32_t)coming;
+      const int fill = stage > 0 ? stage - 1 : kStages - 1;
+      coming = coming >> 32 | (uint64_t)fetch.issue(p, ring[fill], lane) << (32 * (kStages - 2));
+      rows.block(p, ring[stage], live, lane);
+      stage = stage + 1 < kStages ? stage + 1 : 0;
+    }
+    rows.finish();
+    copy_wait<0>();
+    __syncwarp();
+    auto &part = s.ring[warp].part;
+    rows.outputs(lane, [&](int head, int d, const float2 &o) {
+      *reinterpret_cast<float2 *>(&part.o[head][d]) = o;
+    });
+    rows.stats(lane, [&](int head, float m, float l) { part.ml[head] = make_float2(m, l); });
+  }
+  if (lane == 0) s.has[warp] = first < last;
+  __syncthreads();
+  if (ctas > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");  // all of them run
+
+  // parts[i], i < n, joined in order, column by column of four outputs (from begin to end);
+  // those without rows (there(i) false) left out
+  const int cols = p.G * D / 4;
+  auto join = [&](int n, auto part_of, auto there, int begin, int end, auto put) {
+    for (int col = begin + tid; col < end; col += kShortThreads) {
+      const int head = col * 4 / D, d = col * 4 % D;
+      float m = -INFINITY, den = 0.f;
+      for (int i = 0; i < n; ++i)
+        if (there(i)) m = fmaxf(m, part_of(i).ml[head].x);
+      const float sub = m == -INFINITY ? 0.f : m;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < n; ++i) {
+        if (!there(i)) continue;
+        const float2 ml = part_of(i).ml[head];
+        const float f = fast_exp2(ml.x - sub);
+        axpy(f, *reinterpret_cast<const float4 *>(&part_of(i).o[head][d]), sum);
+        den += f * ml.y;
+      }
+      put(col, head, d, sum, m, den);
+    }
+  };
+  const long long row0 = guard((long long)b * p.Hq + h * p.G, p.G, (long long)p.g.B * p.Hq, p.status);
+  auto write = [&](int, int head, int d, const float4 &o, float m, float den) {
+    const float inv = den != 0.f ? 1.f / den : 0.f;  // 0: no row counts
+    *reinterpret_cast<float4 *>(&p.out[(row0 + head) * D + d]) =
+        make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (p.lse != nullptr && d == 0) p.lse[row0 + head] = lse_of(m, den);
+  };
+  auto of_warps = [&](int i) -> const typename ShortSmem<T, D, G>::Partial & { return s.ring[i].part; };
+  auto has = [&](int i) { return s.has[i] != 0; };
+  if (ctas == 1) {
+    join(kShortWarps, of_warps, has, 0, cols, write);
+    return;
+  }
+  // to the CTA whose share of the columns it is; D, the padded G and ctas are powers of two
+  const int share_shift = __ffs(G * D / 4) - 1 - shift;
+  join(kShortWarps, of_warps, has, 0, cols,
+       [&](int col, int head, int d, const float4 &o, float m, float den) {
+         const int to = col >> share_shift;
+         st_cluster(in_cta(&s.parts[rank].o[head][d], to), o);
+         if (d == 0 || (col & ((1 << share_shift) - 1)) == 0)
+           st_cluster(in_cta(&s.parts[rank].ml[head], to), make_float2(m, den));
+       });
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  join(ctas, [&](int i) -> const typename ShortSmem<T, D, G>::Partial & { return s.parts[i]; },
+       [](int) { return true; }, min(rank << share_shift, cols), min((rank + 1) << share_shift, cols), write);
 }
 
 // Joins the partials of the groups that begin in this CTA's kJoinRuns runs and go on, one
@@ -861,43 +1062,79 @@ size_t plan(PagedDecParams *p, int dtype, int sms, void *ws) {
 }
 
 cudaError_t launch_pdl(void (*kernel)(PagedDecParams), dim3 grid, int threads,
-                       const PagedDecParams &p, cudaStream_t st) {
+                       const PagedDecParams &p, cudaStream_t st, int smem = 0, int cluster = 1) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
   count_launches(1);
   return e;
 }
 
+// CTAs of a group's cluster where the table's room is short, 0 where it is not: as many as
+// find a place at once, and few blocks for each of their warps.
 template <typename T, int D, int G>
-cudaError_t launch(const PagedDecParams &p, cudaStream_t st) {
+int short_cluster(const PagedDecParams &p, int sms) {
+  auto places = [&](int ctas) {  // two CTAs an SM where their shared memory has room
+    return (2 * (ShortSmem<T, D, G>::bytes(ctas) + 1024) <= 228 * 1024 ? 2LL : 1LL) * sms;
+  };
+  const long long groups = (long long)p.g.B * p.g.Hkv;
+  int ctas = 1;
+  while (ctas < kMaxCluster && groups * 2 * ctas <= places(2 * ctas)) ctas *= 2;
+  const long long rows = (long long)p.g.max_pages << p.g.shift;
+  const int most = groups * ctas >= sms ? kShortMany : kShortFew;
+  return rows <= (long long)ctas * kShortWarps * most * Cfg<T, D, G>::RB ? ctas : 0;
+}
+
+template <typename T, int D, int G>
+cudaError_t launch(const PagedDecParams &p, int dev, cudaStream_t st) {
+  const int ctas = short_cluster<T, D, G>(p, sm_count(dev));
+  if (ctas > 0) {
+    static std::atomic<bool> attr_set[kMaxDevices];
+    constexpr int most = ShortSmem<T, D, G>::bytes(kMaxCluster);
+    static_assert(most <= 227 * 1024, "shared memory per CTA");
+    if (!attr_set[dev].load(std::memory_order_acquire)) {
+      const cudaError_t e = cudaFuncSetAttribute(
+          paged_short_kernel<T, D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+      if (e != cudaSuccess) return e;
+      attr_set[dev].store(true, std::memory_order_release);
+    }
+    PagedDecParams q = p;
+    q.places = ctas;
+    return launch_pdl(paged_short_kernel<T, D, G>, dim3(p.g.B * p.g.Hkv * ctas), kShortThreads, q,
+                      st, ShortSmem<T, D, G>::bytes(ctas), ctas);
+  }
   const cudaError_t e = launch_pdl(paged_decode_kernel<T, D, G>, dim3(p.n_runs), 32, p, st);
   if (e != cudaSuccess) return e;
-  const int ctas = (p.n_runs + kJoinRuns - 1) / kJoinRuns;
-  return launch_pdl(paged_join_kernel<D>, dim3(ctas, p.G), kJoinThreads, p, st);
+  const int runs = (p.n_runs + kJoinRuns - 1) / kJoinRuns;
+  return launch_pdl(paged_join_kernel<D>, dim3(runs, p.G), kJoinThreads, p, st);
 }
 
 // Heads of a group, padded: for the matrix instructions to 4, 8 or 16, on the CUDA
 // cores to a power of two.
 template <int D>
-cudaError_t launch_d(const PagedDecParams &p, int dtype, cudaStream_t st) {
+cudaError_t launch_d(const PagedDecParams &p, int dtype, int dev, cudaStream_t st) {
   if (dtype == RIPPLE_BF16) {
-    if (p.G <= 4) return launch<__nv_bfloat16, D, 4>(p, st);
-    if (p.G <= 8) return launch<__nv_bfloat16, D, 8>(p, st);
-    return launch<__nv_bfloat16, D, 16>(p, st);
+    if (p.G <= 4) return launch<__nv_bfloat16, D, 4>(p, dev, st);
+    if (p.G <= 8) return launch<__nv_bfloat16, D, 8>(p, dev, st);
+    return launch<__nv_bfloat16, D, 16>(p, dev, st);
   }
-  if (p.G == 1) return launch<float, D, 1>(p, st);
-  if (p.G == 2) return launch<float, D, 2>(p, st);
-  if (p.G <= 4) return launch<float, D, 4>(p, st);
-  if (p.G <= 8) return launch<float, D, 8>(p, st);
-  return launch<float, D, 16>(p, st);
+  if (p.G == 1) return launch<float, D, 1>(p, dev, st);
+  if (p.G == 2) return launch<float, D, 2>(p, dev, st);
+  if (p.G <= 4) return launch<float, D, 4>(p, dev, st);
+  if (p.G <= 8) return launch<float, D, 8>(p, dev, st);
+  return launch<float, D, 16>(p, dev, st);
 }
 
 }  // namespace
@@ -955,7 +1192,7 @@ extern "C" ripple_status ripple_paged_decode_attn(
   p.lse = lse;
   p.status = dev_status;
   cudaStream_t st = (cudaStream_t)stream;
-  RIPPLE_CUDA_TRY(desc->head_dim == 128 ? launch_d<128>(p, desc->dtype, st)
-                                        : launch_d<64>(p, desc->dtype, st));
+  RIPPLE_CUDA_TRY(desc->head_dim == 128 ? launch_d<128>(p, desc->dtype, dev, st)
+                                        : launch_d<64>(p, desc->dtype, dev, st));
   return RIPPLE_OK;
 }

@@ -49,6 +49,24 @@ def test_pages_and_layouts(lib, page, layout, dtype, G, H, d):
     _check(pool, q, lens, out, lse)
 
 
+# tables with room for little, as compressed caches have: clusters of 8, 4, 2 and 1 CTAs a
+# group, every number of query heads, warps without blocks
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [1, 2, 4, 7, 16])
+@pytest.mark.parametrize("lens,H", [([1], 1), ([0, 470, 33], 2), ([250, 100, 0, 1, 17, 249], 4),
+                                    ([100, 3, 64, 0, 31] * 9, 2), ([60, 0, 16, 1] * 50, 2)])
+def test_short_caches(lib, lens, H, G, d, dtype):
+    for page in (1, 32):
+        pool = P.Pool(lib, lens, H, d, page, dtype, 350 + G)
+        q = P.randn((len(lens), G * H, d), dtype, 351)
+        out, lse, st = P.run_decode(lib, pool, q, P.i32(lens))
+        assert int(st.item()) == 0
+        _check(pool, q, lens, out, lse)
+        again, lse2, _ = P.run_decode(lib, pool, q, P.i32(lens))
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
 # few long sequences (split and joined), many short ones, both at once
 @pytest.mark.parametrize("lens,H,G,d,dtype", [
     ([70001], 1, 8, 128, "bf16"), ([33333, 5], 2, 4, 64, "bf16"), ([20011], 1, 2, 128, "f32"),
