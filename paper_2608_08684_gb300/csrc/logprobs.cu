@@ -6,24 +6,29 @@
 //   log P(x) = scale d - log1p(S'),   entropy = log1p(S') - scale T / (1 + S').
 // Leaving the 1 out of the sum keeps the relative precision of log probabilities near 0.
 //
-// Work: one CTA per row, or with few rows one per slice of a row, the slices of a row being
-// a cluster (slices_of). Every thread copies its 16-byte vectors of the row into places of
-// its own in shared memory, kStages chunks ahead (asynchronous copies, waited for by the
-// thread alone), so that the loads in flight cost no registers and no barrier. A warp
-// keeps a maximum, which begins as the largest logit of the CTA's first chunk and so
-// rarely moves (a vote per chunk), and sums per lane. The warps are merged through shared
-// memory, the slices through the shared memory of the cluster's first CTA.
+// Work: one CTA of eight warps per row (of two for many short rows, launch_width), or with few
+// rows one per slice of a row, the slices of a row being a cluster (slices_of). Every thread
+// copies its 16-byte vectors of the row into places of its own in shared memory, kStages
+// chunks ahead (asynchronous copies, waited for by the thread alone), so that the loads in
+// flight cost no registers and no barrier. A warp keeps a maximum, which begins as the
+// largest logit of the CTA's first chunk and so rarely moves (a vote per chunk), and sums
+// per lane. The warps are merged through shared memory, the slices through the shared
+// memory of the cluster's first CTA.
 //
 // Alternatives: keys order logits descending, equal ones by index. The n-th largest of the
-// 32 largest logits of kGroup lanes each bounds the slice's n-th largest key from below.
+// largest logits of kGroups groups of lanes bounds the slice's n-th largest key from below
+// (64 groups and not 32: with 32 alternatives, the least of 32 groups' largest leaves three
+// times as many candidates; 138 and 109 us for 2048 rows of 128256).
 // The largest logit of every lane and segment of the slice (a few chunks) has been kept,
-// so only the segments that reach the bound are read once more (from L2, mostly), and the
-// candidates, a few more than n, are ranked by counting. Where there are more than fit
-// (many ties, sorted rows), the n-th largest of those found is a higher bound, and the
-// reading is repeated with it; every turn drops some.
+// so only the segments that reach the bound are read once more (from the ring if they are
+// its last chunks, from L2 mostly if not), and the candidates, a few more than n, are
+// ranked by counting. Where there are more than fit (many ties, sorted rows), the n-th
+// largest of those found is a higher bound, and the reading is repeated with it; every turn
+// drops some.
 //
-// Bound: the special-function units, 16 exponentials a clock and SM: 57 us for 2048 rows of
-// 128256, with HBM (77 us for bf16) close behind.
+// Bound: 2048 rows of 128256, bf16: HBM (77 us of 85 without alternatives, 94 with one), the
+// special-function units' 16 exponentials a clock and SM close behind (57 us). Many short rows:
+// the instructions that a row costs once (about as many as 14000 tokens by eight warps).
 #include <float.h>
 #include <math.h>
 
@@ -35,17 +40,14 @@
 namespace ripple {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
-constexpr int kCtasPerSm = 3;
-constexpr int kPlaces = 152 * kCtasPerSm;
+constexpr int kWarpsPerSm = 24;
+constexpr int kWide = 8, kNarrow = 2;  // warps of a CTA
+constexpr int kPlaces = 152 * kWarpsPerSm / kWide;
 constexpr int kMaxSlices = 8;
 constexpr int kVecs = 4;               // 16-byte vectors of a thread in a chunk
-constexpr int kChunkVecs = kThreads * kVecs;
 constexpr int kStages = 3;
 constexpr int kSegments = 8;
-constexpr int kGroup = kThreads / 32;  // lanes whose largest logit bounds the alternatives
-constexpr int kCands = 512;            // candidates ranked at a time
+constexpr int kGroups = 64;            // of lanes, whose largest logits bound the alternatives
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kMaxDevices = 64;
 typedef unsigned long long Key;
@@ -268,14 +270,20 @@ struct Lane {
   }
 };
 
+template <int W>
 struct Smem {
+  static constexpr int kThreads = W * 32;
+  static constexpr int kCands = W * 64;  // candidates ranked at a time
   uint4 ring[kStages][kVecs][kThreads];
   float seg[kSegments][kThreads];  // largest logit of a segment's lane
   Key cand[kCands];
-  Key best[kMaxSlices * RIPPLE_MAX_TOP];  // n_top of every slice, in the cluster's first CTA
-  Sums sums[kMaxSlices], warp[kWarps];
-  float first[kWarps], group[32];
-  uint16_t hot[kWarps][kSegments * 32];   // segment * 32 + lane
+  // n_top of every slice, in the cluster's first CTA
+  Key best[(W == kWide ? kMaxSlices : 1) * RIPPLE_MAX_TOP];
+  Sums sums[kMaxSlices], warp[W];
+  float first[W];
+  alignas(16) uint32_t group[kGroups];  // largest logits, as order_of
+  float2 done;                          // of the row: its largest logit, log1p(S')
+  uint16_t hot[W][kSegments * 32];   // segment * 32 + lane
   Key kth;
   int n_cand;
 };
@@ -291,9 +299,9 @@ __device__ __forceinline__ void copy_wait() {
 }
 
 // Ranks `n` keys by counting: f(rank, key) for each; equal keys (0: none) share a rank.
-template <typename F>
+template <int W, typename F>
 __device__ __forceinline__ void rank_keys(const Key *keys, int n, F f) {
-  for (int i = threadIdx.x; i < n; i += kThreads) {
+  for (int i = threadIdx.x; i < n; i += W * 32) {
     const Key k = keys[i];
     int rank = 0;
 #pragma unroll 4
@@ -332,12 +340,13 @@ template <typename T>
 struct Slice {
   int v0, v1, w0, w1;
   __device__ __forceinline__ Slice(const Row<T> &row, int slice, int slices) {
-    v0 = row.n_vec / slices * slice;  // the last slice has the rest
-    v1 = slice + 1 < slices ? v0 + row.n_vec / slices : row.n_vec;
+    const int each = row.n_vec >> (__ffs(slices) - 1);  // (a power of two) the last has the rest
+    v0 = each * slice;
+    v1 = slice + 1 < slices ? v0 + each : row.n_vec;
     w0 = v0 + (v0 < v1 && !row.whole(v0) ? 1 : 0);
     w1 = max(w0, v1 - (v0 < v1 && !row.whole(v1 - 1) ? 1 : 0));
   }
-  __device__ __forceinline__ int chunks() const { return (w1 - w0 + kChunkVecs - 1) / kChunkVecs; }
+  __device__ __forceinline__ int chunks(int vecs) const { return (w1 - w0 + vecs - 1) / vecs; }
   // The partial vectors: the first, the last, or -1.
   __device__ __forceinline__ int partial(int which) const {
     return which == 0 ? (w0 > v0 ? v0 : -1) : (v1 > w1 ? v1 - 1 : -1);
@@ -357,13 +366,15 @@ __device__ __forceinline__ Sums merge_lanes(Sums a, int n, int lane, float scale
               __shfl_sync(kAll, a.one, 0)};
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+template <typename T, int W>
+__global__ void __launch_bounds__(W * 32, kWarpsPerSm / W)
     logprob_kernel(const __grid_constant__ LogprobParams p) {
   extern __shared__ __align__(128) uint8_t smem_raw[];
-  Smem &s = *reinterpret_cast<Smem *>(smem_raw);
+  Smem<W> &s = *reinterpret_cast<Smem<W> *>(smem_raw);
+  constexpr int kThreads = W * 32, kChunkVecs = kThreads * kVecs, kCands = Smem<W>::kCands;
+  constexpr int kGroup = kThreads / kGroups;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const bool many = p.slices > 1;
+  const bool many = W == kWide && p.slices > 1;
   const int slice = many ? (int)cluster_rank() : 0, r = blockIdx.x / p.slices;
   const int n_top = p.n_top;
   pdl_wait();
@@ -371,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 
   const Row<T> row(p, r);
   const Slice<T> part(row, slice, p.slices);
-  const int chunks = part.chunks();
+  const int chunks = part.chunks(kChunkVecs);
   auto fetch = [&](int c, int stage) {  // chunk c; the thread's vectors behind w1 are none
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
@@ -389,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
   // the given token's logit, on its way while the row is read (the warp that writes it)
   float given = 0.f;
   int token = -1;
-  if (slice == 0 && warp == kWarps - 1 && p.tokens != nullptr) {
+  if (slice == 0 && warp == W - 1 && p.tokens != nullptr) {
     token = p.tokens[r];
     if (token >= 0 && token < p.vocab) given = to_f32(row.x[token]);
   }
@@ -420,10 +431,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
       const float mine = warp_max(g);
       if (lane == 0) s.first[warp] = mine;
       __syncthreads();
-      const float of = lane < kWarps ? s.first[lane] : -INFINITY;
+      const float of = lane < W ? s.first[lane] : -INFINITY;
       sum.m = warp_max(of);
       // the first warp that has it owns a logit
-      const int owner = __ffs(__ballot_sync(kAll, lane < kWarps && of == sum.m)) - 1;
+      const int owner = __ffs(__ballot_sync(kAll, lane < W && of == sum.m)) - 1;
       if (sum.m > -INFINITY && warp == owner) sum.own(u, g, lane);
     }
     sum.add(u, g, p.scale2, lane);
@@ -456,23 +467,61 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
   float g = largest;
 #pragma unroll
   for (int o = kGroup / 2; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(kAll, g, o));
-  if (lane % kGroup == 0) s.group[tid / kGroup] = g;
+  if (lane % kGroup == 0) s.group[tid / kGroup] = order_of(g);
   __syncthreads();
 
-  if (n_top > 0) {
-    // the n-th largest of the 32 groups' largest logits
-    Key bound;
-    {
-      const uint32_t o = order_of(s.group[lane]);
-      int above = 0;  // groups before this one, by value and then by lane
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const uint32_t other = __shfl_sync(kAll, o, i);
-        above += other > o || (other == o && i < lane);
+  // Writes a row's outputs but the alternatives (a warp); its largest logit and log1p(S').
+  auto write = [&](Sums all) {
+    if (all.m == INFINITY) all.s = NAN;
+    all.s -= 1.f - all.one;  // S' (no logit but -infinity: -1)
+    const float ls = log1pf(all.s);
+    if (lane == 0) {
+      if (p.lse != nullptr)
+        p.lse[r] = all.m == -INFINITY ? all.m + 0.f * all.s : p.scale * all.m + ls;
+      if (p.entropy != nullptr) p.entropy[r] = ls - p.scale * all.t / (1.f + all.s);
+      if (p.logprob != nullptr) {
+        float y = 0.f;
+        if (token >= p.vocab) {
+          report(p.status, RIPPLE_EBOUNDS);
+          y = NAN;
+        } else if (token >= 0) {
+          y = p.scale * (given - all.m) - ls;
+        }
+        p.logprob[r] = y;
       }
-      const int at = __ffs(__ballot_sync(kAll, above == n_top - 1)) - 1;
-      bound = (Key)__shfl_sync(kAll, o, at) << 32;
+      s.done = make_float2(all.m, ls);
     }
+  };
+  if (warp == W - 1) {
+    const Sums all = merge_lanes(s.warp[lane % W], W, lane, p.scale2);
+    if (!many)
+      write(all);
+    else if (lane == 0)
+      s.sums[slice] = all;
+  }
+
+  if (n_top > 0) {
+    // the n-th largest of the groups' largest logits, a group's threads a part of them each
+    {
+      constexpr int kOthers = kGroups / kGroup / 4;
+      const uint32_t o = s.group[tid / kGroup];
+      int above = 0, same = 0;
+#pragma unroll
+      for (int i = 0; i < kOthers; ++i) {
+        const uint4 x = reinterpret_cast<const uint4 *>(s.group)[tid % kGroup * kOthers + i];
+        above += (x.x > o) + (x.y > o) + (x.z > o) + (x.w > o);
+        same += (x.x == o) + (x.y == o) + (x.z == o) + (x.w == o);
+      }
+#pragma unroll
+      for (int i = 1; i < kGroup; i *= 2) {
+        above += __shfl_xor_sync(kAll, above, i);
+        same += __shfl_xor_sync(kAll, same, i);
+      }
+      // (groups with the same value all write it)
+      if (above < n_top && above + same >= n_top) s.kth = (Key)o << 32;
+    }
+    __syncthreads();
+    Key bound = s.kth;
     // the warp's lanes' segments with candidates
     int n_hot = 0;
     if (__any_sync(kAll, (Key)order_of(largest) << 32 >= bound))
@@ -485,9 +534,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     __syncwarp();
     const int per = per_seg * kVecs;  // vectors of one, at most
     for (;;) {
-      auto look = [&](int v) {
-        float x[Row<T>::E];
-        row.get(v, x);
+      auto look = [&](int v, const float (&x)[Row<T>::E]) {
 #pragma unroll
         for (int e = 0; e < Row<T>::E; ++e) {
           const int idx = row.first(v) + e;
@@ -500,14 +547,26 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
       };
       for (int i = lane; i < n_hot * per; i += 32) {
         const int hot = s.hot[warp][i / per];
-        const int v = part.w0 + (hot / 32 * per + i % per) * kThreads + warp * 32 + hot % 32;
-        if (v < part.w1) look((int)guard(v, 1, row.n_vec, p.status));
+        const int at = hot / 32 * per + i % per, of = warp * 32 + hot % 32;
+        const int v = part.w0 + at * kThreads + of;
+        if (v >= part.w1) continue;
+        float x[Row<T>::E];
+        const int back = chunks - at / kVecs;
+        if (back <= kStages)  // still in the ring
+          unpack16(s.ring[(stage + kStages - back) % kStages][at % kVecs][of], row.x, x);
+        else
+          unpack16(row.load((int)guard(v, 1, row.n_vec, p.status)), row.x, x);
+        look(v, x);
       }
-      if (tid < 2 && part.partial(tid) >= 0) look(part.partial(tid));
+      if (tid < 2 && part.partial(tid) >= 0) {
+        float x[Row<T>::E];
+        row.get(part.partial(tid), x);
+        look(part.partial(tid), x);
+      }
       __syncthreads();
       if (s.n_cand <= kCands) break;
       // too many: a higher bound from those found
-      rank_keys(s.cand, kCands, [&](int rank, Key k) {
+      rank_keys<W>(s.cand, kCands, [&](int rank, Key k) {
         if (rank == n_top - 1) s.kth = k;
       });
       __syncthreads();
@@ -516,19 +575,19 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
       __syncthreads();
     }
   }
-  Sums all = merge_lanes(s.warp[lane % kWarps], kWarps, lane, p.scale2);
   const Key *keys = s.cand;
   int n_keys = n_top > 0 ? s.n_cand : 0;
   if (many) {
     cluster_wait();  // the first CTA runs
     if (n_top > 0) {
       const uint32_t to = in_first(s.best + slice * n_top);
-      rank_keys(keys, n_keys, [&](int rank, Key k) {
+      rank_keys<W>(keys, n_keys, [&](int rank, Key k) {
         if (rank < n_top) st_cluster(to + rank * 8, k);
       });
       if (tid >= n_keys && tid < n_top) st_cluster(to + tid * 8, (Key)0);
     }
-    if (tid == 0) {
+    if (warp == W - 1 && lane == 0 && slice > 0) {
+      const Sums all = s.sums[slice];
       const uint32_t to = in_first(&s.sums[slice]);
       st_cluster(to, all.m);
       st_cluster(to + 4, all.s);
@@ -538,35 +597,18 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     cluster_arrive();
     cluster_wait();
     if (slice != 0) return;
-    all = merge_lanes(s.sums[lane % kMaxSlices], p.slices, lane, p.scale2);
+    if (warp == W - 1) write(merge_lanes(s.sums[lane % kMaxSlices], p.slices, lane, p.scale2));
     keys = s.best;
     n_keys = p.slices * n_top;
+    __syncthreads();
   }
-  if (all.m == INFINITY) all.s = NAN;
-  all.s -= 1.f - all.one;  // S' (no logit but -infinity: -1)
-  const float ls = log1pf(all.s);
-  if (warp == kWarps - 1 && lane == 0) {
-    if (p.lse != nullptr)
-      p.lse[r] = all.m == -INFINITY ? all.m + 0.f * all.s : p.scale * all.m + ls;
-    if (p.entropy != nullptr) p.entropy[r] = ls - p.scale * all.t / (1.f + all.s);
-    if (p.logprob != nullptr) {
-      float y = 0.f;
-      if (token >= p.vocab) {
-        report(p.status, RIPPLE_EBOUNDS);
-        y = NAN;
-      } else if (token >= 0) {
-        y = p.scale * (given - all.m) - ls;
-      }
-      p.logprob[r] = y;
-    }
-  }
-  rank_keys(keys, n_keys, [&](int rank, Key k) {
+  rank_keys<W>(keys, n_keys, [&](int rank, Key k) {
     if (rank >= n_top) return;
     const long long to =
         guard((long long)r * n_top + rank, 1, (long long)p.n_rows * n_top, p.status);
     p.top_idx[to] = (int)~(uint32_t)k;
     if (p.top_logprob != nullptr)
-      p.top_logprob[to] = p.scale * (value_of((uint32_t)(k >> 32)) - all.m) - ls;
+      p.top_logprob[to] = p.scale * (value_of((uint32_t)(k >> 32)) - s.done.x) - s.done.y;
   });
 }
 
@@ -574,25 +616,27 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 int slices_of(int n_rows, long long row_bytes) {
   int c = 1;
   while (c < kMaxSlices && (long long)n_rows * 2 * c <= kPlaces &&
-         row_bytes >= 2LL * c * kChunkVecs * 16)
+         row_bytes >= 2LL * c * kWide * 32 * kVecs * 16)
     c *= 2;
   return c;
 }
 
-template <typename T>
+template <typename T, int W>
 cudaError_t launch(const LogprobParams &p, int dev, cudaStream_t st) {
   static std::atomic<bool> attr_set[kMaxDevices];
-  static_assert(kCtasPerSm * (sizeof(Smem) + 1024) <= 228 * 1024, "shared memory per SM");
+  static_assert(kWarpsPerSm / W * (sizeof(Smem<W>) + 1024) <= 228 * 1024,
+                "shared memory per SM");
   if (!attr_set[dev].load(std::memory_order_acquire)) {
     const cudaError_t e = cudaFuncSetAttribute(
-        logprob_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+        logprob_kernel<T, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        (int)sizeof(Smem<W>));
     if (e != cudaSuccess) return e;
     attr_set[dev].store(true, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.n_rows * p.slices);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = sizeof(Smem);
+  cfg.blockDim = dim3(W * 32);
+  cfg.dynamicSmemBytes = sizeof(Smem<W>);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -603,9 +647,22 @@ cudaError_t launch(const LogprobParams &p, int dev, cudaStream_t st) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.slices > 1 ? 2 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, logprob_kernel<T>, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, logprob_kernel<T, W>, p);
   count_launches(1);
   return e;
+}
+
+// Two warps a row where there are more rows than wide CTAs find a place and rows are short: what
+// a CTA does once per row (sums joined, alternatives) costs eight warps four times as much,
+// but as many two find too little to read ahead of long rows, and leave SMs idle at the end.
+// Measured (no alternatives, us, two and eight warps): bf16, 14562 tokens: 460 rows 7.7 and 8.0,
+// 2874 rows 23.8 and 33.9; 60000 tokens: 460 rows 17.5 and 16.4, 2874 rows 62 and 67; 128256
+// tokens: 1000 rows 48.7 and 46.5, 2000 rows 98 and 84; fp32, 4000 tokens: 2000 rows 9.5 and 13.9,
+// 45864 tokens: 2000 rows 77.5 and 62.6.
+template <typename T>
+cudaError_t launch_width(const LogprobParams &p, long long row_bytes, int dev, cudaStream_t st) {
+  return p.n_rows > kPlaces && row_bytes <= 128 * 1024 ? launch<T, kNarrow>(p, dev, st)
+                                                       : launch<T, kWide>(p, dev, st);
 }
 
 }  // namespace
@@ -635,14 +692,15 @@ extern "C" ripple_status ripple_token_logprobs(
                         (const void *)top_logprob_out, (const void *)dev_status})
     if ((uintptr_t)o & 3u) return RIPPLE_EINVAL;
   const float sc = scale > 0.f ? scale : 1.f;
-  const int slices = slices_of(n_rows, (long long)vocab * (dtype == RIPPLE_F32 ? 4 : 2));
+  const long long row_bytes = (long long)vocab * (dtype == RIPPLE_F32 ? 4 : 2);
+  const int slices = slices_of(n_rows, row_bytes);
   const LogprobParams p{logits, row_stride, n_rows, vocab, n_top, slices, sc, sc * kLog2e, tokens,
                         logprob_out, entropy_out, lse_out, top_idx_out, top_logprob_out,
                         dev_status};
   cudaStream_t st = (cudaStream_t)stream;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return RIPPLE_ECUDA;
-  RIPPLE_CUDA_TRY(dtype == RIPPLE_BF16 ? launch<__nv_bfloat16>(p, dev, st)
-                                       : launch<float>(p, dev, st));
+  RIPPLE_CUDA_TRY(dtype == RIPPLE_BF16 ? launch_width<__nv_bfloat16>(p, row_bytes, dev, st)
+                                       : launch_width<float>(p, row_bytes, dev, st));
   return RIPPLE_OK;
 }

@@ -132,6 +132,30 @@ def test_row_counts(lib, n):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,top", [(3, 1), (700, 32), (4097, 32), (30011, 5), (70001, 0)])
+def test_more_rows_than_places(lib, V, top, dtype):
+    n = 1999
+    x = _logits(n, V, dtype, 600 + V)
+    x[5::7] = 1.5                       # more ties than candidates
+    x[6::7, : V // 2] = -float("inf")   # masked
+    x[11::97, V // 3:] = -float("inf")
+    tok = torch.randint(0, V, (n,), device=DEV, generator=P.gen(V)).to(torch.int32)
+    r = _run(lib, x, tok, top, scale=1.25)
+    assert int(r["status"].item()) == 0
+    has = (x > -float("inf")).any(1)
+    rows = [0, 5, 6, 455, 456, 1100, n - 1] + list(range(0, n, 61))
+    _check(r, x, tok, top, scale=1.25, rows=[i for i in rows if bool(has[i])])
+    again = _run(lib, x, tok, top, scale=1.25)
+    few = _run(lib, x[800:1200], tok[800:1200], top, scale=1.25)  # split otherwise
+    for k in ("logprob", "entropy", "lse", "idx", "top"):
+        if r[k] is not None:
+            a, b = r[k][has], again[k][has]
+            assert torch.equal(a, b), k
+            if k == "idx":
+                assert torch.equal(r[k][800:1200][has[800:1200]], few[k][has[800:1200]])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("top", [1, 2, 31, 32])
 def test_ties_go_to_the_lowest_index(lib, top, dtype):
     V = 20011
