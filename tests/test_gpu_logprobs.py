@@ -215,6 +215,29 @@ def test_masks(lib):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logits_of_every_size(lib, dtype):
+    # masks of the lowest value beside infinite ones, logits and scales at the type's ends
+    V = 4099
+    low = torch.finfo(P.DT[dtype]).min
+    g = P.gen(91)
+    noise = torch.randn((2, V), device=DEV, generator=g)
+    x = torch.full((3, V), low, dtype=P.DT[dtype], device=DEV)
+    x[1, 77] = 0
+    x[2, 100:] = low / 2
+    x[:, ::3] = -float("inf")
+    tok = P.i32([1, 77, 4000])
+    r = _run(lib, x, tok, 4)
+    assert int(r["status"].item()) == 0
+    _check(r, x, tok, 4)
+    for size, scale in ((1e36, 2e-36), (1e35, 2e-35), (1e-30, 1e30)):
+        x = (noise * size).to(P.DT[dtype])
+        x[:, 5::3] = -float("inf")
+        tok = P.i32([0, 3])
+        r = _run(lib, x, tok, 4, scale=scale)
+        _check(r, x, tok, 4, scale=float(np.float32(scale)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_without_a_distribution(lib, dtype):
     V = 5000
     x = _logits(5, V, dtype, 21)
