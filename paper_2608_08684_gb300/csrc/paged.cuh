@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "ripple.h"
 
@@ -34,6 +35,11 @@ inline bool disjoint(int n, const long long *stride, const long long *count, lon
 }
 
 inline bool aligned16_host(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+inline bool aligned4_host(std::initializer_list<const void *> pointers) {
+  for (const void *p : pointers)
+    if (((uintptr_t)p & 3u) != 0) return false;
+  return true;
+}
 
 // Elements of 16 bytes, or 0 for an unknown type.
 inline int vec_elems(int dtype) {

@@ -349,6 +349,7 @@ extern "C" ripple_status ripple_paged_append(
   if (!k_pages || !v_pages || !block_table || !lens || !aligned16_host(k_pages) ||
       !aligned16_host(v_pages))
     return RIPPLE_EINVAL;
+  if (!aligned4_host({seq_starts, positions, block_table, lens, dev_status})) return RIPPLE_EINVAL;
   const int vec = vec_elems(desc->dtype);
   if (!token_rows(k, k_strides, vec, &p.k) || !token_rows(v, v_strides, vec, &p.v))
     return RIPPLE_EINVAL;

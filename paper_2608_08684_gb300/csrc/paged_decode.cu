@@ -1165,7 +1165,7 @@ extern "C" ripple_status ripple_paged_decode_attn(
       ((uintptr_t)workspace & 255u))
     return RIPPLE_EINVAL;
   if (!aligned16_host(q) || !aligned16_host(k_pages) || !aligned16_host(v_pages) ||
-      !aligned16_host(out))
+      !aligned16_host(out) || !aligned4_host({block_table, lens, lse, dev_status}))
     return RIPPLE_EINVAL;
   const int vec = vec_elems(desc->dtype);
   p.q_head = desc->head_dim;

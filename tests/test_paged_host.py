@@ -108,6 +108,13 @@ def test_decode_refuses_bad_arguments(lib):
                                                         ctypes.byref(n)) == E
 
 
+def test_words_are_aligned(lib):
+    for key in ("pos", "table", "lens", "starts"):
+        assert _append(lib, **{key: FAKE + 2}) == lib.EINVAL, key
+    for key in ("table", "lens"):
+        assert _decode(lib, **{key: FAKE + 2}) == lib.EINVAL, key
+
+
 def test_decode_workspace_grows_with_the_call(lib):
     def need(hq=8, **over):
         n = ctypes.c_size_t()
