@@ -34,7 +34,8 @@ def test_paged_calls_checked(lib, chk, dtype, G, H, d, page, lens):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n,V,stride", [(1, 128256, 128256), (9, 5003, 5007), (200, 1001, 1001), (3, 7, 7)])
+@pytest.mark.parametrize("n,V,stride", [(1, 128256, 128256), (9, 5003, 5007), (200, 1001, 1001), (3, 7, 7),
+                                        (700, 2000, 2003)])
 def test_logprobs_checked(lib, chk, n, V, stride, dtype):
     x = P.randn((n, stride), dtype, 80)[:, :V]
     tokens = P.i32([i % V for i in range(n)])

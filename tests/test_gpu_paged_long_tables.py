@@ -6,6 +6,8 @@ import torch
 
 from tests import gpu_common as C
 from tests import paged_common as P
+from tests.test_gpu_checked import chk  # noqa: F401  (fixture)
+from tests.test_gpu_paged_checked import test_paged_calls_checked  # noqa: F401
 from tests.test_gpu_paged_decode import (  # noqa: F401
     test_a_page_shared_by_sequences, test_lengths_around_every_edge, test_pages_and_layouts,
     test_rows_behind_the_length_never_count, test_scale_and_strided_queries, test_short_caches,
