@@ -6,7 +6,7 @@
 // every CTA finds its run by a sum over the sequences. The first runs, one for every
 // place on the GPU, hold most of the blocks, later ones less and less (Runs): SMs differ
 // by a tenth in the bandwidth they get, and the later runs go where a place is free first.
-// (One run of equal length for every warp: 158 us for 64 sequences of 3800 rows, 979 MB,
+// (One run of equal length for every warp: 158 us for 62 sequences of 3800 rows, 965 MB,
 // of which the slowest SMs took 144 and the fastest 120.) What a run covers does not
 // depend on where it goes, so results do not either.
 //
