@@ -740,7 +740,8 @@ constexpr int kMaxCluster = 8;
 // 15.8 and 11.8; 16 sequences of up to 1000 rows 10.2 and 14.0, up to 4000 rows 30.4 and 33.5;
 // 64 of up to 1000 rows 32.3 and 37.5, with 8 heads a group 35.4 and 41.3, 16 heads 43.7 and 53.5.
 // The clusters lose where lengths are far apart (64 of 20 to 2000 rows: 27.8 and 26.4) and where
-// most warps have nothing to do (256 of up to 30 rows: 18.9 and 16.6).
+// most warps of many groups have nothing to do (256 of up to 30 rows: 18.9 and 16.6; 150 of
+// them 11.3 and 12.8).
 constexpr int kShortFew = 8, kShortMany = 32;
 
 template <typename T, int D, int G>
@@ -1093,6 +1094,10 @@ int short_cluster(const PagedDecParams &p, int sms) {
   int ctas = 1;
   while (ctas < kMaxCluster && groups * 2 * ctas <= places(2 * ctas)) ctas *= 2;
   const long long rows = (long long)p.g.max_pages << p.g.shift;
+  // of one block there is nothing to share out: runs, but for groups that all find a place
+  // soon (a block each, clusters and runs: 400 groups 6.5 and 8.2 us, 1024 groups of d 64
+  // 12.3 and 9.0, 2048 of d 128 18.6 and 10.5)
+  if (rows <= Cfg<T, D, G>::RB && groups > 2 * places(1)) return 0;
   const int most = groups * ctas >= sms ? kShortMany : kShortFew;
   return rows <= (long long)ctas * kShortWarps * most * Cfg<T, D, G>::RB ? ctas : 0;
 }

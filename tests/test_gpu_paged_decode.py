@@ -55,7 +55,8 @@ def test_pages_and_layouts(lib, page, layout, dtype, G, H, d):
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("G", [1, 2, 4, 7, 16])
 @pytest.mark.parametrize("lens,H", [([1], 1), ([0, 470, 33], 2), ([250, 100, 0, 1, 17, 249], 4),
-                                    ([100, 3, 64, 0, 31] * 9, 2), ([60, 0, 16, 1] * 50, 2)])
+                                    ([100, 3, 64, 0, 31] * 9, 2), ([60, 0, 16, 1] * 50, 2),
+                                    ([8, 0, 5, 1] * 100, 2)])
 def test_short_caches(lib, lens, H, G, d, dtype):
     for page in (1, 32):
         pool = P.Pool(lib, lens, H, d, page, dtype, 350 + G)
