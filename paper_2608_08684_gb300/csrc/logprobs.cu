@@ -637,7 +637,9 @@ __global__ void __launch_bounds__(W * 32, kWarpsPerSm / W)
   });
 }
 
-// Slices of a row: as many CTAs as find a place at once, of two chunks at least.
+// Slices of a row: as many CTAs as find a place at once, of two chunks at least. More would come
+// to a second turn: 333 rows of 32003, fp32, in halves 14.6 us, whole 10.6; fewer leave
+// places empty.
 int slices_of(int n_rows, long long row_bytes) {
   int c = 1;
   while (c < kMaxSlices && (long long)n_rows * 2 * c <= kPlaces &&
