@@ -797,7 +797,8 @@ __global__ void __launch_bounds__(kShortThreads)
   pdl_wait();
   if (ctas > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   const int b = group / p.g.Hkv, h = group % p.g.Hkv;
-  if (h == 0 && rank == 0 && tid == 0 && (long long)p.lens[b] > (long long)p.g.max_pages << p.g.shift)
+  if (h == 0 && rank == 0 && tid == 0 &&
+      (long long)p.lens[b] > (long long)p.g.max_pages << p.g.shift)
     report(p.status, RIPPLE_EFULL);
   const int len = clamp_len(p, b), blocks = W::blocks_of(len);
   const int worker = rank * kShortWarps + warp, workers = ctas * kShortWarps;
@@ -866,14 +867,16 @@ __global__ void __launch_bounds__(kShortThreads)
       put(col, head, d, sum, m, den);
     }
   };
-  const long long row0 = guard((long long)b * p.Hq + h * p.G, p.G, (long long)p.g.B * p.Hq, p.status);
+  const long long row0 =
+      guard((long long)b * p.Hq + h * p.G, p.G, (long long)p.g.B * p.Hq, p.status);
   auto write = [&](int, int head, int d, const float4 &o, float m, float den) {
     const float inv = den != 0.f ? 1.f / den : 0.f;  // 0: no row counts
     *reinterpret_cast<float4 *>(&p.out[(row0 + head) * D + d]) =
         make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
     if (p.lse != nullptr && d == 0) p.lse[row0 + head] = lse_of(m, den);
   };
-  auto of_warps = [&](int i) -> const typename ShortSmem<T, D, G>::Partial & { return s.ring[i].part; };
+  using Partial = typename ShortSmem<T, D, G>::Partial;
+  auto of_warps = [&](int i) -> const Partial & { return s.ring[i].part; };
   auto has = [&](int i) { return s.has[i] != 0; };
   if (ctas == 1) {
     join(kShortWarps, of_warps, has, 0, cols, write);
@@ -890,8 +893,9 @@ __global__ void __launch_bounds__(kShortThreads)
        });
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-  join(ctas, [&](int i) -> const typename ShortSmem<T, D, G>::Partial & { return s.parts[i]; },
-       [](int) { return true; }, min(rank << share_shift, cols), min((rank + 1) << share_shift, cols), write);
+  join(ctas, [&](int i) -> const Partial & { return s.parts[i]; },
+       [](int) { return true; }, min(rank << share_shift, cols),
+       min((rank + 1) << share_shift, cols), write);
 }
 
 // Joins the partials of the groups that begin in this CTA's kJoinRuns runs and go on, one
@@ -1043,12 +1047,13 @@ bool decode_args(const ripple_paged_desc *d, int n_q_heads, PagedDecParams *p) {
   return p->G <= kMaxGroup;
 }
 
-// Runs of a call and the workspace: records, (max, sum), outputs of the partials. The runs are bounded by the blocks that the table has room for, so that small caches
-// take few CTAs; everything grows with the call. Returns the bytes; fills p's pointers if
-// given a base.
+// Runs of a call and the workspace: records, (max, sum), outputs of the partials. The runs are
+// bounded by the blocks that the table has room for, so that small caches take few CTAs;
+// everything grows with the call. Returns the bytes; fills p's pointers if given a base.
 size_t plan(PagedDecParams *p, int dtype, int sms, void *ws) {
   const int rows = kBlockBytes / (p->g.D * (dtype == RIPPLE_BF16 ? 2 : 4));
-  const long long room = (((long long)p->g.max_pages << p->g.shift) + rows - 1) / rows * p->g.B * p->g.Hkv;
+  const long long room =
+      (((long long)p->g.max_pages << p->g.shift) + rows - 1) / rows * p->g.B * p->g.Hkv;
   p->places = sms * kWarpsPerSm;
   const int phases = (long long)p->g.B * p->g.Hkv <= kFewGroups ? 1 : kPhases;
   p->n_runs = (int)std::min<long long>(phases * p->places, room);
