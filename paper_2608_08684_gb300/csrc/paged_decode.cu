@@ -1096,9 +1096,13 @@ int short_cluster(const PagedDecParams &p, int sms) {
     return (2 * (ShortSmem<T, D, G>::bytes(ctas) + 1024) <= 228 * 1024 ? 2LL : 1LL) * sms;
   };
   const long long groups = (long long)p.g.B * p.g.Hkv;
-  int ctas = 1;
-  while (ctas < kMaxCluster && groups * 2 * ctas <= places(2 * ctas)) ctas *= 2;
   const long long rows = (long long)p.g.max_pages << p.g.shift;
+  int ctas = 1;
+  // (one CTA where its warps get a block each at most: a cluster's joins take 0.8 us; 64 rows 3.2
+  // and 4.0, 8 sequences of 64 rows 3.4 and 4.3; with two blocks each 4.0 and 4.0, with three 4.7
+  // and 4.0)
+  if (rows > kShortWarps * Cfg<T, D, G>::RB)
+    while (ctas < kMaxCluster && groups * 2 * ctas <= places(2 * ctas)) ctas *= 2;
   // of one block there is nothing to share out: runs, but for groups that all find a place
   // soon (a block each, clusters and runs: 400 groups 6.5 and 8.2 us, 1024 groups of d 64
   // 12.3 and 9.0, 2048 of d 128 18.6 and 10.5)
