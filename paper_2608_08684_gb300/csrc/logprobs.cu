@@ -637,13 +637,15 @@ __global__ void __launch_bounds__(W * 32, kWarpsPerSm / W)
   });
 }
 
-// Slices of a row: as many CTAs as find a place at once, of two chunks at least. More would come
-// to a second turn: 333 rows of 32003, fp32, in halves 14.6 us, whole 10.6; fewer leave
-// places empty.
+// Slices of a row: as many CTAs as find a place at once, of a chunk at least. More would come to
+// a second turn: 333 rows of 32003, fp32, in halves 14.6 us, whole 10.6. Rows of four chunks at
+// most stay whole, since a cluster costs more than it saves (a row of 36 KB 3.7 us, in halves
+// 4.4; of 72 KB, bf16, 5.1, in quarters 4.6).
 int slices_of(int n_rows, long long row_bytes) {
+  constexpr long long kChunk = kWide * 32 * kVecs * 16;
   int c = 1;
-  while (c < kMaxSlices && (long long)n_rows * 2 * c <= kPlaces &&
-         row_bytes >= 2LL * c * kWide * 32 * kVecs * 16)
+  if (row_bytes <= 4 * kChunk) return c;
+  while (c < kMaxSlices && (long long)n_rows * 2 * c <= kPlaces && row_bytes >= 2 * c * kChunk)
     c *= 2;
   return c;
 }
