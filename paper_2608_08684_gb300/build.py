@@ -21,6 +21,7 @@ import os
 import shutil
 import subprocess
 import sys
+import warnings
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -99,8 +100,18 @@ def build_library(force: bool = False, verbose: bool = False, extra_nvcc=(),
                   checked: bool = False) -> str:
     """Build libripple.so (libripple_checked.so with checked=True) if it is
     missing or older than its sources, and the binding's extension module; return the
-    library's path."""
-    build_binding(force, verbose)
+    library's path. The library needs neither Python's headers nor PyTorch's: where the
+    extension module cannot be built, this warns, and the calls that need it raise."""
+    path = _build_library(force, verbose, extra_nvcc, checked)
+    try:
+        build_binding(force, verbose)
+    except (RuntimeError, OSError, ImportError) as e:
+        warnings.warn(f"{BINDING} could not be built: the paged calls and the log probabilities "
+                      f"are not available from Python. {e}", RuntimeWarning, stacklevel=2)
+    return path
+
+
+def _build_library(force, verbose, extra_nvcc, checked) -> str:
     lib, build_dir = (LIB_CHECKED, BUILD_CHECKED) if checked else (LIB, BUILD)
     extra = list(extra_nvcc) + (["-DRIPPLE_CHECKED"] if checked else [])
     if not force and not _stale(lib):

@@ -5,7 +5,8 @@ module): every function here passes raw pointers, sizes and
 the current CUDA stream to the entry point of the same name, and raises
 RippleError on a non-zero status. All computation happens in the library's
 kernels (or, for ripple_alloc_budgets, in its host C code). Importing this
-module fails loudly if the library has not been built.
+module fails loudly if the library has not been built, and the first call that needs
+the extension module if that has not been.
 """
 from __future__ import annotations
 
@@ -35,7 +36,17 @@ def _load_binding():
     return module
 
 
-_binding = _load_binding()
+class _Binding:
+    """The extension module's functions, loaded at their first use: what does not need them
+    (compression, the contiguous decode, profiling) works where they could not be built."""
+
+    def __getattr__(self, name):
+        module = _load_binding()
+        self.__dict__.update((k, f) for k, f in vars(module).items() if not k.startswith("_"))
+        return getattr(module, name)
+
+
+_binding = _Binding()
 
 F32, BF16 = 0, 1
 POOL_MAX, POOL_AVG, POOL_NONE = 0, 1, 2
