@@ -1,6 +1,6 @@
 """In-tree build of libripple.so (CUDA kernels for sm_103a + the host C allocator) and of
-the extension module _binding.so (argument marshalling of the per-layer calls, against the
-installed Python and PyTorch).
+the extension module _binding.<versions>.so (argument marshalling of the per-layer calls,
+against the installed Python and PyTorch, which its name tells).
 
 Each translation unit is compiled in parallel with nvcc (CUDA) or gcc (C), then
 linked with nvcc into paper_2608_08684_gb300/libripple.so. The build is skipped
@@ -31,7 +31,6 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libripple.so")
 BUILD_CHECKED = os.path.join(PKG, "_build_checked")
 BINDING_SRC = os.path.join(CSRC, "binding.cpp")
-BINDING = os.path.join(PKG, "_binding.so")
 LIB_CHECKED = os.path.join(PKG, "libripple_checked.so")
 
 NVCC = os.environ.get("NVCC", "nvcc")
@@ -68,10 +67,26 @@ def _compile(src: str, extra: list, build_dir: str) -> str:
     return obj
 
 
+def binding_path() -> str:
+    """The extension module for the running Python and PyTorch. It reads tensors through
+    accessors compiled into it, so one built for another version must not be loaded: the name
+    holds Python's ABI and PyTorch's version, commit and C++ ABI."""
+    import sysconfig
+
+    import torch
+
+    abi = sysconfig.get_config_var("SOABI") or "-".join(map(str, sys.version_info[:2]))
+    commit = str(getattr(torch.version, "git_version", None))[:12]
+    return os.path.join(PKG, f"_binding.{abi}.torch-{torch.__version__}-{commit}-"
+                             f"cxx11abi{int(torch._C._GLIBCXX_USE_CXX11_ABI)}.so")
+
+
 def build_binding(force: bool = False, verbose: bool = False) -> str:
-    """Build _binding.so if it is missing or older than its sources; return its path."""
-    if not force and not _stale(BINDING, [BINDING_SRC, os.path.join(INCLUDE, "ripple.h")]):
-        return BINDING
+    """Build the extension module if it is missing or older than its sources; return its
+    path."""
+    binding = binding_path()
+    if not force and not _stale(binding, [BINDING_SRC, os.path.join(INCLUDE, "ripple.h")]):
+        return binding
     import sysconfig
 
     import torch
@@ -79,7 +94,7 @@ def build_binding(force: bool = False, verbose: bool = False) -> str:
     at = os.path.join(os.path.dirname(torch.__file__), "")
     nvcc = shutil.which(NVCC)
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc))) if nvcc else "/usr/local/cuda"
-    tmp = BINDING + ".tmp"
+    tmp = f"{binding}.{os.getpid()}.tmp"  # (processes may build at the same time)
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", BINDING_SRC,
            "-o", tmp, "-I", INCLUDE, "-I", at + "include",
            "-I", at + "include/torch/csrc/api/include", "-I", os.path.join(cuda, "include"),
@@ -87,13 +102,17 @@ def build_binding(force: bool = False, verbose: bool = False) -> str:
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-L", at + "lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda",
            f"-Wl,-rpath,{at}lib"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, BINDING)
+    try:
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+        os.replace(tmp, binding)
+    finally:
+        if os.path.exists(tmp):
+            os.remove(tmp)
     if verbose:
-        print(f"built {BINDING}", file=sys.stderr)
-    return BINDING
+        print(f"built {binding}", file=sys.stderr)
+    return binding
 
 
 def build_library(force: bool = False, verbose: bool = False, extra_nvcc=(),
@@ -106,8 +125,8 @@ def build_library(force: bool = False, verbose: bool = False, extra_nvcc=(),
     try:
         build_binding(force, verbose)
     except (RuntimeError, OSError, ImportError) as e:
-        warnings.warn(f"{BINDING} could not be built: the paged calls and the log probabilities "
-                      f"are not available from Python. {e}", RuntimeWarning, stacklevel=2)
+        warnings.warn("the extension module could not be built: the paged calls and the log "
+                      f"probabilities are not available from Python. {e}", RuntimeWarning, stacklevel=2)
     return path
 
 

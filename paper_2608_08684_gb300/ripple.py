@@ -27,7 +27,9 @@ _lib = ctypes.CDLL(LIB_PATH)
 
 
 def _load_binding():
-    path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_binding.so")
+    from paper_2608_08684_gb300.build import binding_path
+
+    path = binding_path()
     if not os.path.exists(path):
         raise ImportError(f"{path} is not built: call paper_2608_08684_gb300.build.build_library()")
     spec = importlib.util.spec_from_file_location("_binding", path)
