@@ -448,19 +448,22 @@ typedef struct {
  * rope       NULL: nothing is rotated (for rows that are rotated already, such as
  *            those ripple_compress_layer keeps).
  * q, q_out   [tokens][n_q_heads][d] by their strides, or both NULL. q_out == q
- *            with the same strides rotates in place. Queries of idle sequences are
- *            rotated like the others.
+ *            with the same strides rotates in place; otherwise no place of q_out
+ *            may lie in a row of q, k or v (rows beside one another in a token's row
+ *            of one buffer are fine). Queries of idle sequences are rotated like the
+ *            others.
  * k, v       [tokens][Hkv][d] by their strides
  * positions  device int32 [n_tokens] in token order, or NULL: a token's position is
  *            its cache row. A compressed cache has fewer rows than positions.
  * A page that receives tokens belongs to one sequence only (pages shared for
- * reading are fine).
+ * reading are fine). The two pools have no place in common, and the places that the
+ * call stores to are none that it reads.
  * Tokens whose row is negative while lens[b] > 0 (more tokens than rows) or whose
  * page entry is out of range are not stored and reported as RIPPLE_EBOUNDS, rows at or
  * behind max_pages * page_size as RIPPLE_EFULL.
  * n_tokens == 0 does nothing. One launch. The call may be captured in a CUDA graph.
  * Errors: RIPPLE_EINVAL (bad desc, strides or rope, NULL or not 16-byte aligned
- * pointers), RIPPLE_ECUDA.
+ * pointers, q_out overlapping q, k or v, overlapping pools), RIPPLE_ECUDA.
  */
 ripple_status ripple_paged_append(const ripple_paged_desc *desc, const ripple_rope *rope,
                                   int32_t n_tokens, const int32_t *seq_starts,

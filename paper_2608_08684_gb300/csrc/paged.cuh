@@ -12,10 +12,20 @@
 
 namespace ripple {
 
+// Rows of `inner` elements at at + the sum of i_j stride_j, i_j < count_j (places in elements).
+struct RowSet {
+  long long at, stride[3], count[3];
+};
+
 struct PagedGeom {
   int B, Hkv, D, shift;        // page_size == 1 << shift
   int n_pages, max_pages;
   long long page_stride, head_stride, row_stride;  // elements
+  RowSet rows(const void *pages, int elem) const {  // of a pool
+    return RowSet{(long long)((uintptr_t)pages / elem),
+                  {row_stride, head_stride, page_stride},
+                  {1LL << shift, Hkv, n_pages}};
+  }
 };
 
 // Whether the places i * stride (i < count) of the dimensions, each `inner` long
@@ -32,6 +42,60 @@ inline bool disjoint(int n, const long long *stride, const long long *count, lon
     extent += stride[d] * (count[d] - 1);
   }
   return true;
+}
+
+// Whether an element lies in a row of `a` and in one of `b`. Dimensions that both have with
+// the same stride are looked at row by row (by the difference of the indices), the others as
+// the span that they reach over: what is said to be apart is, and two views of one buffer
+// that interleave (heads side by side in a token's row) are told from ones that overlap.
+inline bool overlap(const RowSet &a, const RowSet &b, long long inner) {
+  long long span_a = inner, span_b = inner;
+  long long stride[3], most[3], least[3];  // of the shared dimensions, and the index differences
+  int n = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (a.count[i] > 1 && b.count[i] > 1 && a.stride[i] != b.stride[i]) {
+      span_a += a.stride[i] * (a.count[i] - 1);
+      span_b += b.stride[i] * (b.count[i] - 1);
+    } else if (a.count[i] > 1 || b.count[i] > 1) {
+      int j = n++;  // by descending stride
+      const long long s = a.count[i] > 1 ? a.stride[i] : b.stride[i];
+      for (; j > 0 && stride[j - 1] < s; --j) {
+        stride[j] = stride[j - 1];
+        most[j] = most[j - 1];
+        least[j] = least[j - 1];
+      }
+      stride[j] = s;
+      most[j] = a.count[i] - 1;
+      least[j] = 1 - b.count[i];
+    }
+  }
+  // is a sum of difference_j stride_j in [lo, hi] ?
+  struct Search {
+    const long long *stride, *most, *least;
+    int n;
+    bool find(int j, long long lo, long long hi) const {
+      long long up = 0, down = 0;  // what the dimensions from j on reach
+      for (int i = j; i < n; ++i) {
+        up += most[i] * stride[i];
+        down += least[i] * stride[i];
+      }
+      if (lo > up || hi < down) return false;
+      if (j == n) return true;
+      const long long s = stride[j];
+      if (s == 0) return find(j + 1, lo, hi);
+      up -= most[j] * s;
+      down -= least[j] * s;
+      const auto floor_div = [](long long x, long long y) { return x / y - (x % y < 0 ? 1 : 0); };
+      const long long first = std::max(least[j], -floor_div(up - lo, s));
+      const long long last = std::min(most[j], floor_div(hi - down, s));
+      if (last - first > 64) return true;  // (no layout of rows that lie apart)
+      for (long long i = first; i <= last; ++i)
+        if (find(j + 1, lo - i * s, hi - i * s)) return true;
+      return false;
+    }
+  };
+  const long long d = b.at - a.at;
+  return Search{stride, most, least, n}.find(0, d - span_a + 1, d + span_b - 1);
 }
 
 inline bool aligned16_host(const void *p) { return ((uintptr_t)p & 15u) == 0; }

@@ -307,12 +307,23 @@ cudaError_t launch(const AppendParams &p, bool inter, int grid, cudaStream_t st)
                : launch_as<T, D, false, kMany>(p, grid, st);
 }
 
-// A tensor of tokens: pointer and strides in place, and for outputs disjoint places.
+// A tensor of tokens: pointer and strides in place.
 bool token_rows(const void *data, const ripple_token_strides *s, int vec, TokenRows *out) {
   if (data == nullptr || s == nullptr || !aligned16_host(data)) return false;
   for (const int64_t x : {s->seq_stride, s->token_stride, s->head_stride})
     if (x < 0 || x > (1LL << 40) || x % vec != 0) return false;
   *out = TokenRows{data, s->seq_stride, s->token_stride, s->head_stride};
+  return true;
+}
+
+// The rows of a tensor of tokens with `heads` heads; spans beyond 2^48 elements, which no
+// tensor has, are refused.
+bool row_set(const TokenRows &t, const AppendParams &p, int heads, int elem, RowSet *out) {
+  *out = RowSet{(long long)((uintptr_t)t.data / elem),
+                {t.seq, t.token, t.head},
+                {p.per_seq > 0 ? p.g.B : 1, p.per_seq > 0 ? p.per_seq : p.n_tokens, heads}};
+  for (int i = 0; i < 3; ++i)
+    if (out->count[i] > 1 && out->stride[i] > (1LL << 48) / out->count[i]) return false;
   return true;
 }
 
@@ -355,7 +366,14 @@ extern "C" ripple_status ripple_paged_append(
     return RIPPLE_EINVAL;
   p.Hq = 0;
   p.q = p.q_out = TokenRows{};
+  p.n_tokens = n_tokens;
   p.per_seq = seq_starts == nullptr ? n_tokens / desc->batch : 0;
+  // What one warp reads no other may write: the queries' places lie apart from each other's, the
+  // keys' and the values', and the pools from each other.
+  const int elem = 16 / vec;
+  RowSet in[3], to;  // q, k, v; q_out
+  if (!row_set(p.k, p, p.g.Hkv, elem, &in[1]) || !row_set(p.v, p, p.g.Hkv, elem, &in[2]))
+    return RIPPLE_EINVAL;
   if (q != nullptr) {
     if (n_q_heads < 1 || n_q_heads > (1 << 16)) return RIPPLE_EINVAL;
     if (!token_rows(q, q_strides, vec, &p.q) || !token_rows(q_out, q_out_strides, vec, &p.q_out))
@@ -363,13 +381,16 @@ extern "C" ripple_status ripple_paged_append(
     if (q == q_out && (p.q.seq != p.q_out.seq || p.q.token != p.q_out.token ||
                        p.q.head != p.q_out.head))
       return RIPPLE_EINVAL;
-    const long long stride[3] = {p.q_out.seq, p.q_out.token, p.q_out.head};
-    const long long count[3] = {p.per_seq > 0 ? desc->batch : 1,
-                                p.per_seq > 0 ? p.per_seq : n_tokens, n_q_heads};
-    if (!disjoint(3, stride, count, desc->head_dim)) return RIPPLE_EINVAL;
+    if (!row_set(p.q, p, n_q_heads, elem, &in[0]) ||
+        !row_set(p.q_out, p, n_q_heads, elem, &to) ||
+        !disjoint(3, to.stride, to.count, desc->head_dim))
+      return RIPPLE_EINVAL;
+    for (int i = q == q_out ? 1 : 0; i < 3; ++i)
+      if (overlap(in[i], to, desc->head_dim)) return RIPPLE_EINVAL;
     p.Hq = n_q_heads;
   }
-  p.n_tokens = n_tokens;
+  const RowSet pool[2] = {p.g.rows(k_pages, elem), p.g.rows(v_pages, elem)};
+  if (overlap(pool[0], pool[1], desc->head_dim)) return RIPPLE_EINVAL;
   p.starts = seq_starts;
   p.positions = positions;
   p.table = block_table;
