@@ -403,7 +403,7 @@ ripple_status ripple_decode_attn_noalloc(const ripple_decode_desc *desc, const v
  */
 typedef struct {
   int32_t batch;      /* B: sequences, rows of the block table, 1..65536 */
-  int32_t n_kv_heads; /* Hkv >= 1 */
+  int32_t n_kv_heads; /* Hkv >= 1, batch * Hkv <= 2^24 */
   int32_t head_dim;   /* d: 64 or 128 */
   int32_t page_size;  /* cache rows per page: a power of two, 1..1024 */
   int32_t n_pages;    /* pages of each pool, >= 1 */
@@ -477,8 +477,10 @@ ripple_status ripple_paged_append(const ripple_paged_desc *desc, const ripple_ro
                                   int32_t *dev_status, void *stream);
 
 /* Device workspace bytes ripple_paged_decode_attn needs on the current device; the
- * same for every length. Never fewer for a larger batch, more heads or a larger
- * block table: a workspace made for a program's largest step serves all. */
+ * same for every length. Never fewer for a larger batch, a larger block table, more KV
+ * heads of as many query heads each, or more query heads a KV head: a workspace made
+ * for the largest of each serves all. (The same query heads on more KV heads may need
+ * fewer: a partial holds a KV head's queries.) */
 ripple_status ripple_paged_decode_workspace_bytes(const ripple_paged_desc *desc,
                                                   int32_t n_q_heads, size_t *bytes_host);
 
