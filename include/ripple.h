@@ -494,7 +494,7 @@ ripple_status ripple_paged_decode_workspace_bytes(const ripple_paged_desc *desc,
  * outputs of several caches can be joined by their lse.
  *
  * n_q_heads  a multiple of Hkv, G <= 16
- * scale      logit scale; 0 means 1 / sqrt(d)
+ * scale      logit scale, >= 0, at most 2^127; 0 means 1 / sqrt(d)
  * q          [B][n_q_heads][d] by q_strides (its token_stride is not used; NULL: dense)
  * out        device fp32 [B][n_q_heads][d]
  * lse        device fp32 [B][n_q_heads], or NULL
@@ -533,7 +533,7 @@ ripple_status ripple_paged_decode_attn(const ripple_paged_desc *desc, int32_t n_
  * dtype       ripple_dtype of the logits; -infinity masks a token. A row that holds a
  *             NaN, +infinity or nothing but -infinity has no distribution: its outputs
  *             are NaN (its lse is -infinity if every logit is), its indices any tokens, each once.
- * scale       inverse temperature, > 0, finite; 0 means 1
+ * scale       inverse temperature, > 0, at most 2^127; 0 means 1
  * n_top       0 .. min(RIPPLE_MAX_TOP, vocab)
  * tokens      device int32 [n_rows], or NULL (logprob_out NULL as well). A negative
  *             token is padding: log probability 0. One >= vocab is reported as

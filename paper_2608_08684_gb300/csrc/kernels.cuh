@@ -9,6 +9,10 @@
 
 namespace ripple {
 
+// The largest logit scale of the paged decode and the log probabilities: its product with
+// log2 e is finite.
+constexpr float kMaxScale = 0x1p127f;
+
 // Host-side count of kernel launches (ripple_kernel_launches).
 void count_launches(int n);
 

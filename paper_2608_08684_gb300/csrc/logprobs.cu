@@ -708,7 +708,7 @@ extern "C" ripple_status ripple_token_logprobs(
       row_stride > (1LL << 40))
     return RIPPLE_EINVAL;
   if (dtype != RIPPLE_F32 && dtype != RIPPLE_BF16) return RIPPLE_EINVAL;
-  if (!(scale >= 0.f) || isinf(scale)) return RIPPLE_EINVAL;
+  if (!(scale >= 0.f) || scale > kMaxScale) return RIPPLE_EINVAL;
   if (n_top < 0 || n_top > RIPPLE_MAX_TOP || n_top > vocab) return RIPPLE_EINVAL;
   if ((tokens == nullptr) != (logprob_out == nullptr)) return RIPPLE_EINVAL;
   if (n_rows == 0) return RIPPLE_OK;

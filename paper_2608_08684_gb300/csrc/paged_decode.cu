@@ -1174,7 +1174,7 @@ extern "C" ripple_status ripple_paged_decode_attn(
     size_t workspace_bytes, int32_t *dev_status, void *stream) {
   PagedDecParams p;
   if (!decode_args(desc, n_q_heads, &p)) return RIPPLE_EINVAL;
-  if (!(scale >= 0.f) || isinf(scale)) return RIPPLE_EINVAL;
+  if (!(scale >= 0.f) || scale > kMaxScale) return RIPPLE_EINVAL;
   if (!q || !k_pages || !v_pages || !block_table || !lens || !out || !workspace ||
       ((uintptr_t)workspace & 255u))
     return RIPPLE_EINVAL;
