@@ -81,6 +81,15 @@ void *stream_of(PyObject *o) {
   return s;
 }
 
+// A logit scale; one that fp32 would turn into 0 is none (0 stands for the default).
+float scale_of(PyObject *o) {
+  const double x = PyFloat_AsDouble(o);
+  if (x == -1.0 && PyErr_Occurred()) throw Refused{nullptr};
+  const float scale = static_cast<float>(x);
+  need(scale != 0.f || x == 0.0, "the scale is smaller than any fp32 value");
+  return scale;
+}
+
 template <typename F>
 F *entry(PyObject *o) {
   void *f = PyLong_AsVoidPtr(o);
@@ -200,6 +209,7 @@ PyObject *paged_decode_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!args_are(n, 10)) return nullptr;
   return guarded([&] {
     auto *call = entry<decltype(ripple_paged_decode_attn)>(a[0]);
+    const float scale = scale_of(a[7]);
     const Cache &c = cache_of(a[1]);
     need(c10::cuda::current_device() == c.device, kDevice);
     const Tokens q(a[2], c, false);
@@ -221,13 +231,11 @@ PyObject *paged_decode_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
            "lse must be fp32 [B][Hq]");
       lse = dense<float>(a[6], c.device, at::kFloat, "lse must be fp32 [B][Hq]");
     }
-    const double scale = PyFloat_AsDouble(a[7]);
-    if (scale == -1.0 && PyErr_Occurred()) throw Refused{nullptr};
     int32_t *status = dense<int32_t>(a[8], c.device, at::kInt, "dev_status must be int32");
     void *stream = stream_of(a[9]);
     ripple_status s;
     Py_BEGIN_ALLOW_THREADS
-    s = call(&c.desc, (int32_t)q.heads, (float)scale, q.data, &q.strides, c.k, c.v, c.table, lens,
+    s = call(&c.desc, (int32_t)q.heads, scale, q.data, &q.strides, c.k, c.v, c.table, lens,
              out, lse, w.data_ptr(), w.nbytes(), status, stream);
     Py_END_ALLOW_THREADS
     return (long)s;
@@ -240,6 +248,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!args_are(n, 11)) return nullptr;
   return guarded([&] {
     auto *call = entry<decltype(ripple_token_logprobs)>(a[0]);
+    const float scale = scale_of(a[8]);
     const at::Tensor &x = tensor(a[1]);
     need(x.dim() == 2 && (x.stride(1) == 1 || x.size(1) == 1),
          "logits must be [n][V], a row's logits consecutive");
@@ -271,14 +280,12 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
       }
       need(k <= RIPPLE_MAX_TOP, "too many alternatives");
     }
-    const double scale = PyFloat_AsDouble(a[8]);
-    if (scale == -1.0 && PyErr_Occurred()) throw Refused{nullptr};
     int32_t *status = dense<int32_t>(a[9], device, at::kInt, "dev_status must be int32");
     void *stream = stream_of(a[10]);
     ripple_status s;
     Py_BEGIN_ALLOW_THREADS
     s = call((int32_t)rows, (int32_t)vocab, x.stride(0),
-             x.scalar_type() == at::kFloat ? RIPPLE_F32 : RIPPLE_BF16, (float)scale, (int32_t)k,
+             x.scalar_type() == at::kFloat ? RIPPLE_F32 : RIPPLE_BF16, scale, (int32_t)k,
              x.data_ptr(), tokens, logprob, entropy, lse, k > 0 ? idx : nullptr,
              k > 0 ? top : nullptr, status, stream);
     Py_END_ALLOW_THREADS

@@ -46,3 +46,13 @@ def test_decode(lib, dtype):
     want = (w[:, None] * pool.seq("v", 0)[0]).sum(0) / w.sum()
     np.testing.assert_allclose(out[0].cpu().numpy(), np.broadcast_to(want, (4, 64)), atol=1e-5)
     np.testing.assert_allclose(lse[0].cpu().numpy(), math.log(w.sum()), rtol=1e-5)
+
+
+def test_scales_that_fp32_rounds_to_0_are_refused(lib):
+    pool = P.Pool(lib, [3], 1, 64, 16, "f32", 5)
+    q = torch.ones(1, 4, 64, device=DEV)
+    with pytest.raises(ValueError, match="scale"):
+        P.run_decode(lib, pool, q, P.i32([3]), scale=1e-46)
+    # the smallest one: all rows alike
+    out, lse, _ = P.run_decode(lib, pool, q, P.i32([3]), scale=2.0 ** -149)
+    np.testing.assert_allclose(out[0, 0].cpu().numpy(), pool.seq("v", 0)[0].mean(0), atol=1e-5)
