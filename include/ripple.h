@@ -534,6 +534,8 @@ ripple_status ripple_paged_decode_attn(const ripple_paged_desc *desc, int32_t n_
  *             NaN, +infinity or nothing but -infinity has no distribution: its outputs
  *             are NaN (its lse is -infinity if every logit is), its indices any tokens, each once.
  * scale       inverse temperature, > 0, at most 2^127; 0 means 1
+ *             (A logit further below the row's largest than the largest fp32 value, which
+ *             counts at scales below 1e-36 only, has probability 0.)
  * n_top       0 .. min(RIPPLE_MAX_TOP, vocab)
  * tokens      device int32 [n_rows], or NULL (logprob_out NULL as well). A negative
  *             token is padding: log probability 0. One >= vocab is reported as

@@ -5,6 +5,9 @@
 // row without one largest logit (whose w is 1) and T the sum of w d:
 //   log P(x) = scale d - log1p(S'),   entropy = log1p(S') - scale T / (1 + S').
 // Leaving the 1 out of the sum keeps the relative precision of log probabilities near 0.
+// With y = scale d log2 e, w |y| is at most 0.54, so T stays below 0.54 V / (scale log2 e):
+// in fp32 down to scales of kScaleOfD. Below, and for fp32 logits at every scale, T is the
+// sum of w y and its factor ln 2. (For bf16 that costs 3%: 2048 rows of 128256 82.6 us, 85.2.)
 //
 // Work: one CTA of eight warps per row (of two for many short rows, launch_width), or with few
 // rows one per slice of a row, the slices of a row being a cluster (slices_of). Every thread
@@ -49,15 +52,23 @@ constexpr int kVecs = 4;               // 16-byte vectors of a thread in a chunk
 constexpr int kStages = 3;
 constexpr int kSegments = 8;
 constexpr int kGroups = 64;            // of lanes, whose largest logits bound the alternatives
+constexpr float kScaleOfD = 1e-29f;    // of the scale in base 2 (2^30 * 0.54 / 1e-29 < 2^127)
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kMaxDevices = 64;
 typedef unsigned long long Key;
+
+struct Scale {
+  float two;    // scale * log2 e
+  float of_t;   // factor of T: scale where it sums w d, ln 2 where w y
+  bool sums_y;
+};
 
 struct LogprobParams {
   const void *logits;
   long long row_stride;
   int n_rows, vocab, n_top, slices;
-  float scale, scale2;
+  float scale;
+  Scale by;
   const int32_t *tokens;
   float *logprob, *entropy, *lse;
   int32_t *top_idx;
@@ -83,17 +94,17 @@ struct Sums {
 };
 // A sum n of terms relative to m_from, and its t, to a larger m.
 __device__ __forceinline__ void rebase(float n, float &t, float &s, float m_from, float m,
-                                       float scale2) {
-  const float d = m_from == -INFINITY ? 0.f : fmaxf(m_from - m, -FLT_MAX);
-  const float e = fast_exp2(d * scale2);
-  t = e > 0.f ? e * (t + n * d) : 0.f;
+                                       const Scale &by) {
+  const float d = m_from == -INFINITY ? 0.f : fmaxf(m_from - m, -FLT_MAX), y = d * by.two;
+  const float e = fast_exp2(y);
+  t = e > 0.f ? e * (t + n * (by.sums_y ? y : d)) : 0.f;
   s = n * e;
 }
-__device__ __forceinline__ Sums merge(const Sums &a, const Sums &b, float scale2) {
+__device__ __forceinline__ Sums merge(const Sums &a, const Sums &b, const Scale &by) {
   const bool first = a.m > b.m || (a.m == b.m && a.one >= b.one);
   const Sums &hi = first ? a : b, &lo = first ? b : a;
   float s, t = lo.t;
-  rebase(lo.one + lo.s, t, s, lo.m, hi.m, scale2);
+  rebase(lo.one + lo.s, t, s, lo.m, hi.m, by);
   return Sums{hi.m, hi.s + s, hi.t + t, hi.one};
 }
 
@@ -250,11 +261,11 @@ struct Lane {
   }
   // N vectors of every lane, this lane's largest being g.
   template <int N>
-  __device__ __forceinline__ void add(uint4 (&u)[N], float g, float scale2, int lane) {
+  __device__ __forceinline__ void add(uint4 (&u)[N], float g, const Scale &by, int lane) {
     if (__any_sync(kAll, g > m)) {
       const float mn = warp_max(g);
       float ss, tt = t.x + t.y;
-      rebase(s.x + s.y + (owns ? 1.f : 0.f), tt, ss, m, mn, scale2);
+      rebase(s.x + s.y + (owns ? 1.f : 0.f), tt, ss, m, mn, by);
       s = make_float2(ss, 0.f);
       t = make_float2(tt, 0.f);
       m = mn;
@@ -262,17 +273,17 @@ struct Lane {
     }
     // bf16 is made finite two at a time, where the lowest bf16 relative to m is finite and has no
     // weight (2048 rows of 128256: 83.6 us, 85.1 logit by logit); else, and fp32, d logit by logit
-    if (sizeof(T) == 2 && fabsf(m) <= 1e36f && scale2 >= 1e-30f)
-      terms<true>(u, scale2);
+    if (sizeof(T) == 2 && fabsf(m) <= 1e36f && !by.sums_y)
+      terms<true>(u, by);
     else
-      terms<false>(u, scale2);
+      terms<false>(u, by);
   }
   template <bool kFinite, int N>
-  __device__ __forceinline__ void terms(const uint4 (&u)[N], float scale2) {
+  __device__ __forceinline__ void terms(const uint4 (&u)[N], const Scale &by) {
     constexpr int E = 16 / (int)sizeof(T);
     const T *type = nullptr;
     const float m0 = fmaxf(m, -FLT_MAX);  // nothing but -infinity so far: w = 0
-    const float2 minus = make_float2(-m0, -m0), c = make_float2(scale2, scale2);
+    const float2 minus = make_float2(-m0, -m0), c = make_float2(by.two, by.two);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float x[E];
@@ -286,6 +297,7 @@ struct Lane {
         const float2 w = make_float2(fast_exp2(y.x), fast_exp2(y.y));
         s = __fadd2_rn(s, w);
         if (!kFinite) {
+          if (sizeof(T) == 4 || by.sums_y) d = y;
           d.x = fmaxf(d.x, -FLT_MAX);  // 0 times -infinity is no term
           d.y = fmaxf(d.y, -FLT_MAX);
         }
@@ -379,13 +391,13 @@ struct Slice {
 };
 
 // The Sums of lanes 0 .. n - 1, n <= 8, merged in a fixed order; on every lane.
-__device__ __forceinline__ Sums merge_lanes(Sums a, int n, int lane, float scale2) {
+__device__ __forceinline__ Sums merge_lanes(Sums a, int n, int lane, const Scale &by) {
   if (lane >= n) a = Sums{-INFINITY, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int o = 1; o < 8; o *= 2) {
     const Sums b{__shfl_xor_sync(kAll, a.m, o), __shfl_xor_sync(kAll, a.s, o),
                  __shfl_xor_sync(kAll, a.t, o), __shfl_xor_sync(kAll, a.one, o)};
-    a = lane & o ? merge(b, a, scale2) : merge(a, b, scale2);
+    a = lane & o ? merge(b, a, by) : merge(a, b, by);
   }
   return Sums{__shfl_sync(kAll, a.m, 0), __shfl_sync(kAll, a.s, 0), __shfl_sync(kAll, a.t, 0),
               __shfl_sync(kAll, a.one, 0)};
@@ -462,7 +474,7 @@ __global__ void __launch_bounds__(W * 32, kWarpsPerSm / W)
       const int owner = __ffs(__ballot_sync(kAll, lane < W && of == sum.m)) - 1;
       if (sum.m > -INFINITY && warp == owner) sum.own(u, g, lane);
     }
-    sum.add(u, g, p.scale2, lane);
+    sum.add(u, g, p.by, lane);
     if (++in_seg == per_seg || c == chunks - 1) {  // the segment's end
       s.seg[seg++][tid] = sum.top;
       largest = fmaxf(largest, sum.top);
@@ -475,7 +487,7 @@ __global__ void __launch_bounds__(W * 32, kWarpsPerSm / W)
     if (lane < 2 && part.partial(lane) >= 0) x[0] = row.get_raw(part.partial(lane));
     const float g = Lane<T>::largest(x);
     largest = fmaxf(largest, g);  // (looked at apart from the segments)
-    sum.add(x, g, p.scale2, lane);
+    sum.add(x, g, p.by, lane);
   }
 
   // the warp, the slice
@@ -503,7 +515,7 @@ __global__ void __launch_bounds__(W * 32, kWarpsPerSm / W)
     if (lane == 0) {
       if (p.lse != nullptr)
         p.lse[r] = all.m == -INFINITY ? all.m + 0.f * all.s : p.scale * all.m + ls;
-      if (p.entropy != nullptr) p.entropy[r] = ls - p.scale * all.t / (1.f + all.s);
+      if (p.entropy != nullptr) p.entropy[r] = ls - p.by.of_t * all.t / (1.f + all.s);
       if (p.logprob != nullptr) {
         float y = 0.f;
         if (token >= p.vocab) {
@@ -518,7 +530,7 @@ __global__ void __launch_bounds__(W * 32, kWarpsPerSm / W)
     }
   };
   if (warp == W - 1) {
-    const Sums all = merge_lanes(s.warp[lane % W], W, lane, p.scale2);
+    const Sums all = merge_lanes(s.warp[lane % W], W, lane, p.by);
     if (!many)
       write(all);
     else if (lane == 0)
@@ -622,7 +634,7 @@ __global__ void __launch_bounds__(W * 32, kWarpsPerSm / W)
     cluster_arrive();
     cluster_wait();
     if (slice != 0) return;
-    if (warp == W - 1) write(merge_lanes(s.sums[lane % kMaxSlices], p.slices, lane, p.scale2));
+    if (warp == W - 1) write(merge_lanes(s.sums[lane % kMaxSlices], p.slices, lane, p.by));
     keys = s.best;
     n_keys = p.slices * n_top;
     __syncthreads();
@@ -723,7 +735,10 @@ extern "C" ripple_status ripple_token_logprobs(
   const float sc = scale > 0.f ? scale : 1.f;
   const long long row_bytes = (long long)vocab * (dtype == RIPPLE_F32 ? 4 : 2);
   const int slices = slices_of(n_rows, row_bytes);
-  const LogprobParams p{logits, row_stride, n_rows, vocab, n_top, slices, sc, sc * kLog2e, tokens,
+  const float two = sc * kLog2e;
+  const bool sums_y = dtype == RIPPLE_F32 || two < kScaleOfD;
+  const Scale by{two, sums_y ? 0.6931471805599453f : sc, sums_y};
+  const LogprobParams p{logits, row_stride, n_rows, vocab, n_top, slices, sc, by, tokens,
                         logprob_out, entropy_out, lse_out, top_idx_out, top_logprob_out,
                         dev_status};
   cudaStream_t st = (cudaStream_t)stream;
