@@ -24,7 +24,7 @@
 namespace ripple {
 namespace {
 
-constexpr int kAppendWarps = 4;  // per CTA (8: 142 us for 63k tokens of 48 head rows; 4: 131)
+constexpr int kAppendWarps = 4;  // per CTA (8: 142 us for 33.6k tokens of 48 head rows; 4: 131)
 constexpr int kMaxPairs = 64;
 
 struct TokenRows {

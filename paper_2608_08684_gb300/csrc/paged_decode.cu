@@ -56,11 +56,24 @@ constexpr int kMaxDevices = 64;
 // The runs: kPhases times one for every place (warp) on the GPU, the phases' shares of the
 // blocks in 1/256. Few blocks, and few groups (of which each would be left in hundreds of
 // partials), are one phase.
+// Shares measured (us; D 128, 8 KV heads): 64 sequences of 3800 rows, 4 heads a group, with
+// ends at 170 and 225: 148.8, 190 and 236: 147.8, 210 and 245: 146.0, one phase 152.9; of 64 to
+// 32768 rows 152.7, 151.9, 150.7, one phase 156.6; 9 of 12970 rows 66.0, 66.3, 68.3.
 constexpr int kPhases = 3;
 __device__ __forceinline__ int share_before(int phase) {
   return phase == 0 ? 0 : phase == 1 ? 190 : phase == 2 ? 236 : 256;
 }
-constexpr int kOnePhase = 32;   // blocks per place, at most
+// Blocks per place, at most. One phase and three (us, 64 sequences of equal lengths, bf16 with
+// 4 and 8 heads a group, fp32 with one head of 64): 24 blocks 45.8 and 48.0, 48.6 and 54.3, 42.6
+// and 45.3; 30 blocks 53.6 and 55.6, 57.9 and 62.8, 51.1 and 52.9; 34 blocks 59.4 and 61.1, 62.5
+// and 68.2, 56.4 and 58.0; 48 blocks 79.3 and 79.3, 82.9 and 87.4, 76.3 and 76.4; 96 blocks 146.7
+// and 142.8, 152.5 and 151.9, 140.8 and 137.2. (Three phases gain above about 48 blocks, and
+// with 8 heads a group above 90.)
+constexpr int kOnePhase = 32;
+// One phase and three (us, 8 KV heads, 48 blocks a place): 1 sequence 79.7 and 93.4, 2 79.1
+// and 87.5, 4 (32 groups) 77.3 and 82.2, 7 (56) 78.2 and 81.0, 8 (64) 61.6 and 65.0 (with twice
+// the rows 113.5 and 113.7), 9 (72) 64.2 and 66.3, with twice the rows 117.9 and 116.8, 16 (128)
+// with twice the rows 130.9 and 128.8.
 constexpr int kFewGroups = 64;
 
 struct PagedDecParams {
@@ -742,6 +755,14 @@ constexpr int kMaxCluster = 8;
 // The clusters lose where lengths are far apart (64 of 20 to 2000 rows: 27.8 and 26.4) and where
 // most warps of many groups have nothing to do (256 of up to 30 rows: 18.9 and 16.6; 150 of
 // them 11.3 and 12.8).
+// fp32 (blocks of 8 rows of 128 or 16 of 64), where equal lengths and few heads a group agree
+// with these bounds: D 128, 8 KV heads, 4 heads a group: 1 sequence of 1000 rows 6.6 and 8.7, of
+// 2000 9.1 and 10.6, of 4000 (behind the bound) 14.6 and 13.6; 9 of 4000 38.0 and 46.9, 64 of
+// 1000 77.9 and 86.2, 64 of 2000 (behind it) 147.7 and 155.0. With many heads a block costs a
+// warp more, and the clusters lose sooner: D 64, 16 heads a group: 1 sequence of 2000 rows 10.6
+// and 9.4, of 4000 15.8 and 10.4; and where lengths are far apart: 64 of 66 to 4000 rows, 16 heads
+// on one KV head, 29.5 and 21.9; 64 of 33 to 2000, 7 on each of 4, 32.1 and 25.2; 9 of which one
+// has 5979 and the next 1792, 7 on each of 4, 15.7 and 14.0 (1437 and 897: 7.9 and 10.9).
 constexpr int kShortFew = 8, kShortMany = 32;
 
 template <typename T, int D, int G>
