@@ -496,7 +496,8 @@ ripple_status ripple_paged_decode_workspace_bytes(const ripple_paged_desc *desc,
  * n_q_heads  a multiple of Hkv, G <= 16
  * scale      logit scale, >= 0, at most 2^127; 0 means 1 / sqrt(d)
  * q          [B][n_q_heads][d] by q_strides (its token_stride is not used; NULL: dense)
- * out        device fp32 [B][n_q_heads][d]
+ * out        device fp32 [B][n_q_heads][d]; the outputs share no memory with the
+ *            inputs
  * lse        device fp32 [B][n_q_heads], or NULL
  * workspace  device scratch, 256-byte aligned; its contents need no initialisation.
  *            Calls that share a workspace must be ordered on the GPU.
@@ -543,12 +544,12 @@ ripple_status ripple_paged_decode_attn(const ripple_paged_desc *desc, int32_t n_
  * logprob_out, entropy_out, lse_out  device fp32 [n_rows]; each may be NULL
  * top_idx_out, top_logprob_out       device int32 and fp32 [n_rows][n_top], NULL where
  *             n_top is 0; top_logprob_out may be NULL
- * Logits are aligned to their element, outputs to 4 bytes. The logits are read from
- * HBM once. Sums are fp32, of the terms relative to the row's largest logit, whose own
- * term is left out: with S' the sum of the others, log P = scale (x - max) -
- * log1p(S'), so that log probabilities near 0 and small entropies keep their relative
- * precision. Results do not depend on the run. One launch, no workspace. The call may
- * be captured in a CUDA graph.
+ * Logits are aligned to their element, outputs to 4 bytes; the outputs share no
+ * memory with the inputs. The logits are read from HBM once. Sums are fp32, of the
+ * terms relative to the row's largest logit, whose own term is left out: with S' the
+ * sum of the others, log P = scale (x - max) - log1p(S'), so that log probabilities
+ * near 0 and small entropies keep their relative precision. Results do not depend on
+ * the run. One launch, no workspace. The call may be captured in a CUDA graph.
  * Errors: RIPPLE_EINVAL, RIPPLE_ECUDA. Device status: RIPPLE_EBOUNDS.
  */
 ripple_status ripple_token_logprobs(int32_t n_rows, int32_t vocab, int64_t row_stride,
