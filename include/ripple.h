@@ -516,6 +516,170 @@ ripple_status ripple_paged_decode_attn(const ripple_paged_desc *desc, int32_t n_
                                        size_t workspace_bytes, int32_t *dev_status,
                                        void *stream);
 
+/*
+ * A paged cache in 8 bits. A row x of d values (one head's key or value of a token) is
+ * held as d codes (e4m3: sign, 4 exponent, 3 mantissa bits, largest value 448) in the
+ * pages and one byte s in the scales: x_i stands as code_i * 2^(s - 127). The append
+ * takes the least e with max_i |x_i| <= 448 * 2^e, at least -120; s = e + 127 and code_i
+ * is x_i * 2^-e rounded to nearest (even). So an element is off by at most 2^-4 of itself, or, below
+ * 2^-14 of the row's largest, by 2^-18 of that; what a row stands for is a bf16 value and
+ * finite (elements beyond 1.9375 * 2^127 are held as 1.875 * 2^127). A row that holds a
+ * NaN or an infinity is held as s = 255, which makes every element of it a NaN, and codes 0.
+ *
+ * The calls take a ripple_paged_desc whose dtype is that of q, k and v (and of the
+ * attention over a tree's output); its strides are those of the pages of codes, in bytes,
+ * multiples of 16. Row r of a sequence and head has its scale at
+ *   k_scales + page * page_stride + h * head_stride + slot * row_stride (bytes),
+ * v_scales likewise; all three strides 0 mean dense [n_pages][Hkv][page_size]. No
+ * place of the scales lies in the pages or in the other's. Pages that were written by
+ * other means hold no codes of a NaN (0x7f, 0xff); s is 7..247 or 255.
+ */
+typedef struct {
+  uint8_t *k_scales, *v_scales; /* device */
+  int64_t page_stride, head_stride, row_stride;
+} ripple_paged_scales;
+
+/*
+ * ripple_paged_append_q8 -- ripple_paged_append into a paged cache in 8 bits: the keys
+ * rotated and the values are held as above, from their fp32 values (one rounding); the
+ * queries as there. A row that is not stored leaves its scale alone as well.
+ * Errors: as ripple_paged_append; RIPPLE_EINVAL also for scales that overlap one another
+ * or the pages.
+ */
+ripple_status ripple_paged_append_q8(const ripple_paged_desc *desc,
+                                     const ripple_paged_scales *scales, const ripple_rope *rope,
+                                     int32_t n_tokens, const int32_t *seq_starts,
+                                     int32_t n_q_heads, const void *q,
+                                     const ripple_token_strides *q_strides, void *q_out,
+                                     const ripple_token_strides *q_out_strides, const void *k,
+                                     const ripple_token_strides *k_strides, const void *v,
+                                     const ripple_token_strides *v_strides,
+                                     const int32_t *positions, void *k_pages, void *v_pages,
+                                     const int32_t *block_table, const int32_t *lens,
+                                     int32_t *dev_status, void *stream);
+
+/* ripple_paged_decode_workspace_bytes for ripple_paged_decode_attn_q8. */
+ripple_status ripple_paged_decode_q8_workspace_bytes(const ripple_paged_desc *desc,
+                                                     int32_t n_q_heads, size_t *bytes_host);
+
+/*
+ * ripple_paged_decode_attn_q8 -- ripple_paged_decode_attn over a paged cache in 8 bits,
+ * with the same arguments and rules; out and lse are those of the values that the rows
+ * stand for, to fp32's precision. (An element of a query below 2^-39 of the head's
+ * largest, and a query below 2^-110, may count as 0.)
+ */
+ripple_status ripple_paged_decode_attn_q8(const ripple_paged_desc *desc,
+                                          const ripple_paged_scales *scales, int32_t n_q_heads,
+                                          float scale, const void *q,
+                                          const ripple_token_strides *q_strides,
+                                          const void *k_pages, const void *v_pages,
+                                          const int32_t *block_table, const int32_t *lens,
+                                          float *out, float *lse, void *workspace,
+                                          size_t workspace_bytes, int32_t *dev_status,
+                                          void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* Drafted tokens: several tokens of a sequence, a chain or a tree of guesses, */
+/* looked at in one step. They are appended first (ripple_paged_append, with   */
+/* their positions), attend (ripple_paged_tree_attn), and the accepted ones'   */
+/* rows are moved up (ripple_paged_keep_rows).                                 */
+/* ------------------------------------------------------------------------ */
+
+/* Most drafted tokens of a sequence. */
+#define RIPPLE_MAX_DRAFT 64
+
+/* Device workspace bytes ripple_paged_tree_attn needs on the current device, the same for
+ * every length; scales as in the call. Never fewer for a larger batch, a larger block
+ * table, or more tokens or query heads on as many KV heads. */
+ripple_status ripple_paged_tree_workspace_bytes(const ripple_paged_desc *desc,
+                                                const ripple_paged_scales *scales,
+                                                int32_t n_q_heads, int32_t max_tokens,
+                                                size_t *bytes_host);
+
+/*
+ * ripple_paged_tree_attn -- attention of the drafted tokens of every sequence over a paged
+ * cache that holds their rows last. With n_b drafted tokens, token i of sequence b sees
+ * the rows before the draft, r < lens[b] - n_b, and of the draft's own rows
+ * lens[b] - n_b + j those with bit j of its mask set:
+ *   out[i][q] = sum over the rows r that it sees of softmax_r(scale * q[i][q] . k[h][r]) * v[h][r],
+ *   lse[i][q] = log of the sum over them of exp(scale * q[i][q] . k[h][r]),
+ * KV head h = q / G, G = n_q_heads / Hkv. What a hidden row holds counts for nothing, also
+ * where it is infinite or NaN. A token that sees no row (an idle sequence, lens[b] <= 0; an
+ * empty mask and nothing before the draft) has out = 0 and lse = -infinity.
+ *
+ * scales      NULL: pages in dtype; otherwise pages in 8 bits
+ * n_tokens, seq_starts  the drafted tokens, as in ripple_paged_append: n_tokens / B of
+ *             every sequence, or those of seq_starts. Tokens outside
+ *             [seq_starts[0], seq_starts[B]) are left alone, their outputs too.
+ * max_tokens  most tokens of a sequence, 1..RIPPLE_MAX_DRAFT (uniform batches: at least
+ *             n_tokens / B). A sequence of seq_starts with more is reported as
+ *             RIPPLE_EBOUNDS and its outputs are unspecified.
+ * masks       device uint64 [n_tokens] in token order, or NULL: token i sees j <= i (a
+ *             chain). Bits from n_b on are not looked at.
+ * n_q_heads   a multiple of Hkv, G <= 16
+ * scale       as in ripple_paged_decode_attn
+ * q           [tokens][n_q_heads][d] by q_strides
+ * out         device [n_tokens][n_q_heads][d] in dtype; the outputs share no memory with
+ *             the inputs
+ * lse         device fp32 [n_tokens][n_q_heads], or NULL
+ * workspace   device scratch, 256-byte aligned; its contents need no initialisation.
+ *             Calls that share a workspace must be ordered on the GPU.
+ * Rows whose page entry is out of range, drafted tokens whose row is negative while
+ * lens[b] > 0 (both RIPPLE_EBOUNDS) and rows behind max_pages * page_size (RIPPLE_EFULL)
+ * are left out of the attention. Softmax statistics and sums are fp32. With dtype bf16
+ * the probabilities are rounded to bf16 (8-bit pages: fp16) for the matrix instructions, as the
+ * output is. Results do not depend on the run. The call may be captured in a CUDA graph:
+ * lengths, starts, masks and the table are read on the device.
+ * Errors: RIPPLE_EINVAL, RIPPLE_EWORKSPACE, RIPPLE_ECUDA. Device status: also RIPPLE_ETIMEOUT.
+ */
+ripple_status ripple_paged_tree_attn(const ripple_paged_desc *desc,
+                                     const ripple_paged_scales *scales, int32_t n_tokens,
+                                     const int32_t *seq_starts, int32_t max_tokens,
+                                     const uint64_t *masks, int32_t n_q_heads, float scale,
+                                     const void *q, const ripple_token_strides *q_strides,
+                                     const void *k_pages, const void *v_pages,
+                                     const int32_t *block_table, const int32_t *lens, void *out,
+                                     float *lse, void *workspace, size_t workspace_bytes,
+                                     int32_t *dev_status, void *stream);
+
+/*
+ * ripple_paged_keep_rows -- after a draft has been looked at: the accepted drafted tokens'
+ * rows moved up behind the rows before the draft, in the caches of n_layers layers of one
+ * shape, and the lengths without the rejected ones. For every layer l and sequence b with
+ * n_b drafted tokens, the keys and values (and scales) of row lens[l][b] - n_b + kept[b][j] go to
+ * row lens[l][b] - n_b + j, j ascending up to the end of kept[b], and
+ *   lens_out[l][b] = lens[l][b] - n_b + (tokens kept).
+ * Rows behind are left as they are.
+ *
+ * desc           of every layer's cache (the batch and the block tables' shape are theirs)
+ * scales_host    host [n_layers], strides all alike, or NULL: pages in desc->dtype
+ * n_layers       1..RIPPLE_MAX_LAYERS
+ * k_pages_host, v_pages_host, block_tables_host  host arrays of n_layers device pointers.
+ *                No two layers' pools have a place in common; a page that holds drafted
+ *                rows belongs to one sequence only.
+ * n_tokens, seq_starts  the drafted tokens, as in ripple_paged_append
+ * max_kept       0..RIPPLE_MAX_DRAFT
+ * kept           device int32 [B][max_kept] (NULL where max_kept is 0): the accepted tokens
+ *                of the draft, ascending, each once; a negative entry ends a sequence's list.
+ *                An entry that is no token of the draft or does not ascend is reported as
+ *                RIPPLE_EBOUNDS and ends it too.
+ * lens           device int32 [n_layers][B], the drafted tokens included; a sequence with
+ *                lens <= 0 is idle: nothing is moved, lens_out is lens
+ * lens_out       device int32 [n_layers][B]; may be lens, else apart from it
+ * Rows whose page entry is out of range, and a draft with more tokens than rows
+ * (lens_out is then lens), are reported as RIPPLE_EBOUNDS and not moved, rows behind
+ * max_pages * page_size as RIPPLE_EFULL. One launch; no workspace. The call may be captured
+ * in a CUDA graph.
+ * Errors: RIPPLE_EINVAL, RIPPLE_ECUDA.
+ */
+ripple_status ripple_paged_keep_rows(const ripple_paged_desc *desc,
+                                     const ripple_paged_scales *scales_host, int32_t n_layers,
+                                     void *const *k_pages_host, void *const *v_pages_host,
+                                     const int32_t *const *block_tables_host, int32_t n_tokens,
+                                     const int32_t *seq_starts, int32_t max_kept,
+                                     const int32_t *kept, const int32_t *lens, int32_t *lens_out,
+                                     int32_t *dev_status, void *stream);
+
 /* Largest number of alternatives ripple_token_logprobs gives. */
 #define RIPPLE_MAX_TOP 32
 

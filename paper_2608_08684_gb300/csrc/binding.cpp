@@ -18,7 +18,9 @@ struct Cache {
   void *k, *v;
   const int32_t *table;
   int device;
-  at::ScalarType type;
+  at::ScalarType type;            // of q, k and v
+  ripple_paged_scales scales;     // of 8-bit pages, NULL pointers otherwise
+  const ripple_paged_scales *codes() const { return scales.k_scales != nullptr ? &scales : nullptr; }
 };
 
 // A call's refusal; the message goes into a ValueError.
@@ -90,11 +92,14 @@ float scale_of(PyObject *o) {
   return scale;
 }
 
-template <typename F>
-F *entry(PyObject *o) {
+void *entry(PyObject *o) {
   void *f = PyLong_AsVoidPtr(o);
   if (f == nullptr) throw Refused{PyErr_Occurred() ? nullptr : "no entry point"};
-  return reinterpret_cast<F *>(f);
+  return f;
+}
+template <typename F>
+F *entry(PyObject *o) {
+  return reinterpret_cast<F *>(entry(o));
 }
 
 const Cache &cache_of(PyObject *o) {
@@ -120,9 +125,9 @@ bool args_are(Py_ssize_t n, Py_ssize_t want) {
   return n == want;
 }
 
-// cache(desc address, k, v, table addresses, device, is bf16)
+// cache(desc address, k, v, table addresses, device, is bf16, scales address or None)
 PyObject *cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  if (!args_are(n, 6)) return nullptr;
+  if (!args_are(n, 7)) return nullptr;
   const void *desc = PyLong_AsVoidPtr(a[0]);
   Cache c;
   c.k = PyLong_AsVoidPtr(a[1]);
@@ -130,7 +135,10 @@ PyObject *cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
   c.table = static_cast<const int32_t *>(PyLong_AsVoidPtr(a[3]));
   c.device = (int)PyLong_AsLong(a[4]);
   c.type = PyObject_IsTrue(a[5]) == 1 ? at::kBFloat16 : at::kFloat;
+  c.scales = ripple_paged_scales{};
+  const void *scales = a[6] == Py_None ? nullptr : PyLong_AsVoidPtr(a[6]);
   if (PyErr_Occurred()) return nullptr;
+  if (scales != nullptr) c.scales = *static_cast<const ripple_paged_scales *>(scales);
   if (desc == nullptr) {
     PyErr_SetString(PyExc_ValueError, "no descriptor");
     return nullptr;
@@ -145,12 +153,12 @@ PyObject *cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return o;
 }
 
-// paged_append(entry, cache, rope address or None, lens, k, v, positions, seq_starts, q, q_out,
+// paged_append(entry (of the cache's kind: 8-bit pages have one of their own), cache, rope address or None, lens, k, v, positions, seq_starts, q, q_out,
 // dev_status, stream)
 PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!args_are(n, 12)) return nullptr;
   return guarded([&] {
-    auto *call = entry<decltype(ripple_paged_append)>(a[0]);
+    void *call = entry(a[0]);
     const Cache &c = cache_of(a[1]);
     const ripple_rope *rope = nullptr;
     if (a[2] != Py_None) {
@@ -197,8 +205,14 @@ PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *stream = stream_of(a[11]);
     ripple_status s;
     Py_BEGIN_ALLOW_THREADS
-    s = call(&c.desc, rope, (int32_t)tokens, starts, (int32_t)heads, q, &qs, q_out, &os, k.data,
-             &k.strides, v.data, &v.strides, positions, c.k, c.v, c.table, lens, status, stream);
+    if (c.codes() != nullptr)
+      s = reinterpret_cast<decltype(ripple_paged_append_q8) *>(call)(
+          &c.desc, &c.scales, rope, (int32_t)tokens, starts, (int32_t)heads, q, &qs, q_out, &os,
+          k.data, &k.strides, v.data, &v.strides, positions, c.k, c.v, c.table, lens, status, stream);
+    else
+      s = reinterpret_cast<decltype(ripple_paged_append) *>(call)(
+          &c.desc, rope, (int32_t)tokens, starts, (int32_t)heads, q, &qs, q_out, &os, k.data,
+          &k.strides, v.data, &v.strides, positions, c.k, c.v, c.table, lens, status, stream);
     Py_END_ALLOW_THREADS
     return (long)s;
   });
@@ -208,7 +222,7 @@ PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyObject *paged_decode_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!args_are(n, 10)) return nullptr;
   return guarded([&] {
-    auto *call = entry<decltype(ripple_paged_decode_attn)>(a[0]);
+    void *call = entry(a[0]);
     const float scale = scale_of(a[7]);
     const Cache &c = cache_of(a[1]);
     need(c10::cuda::current_device() == c.device, kDevice);
@@ -235,8 +249,72 @@ PyObject *paged_decode_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *stream = stream_of(a[9]);
     ripple_status s;
     Py_BEGIN_ALLOW_THREADS
-    s = call(&c.desc, (int32_t)q.heads, scale, q.data, &q.strides, c.k, c.v, c.table, lens,
-             out, lse, w.data_ptr(), w.nbytes(), status, stream);
+    if (c.codes() != nullptr)
+      s = reinterpret_cast<decltype(ripple_paged_decode_attn_q8) *>(call)(
+          &c.desc, &c.scales, (int32_t)q.heads, scale, q.data, &q.strides, c.k, c.v, c.table, lens,
+          out, lse, w.data_ptr(), w.nbytes(), status, stream);
+    else
+      s = reinterpret_cast<decltype(ripple_paged_decode_attn) *>(call)(
+          &c.desc, (int32_t)q.heads, scale, q.data, &q.strides, c.k, c.v, c.table, lens, out, lse,
+          w.data_ptr(), w.nbytes(), status, stream);
+    Py_END_ALLOW_THREADS
+    return (long)s;
+  });
+}
+
+// paged_tree_attn(entry, cache, q, lens, out, workspace, masks, seq_starts, max_tokens or None, lse,
+// scale, dev_status, stream)
+PyObject *paged_tree_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!args_are(n, 13)) return nullptr;
+  return guarded([&] {
+    auto *call = entry<decltype(ripple_paged_tree_attn)>(a[0]);
+    const float scale = scale_of(a[10]);
+    const Cache &c = cache_of(a[1]);
+    need(c10::cuda::current_device() == c.device, kDevice);
+    const bool ragged = a[7] != Py_None;
+    const Tokens q(a[2], c, ragged);
+    need(ragged || (q.dim == 4 && q.lead[0] == c.desc.batch),
+         "q must be [B][n][Hq][d], or with seq_starts [tokens][Hq][d]");
+    const int64_t tokens = q.lead[0] * q.lead[1];
+    need(tokens <= 0x7fffffff && q.heads <= 0x7fffffff, "too many tokens");
+    need(a[3] != Py_None && a[4] != Py_None && a[5] != Py_None, "expected a tensor");
+    const int32_t *lens = dense<int32_t>(a[3], c.device, at::kInt, "lens must be int32 [B]", c.desc.batch);
+    const at::Tensor &t = tensor(a[2]), &o = tensor(a[4]);
+    need(o.sizes() == t.sizes(), "out must have q's shape and dtype");
+    void *out = dense<void>(a[4], c.device, c.type, "out must have q's shape and dtype");
+    const at::Tensor &w = tensor(a[5]);
+    need(w.get_device() == c.device, kDevice);
+    need(w.is_contiguous(), "expected a contiguous tensor");
+    const at::IntArrayRef lead = t.sizes().slice(0, t.dim() - 2);
+    const uint64_t *masks = nullptr;
+    if (a[6] != Py_None) {
+      need(tensor(a[6]).sizes() == lead, "masks must be int64 with q's leading sizes");
+      masks = dense<uint64_t>(a[6], c.device, at::kLong, "masks must be int64 with q's leading sizes");
+    }
+    const int32_t *starts = dense<int32_t>(a[7], c.device, at::kInt,
+                                           "seq_starts must be int32 [B + 1]",
+                                           (int64_t)c.desc.batch + 1);
+    int64_t most = RIPPLE_MAX_DRAFT;
+    if (a[8] != Py_None) {
+      most = PyLong_AsLongLong(a[8]);
+      if (PyErr_Occurred()) throw Refused{nullptr};
+      need(most >= 0 && most <= RIPPLE_MAX_DRAFT, "too many tokens of a sequence");
+    } else if (!ragged) {
+      most = q.lead[1];
+      need(most <= RIPPLE_MAX_DRAFT, "too many tokens of a sequence");
+    }
+    float *lse = nullptr;
+    if (a[9] != Py_None) {
+      need(tensor(a[9]).sizes() == t.sizes().slice(0, t.dim() - 1), "lse must be fp32 [..][Hq]");
+      lse = dense<float>(a[9], c.device, at::kFloat, "lse must be fp32 [..][Hq]");
+    }
+    int32_t *status = dense<int32_t>(a[11], c.device, at::kInt, "dev_status must be int32");
+    void *stream = stream_of(a[12]);
+    ripple_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = call(&c.desc, c.codes(), (int32_t)tokens, starts, (int32_t)most, masks, (int32_t)q.heads,
+             scale, q.data, &q.strides, c.k, c.v, c.table, lens, out, lse, w.data_ptr(), w.nbytes(),
+             status, stream);
     Py_END_ALLOW_THREADS
     return (long)s;
   });
@@ -296,7 +374,8 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
 #define RIPPLE_METHOD(name) \
   {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {RIPPLE_METHOD(cache), RIPPLE_METHOD(paged_append),
-                          RIPPLE_METHOD(paged_decode_attn), RIPPLE_METHOD(token_logprobs),
+                          RIPPLE_METHOD(paged_decode_attn), RIPPLE_METHOD(paged_tree_attn),
+                          RIPPLE_METHOD(token_logprobs),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};

@@ -44,12 +44,12 @@ inline bool disjoint(int n, const long long *stride, const long long *count, lon
   return true;
 }
 
-// Whether an element lies in a row of `a` and in one of `b`. Dimensions that both have with
+// Whether an element lies in a row of `a` (inner elements) and in one of `b` (inner_b, or as many). Dimensions that both have with
 // the same stride are looked at row by row (by the difference of the indices), the others as
 // the span that they reach over: what is said to be apart is, and two views of one buffer
 // that interleave (heads side by side in a token's row) are told from ones that overlap.
-inline bool overlap(const RowSet &a, const RowSet &b, long long inner) {
-  long long span_a = inner, span_b = inner;
+inline bool overlap(const RowSet &a, const RowSet &b, long long inner, long long inner_b = -1) {
+  long long span_a = inner, span_b = inner_b < 0 ? inner : inner_b;
   long long stride[3], most[3], least[3];  // of the shared dimensions, and the index differences
   int n = 0;
   for (int i = 0; i < 3; ++i) {
@@ -110,10 +110,13 @@ inline int vec_elems(int dtype) {
   return dtype == RIPPLE_BF16 ? 8 : dtype == RIPPLE_F32 ? 4 : 0;
 }
 
-inline bool paged_geom(const ripple_paged_desc *d, PagedGeom *g) {
+// codes: pages of 8-bit codes, whose strides count bytes.
+inline bool paged_geom(const ripple_paged_desc *d, PagedGeom *g, bool codes = false) {
   if (d == nullptr) return false;
-  const int vec = vec_elems(d->dtype);
-  if (vec == 0 || d->batch < 1 || d->n_kv_heads < 1 || d->n_pages < 1 || d->max_pages < 1)
+  int vec = vec_elems(d->dtype);
+  if (vec == 0) return false;
+  if (codes) vec = 16;
+  if (d->batch < 1 || d->n_kv_heads < 1 || d->n_pages < 1 || d->max_pages < 1)
     return false;
   if (d->head_dim != 64 && d->head_dim != 128) return false;
   if (d->page_size < 1 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)) != 0)
@@ -142,6 +145,33 @@ inline bool paged_geom(const ripple_paged_desc *d, PagedGeom *g) {
   for (int i = 0; i < 3; ++i)
     if (stride[i] < 0 || stride[i] > (1LL << 48) / count[i] || stride[i] % vec != 0) return false;
   return disjoint(3, stride, count, d->head_dim);
+}
+
+// The scales of 8-bit pages, a byte a row and head.
+struct ScaleGeom {
+  uint8_t *k, *v;
+  long long page_stride, head_stride, row_stride;  // bytes
+  RowSet rows(const uint8_t *scales, const PagedGeom &g) const {
+    return RowSet{(long long)(uintptr_t)scales,
+                  {row_stride, head_stride, page_stride},
+                  {1LL << g.shift, g.Hkv, g.n_pages}};
+  }
+};
+
+// desc has passed paged_geom.
+inline bool scale_geom(const ripple_paged_desc *d, const ripple_paged_scales *s, ScaleGeom *g) {
+  if (s == nullptr || s->k_scales == nullptr || s->v_scales == nullptr) return false;
+  *g = ScaleGeom{s->k_scales, s->v_scales, s->page_stride, s->head_stride, s->row_stride};
+  if (s->row_stride == 0 && s->head_stride == 0 && s->page_stride == 0) {
+    g->row_stride = 1;
+    g->head_stride = d->page_size;
+    g->page_stride = (long long)d->n_kv_heads * d->page_size;
+  }
+  const long long stride[3] = {g->row_stride, g->head_stride, g->page_stride};
+  const long long count[3] = {d->page_size, d->n_kv_heads, d->n_pages};
+  for (int i = 0; i < 3; ++i)
+    if (stride[i] < 0 || stride[i] > (1LL << 48) / count[i]) return false;
+  return disjoint(3, stride, count, 1);
 }
 
 }  // namespace ripple

@@ -1,5 +1,5 @@
-// ripple_paged_append: new tokens' keys and values into a paged cache, keys and
-// queries rotated to their positions on the way, one pass over q, k and v.
+// ripple_paged_append and ripple_paged_append_q8: new tokens' keys and values into a paged
+// cache, keys and queries rotated to their positions on the way, one pass over q, k and v.
 //
 // Rotation: the angle pos * inv_freq is only needed modulo a turn. The host gives
 // f_j = inv_freq_j / (2 pi) as a 64-bit fraction of a turn (modulo one turn, to
@@ -15,6 +15,10 @@
 // same eight compute them together). A token's Hq + 2 Hkv head rows are cut into groups
 // of 32 / (d / 16) rows, one per warp step; with few tokens every warp takes one group,
 // with many a warp takes several, the loads of kAhead of them in flight at a time.
+// 8-bit pages: the lanes of a head row, which all have it in registers as fp32, find its
+// largest magnitude by shuffles (as integers, so that NaNs count as the largest), and each
+// writes 16 codes. The scale is a power of two, so that scaling rounds nothing.
+#include <cuda_fp8.h>
 #include <math.h>
 
 #include "common.cuh"
@@ -40,6 +44,7 @@ struct AppendParams {
   TokenRows q, k, v, q_out;
   const int32_t *starts, *positions, *table, *lens;
   void *k_pages, *v_pages;
+  ScaleGeom sc;                // 8-bit pages
   int32_t *status;
   unsigned long long freq[kMaxPairs];  // turns per position, times 2^64
 };
@@ -95,6 +100,31 @@ __device__ __forceinline__ void pack(const float (&x)[8], Raw8<__nv_bfloat16> &r
   r.u[0] = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// The scale byte of a row whose largest magnitude has these bits: the least e >= -120 with
+// it <= 448 2^e = 1.75 2^(e + 8), plus 127; 255 for an infinity or a NaN.
+__device__ __forceinline__ int scale_byte(uint32_t most) {
+  if (most >= 0x7f800000u) return 255;
+  const int e = (int)(most >> 23) - 127 - 8 + ((most & 0x7fffffu) > 0x600000u);
+  return max(e, -120) + 127;
+}
+// Eight values over the scale, to nearest even in e4m3. (247: 256 2^120 would be infinite.)
+__device__ __forceinline__ uint2 codes_of(const float (&x)[8], int byte) {
+  if (byte == 255) return make_uint2(0, 0);
+  const float f = __int_as_float((254 - byte) << 23);
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo = x[2 * i] * f, hi = x[2 * i + 1] * f;
+    if (byte == 247) {
+      lo = fminf(fmaxf(lo, -240.f), 240.f);
+      hi = fminf(fmaxf(hi, -240.f), 240.f);
+    }
+    const uint32_t c = __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+    w[i / 2] |= c << (16 * (i & 1));
+  }
+  return make_uint2(w[0], w[1]);
+}
+
 // Cosine and sine of `turns` / 2^64 turns.
 __device__ __forceinline__ void cos_sin(unsigned long long turns, float &c, float &s) {
   const uint32_t x = (uint32_t)(turns >> 32);
@@ -123,8 +153,8 @@ __device__ __forceinline__ int find_seq(const int32_t *starts, int B, int t, int
   }
 }
 
-// kAhead: groups whose loads are in flight at a time.
-template <typename T, int D, bool kInter, int kAhead>
+// kAhead: groups whose loads are in flight at a time. kCodes: 8-bit pages.
+template <typename T, int D, bool kInter, int kAhead, bool kCodes>
 __global__ void __launch_bounds__(kAppendWarps * 32)
     append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int kLanes = D / 16;       // lanes per head row
@@ -181,6 +211,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32)
   const long long pos = p.positions != nullptr ? (long long)p.positions[t] : row;
   int32_t bad = 0;
   long long place = -1;  // element offset of the row, head 0
+  long long scale_at = 0;
   if (len > 0) {
     const long long pg = row >> p.g.shift;
     if (row < 0) {
@@ -192,9 +223,13 @@ __global__ void __launch_bounds__(kAppendWarps * 32)
                                      (long long)p.g.B * p.g.max_pages, p.status)];
       if ((unsigned)page >= (unsigned)p.g.n_pages)
         bad = RIPPLE_EBOUNDS;
-      else
-        place = guard(page, 1, p.g.n_pages, p.status) * p.g.page_stride +
-                (row & ((1 << p.g.shift) - 1)) * p.g.row_stride;
+      else {
+        const long long slot = row & ((1 << p.g.shift) - 1);
+        place = guard(page, 1, p.g.n_pages, p.status) * p.g.page_stride + slot * p.g.row_stride;
+        if (kCodes)
+          scale_at = guard(page, 1, p.g.n_pages, p.status) * p.sc.page_stride +
+                     slot * p.sc.row_stride;
+      }
     }
   }
   if (bad != 0 && part == 0 && lane == 0) report(p.status, bad);
@@ -226,13 +261,13 @@ __global__ void __launch_bounds__(kAppendWarps * 32)
       const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.g.Hkv;
       if (!is_q && place < 0) continue;
       const int h = is_q ? r : is_v ? r - p.Hq - p.g.Hkv : r - p.Hq;
-      T *to = is_q ? (T *)p.q_out.data + src_b * p.q_out.seq + src_i * p.q_out.token +
-                         h * p.q_out.head
-                   : (T *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
-      if (turns && !is_v) {
-        float a[8], d[8];
+      float a[8], d[8];
+      const bool turned = turns && !is_v;
+      if (turned || (kCodes && !is_q)) {
         unpack(x[u], a);
         unpack(y[u], d);
+      }
+      if (turned) {
         if (kInter) {  // pairs (0, 1), (2, 3), .. of the 16 elements a, d
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -250,6 +285,26 @@ __global__ void __launch_bounds__(kAppendWarps * 32)
             d[j] = d0 * c[j] + a0 * s[j];
           }
         }
+      }
+      if (kCodes && !is_q) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          most = max(most, max(__float_as_uint(a[j]) & 0x7fffffffu, __float_as_uint(d[j]) & 0x7fffffffu));
+        const uint32_t row_lanes = ((1u << kLanes) - 1) << (sub * kLanes);
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) most = max(most, __shfl_xor_sync(row_lanes, most, o));
+        const int byte = scale_byte(most);
+        uint8_t *to = (uint8_t *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
+        *reinterpret_cast<uint2 *>(to + o0) = codes_of(a, byte);
+        *reinterpret_cast<uint2 *>(to + o1) = codes_of(d, byte);
+        if (l == 0) (is_v ? p.sc.v : p.sc.k)[scale_at + h * p.sc.head_stride] = (uint8_t)byte;
+        continue;
+      }
+      T *to = is_q ? (T *)p.q_out.data + src_b * p.q_out.seq + src_i * p.q_out.token +
+                         h * p.q_out.head
+                   : (T *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
+      if (turned) {
         pack(a, x[u]);
         pack(d, y[u]);
       }
@@ -282,7 +337,7 @@ unsigned long long to_turns(double inv_freq) {
 // A programmatic dependent of the kernel before it, as that one ends: without a trigger in
 // it, since CTAs that wait in its SMs cost more (a batch of 108 tokens 5.2 us from a graph,
 // 3.7 without) than an earlier start gains (one token 2.9, 3.0).
-template <typename T, int D, bool kInter, int kAhead>
+template <typename T, int D, bool kInter, int kAhead, bool kCodes>
 cudaError_t launch_as(const AppendParams &p, int grid, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
@@ -293,18 +348,28 @@ cudaError_t launch_as(const AppendParams &p, int grid, cudaStream_t st) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, append_kernel<T, D, kInter, kAhead>, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, append_kernel<T, D, kInter, kAhead, kCodes>, p);
   count_launches(1);
   return e;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kCodes>
 cudaError_t launch(const AppendParams &p, bool inter, int grid, cudaStream_t st) {
   constexpr int kMany = sizeof(T) == 2 && D == 64 ? 4 : 2;  // 4 to 8 loads of a lane in flight
   if (p.per_warp == 1)
-    return inter ? launch_as<T, D, true, 1>(p, grid, st) : launch_as<T, D, false, 1>(p, grid, st);
-  return inter ? launch_as<T, D, true, kMany>(p, grid, st)
-               : launch_as<T, D, false, kMany>(p, grid, st);
+    return inter ? launch_as<T, D, true, 1, kCodes>(p, grid, st)
+                 : launch_as<T, D, false, 1, kCodes>(p, grid, st);
+  return inter ? launch_as<T, D, true, kMany, kCodes>(p, grid, st)
+               : launch_as<T, D, false, kMany, kCodes>(p, grid, st);
+}
+
+template <bool kCodes>
+cudaError_t launch_any(const AppendParams &p, int dtype, bool inter, int grid, cudaStream_t st) {
+  if (dtype == RIPPLE_BF16)
+    return p.g.D == 128 ? launch<__nv_bfloat16, 128, kCodes>(p, inter, grid, st)
+                        : launch<__nv_bfloat16, 64, kCodes>(p, inter, grid, st);
+  return p.g.D == 128 ? launch<float, 128, kCodes>(p, inter, grid, st)
+                      : launch<float, 64, kCodes>(p, inter, grid, st);
 }
 
 // A tensor of tokens: pointer and strides in place.
@@ -327,20 +392,18 @@ bool row_set(const TokenRows &t, const AppendParams &p, int heads, int elem, Row
   return true;
 }
 
-}  // namespace
-}  // namespace ripple
-
-using namespace ripple;
-
-extern "C" ripple_status ripple_paged_append(
-    const ripple_paged_desc *desc, const ripple_rope *rope, int32_t n_tokens,
+// scales: NULL for pages in desc->dtype.
+ripple_status append(
+    const ripple_paged_desc *desc, const ripple_paged_scales *scales, const ripple_rope *rope, int32_t n_tokens,
     const int32_t *seq_starts, int32_t n_q_heads, const void *q,
     const ripple_token_strides *q_strides, void *q_out, const ripple_token_strides *q_out_strides,
     const void *k, const ripple_token_strides *k_strides, const void *v,
     const ripple_token_strides *v_strides, const int32_t *positions, void *k_pages, void *v_pages,
     const int32_t *block_table, const int32_t *lens, int32_t *dev_status, void *stream) {
   AppendParams p;
-  if (!paged_geom(desc, &p.g) || n_tokens < 0) return RIPPLE_EINVAL;
+  const bool codes = scales != nullptr;
+  p.sc = ScaleGeom{};
+  if (!paged_geom(desc, &p.g, codes) || (codes && !scale_geom(desc, scales, &p.sc)) || n_tokens < 0) return RIPPLE_EINVAL;
   if (seq_starts == nullptr && n_tokens % desc->batch != 0) return RIPPLE_EINVAL;
   if ((q == nullptr) != (q_out == nullptr)) return RIPPLE_EINVAL;
   p.rot = 0;
@@ -389,8 +452,15 @@ extern "C" ripple_status ripple_paged_append(
       if (overlap(in[i], to, desc->head_dim)) return RIPPLE_EINVAL;
     p.Hq = n_q_heads;
   }
-  const RowSet pool[2] = {p.g.rows(k_pages, elem), p.g.rows(v_pages, elem)};
+  const int page_elem = codes ? 1 : elem;
+  const RowSet pool[2] = {p.g.rows(k_pages, page_elem), p.g.rows(v_pages, page_elem)};
   if (overlap(pool[0], pool[1], desc->head_dim)) return RIPPLE_EINVAL;
+  if (codes) {
+    const RowSet sc[2] = {p.sc.rows(p.sc.k, p.g), p.sc.rows(p.sc.v, p.g)};
+    if (overlap(sc[0], sc[1], 1)) return RIPPLE_EINVAL;
+    for (int i = 0; i < 4; ++i)
+      if (overlap(pool[i / 2], sc[i % 2], desc->head_dim, 1)) return RIPPLE_EINVAL;
+  }
   p.starts = seq_starts;
   p.positions = positions;
   p.table = block_table;
@@ -409,13 +479,37 @@ extern "C" ripple_status ripple_paged_append(
   const long long ctas = ((long long)n_tokens * p.warps + kAppendWarps - 1) / kAppendWarps;
   if (ctas > 0x7fffffffLL / kAppendWarps) return RIPPLE_EINVAL;
   cudaStream_t st = (cudaStream_t)stream;
-  cudaError_t e;
-  if (desc->dtype == RIPPLE_BF16)
-    e = desc->head_dim == 128 ? launch<__nv_bfloat16, 128>(p, inter, (int)ctas, st)
-                              : launch<__nv_bfloat16, 64>(p, inter, (int)ctas, st);
-  else
-    e = desc->head_dim == 128 ? launch<float, 128>(p, inter, (int)ctas, st)
-                              : launch<float, 64>(p, inter, (int)ctas, st);
-  RIPPLE_CUDA_TRY(e);
+  RIPPLE_CUDA_TRY(codes ? launch_any<true>(p, desc->dtype, inter, (int)ctas, st)
+                        : launch_any<false>(p, desc->dtype, inter, (int)ctas, st));
   return RIPPLE_OK;
+}
+
+}  // namespace
+}  // namespace ripple
+
+using namespace ripple;
+
+extern "C" ripple_status ripple_paged_append(
+    const ripple_paged_desc *desc, const ripple_rope *rope, int32_t n_tokens,
+    const int32_t *seq_starts, int32_t n_q_heads, const void *q,
+    const ripple_token_strides *q_strides, void *q_out, const ripple_token_strides *q_out_strides,
+    const void *k, const ripple_token_strides *k_strides, const void *v,
+    const ripple_token_strides *v_strides, const int32_t *positions, void *k_pages, void *v_pages,
+    const int32_t *block_table, const int32_t *lens, int32_t *dev_status, void *stream) {
+  return append(desc, nullptr, rope, n_tokens, seq_starts, n_q_heads, q, q_strides, q_out,
+                q_out_strides, k, k_strides, v, v_strides, positions, k_pages, v_pages, block_table,
+                lens, dev_status, stream);
+}
+
+extern "C" ripple_status ripple_paged_append_q8(
+    const ripple_paged_desc *desc, const ripple_paged_scales *scales, const ripple_rope *rope, int32_t n_tokens,
+    const int32_t *seq_starts, int32_t n_q_heads, const void *q,
+    const ripple_token_strides *q_strides, void *q_out, const ripple_token_strides *q_out_strides,
+    const void *k, const ripple_token_strides *k_strides, const void *v,
+    const ripple_token_strides *v_strides, const int32_t *positions, void *k_pages, void *v_pages,
+    const int32_t *block_table, const int32_t *lens, int32_t *dev_status, void *stream) {
+  if (scales == nullptr) return RIPPLE_EINVAL;
+  return append(desc, scales, rope, n_tokens, seq_starts, n_q_heads, q, q_strides, q_out,
+                q_out_strides, k, k_strides, v, v_strides, positions, k_pages, v_pages, block_table,
+                lens, dev_status, stream);
 }

@@ -1,0 +1,535 @@
+// ripple_paged_tree_attn: attention of a tree of drafted tokens per sequence over a paged
+// cache. Entry points, the kernel on the CUDA cores (fp32 queries) and the join.
+//
+// fp32: a CTA of four warps has 32 query rows and takes blocks of 32 keys. Scores: a thread
+// has 4 rows x 2 keys, outputs: 4 rows x D / 16 dims, both from shared memory by 16 bytes
+// (24 and 40 FMAs for six and three loads); the next block's rows are loaded into registers
+// meanwhile. Bound by the FMAs above a few rows a KV head: 4 n G d of them a cache row, which has
+// 8 d bytes.
+#include "paged_tree.cuh"
+
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include <atomic>
+
+namespace ripple {
+namespace {
+
+constexpr int kMaxDevices = 64;
+constexpr int kThreads = 128;
+constexpr int R = kTreeSimtRows, KB = kTreeSimtKeys;
+constexpr float kSlack = 8.f;
+
+// 16 bytes of a page's row: 4 fp32 values, or 16 codes.
+template <typename T>
+struct Piece;
+template <>
+struct Piece<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void put(float *to, const uint4 &u, float) {
+    *reinterpret_cast<uint4 *>(to) = u;
+  }
+};
+template <>
+struct Piece<uint8_t> {
+  static constexpr int N = 16;
+  static __device__ __forceinline__ void put(float *to, const uint4 &u, float scale) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float x[4];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i] >> (16 * j)), __NV_E4M3);
+        const float2 f = __half22float2(__half2(h));
+        x[2 * j] = f.x * scale;
+        x[2 * j + 1] = f.y * scale;
+      }
+      *reinterpret_cast<float4 *>(to + 4 * i) = make_float4(x[0], x[1], x[2], x[3]);
+    }
+  }
+};
+
+template <int D>
+struct SimtSmem {
+  static constexpr int LD = D + 4;  // rows of a quarter warp start in other banks
+  float q[R][LD], k[KB][LD], v[KB][D];
+  float p[KB][R + 4];   // probabilities; negative: the key is hidden from the row
+  float m[R], l[R], a[R];
+  uint64_t mask[R];
+};
+
+__device__ __forceinline__ float scale_of_byte(int s) {
+  return s == 255 ? __int_as_float(0x7fffffff) : __int_as_float(s << 23);  // (7..247)
+}
+
+// T: float, or uint8_t for codes. Queries and outputs fp32.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
+    tree_simt_kernel(const __grid_constant__ TreeParams p) {
+  using P = Piece<T>;
+  using W = TreeWalk<KB>;
+  constexpr int kPieces = D / P::N;                        // of a row
+  constexpr int kMine = KB * kPieces / kThreads;           // of a block's keys, a thread
+  constexpr bool kCodes = sizeof(T) == 1;
+  constexpr int LD = SimtSmem<D>::LD;
+  constexpr int DT = D / 16;                               // output dims of a thread
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  SimtSmem<D> &s = *reinterpret_cast<SimtSmem<D> *>(smem_raw);
+  static_assert(KB * kPieces % kThreads == 0, "");
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int run = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
+  pdl_wait();
+  if (blockIdx.x == 0)
+    for (int b = tid; b < p.g.B; b += kThreads) TreeSeq::check(p, b);
+  W w;
+  const long long total = w.start(p, run, lane);
+  int2 rec = make_int2(0, 0);
+  long long t = 0;
+  const int runs = (int)min((long long)p.n_runs, total);
+  if (total > 0) t = run_start(total, runs, run);
+  for (bool more = total > 0; more; t += w.count(), more = w.next(p)) {
+    const TreeSeq seq(p, w.b);
+    const bool here = w.block == 0, ends = w.block + w.count() == w.blocks();
+    if (here && !ends) rec = make_int2(w.b * p.g.Hkv + w.h, run_of(total, runs, t + w.blocks() - 1) - run + 1);
+    const int n_rows = min(seq.tokens * p.G - tile * R, R);
+    if (n_rows <= 0) continue;
+    // this tile's queries (scaled) and masks; row r is token r / G, head r % G
+    for (int i = tid; i < R * (D / 4); i += kThreads) {
+      const int r = i / (D / 4), c = i % (D / 4) * 4;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < n_rows) {
+        const int row = tile * R + r, tok = row / p.G, head = w.h * p.G + row % p.G;
+        const float *q = (const float *)p.q + head * p.q_head +
+                         (p.starts == nullptr ? w.b * p.q_seq + tok * p.q_token
+                                              : (long long)(seq.first + tok) * p.q_token);
+        x = *reinterpret_cast<const float4 *>(q + c);
+        x = make_float4(x.x * p.scale2, x.y * p.scale2, x.z * p.scale2, x.w * p.scale2);
+      }
+      *reinterpret_cast<float4 *>(&s.q[r][c]) = x;
+    }
+    if (tid < R) {
+      const int tok = (tile * R + tid) / p.G;
+      uint64_t mask = 0;
+      if (tid < n_rows)
+        mask = p.masks == nullptr ? ~0ull >> (63 - tok) : p.masks[seq.first + tok];
+      s.mask[tid] = mask;
+      s.m[tid] = -INFINITY;
+      s.l[tid] = 0.f;
+    }
+    float o[4][DT];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < DT; ++j) o[i][j] = 0.f;
+    const int rg = tid / 16 * 4, cg = tid % 16;  // rows rg.., keys cg and cg + 16, dims 4 cg + 64 j..
+
+    uint4 kx[kMine], vx[kMine];
+    uint32_t there = 0;  // the block's rows that are in the cache (this thread's pieces' rows)
+    float ksc[kCodes ? kMine : 1], vsc[kCodes ? kMine : 1];
+    auto load = [&](int row0) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int e = tid + i * kThreads, row = row0 + e / kPieces, pc = e % kPieces;
+        kx[i] = vx[i] = make_uint4(0, 0, 0, 0);
+        if (kCodes) ksc[i % (kCodes ? kMine : 1)] = vsc[i % (kCodes ? kMine : 1)] = 1.f;
+        there &= ~(1u << i);
+        if (row >= w.end) continue;
+        const int page = p.table[guard((long long)w.b * p.g.max_pages + (row >> p.g.shift), 1,
+                                       (long long)p.g.B * p.g.max_pages, p.status)];
+        if ((unsigned)page >= (unsigned)p.g.n_pages) {
+          report(p.status, RIPPLE_EBOUNDS);
+          continue;
+        }
+        there |= 1u << i;
+        const int slot = row & ((1 << p.g.shift) - 1);
+        const long long at = page * p.g.page_stride + w.h * p.g.head_stride +
+                             slot * p.g.row_stride + pc * P::N;
+        kx[i] = *reinterpret_cast<const uint4 *>((const T *)p.k_pages + at);
+        vx[i] = *reinterpret_cast<const uint4 *>((const T *)p.v_pages + at);
+        if constexpr (kCodes) {
+          const long long sc = page * p.scale_page + w.h * p.scale_head + slot * p.scale_row;
+          ksc[i] = scale_of_byte(p.k_scales[sc]);
+          vsc[i] = scale_of_byte(p.v_scales[sc]);
+        }
+      }
+    };
+    __shared__ uint32_t row_there;
+    load(w.begin);
+    for (int row0 = w.begin; row0 < w.end; row0 += KB) {
+      __syncthreads();  // the block before has been read
+      if (tid == 0) row_there = 0;
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int e = tid + i * kThreads, r = e / kPieces, c = e % kPieces * P::N;
+        P::put(&s.k[r][c], kx[i], kCodes ? ksc[i % (kCodes ? kMine : 1)] : 1.f);
+        P::put(&s.v[r][c], vx[i], kCodes ? vsc[i % (kCodes ? kMine : 1)] : 1.f);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int e = tid + i * kThreads;
+        if (e % kPieces == 0 && (there >> i & 1)) atomicOr(&row_there, 1u << (e / kPieces));
+      }
+      __syncthreads();
+      const uint32_t present = row_there;
+      if (row0 + KB < w.end) load(row0 + KB);
+      // scores
+      float x[4][2];
+      {
+        float2 d[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i][0] = d[i][1] = make_float2(0.f, 0.f);
+#pragma unroll 4
+        for (int c = 0; c < D; c += 4) {
+          float4 kk[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) kk[j] = *reinterpret_cast<const float4 *>(&s.k[cg + 16 * j][c]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 qq = *reinterpret_cast<const float4 *>(&s.q[rg + i][c]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              d[i][j] = __ffma2_rn(make_float2(qq.x, qq.y), make_float2(kk[j].x, kk[j].y), d[i][j]);
+              d[i][j] = __ffma2_rn(make_float2(qq.z, qq.w), make_float2(kk[j].z, kk[j].w), d[i][j]);
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) x[i][j] = d[i][j].x + d[i][j].y;
+      }
+      // the 16 threads of a row are half a warp
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = rg + i;
+        const uint64_t mask = s.mask[r];
+        bool on[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int c = cg + 16 * j;
+          const long long of_draft = row0 + c - seq.prefix;
+          on[j] = (present >> c & 1) && (of_draft < 0 || (mask >> (of_draft & 63) & 1));
+          if (!on[j]) x[i][j] = -INFINITY;
+        }
+        float mb = fmaxf(x[i][0], x[i][1]);
+#pragma unroll
+        for (int k = 1; k < 16; k <<= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, k));
+        const float was = s.m[r];
+        const float m = mb > was + kSlack ? mb : was;
+        const float sub = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float e = on[j] ? fast_exp2(x[i][j] - sub) : 0.f;
+          sum += e;
+          s.p[cg + 16 * j][r] = on[j] ? e : -1.f;
+        }
+#pragma unroll
+        for (int k = 1; k < 16; k <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+        __syncwarp();  // s.m has been read
+        const float a = m == was ? 1.f : fast_exp2(was - m);
+        if (cg == 0) {
+          s.m[r] = m;
+          s.l[r] = s.l[r] * a + sum;
+        }
+        if (a != 1.f) {
+#pragma unroll
+          for (int j = 0; j < DT; ++j) o[i][j] *= a;
+        }
+      }
+      __syncthreads();
+      // outputs: a negative probability's key counts for nothing, whatever its value holds
+      auto add = [&](bool hidden) {
+#pragma unroll 4
+        for (int c = 0; c < KB; ++c) {
+          const float4 pr = *reinterpret_cast<const float4 *>(&s.p[c][rg]);
+          const float pp[4] = {pr.x, pr.y, pr.z, pr.w};
+#pragma unroll
+          for (int j = 0; j < DT; j += 4) {
+            const float4 vv = *reinterpret_cast<const float4 *>(&s.v[c][4 * cg + 16 * j]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (hidden && pp[i] < 0.f) continue;
+              o[i][j] = fmaf(pp[i], vv.x, o[i][j]);
+              o[i][j + 1] = fmaf(pp[i], vv.y, o[i][j + 1]);
+              o[i][j + 2] = fmaf(pp[i], vv.z, o[i][j + 2]);
+              o[i][j + 3] = fmaf(pp[i], vv.w, o[i][j + 3]);
+            }
+          }
+        }
+      };
+      if (present != 0xffffffffu || row0 + KB > seq.prefix)
+        add(true);
+      else
+        add(false);
+    }
+    __syncthreads();
+    const bool whole = here && ends;
+    const long long slot = ((2LL * run + (here ? 1 : 0)) * p.tiles + tile) * p.tile_rows;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = rg + i;
+      if (r >= n_rows) continue;
+      const float m = s.m[r], l = s.l[r];
+      const int row = tile * R + r;
+      const long long at = (long long)(seq.first + row / p.G) * p.Hq + w.h * p.G + row % p.G;
+      const float inv = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;  // 0: no row counts
+      float *to = whole ? (float *)p.out + at * D : p.ws_o + (slot + r) * D;
+#pragma unroll
+      for (int j = 0; j < DT; j += 4)
+        put4(to + 4 * cg + 16 * j,
+             make_float4(o[i][j] * inv, o[i][j + 1] * inv, o[i][j + 2] * inv, o[i][j + 3] * inv));
+      if (cg == 0) {
+        if (!whole)
+          p.ws_ml[slot + r] = make_float2(m, l);
+        else if (p.lse != nullptr)
+          p.lse[at] = tree_lse(m, l);
+      }
+    }
+    __syncthreads();
+  }
+  if (tile == 0 && tid == 0) p.rec[run] = rec;
+}
+
+// Joins the partials of the group that begins in run blockIdx.x and goes on, kJoinRows of its
+// query rows per blockIdx.y; and writes the outputs of idle sequences.
+constexpr int kJoinThreads = 256;
+
+template <typename O, int D>
+__global__ void __launch_bounds__(kJoinThreads)
+    tree_join_kernel(const __grid_constant__ TreeParams p) {
+  constexpr int kCols = D / 4, kRows = kJoinThreads / kCols;
+  constexpr int kAt = 4;  // partials loaded at a time
+  const int tid = threadIdx.x, col = tid % kCols, sub = tid / kCols;
+  pdl_wait();
+  const int run = blockIdx.x;
+  const int2 rec = __ldcg(&p.rec[run]);
+  if (rec.y > 0) {
+    const int b = rec.x / p.g.Hkv, h = rec.x % p.g.Hkv;
+    const TreeSeq seq(p, b);
+    const int row = blockIdx.y * kRows + sub;
+    if (row < seq.tokens * p.G) {
+      const int tile = row / p.tile_rows, r = row % p.tile_rows;
+      float m = -INFINITY, den = 0.f;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k0 = 0; k0 < rec.y; k0 += kAt) {
+        float2 ml[kAt];
+        float4 o[kAt];
+#pragma unroll
+        for (int i = 0; i < kAt; ++i) {
+          const int k = min(k0 + i, rec.y - 1);
+          const long long slot =
+              ((2LL * (run + k) + (k == 0 ? 1 : 0)) * p.tiles + tile) * p.tile_rows + r;
+          ml[i] = __ldcg(&p.ws_ml[slot]);
+          o[i] = __ldcg(reinterpret_cast<const float4 *>(p.ws_o + slot * D) + col);
+        }
+        float mn = m;
+#pragma unroll
+        for (int i = 0; i < kAt; ++i) mn = fmaxf(mn, ml[i].x);  // (repeats change no maximum)
+        const float subm = mn == -INFINITY ? 0.f : mn, a = fast_exp2(m - subm);
+        sum = make_float4(sum.x * a, sum.y * a, sum.z * a, sum.w * a);
+        den *= a;
+        m = mn;
+#pragma unroll
+        for (int i = 0; i < kAt; ++i)
+          if (k0 + i < rec.y) {
+            const float f = fast_exp2(ml[i].x - subm);
+            sum.x += f * o[i].x;
+            sum.y += f * o[i].y;
+            sum.z += f * o[i].z;
+            sum.w += f * o[i].w;
+            den += f * ml[i].y;
+          }
+      }
+      const long long at = (long long)(seq.first + row / p.G) * p.Hq + h * p.G + row % p.G;
+      const float inv = den != 0.f ? 1.f / den : 0.f;  // 0: no row counts
+      put4((O *)p.out + at * D + 4 * col,
+           make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+      if (p.lse != nullptr && col == 0) p.lse[at] = tree_lse(m, den);
+    }
+  }
+  // idle sequences
+  const int blocks = gridDim.x * gridDim.y, me = blockIdx.y * gridDim.x + blockIdx.x;
+  for (int b = me; b < p.g.B; b += blocks) {
+    const TreeSeq seq(p, b);
+    if (seq.len > 0) continue;
+    for (long long i = tid; i < (long long)seq.tokens * p.Hq * kCols; i += kJoinThreads) {
+      put4((O *)p.out + (long long)seq.first * p.Hq * D + 4 * i, make_float4(0.f, 0.f, 0.f, 0.f));
+      if (p.lse != nullptr && i % kCols == 0) p.lse[(long long)seq.first * p.Hq + i / kCols] = -INFINITY;
+    }
+  }
+}
+
+cudaError_t launch_pdl(void (*kernel)(TreeParams), dim3 grid, int threads, const TreeParams &p,
+                       cudaStream_t st, int smem = 0) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+  count_launches(1);
+  return e;
+}
+
+template <typename T, int D>
+cudaError_t launch_simt(const TreeParams &p, int dev, cudaStream_t st) {
+  static std::atomic<bool> attr_set[kMaxDevices];
+  constexpr int smem = (int)sizeof(SimtSmem<D>);
+  if (!attr_set[dev].load(std::memory_order_acquire)) {
+    const cudaError_t e = cudaFuncSetAttribute(tree_simt_kernel<T, D>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    attr_set[dev].store(true, std::memory_order_release);
+  }
+  return launch_pdl(tree_simt_kernel<T, D>, dim3(p.n_runs * p.tiles), kThreads, p, st, smem);
+}
+
+template <typename O, int D>
+cudaError_t launch_join(const TreeParams &p, cudaStream_t st) {
+  const int rows = kJoinThreads / (D / 4);
+  return launch_pdl(tree_join_kernel<O, D>, dim3(p.n_runs, (p.max_tokens * p.G + rows - 1) / rows),
+                    kJoinThreads, p, st);
+}
+
+int sm_count(int dev) {
+  static std::atomic<int> n[kMaxDevices];
+  int v = n[dev].load(std::memory_order_relaxed);
+  if (v == 0) {
+    cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev);
+    v = v > 0 ? v : 1;
+    n[dev].store(v, std::memory_order_relaxed);
+  }
+  return v;
+}
+
+size_t round_up(size_t x) { return (x + 255) & ~(size_t)255; }
+
+bool tree_args(const ripple_paged_desc *d, const ripple_paged_scales *scales, int n_q_heads,
+               int max_tokens, TreeParams *p, ScaleGeom *s) {
+  *s = ScaleGeom{};
+  if (!paged_geom(d, &p->g, scales != nullptr)) return false;
+  if (scales != nullptr && !scale_geom(d, scales, s)) return false;
+  if (n_q_heads < 1 || n_q_heads % d->n_kv_heads != 0) return false;
+  if (max_tokens < 1 || max_tokens > RIPPLE_MAX_DRAFT) return false;
+  p->Hq = n_q_heads;
+  p->G = n_q_heads / d->n_kv_heads;
+  p->max_tokens = max_tokens;
+  return p->G <= 16;
+}
+
+// Tiles and runs of a call and the workspace: records, (max, sum), outputs of the partials. The
+// runs are bounded by the blocks that the table has room for; everything grows with the call.
+// Returns the bytes; fills p's pointers if given a base.
+size_t plan(TreeParams *p, int tile, int block, int places, void *ws) {
+  const int rows = p->max_tokens * p->G;
+  p->tiles = (rows + tile - 1) / tile;
+  p->tile_rows = rows < tile ? rows : tile;
+  const long long room = (((long long)p->g.max_pages << p->g.shift) + block - 1) / block *
+                         p->g.B * p->g.Hkv;
+  // (as many for one tile as for several, so that the workspace of more tokens is no smaller)
+  p->n_runs = (int)std::min<long long>(std::max(1, places / p->tiles), room);
+  const long long most = std::min<long long>(places, room);
+  const size_t slots = 2 * (size_t)std::max<long long>((long long)p->n_runs * p->tiles, most) * p->tile_rows;
+  const size_t rec = round_up((size_t)std::min<long long>(places, room) * sizeof(int2));
+  const size_t ml = round_up(slots * sizeof(float2));
+  uint8_t *base = (uint8_t *)ws;
+  p->rec = (int2 *)base;
+  p->ws_ml = (float2 *)(base + rec);
+  p->ws_o = (float *)(base + rec + ml);
+  return rec + ml + round_up(slots * p->g.D * sizeof(float));
+}
+size_t plan(TreeParams *p, int dtype, int sms, void *ws) {
+  (void)dtype;
+  return plan(p, kTreeSimtRows, kTreeSimtKeys, kTreeSimtCtas * sms, ws);
+}
+
+}  // namespace
+
+}  // namespace ripple
+
+using namespace ripple;
+
+extern "C" ripple_status ripple_paged_tree_workspace_bytes(const ripple_paged_desc *desc,
+                                                           const ripple_paged_scales *scales,
+                                                           int32_t n_q_heads, int32_t max_tokens,
+                                                           size_t *bytes_host) {
+  TreeParams p;
+  ScaleGeom s;
+  if (!tree_args(desc, scales, n_q_heads, max_tokens, &p, &s) || bytes_host == nullptr)
+    return RIPPLE_EINVAL;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
+  *bytes_host = plan(&p, desc->dtype, sm_count(dev), nullptr);
+  return RIPPLE_OK;
+}
+
+extern "C" ripple_status ripple_paged_tree_attn(
+    const ripple_paged_desc *desc, const ripple_paged_scales *scales, int32_t n_tokens,
+    const int32_t *seq_starts, int32_t max_tokens, const uint64_t *masks, int32_t n_q_heads,
+    float scale, const void *q, const ripple_token_strides *q_strides, const void *k_pages,
+    const void *v_pages, const int32_t *block_table, const int32_t *lens, void *out, float *lse,
+    void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream) {
+  TreeParams p;
+  ScaleGeom s;
+  if (n_tokens < 0 || (seq_starts == nullptr && desc != nullptr && desc->batch > 0 &&
+                       n_tokens % desc->batch != 0))
+    return RIPPLE_EINVAL;
+  if (!tree_args(desc, scales, n_q_heads, max_tokens, &p, &s)) return RIPPLE_EINVAL;
+  p.per_seq = seq_starts == nullptr ? n_tokens / desc->batch : 0;
+  if (p.per_seq > max_tokens) return RIPPLE_EINVAL;
+  if (!(scale >= 0.f) || scale > kMaxScale) return RIPPLE_EINVAL;
+  if (n_tokens == 0) return RIPPLE_OK;
+  if (!q || !q_strides || !k_pages || !v_pages || !block_table || !lens || !out || !workspace ||
+      ((uintptr_t)workspace & 255u))
+    return RIPPLE_EINVAL;
+  if (!aligned16_host(q) || !aligned16_host(k_pages) || !aligned16_host(v_pages) ||
+      !aligned16_host(out) || !aligned4_host({block_table, lens, lse, seq_starts, dev_status}) ||
+      ((uintptr_t)masks & 7u) != 0)
+    return RIPPLE_EINVAL;
+  for (const int64_t x : {q_strides->seq_stride, q_strides->token_stride, q_strides->head_stride})
+    if (x < 0 || x > (1LL << 40) || x % vec_elems(desc->dtype) != 0) return RIPPLE_EINVAL;
+  int dev = 0;
+  const cudaError_t got = cudaGetDevice(&dev);
+  if (got != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
+  if (workspace_bytes < plan(&p, desc->dtype, sm_count(dev), workspace)) return RIPPLE_EWORKSPACE;
+  if (got != cudaSuccess) return RIPPLE_ECUDA;
+  p.scale2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)desc->head_dim)) * kLog2e;
+  p.q = q;
+  p.q_seq = q_strides->seq_stride;
+  p.q_token = q_strides->token_stride;
+  p.q_head = q_strides->head_stride;
+  p.k_pages = k_pages;
+  p.v_pages = v_pages;
+  p.k_scales = s.k;
+  p.v_scales = s.v;
+  p.scale_page = s.page_stride;
+  p.scale_head = s.head_stride;
+  p.scale_row = s.row_stride;
+  p.table = block_table;
+  p.lens = lens;
+  p.starts = seq_starts;
+  p.masks = masks;
+  p.out = out;
+  p.lse = lse;
+  p.status = dev_status;
+  p.n_tokens = n_tokens;
+  p.wait_cycles = wait_limit_cycles();
+  cudaStream_t st = (cudaStream_t)stream;
+  const bool d128 = desc->head_dim == 128;
+  if (desc->dtype == RIPPLE_BF16) return RIPPLE_EINVAL;
+  RIPPLE_CUDA_TRY((scales != nullptr ? (d128 ? launch_simt<uint8_t, 128>(p, dev, st)
+                                             : launch_simt<uint8_t, 64>(p, dev, st))
+                                     : (d128 ? launch_simt<float, 128>(p, dev, st)
+                                             : launch_simt<float, 64>(p, dev, st))));
+  RIPPLE_CUDA_TRY((d128 ? launch_join<float, 128>(p, st) : launch_join<float, 64>(p, st)));
+  return RIPPLE_OK;
+}

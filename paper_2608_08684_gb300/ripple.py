@@ -94,6 +94,12 @@ class PagedDesc(ctypes.Structure):
                 ("head_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
 
 
+class PagedScales(ctypes.Structure):
+    _fields_ = [("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64)]
+
+
 class TokenStrides(ctypes.Structure):
     _fields_ = [("seq_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
                 ("head_stride", ctypes.c_int64)]
@@ -160,6 +166,24 @@ _lib.ripple_paged_decode_workspace_bytes.restype = _i32
 _lib.ripple_paged_decode_attn.argtypes = [_p, _i32, ctypes.c_float, _p, _p, _p, _p, _p, _p, _p, _p,
                                           _p, _sz, _p, _p]
 _lib.ripple_paged_decode_attn.restype = _i32
+_lib.ripple_paged_append_q8.argtypes = [_p] + _lib.ripple_paged_append.argtypes
+_lib.ripple_paged_append_q8.restype = _i32
+_lib.ripple_paged_decode_q8_workspace_bytes.argtypes = [ctypes.POINTER(PagedDesc), _i32,
+                                                        ctypes.POINTER(_sz)]
+_lib.ripple_paged_decode_q8_workspace_bytes.restype = _i32
+_lib.ripple_paged_decode_attn_q8.argtypes = [_p] + _lib.ripple_paged_decode_attn.argtypes
+_lib.ripple_paged_decode_attn_q8.restype = _i32
+_lib.ripple_paged_tree_workspace_bytes.argtypes = [ctypes.POINTER(PagedDesc),
+                                                   ctypes.POINTER(PagedScales), _i32, _i32,
+                                                   ctypes.POINTER(_sz)]
+_lib.ripple_paged_tree_workspace_bytes.restype = _i32
+_lib.ripple_paged_tree_attn.argtypes = [_p, _p, _i32, _p, _i32, _p, _i32, ctypes.c_float, _p, _p, _p,
+                                        _p, _p, _p, _p, _p, _p, _sz, _p, _p]
+_lib.ripple_paged_tree_attn.restype = _i32
+_lib.ripple_paged_keep_rows.argtypes = [ctypes.POINTER(PagedDesc), ctypes.POINTER(PagedScales), _i32,
+                                        ctypes.POINTER(_p), ctypes.POINTER(_p), ctypes.POINTER(_p),
+                                        _i32, _p, _i32, _p, _p, _p, _p, _p]
+_lib.ripple_paged_keep_rows.restype = _i32
 _lib.ripple_token_logprobs.argtypes = [_i32, _i32, _i64, _i32, ctypes.c_float, _i32, _p, _p, _p, _p,
                                        _p, _p, _p, _p, _p]
 _lib.ripple_token_logprobs.restype = _i32
@@ -403,18 +427,31 @@ MAX_TOP = 32
 
 # A decode step makes these calls once per layer, so that their host time counts: the
 # checks and the marshalling are those of the extension module (csrc/binding.cpp).
-_paged_append, _paged_decode_attn, _token_logprobs = (
-    ctypes.cast(f, _p).value for f in (_lib.ripple_paged_append, _lib.ripple_paged_decode_attn,
-                                       _lib.ripple_token_logprobs))
+def _address(f):
+    return ctypes.cast(f, _p).value
+
+
+# by whether the pages are 8-bit ones
+_paged_append = (_address(_lib.ripple_paged_append), _address(_lib.ripple_paged_append_q8))
+_paged_decode_attn = (_address(_lib.ripple_paged_decode_attn),
+                      _address(_lib.ripple_paged_decode_attn_q8))
+_paged_tree_attn = _address(_lib.ripple_paged_tree_attn)
+_token_logprobs = _address(_lib.ripple_token_logprobs)
+
+MAX_DRAFT = 64
 
 
 class PagedCache:
     """One layer's paged cache: pools k_pages, v_pages [n_pages][Hkv][page_size][d] (any
     strides with the dims of a row consecutive, both alike: a pool laid out
     [n_pages][page_size][Hkv][d] is passed transposed) and block_table int32
-    [B][max_pages]. Holds pointers and sizes; built once."""
+    [B][max_pages]. Holds pointers and sizes; built once.
 
-    def __init__(self, k_pages, v_pages, block_table):
+    In 8 bits: k_pages, v_pages torch.float8_e4m3fn, k_scales, v_scales
+    torch.float8_e8m0fnu [n_pages][Hkv][page_size] (any strides, both alike); dtype is that
+    of q, k and v. A row stands for k_pages[..].float() * k_scales[..].float()."""
+
+    def __init__(self, k_pages, v_pages, block_table, k_scales=None, v_scales=None, dtype=None):
         if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or \
                 k_pages.stride() != v_pages.stride() or k_pages.dtype != v_pages.dtype:
             raise ValueError("k_pages and v_pages must be [n_pages][Hkv][page_size][d], alike")
@@ -428,12 +465,32 @@ class PagedCache:
         if self.device < 0 or v_pages.get_device() != self.device or \
                 block_table.get_device() != self.device:
             raise ValueError("expected CUDA tensors on one device")
-        self.desc = PagedDesc(B, H, d, ps, n_pages, width, _DTYPES[k_pages.dtype],
+        self.codes = k_pages.dtype is torch.float8_e4m3fn
+        if not self.codes:
+            if k_scales is not None or v_scales is not None or dtype not in (None, k_pages.dtype):
+                raise ValueError("scales and a dtype of their own belong to 8-bit pages")
+            self.dtype, self.scales = k_pages.dtype, None
+        else:
+            self.dtype = torch.bfloat16 if dtype is None else dtype
+            if k_scales is None or v_scales is None:
+                raise ValueError("8-bit pages need k_scales and v_scales")
+            if k_scales.shape != k_pages.shape[:3] or v_scales.shape != k_scales.shape or \
+                    k_scales.stride() != v_scales.stride() or \
+                    not k_scales.dtype is v_scales.dtype is torch.float8_e8m0fnu:
+                raise ValueError("k_scales and v_scales must be float8_e8m0fnu "
+                                 "[n_pages][Hkv][page_size], alike")
+            if k_scales.get_device() != self.device or v_scales.get_device() != self.device:
+                raise ValueError("expected CUDA tensors on one device")
+            self.scales = PagedScales(k_scales.data_ptr(), v_scales.data_ptr(), *k_scales.stride())
+        if self.dtype not in _DTYPES:
+            raise ValueError("the cache must be bf16, fp32 or float8_e4m3fn, for bf16 or fp32 queries")
+        self.desc = PagedDesc(B, H, d, ps, n_pages, width, _DTYPES[self.dtype],
                               *k_pages.stride()[:3])
         self._handle = _binding.cache(ctypes.addressof(self.desc), k_pages.data_ptr(),
                                       v_pages.data_ptr(), _ptr(block_table), self.device,
-                                      k_pages.dtype is torch.bfloat16)
-        self._keep = (k_pages, v_pages, block_table)
+                                      self.dtype is torch.bfloat16,
+                                      None if self.scales is None else ctypes.addressof(self.scales))
+        self._keep = (k_pages, v_pages, block_table, k_scales, v_scales)
 
 
 class Rope:
@@ -454,8 +511,8 @@ def ripple_paged_append(cache: PagedCache, lens, k, v, rope: Rope | None = None,
     their queries q into q_out (which may be q). k, v: [B][Hkv][d] (one token per sequence),
     [B][n][Hkv][d], or with seq_starts (int32 [B + 1]) [tokens][Hkv][d]; q, q_out likewise
     with the query heads; any strides with the dims consecutive. lens (int32 [B]) counts the
-    new tokens; positions: int32, k's leading sizes, or None (a token's cache row)."""
-    st = _binding.paged_append(_paged_append, cache._handle, None if rope is None else rope._addr,
+    new tokens (8-bit pages: ripple_paged_append_q8); positions: int32, k's leading sizes, or None (a token's cache row)."""
+    st = _binding.paged_append(_paged_append[cache.codes], cache._handle, None if rope is None else rope._addr,
                                lens, k, v, positions, seq_starts, q, q_out, dev_status,
                                None if stream is None else _stream(stream))
     if st != OK:
@@ -464,8 +521,9 @@ def ripple_paged_append(cache: PagedCache, lens, k, v, rope: Rope | None = None,
 
 def ripple_paged_decode_workspace_bytes(cache: PagedCache, n_q_heads: int) -> int:
     out = _sz()
-    _check(_lib.ripple_paged_decode_workspace_bytes(ctypes.byref(cache.desc), int(n_q_heads),
-                                                    ctypes.byref(out)),
+    query = (_lib.ripple_paged_decode_q8_workspace_bytes if cache.codes
+             else _lib.ripple_paged_decode_workspace_bytes)
+    _check(query(ctypes.byref(cache.desc), int(n_q_heads), ctypes.byref(out)),
            "ripple_paged_decode_workspace_bytes")
     return out.value
 
@@ -474,12 +532,88 @@ def ripple_paged_decode_attn(cache: PagedCache, q, lens, out, workspace, lse=Non
                              scale: float = 0.0, dev_status=None, stream=None):
     """Attention of one token per sequence over the first lens[b] rows of the paged cache:
     q [B][Hq][d] (any strides with the dims consecutive), out fp32 [B][Hq][d], lse fp32
-    [B][Hq] or None."""
-    st = _binding.paged_decode_attn(_paged_decode_attn, cache._handle, q, lens, out, workspace,
+    [B][Hq] or None (8-bit pages: ripple_paged_decode_attn_q8)."""
+    st = _binding.paged_decode_attn(_paged_decode_attn[cache.codes], cache._handle, q, lens, out, workspace,
                                     lse, scale, dev_status,
                                     None if stream is None else _stream(stream))
     if st != OK:
         raise RippleError(st, "ripple_paged_decode_attn")
+
+
+def ripple_paged_tree_workspace_bytes(cache: PagedCache, n_q_heads: int,
+                                      max_tokens: int = MAX_DRAFT) -> int:
+    out = _sz()
+    scales = None if cache.scales is None else ctypes.byref(cache.scales)
+    _check(_lib.ripple_paged_tree_workspace_bytes(ctypes.byref(cache.desc), scales, int(n_q_heads),
+                                                  int(max_tokens), ctypes.byref(out)),
+           "ripple_paged_tree_workspace_bytes")
+    return out.value
+
+
+def ripple_paged_tree_attn(cache: PagedCache, q, lens, out, workspace, masks=None, seq_starts=None,
+                           max_tokens: int | None = None, lse=None, scale: float = 0.0,
+                           dev_status=None, stream=None):
+    """Attention of up to 64 drafted tokens per sequence over the paged cache, whose last
+    rows are theirs: q [B][n][Hq][d], or with seq_starts (int32 [B + 1]) [tokens][Hq][d] (any
+    strides with the dims consecutive), out like q, dense, lse fp32 [..][Hq] or None. masks:
+    int64, q's leading sizes, bit j of a token's: it sees token j of its sequence's draft; None:
+    a chain. max_tokens: most tokens of a sequence (n, or with seq_starts 64 if None)."""
+    st = _binding.paged_tree_attn(_paged_tree_attn, cache._handle, q, lens, out, workspace, masks,
+                                  seq_starts, max_tokens, lse, scale, dev_status,
+                                  None if stream is None else _stream(stream))
+    if st != OK:
+        raise RippleError(st, "ripple_paged_tree_attn")
+
+
+class KeepTables:
+    """Host arrays (pools, tables) of ripple_paged_keep_rows, built once from a PagedCache
+    per layer, all of one shape."""
+
+    def __init__(self, caches):
+        caches = list(caches)
+        L = self.n_layers = len(caches)
+        if not 1 <= L <= MAX_LAYERS:
+            raise ValueError(f"1 to {MAX_LAYERS} layers")
+        c0 = caches[0]
+        if any(bytes(c.desc) != bytes(c0.desc) or c.codes != c0.codes or c.device != c0.device
+               for c in caches):
+            raise ValueError("the layers' caches must be of one shape, dtype and device")
+        self.desc, self.device = c0.desc, c0.device
+        self.k, self.v, self.table = ((_p * L)(*[c._keep[i].data_ptr() for c in caches])
+                                      for i in range(3))
+        self.scales = (PagedScales * L)(*[c.scales for c in caches]) if c0.codes else None
+        self._keep = caches
+
+
+def ripple_paged_keep_rows(tables: KeepTables, lens, kept, n_tokens: int | None = None,
+                           seq_starts=None, lens_out=None, dev_status=None, stream=None):
+    """Move the accepted drafted tokens' rows up behind the rows before the draft, in every
+    layer. lens: int32 [L][B], the draft included; kept: int32 [B][m], a sequence's accepted
+    tokens of its draft, ascending, ended by a negative entry; n_tokens: drafted tokens of every
+    sequence, or seq_starts (int32 [B + 1]). lens_out (int32 [L][B], default: lens) gets the new
+    lengths."""
+    lens_out = lens if lens_out is None else lens_out
+    L, B = tables.n_layers, tables.desc.batch
+    for t, shape in ((lens, (L, B)), (lens_out, (L, B)), (kept, (B, kept.shape[-1])),
+                     (seq_starts, (B + 1,))):
+        if t is None:
+            continue
+        if t.dtype is not torch.int32 or tuple(t.shape) != shape:
+            raise ValueError("lens and lens_out must be int32 [L][B], kept int32 [B][m], "
+                             "seq_starts int32 [B + 1]")
+        if t.get_device() != tables.device:
+            raise ValueError("expected CUDA tensors on one device, the current one")
+    if torch.cuda.current_device() != tables.device:
+        raise ValueError("expected CUDA tensors on one device, the current one")
+    if (n_tokens is None) == (seq_starts is None):
+        raise ValueError("n_tokens or seq_starts")
+    m = kept.shape[1]
+    _check(_lib.ripple_paged_keep_rows(ctypes.byref(tables.desc), tables.scales, L, tables.k,
+                                       tables.v, tables.table,
+                                       0 if n_tokens is None else int(n_tokens) * B,
+                                       _ptr(seq_starts), m, _ptr(kept) if m else None, _ptr(lens),
+                                       _ptr(lens_out), _ptr(dev_status), _stream(stream)),
+           "ripple_paged_keep_rows")
 
 
 def ripple_token_logprobs(logits, tokens=None, logprob_out=None, entropy_out=None, lse_out=None,
