@@ -73,7 +73,6 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
   constexpr int kPieces = D / P::N;                        // of a row
   constexpr int kMine = KB * kPieces / kThreads;           // of a block's keys, a thread
   constexpr bool kCodes = sizeof(T) == 1;
-  constexpr int LD = SimtSmem<D>::LD;
   constexpr int DT = D / 16;                               // output dims of a thread
   extern __shared__ __align__(16) uint8_t smem_raw[];
   SimtSmem<D> &s = *reinterpret_cast<SimtSmem<D> *>(smem_raw);
@@ -448,7 +447,8 @@ size_t plan(TreeParams *p, int tile, int block, int places, void *ws) {
   return rec + ml + round_up(slots * p->g.D * sizeof(float));
 }
 size_t plan(TreeParams *p, int dtype, int sms, void *ws) {
-  (void)dtype;
+  if (dtype == RIPPLE_BF16)
+    return plan(p, kTreeTcRows, kTreeTcKeys, kTreeTcCtas * sms, ws);
   return plan(p, kTreeSimtRows, kTreeSimtKeys, kTreeSimtCtas * sms, ws);
 }
 
@@ -525,7 +525,12 @@ extern "C" ripple_status ripple_paged_tree_attn(
   p.wait_cycles = wait_limit_cycles();
   cudaStream_t st = (cudaStream_t)stream;
   const bool d128 = desc->head_dim == 128;
-  if (desc->dtype == RIPPLE_BF16) return RIPPLE_EINVAL;
+  if (desc->dtype == RIPPLE_BF16) {
+    RIPPLE_CUDA_TRY(launch_tree_tc(p, scales != nullptr, dev, st));
+    RIPPLE_CUDA_TRY((d128 ? launch_join<__nv_bfloat16, 128>(p, st)
+                          : launch_join<__nv_bfloat16, 64>(p, st)));
+    return RIPPLE_OK;
+  }
   RIPPLE_CUDA_TRY((scales != nullptr ? (d128 ? launch_simt<uint8_t, 128>(p, dev, st)
                                              : launch_simt<uint8_t, 64>(p, dev, st))
                                      : (d128 ? launch_simt<float, 128>(p, dev, st)

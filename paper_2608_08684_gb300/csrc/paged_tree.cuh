@@ -173,13 +173,11 @@ __device__ __forceinline__ void put4(__nv_bfloat16 *p, const float4 &x) {
                                              *reinterpret_cast<const uint32_t *>(&b));
 }
 
-cudaError_t launch_tree_simt(const TreeParams &p, int dtype, cudaStream_t st);
-// Whether the tensor cores take the call; tiles, runs and rows are then theirs.
-bool tree_tc_supported(int dtype);
-cudaError_t launch_tree_tc(const TreeParams &p, int dev, cudaStream_t st);
-
-constexpr int kTreeSimtRows = 32;  // of a tile
-constexpr int kTreeSimtKeys = 32;  // of a block
-constexpr int kTreeSimtCtas = 3;   // of an SM
+// bf16 queries: on the tensor cores (paged_tree_tc.cu). Rows of a tile, keys of a block, CTAs
+// of an SM.
+constexpr int kTreeTcRows = 128, kTreeTcKeys = 64, kTreeTcCtas = 2;
+cudaError_t launch_tree_tc(const TreeParams &p, bool codes, int dev, cudaStream_t st);
+// fp32 queries: on the CUDA cores (paged_tree.cu).
+constexpr int kTreeSimtRows = 32, kTreeSimtKeys = 32, kTreeSimtCtas = 3;
 
 }  // namespace ripple
