@@ -40,6 +40,8 @@ struct TreeParams {
   int tiles, tile_rows;                  // row tiles of a group at most, rows of a partial
   int n_runs;
   long long wait_cycles;
+  uint32_t suspend_ns;                   // of a poll of an mbarrier, at most
+  bool tma;                              // whole blocks by TMA
   int2 *rec;      // [n_runs] the group that begins in the run and goes on, and its runs (0: none)
   float *ws_o;    // [2 * n_runs][tiles][tile_rows][D] partials: of the group begun before, begun here
   float2 *ws_ml;  // [2 * n_runs][tiles][tile_rows] their maximum (log2) and sum

@@ -7,11 +7,12 @@
 // block is 32 KB, 1400 cycles of an SM's share of HBM, and 512 of its tensor cores.
 //
 // Warps 0-3: softmax and outputs; warp 4: issues the MMAs; warps 5, 6 fetch keys (and a
-// group's queries), 7, 8 values, with 16-byte copies into two stages each, for pages of any
-// size and layout, in the layout that a tensor map's 128-byte swizzle would give. 8-bit pages
-// come through registers and become the bf16 values that they stand for, exactly, so that
-// all else is the same. Scores of the next block are on their way while a block's softmax
-// runs; S and P of two blocks and O fill half of the TMEM, the other CTA's the other half.
+// group's queries), 7, 8 values: a block by TMA (a box a page, with the 128-byte swizzle that
+// the MMAs read), or, where rows of it are missing or pages have fewer than 8, by 16-byte copies to
+// the same places. 8-bit pages come into a ring of their own, two blocks ahead, and these
+// warps make them the bf16 values that they stand for, exactly, so that all else is the same.
+// Scores of the next block are on their way while a block's softmax runs; S and P of two
+// blocks and O fill half of the TMEM, the other CTA's the other half.
 //
 // P in one bf16 part: the output is rounded to bf16 as well, and a probability's rounding
 // (2^-9) enters the output as part of a mean. The sum is of the unrounded ones, in fp32.
@@ -30,7 +31,7 @@ constexpr int KB = kTreeTcKeys;
 constexpr int kRows = kTreeTcRows;
 constexpr int kThreads = 288;
 constexpr int kFetchers = 64;  // threads that fetch keys, and values
-constexpr int kStages = 2;
+constexpr int kRing = 3;       // blocks of 8-bit rows on their way or being widened
 constexpr uint32_t kTmemCols = 256;  // S and P of two blocks (64 each), O (d) from 128 on
 constexpr uint32_t kOCol = 128;
 constexpr float kSlack = 8.f;
@@ -39,20 +40,70 @@ constexpr int kMaxDevices = 64;
 constexpr int kSlots = 4;  // of the blocks' present rows
 
 struct Sync {
-  uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
+  uint64_t ring_full[2][kRing];                         // of keys, of values
   uint64_t s_full[2], p_full[2], pv_done[2], mma_done;  // (of even and odd blocks)
   unsigned long long present[kSlots];  // rows of a block that are there
   unsigned long long bad;              // drafted tokens whose values are not all finite
   uint32_t tmem;
+  int abort;                           // a role has given up waiting
+  uint8_t scale[2][kRing][KB];         // of the ring's rows
 };
 
-template <int D>
+template <int D, bool kCodes>
 struct Smem {
+  static constexpr int STAGES = kCodes ? 1 : 2;  // of bf16 blocks of keys, and of values
   static constexpr int Q = kRows * D * 2, TILE = KB * D * 2;
+  static constexpr int RAW = KB * D;             // a block of 8-bit rows
   static constexpr int HALF_Q = kRows * 128, HALF = KB * 128;  // of 64 dims
-  static constexpr int K0 = Q, V0 = Q + kStages * TILE, SYNC = V0 + kStages * TILE;
-  static constexpr int BYTES = SYNC + (int)sizeof(Sync) + 1024;  // (the tiles start at 1 KB)
+  static constexpr int K0 = Q, V0 = Q + STAGES * TILE, RING = V0 + STAGES * TILE;
+  static constexpr int SYNC = RING + (kCodes ? 2 * kRing * RAW : 0);
+  static constexpr int BYTES = SYNC + (int)sizeof(Sync);
+  static_assert(2 * (BYTES + 1024) <= 228 * 1024, "two CTAs an SM");
 };
+
+// The pools as TMA sees them: boxes of 64 dims (8-bit: a row) x rows of a page.
+struct Maps {
+  CUtensorMap k, v;
+};
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z,
+                                            int w, uint64_t *bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"((uint64_t)map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+      : "memory");
+}
+// The thread's arrival on `bar` once its copies so far have landed.
+__device__ __forceinline__ void copies_arrive(uint64_t *bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// Bounded wait: gives up after the bound, or when another role has. A poll suspends the thread
+// for a quarter of the bound at most.
+__device__ __forceinline__ bool try_wait_for(uint64_t *bar, uint32_t parity, uint32_t ns) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n"
+      " mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\n"
+      " selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity), "r"(ns)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool wait_bar(uint64_t *bar, int phase, const TreeParams &p, int *abort) {
+  if (try_wait_for(bar, phase & 1, p.suspend_ns)) return true;
+  const long long t0 = clock64();
+  for (;;) {
+    if (try_wait_for(bar, phase & 1, p.suspend_ns)) return true;
+    if (*(volatile int *)abort) return false;
+    if (clock64() - t0 > p.wait_cycles) {
+      *(volatile int *)abort = 1;
+      report(p.status, RIPPLE_ETIMEOUT);
+      return false;
+    }
+  }
+}
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
@@ -134,16 +185,21 @@ __device__ __forceinline__ void widen(const uint4 &u, float scale, uint32_t (&o)
 // kCodes: 8-bit pages.
 template <int D, bool kCodes>
 __global__ void __launch_bounds__(kThreads, 2)
-    tree_tc_kernel(const __grid_constant__ TreeParams p) {
-  using S = Smem<D>;
+    tree_tc_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ Maps maps) {
+  using S = Smem<D, kCodes>;
+  constexpr int ST = S::STAGES;
   using W = TreeWalk<KB>;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t *const tiles = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  extern __shared__ __align__(1024) uint8_t tiles[];
   Sync *const sy = (Sync *)(tiles + S::SYNC);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int run = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
   if (tid == 0) {
-    for (int i = 0; i < kStages; ++i) {
+    sy->abort = 0;
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(&sy->ring_full[0][i], kFetchers);
+      mbar_init(&sy->ring_full[1][i], kFetchers);
+    }
+    for (int i = 0; i < 2; ++i) {
       mbar_init(&sy->k_full[i], kFetchers);
       mbar_init(&sy->v_full[i], kFetchers);
       mbar_init(&sy->k_empty[i], 1);
@@ -175,6 +231,10 @@ __global__ void __launch_bounds__(kThreads, 2)
   int n = 0;  // blocks of this CTA so far
   bool ok = true;
 
+  auto wait_for = [&](uint64_t *bar, int phase) {  // by a whole warp
+    return __all_sync(kAll, wait_bar(bar, phase, p, &sy->abort));
+  };
+
   if (warp >= 5) {
     // -------------------------------------------------- keys (and queries), values
     const bool keys = warp < 7;
@@ -182,96 +242,125 @@ __global__ void __launch_bounds__(kThreads, 2)
     uint64_t *const full = keys ? sy->k_full : sy->v_full, *const empty = keys ? sy->k_empty : sy->v_empty;
     const uint32_t stages = keys ? ks : vs;
     const uint8_t *const pool = (const uint8_t *)(keys ? p.k_pages : p.v_pages);
-    const uint8_t *const scales = keys ? p.k_scales : p.v_scales;
+    const CUtensorMap *const map = keys ? &maps.k : &maps.v;
     constexpr int kElem = kCodes ? 1 : 2;
     constexpr int kPieces = D * kElem / 16;     // of a row in its page
     constexpr int kRowsWarp = 32 / kPieces;     // rows of a warp's copy
     constexpr int kSteps = KB / (2 * kRowsWarp);
     const int sub = lane / kPieces, pc = lane % kPieces;
+    const int page_rows = 1 << p.g.shift, box = min(page_rows, KB);
+    // entries of the block table for the rows lane and lane + 32 of the next block
+    int entry[2];
+    auto look_up = [&](int row0) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = row0 + lane + 32 * i;
+        entry[i] = -1;
+        if (row < w.end)
+          entry[i] = p.table[guard((long long)w.b * p.g.max_pages + (row >> p.g.shift), 1,
+                                   (long long)p.g.B * p.g.max_pages, p.status)];
+      }
+    };
+    // The block at row0 on its way to `to`: by TMA where all its rows are there (and `allowed`);
+    // returns whether so. Then `bar` has this thread's arrival and gets the bytes; otherwise the
+    // thread's copies have been issued.
+    unsigned long long present;
+    auto fetch = [&](int row0, uint32_t to, uint64_t *bar, bool allowed) {
+      bool there[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        there[i] = (unsigned)entry[i] < (unsigned)p.g.n_pages;
+        if (!there[i] && row0 + lane + 32 * i < w.end) report(p.status, RIPPLE_EBOUNDS);
+      }
+      const uint32_t lo = __ballot_sync(kAll, there[0]), hi = __ballot_sync(kAll, there[1]);
+      present = (unsigned long long)hi << 32 | lo;
+      if (!kCodes && keys && th == 0) sy->present[n % kSlots] = present;
+      if (allowed && p.tma && present == ~0ull) {
+        if (th == 0) mbar_arrive_expect_tx(bar, KB * D * kElem);
+        if (wk == 0) {
+          __syncwarp();
+          // a lane a page: the entry of its first row
+          const int boxes = KB / box, first = lane * box;
+          const int e0 = __shfl_sync(kAll, entry[0], first & 31), e1 = __shfl_sync(kAll, entry[1], first & 31);
+          if (lane < boxes) {
+            const int page = first < 32 ? e0 : e1, slot = (row0 + first) & (page_rows - 1);
+            if constexpr (kCodes) {
+              tma_load_4d(to + first * D, map, 0, slot, w.h, page, bar);
+            } else {
+#pragma unroll
+              for (int half = 0; half < D / 64; ++half)
+                tma_load_4d(to + half * S::HALF + first * 128, map, 64 * half, slot, w.h, page, bar);
+            }
+          }
+          __syncwarp();
+        }
+        if (th != 0) mbar_arrive(bar);
+        return true;
+      }
+      long long place[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = row0 + lane + 32 * i;
+        place[i] = there[i] ? (entry[i] * p.g.page_stride + w.h * p.g.head_stride +
+                               (row & (page_rows - 1)) * p.g.row_stride) * kElem
+                            : -1;
+      }
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const int row = (2 * i + wk) * kRowsWarp + sub;
+        const long long at = __shfl_sync(kAll, row < 32 ? place[0] : place[1], row & 31);
+        copy16(kCodes ? to + row * D + 16 * pc
+                      : to + (pc >> 3) * S::HALF + row * 128 + (((pc & 7) ^ (row & 7)) << 4),
+               pool + (at >= 0 ? at + 16 * pc : 0), at >= 0);
+      }
+      return false;
+    };
+    // What both warps of keys (of values) agree on: they fetch a block, or neither does, so that
+    // what is on its way is waited for by its barrier also when a wait has given up.
+    auto both = [&](bool mine) {
+      int all;
+      asm volatile(
+          "{\n .reg .pred p, q;\n setp.ne.b32 q, %1, 0;\n"
+          " barrier.cta.red.and.pred p, %2, %3, q;\n selp.s32 %0, 1, 0, p;\n}\n"
+          : "=r"(all)
+          : "r"((int)mine), "r"(keys ? 2 : 3), "r"(kFetchers)
+          : "memory");
+      return all != 0;
+    };
+    int ring_n = 0, issued = 0;  // blocks that have gone through the ring, that were put there
     for (bool more = any; more && ok; more = w.next(p)) {
       const TreeSeq seq(p, w.b);
       const int n_rows = min(seq.tokens * p.G - tile * kRows, kRows);
       if (n_rows <= 0) continue;
-      // places of the block's rows lane and lane + 32 (-1: not there), of the block at row0
-      long long place[2], scale_at[2];
-      auto look_up = [&](int row0) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int row = row0 + lane + 32 * i;
-          place[i] = -1;
-          scale_at[i] = 0;
-          if (row >= w.end) continue;
-          const int page = p.table[guard((long long)w.b * p.g.max_pages + (row >> p.g.shift), 1,
-                                         (long long)p.g.B * p.g.max_pages, p.status)];
-          if ((unsigned)page >= (unsigned)p.g.n_pages) {
-            report(p.status, RIPPLE_EBOUNDS);
-            continue;
-          }
-          const int slot = row & ((1 << p.g.shift) - 1);
-          place[i] = (page * p.g.page_stride + w.h * p.g.head_stride + slot * p.g.row_stride) * kElem;
-          if (kCodes) scale_at[i] = page * p.scale_page + w.h * p.scale_head + slot * p.scale_row;
-        }
-      };
       look_up(w.begin);
-      // 8-bit pages: a block's codes and scales, on their way while the block before is used
-      uint4 x[kCodes ? kSteps : 1];
-      int byte[2];
-      auto load = [&]() {
-        if constexpr (kCodes) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) byte[i] = place[i] >= 0 ? scales[scale_at[i]] : 0;
-#pragma unroll
-          for (int i = 0; i < kSteps; ++i) {
-            const int row = (2 * i + wk) * kRowsWarp + sub;
-            const long long at = __shfl_sync(kAll, row < 32 ? place[0] : place[1], row & 31);
-            x[i] = make_uint4(0, 0, 0, 0);
-            if (at >= 0) x[i] = __ldcs(reinterpret_cast<const uint4 *>(pool + at) + pc);
-          }
+      // the group's queries, once the scores of the group before are done
+      auto fetch_queries = [&]() {
+        if (n > 0 && !both(wait_for(&sy->k_empty[(n - 1) % ST], (n - 1) / ST))) return false;
+        constexpr int kQPieces = D / 8;
+        for (int i = th; i < kRows * kQPieces; i += kFetchers) {
+          const int r = i / kQPieces, c = i % kQPieces;
+          const bool there = r < n_rows;
+          const int row = tile * kRows + (there ? r : 0), tok = row / p.G, head = w.h * p.G + row % p.G;
+          const __nv_bfloat16 *q = (const __nv_bfloat16 *)p.q + head * p.q_head +
+                                   (p.starts == nullptr ? w.b * p.q_seq + tok * p.q_token
+                                                        : (long long)(seq.first + tok) * p.q_token);
+          copy16(qs + (c >> 3) * S::HALF_Q + r * 128 + (((c & 7) ^ (r & 7)) << 4), q + 8 * c, there);
         }
+        return true;
       };
-      if (kCodes) load();
-      bool first = true;
-      for (int row0 = w.begin; row0 < w.end; row0 += KB, ++n, first = false) {
-        const int stage = n % kStages;
-        if (n >= kStages && !mbar_wait(&empty[stage], (n / kStages - 1) & 1, p.status, p.wait_cycles)) {
-          ok = false;
-          break;
-        }
-        if (keys && first) {
-          // the group's queries, once the scores of the group before are done
-          if (n > 0 && !mbar_wait(&sy->k_empty[(n - 1) % kStages], (n - 1) / kStages & 1, p.status,
-                                  p.wait_cycles)) {
-            ok = false;
-            break;
-          }
-          constexpr int kQPieces = D / 8;
-          for (int i = th; i < kRows * kQPieces; i += kFetchers) {
-            const int r = i / kQPieces, c = i % kQPieces;
-            const bool there = r < n_rows;
-            const int row = tile * kRows + (there ? r : 0), tok = row / p.G, head = w.h * p.G + row % p.G;
-            const __nv_bfloat16 *q = (const __nv_bfloat16 *)p.q + head * p.q_head +
-                                     (p.starts == nullptr ? w.b * p.q_seq + tok * p.q_token
-                                                          : (long long)(seq.first + tok) * p.q_token);
-            copy16(qs + (c >> 3) * S::HALF_Q + r * 128 + (((c & 7) ^ (r & 7)) << 4), q + 8 * c, there);
-          }
-        }
-        const uint32_t to = stages + stage * S::TILE;
-        if (keys) {
-          const uint32_t lo = __ballot_sync(kAll, place[0] >= 0), hi = __ballot_sync(kAll, place[1] >= 0);
-          if (th == 0) sy->present[n % kSlots] = (unsigned long long)hi << 32 | lo;
-        }
-        // drafted tokens' values that are not finite are left out here (a hidden one's weight is
-        // 0, and 0 times them is NaN) and added to the outputs of the rows that see them
-        const bool draft = !keys && row0 + KB > seq.prefix;
-        if constexpr (!kCodes) {
-#pragma unroll
-          for (int i = 0; i < kSteps; ++i) {
-            const int row = (2 * i + wk) * kRowsWarp + sub;
-            const long long at = __shfl_sync(kAll, row < 32 ? place[0] : place[1], row & 31);
-            copy16(to + (pc >> 3) * S::HALF + row * 128 + (((pc & 7) ^ (row & 7)) << 4),
-                   pool + (at >= 0 ? at + 16 * pc : 0), at >= 0);
-          }
+      if constexpr (!kCodes) {
+        for (int row0 = w.begin; row0 < w.end; row0 += KB, ++n) {
+          const int stage = n % ST;
+          if (n >= ST && !(ok = both(wait_for(&empty[stage], n / ST - 1)))) break;
+          // drafted tokens' values that are not finite are left out here (a hidden one's weight is
+          // 0, and 0 times them is NaN) and added to the outputs of the rows that see them
+          const bool draft = !keys && row0 + KB > seq.prefix, queries = keys && row0 == w.begin;
+          const uint32_t to = stages + stage * S::TILE;
+          if (queries && !(ok = fetch_queries())) break;
+          // (the queries are waited for below, and this thread arrives after that)
+          const bool by_tma = fetch(row0, to, &full[stage], !draft && !queries);
           if (row0 + KB < w.end) look_up(row0 + KB);
+          if (by_tma) continue;
           asm volatile("cp.async.wait_all;" ::: "memory");
           if (draft) {
 #pragma unroll 1
@@ -285,50 +374,98 @@ __global__ void __launch_bounds__(kThreads, 2)
             }
           }
           fence_proxy_async_smem();
-        } else {
+          mbar_arrive(&full[stage]);
+        }
+      } else {
+        const uint8_t *const scales = keys ? p.k_scales : p.v_scales;
+        uint8_t(*const scale_ring)[KB] = sy->scale[keys ? 0 : 1];
+        uint64_t *const ring_full = sy->ring_full[keys ? 0 : 1];
+        const uint32_t ring = qs + S::RING + (keys ? 0 : kRing * S::RAW);
+        const int my_row = 32 * wk + lane;
+        int byte = 0, byte_slot = -1;  // of the thread's row of the block issued last
+        auto put_scale = [&]() {
+          if (byte_slot >= 0) scale_ring[byte_slot][my_row] = (uint8_t)byte;
+          byte_slot = -1;
+        };
+        // the block at row0 into the ring; its scales are put there when the next one is issued
+        unsigned long long ring_present[kRing];
+        auto issue = [&](int row0, int i) {
+          const int slot = i % kRing;
+          issued = i + 1;
+          put_scale();
+          const int page = wk == 0 ? entry[0] : entry[1], row = row0 + my_row;
+          byte = 0;
+          if ((unsigned)page < (unsigned)p.g.n_pages)
+            byte = scales[page * p.scale_page + w.h * p.scale_head + (row & (page_rows - 1)) * p.scale_row];
+          byte_slot = slot;
+          if (!fetch(row0, ring + slot * S::RAW, &ring_full[slot], true)) copies_arrive(&ring_full[slot]);
+#pragma unroll
+          for (int k = 0; k < kRing; ++k)
+            if (k == slot) ring_present[k] = present;
+          if (row0 + KB < w.end) look_up(row0 + KB);
+        };
+        issue(w.begin, ring_n);
+        if (w.begin + KB < w.end) issue(w.begin + KB, ring_n + 1);
+        for (int row0 = w.begin; row0 < w.end; row0 += KB, ++n, ++ring_n) {
+          put_scale();
+          if (row0 + 2 * KB < w.end) issue(row0 + 2 * KB, ring_n + 2);
+          const int slot = ring_n % kRing, stage = n % ST;
+          // (then the scales of this block are there as well)
+          ok = both(wait_for(&ring_full[slot], ring_n / kRing) &&
+                    (n < ST || wait_for(&empty[stage], n / ST - 1)));
+          if (!ok) break;
+          if (keys && row0 == w.begin && !(ok = fetch_queries())) break;
+          if (keys && th == 0) {
+#pragma unroll
+            for (int k = 0; k < kRing; ++k)
+              if (k == slot) sy->present[n % kSlots] = ring_present[k];
+          }
+          const uint32_t from = ring + slot * S::RAW, to = stages + stage * S::TILE;
+          const bool draft = !keys && row0 + KB > seq.prefix;
 #pragma unroll
           for (int i = 0; i < kSteps; ++i) {
             const int row = (2 * i + wk) * kRowsWarp + sub;
-            const int s = __shfl_sync(kAll, row < 32 ? byte[0] : byte[1], row & 31);
-            float f = scale_of_byte(s);
-            uint4 u = x[i];
-            if (draft && s == 255 && row0 + row >= seq.prefix) {
+            float f = scale_of_byte(scale_ring[slot][row]);
+            uint4 u = ld_shared16(from + row * D + 16 * pc);
+            if (draft && f != f && row0 + row >= seq.prefix) {  // as infinite values of bf16 pages
               f = 0.f;
               u = make_uint4(0, 0, 0, 0);
             }
             uint32_t o[8];
             widen(u, f, o);
-            const int c = 2 * pc;  // of 16-byte pieces in shared memory
+            const int c = 2 * pc;  // of 16-byte pieces in the stage
             const uint32_t at = to + (c >> 3) * S::HALF + row * 128;
             st_shared16(at + (((c & 7) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
             st_shared16(at + ((((c & 7) + 1) ^ (row & 7)) << 4), o[4], o[5], o[6], o[7]);
           }
-          if (keys && first) asm volatile("cp.async.wait_all;" ::: "memory");
+          if (keys && row0 == w.begin) asm volatile("cp.async.wait_all;" ::: "memory");
           fence_proxy_async_smem();
-          if (row0 + KB < w.end) {
-            look_up(row0 + KB);
-            load();
-          }
+          mbar_arrive(&full[stage]);
+          named_bar_sync(keys ? 2 : 3, kFetchers);  // the slot has been read
         }
-        mbar_arrive(&full[stage]);
       }
     }
     copies_landed();
+    if (!ok) {  // what TMA still has on its way lands before the CTA leaves
+      if (!kCodes) {
+        for (int i = max(0, n - ST); i < n; ++i) mbar_wait(&full[i % ST], i / ST & 1, nullptr);
+      } else {
+        for (int i = max(0, issued - kRing); i < issued; ++i)
+          mbar_wait(&sy->ring_full[keys ? 0 : 1][i % kRing], i / kRing & 1, nullptr);
+      }
+    }
   } else if (warp == 4) {
     // -------------------------------------------------- MMAs (the whole warp waits, one lane issues)
     constexpr uint32_t id_qk = idesc_bf16(kRows, KB);
     constexpr uint32_t id_pv = idesc_bf16(kRows, D) | (1u << 16);  // V: d is the contiguous one
     const uint64_t qd = sw128_desc(qs);
-    auto wait = [&](uint64_t *bar, int phase) {
-      return __all_sync(kAll, mbar_wait(bar, phase & 1, p.status, p.wait_cycles));
-    };
     // scores of block i: S(i). The products P . V of the blocks up to n - 1 have been issued, and
     // all of them have to be done: P of block i - 2 lies where S(i) goes, and a barrier that has
     // gone on by two phases cannot be waited for.
     auto scores = [&](int i) {
-      const int st = i % kStages;
-      if (!wait(&sy->k_full[st], i / kStages)) return false;
-      if (n > 0 && !wait(&sy->pv_done[(n - 1) & 1], (n - 1) / 2)) return false;
+      const int st = i % ST;
+      if (!wait_for(&sy->k_full[st], i / ST)) return false;
+      if (n > 0 && !wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2)) return false;
       tc_fence_after();
       if (elect_one()) {
         const uint64_t kd = sw128_desc(ks + st * S::TILE);
@@ -351,8 +488,8 @@ __global__ void __launch_bounds__(kThreads, 2)
       ok = scores(n);
       for (int i = 0; i < count && ok; ++i, ++n) {
         if (i + 1 < count && !(ok = scores(n + 1))) break;
-        const int st = n % kStages;
-        if (!wait(&sy->p_full[n & 1], n / 2) || !wait(&sy->v_full[st], n / kStages)) {
+        const int st = n % ST;
+        if (!wait_for(&sy->p_full[n & 1], n / 2) || !wait_for(&sy->v_full[st], n / ST)) {
           ok = false;
           break;
         }
@@ -422,10 +559,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       float m = -INFINITY, l = 0.f;
       bool begun = false;  // O has a block
       for (int row0 = w.begin; row0 < w.end && ok; row0 += KB, ++n, begun = true) {
-        if (!__all_sync(kAll, mbar_wait(&sy->s_full[n & 1], n / 2 & 1, p.status, p.wait_cycles))) {
-          ok = false;
-          break;
-        }
+        if (!(ok = wait_for(&sy->s_full[n & 1], n / 2))) break;
         if (warp_live) {
           tc_fence_after();
           const uint32_t s_at = lanes + (n & 1) * KB;
@@ -469,10 +603,7 @@ __global__ void __launch_bounds__(kThreads, 2)
           }
           if (__any_sync(kAll, grow) && begun) {
             // O of the blocks before, once they are in it
-            if (!__all_sync(kAll, mbar_wait(&sy->pv_done[(n - 1) & 1], (n - 1) / 2 & 1, p.status, p.wait_cycles))) {
-              ok = false;
-              break;
-            }
+            if (!(ok = wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2))) break;
             tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
@@ -514,11 +645,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         __syncwarp();
         if (lane == 0) mbar_arrive(&sy->p_full[n & 1]);
       }
-      if (!ok) break;
-      if (!__all_sync(kAll, mbar_wait(&sy->pv_done[(n - 1) & 1], (n - 1) / 2 & 1, p.status, p.wait_cycles))) {
-        ok = false;
-        break;
-      }
+      if (!ok || !(ok = wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2))) break;
       if (!warp_live) continue;
       tc_fence_after();
       const bool whole = here && ends;
@@ -578,26 +705,75 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (warp == 4) tmem_dealloc(tmem, kTmemCols);
 }
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
+                                  const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+  static std::atomic<EncodeTiledFn> fn{nullptr};
+  EncodeTiledFn f = fn.load(std::memory_order_relaxed);
+  if (f == nullptr) {
+    void *ptr = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault,
+                                         &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess) {
+      f = (EncodeTiledFn)ptr;
+      fn.store(f, std::memory_order_relaxed);
+    }
+  }
+  return f;
+}
+
+// A pool as [pages][heads][rows][dims] in boxes of up to KB rows of one page and head; false
+// where its strides are none that a tensor map can have (the copies then go by 16 bytes).
+bool encode(CUtensorMap *map, const PagedGeom &g, const void *pool, bool codes) {
+  const EncodeTiledFn fn = encode_fn();
+  if (fn == nullptr) return false;
+  const int elem = codes ? 1 : 2;
+  const cuuint64_t dims[4] = {(cuuint64_t)g.D, (cuuint64_t)1 << g.shift, (cuuint64_t)g.Hkv,
+                              (cuuint64_t)g.n_pages};
+  cuuint64_t strides[3] = {(cuuint64_t)g.row_stride * elem, (cuuint64_t)g.head_stride * elem,
+                           (cuuint64_t)g.page_stride * elem};
+  for (int i = 0; i < 3; ++i) {
+    if (dims[i + 1] == 1) strides[i] = (cuuint64_t)g.D * elem;  // (of no use, but it has to be one)
+    if (strides[i] == 0 || strides[i] >= (1ull << 40)) return false;
+  }
+  const cuuint32_t box[4] = {(cuuint32_t)(codes ? g.D : 64), (cuuint32_t)std::min(1 << g.shift, KB), 1, 1};
+  const cuuint32_t one[4] = {1, 1, 1, 1};
+  return fn(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+            const_cast<void *>(pool), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            codes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D, bool kCodes>
-cudaError_t launch(const TreeParams &p, int dev, cudaStream_t st) {
+cudaError_t launch(TreeParams p, int dev, cudaStream_t st) {
   static std::atomic<bool> attr_set[kMaxDevices];
+  constexpr int smem = Smem<D, kCodes>::BYTES;
+  Maps maps;
+  // (boxes of fewer than 8 rows would not lie on the swizzle's 1 KB)
+  p.tma = p.g.shift >= 3 && encode(&maps.k, p.g, p.k_pages, kCodes) &&
+          encode(&maps.v, p.g, p.v_pages, kCodes);
+  p.suspend_ns = (uint32_t)std::min<long long>(p.wait_cycles / 4, 1000000);
   if (!attr_set[dev].load(std::memory_order_acquire)) {
     const cudaError_t e = cudaFuncSetAttribute(
-        tree_tc_kernel<D, kCodes>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::BYTES);
+        tree_tc_kernel<D, kCodes>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     attr_set[dev].store(true, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.n_runs * p.tiles);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Smem<D>::BYTES;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, tree_tc_kernel<D, kCodes>, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, tree_tc_kernel<D, kCodes>, p, maps);
   count_launches(1);
   return e;
 }

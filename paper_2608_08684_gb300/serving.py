@@ -90,6 +90,7 @@ class PagedDecodeLoop:
         not rotated, in the caches' dtype, any strides with the dims consecutive (views of
         a fused projection's output); called while the step is issued (and captured).
     after(l, out): consumes layer l's attention output out [B][Hq][d] fp32.
+    Caches in 8 bits (ripple.PagedCache with scales) are served alike.
 
     Pages are the caller's: before a step, every active sequence's table has an entry for
     its next row. status holds RIPPLE_EFULL or RIPPLE_EBOUNDS where it had not.
@@ -101,12 +102,12 @@ class PagedDecodeLoop:
         self.caches, self.before, self.after = list(caches), before, after
         self.lens, self.positions, self.active = lens, positions, active
         self.rope, self.scale = rope, scale
-        k = caches[0]._keep[0]
+        k, dtype = caches[0]._keep[0], caches[0].dtype
         B, d = positions.numel(), k.shape[-1]
         # calls are ordered on one stream, so every layer shares the scratch buffers
         ws = max(R.ripple_paged_decode_workspace_bytes(c, n_q_heads) for c in caches)
         self.ws = torch.empty(ws, dtype=torch.uint8, device=k.device)
-        self.q = torch.empty(B, n_q_heads, d, dtype=k.dtype, device=k.device)
+        self.q = torch.empty(B, n_q_heads, d, dtype=dtype, device=k.device)
         self.out = [torch.empty(B, n_q_heads, d, dtype=torch.float32, device=k.device)
                     for _ in caches]
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
@@ -135,3 +136,77 @@ class PagedDecodeLoop:
 
     def replay(self):
         self.graph.replay()
+
+
+class PagedDraftLoop:
+    """One step of L layers over paged caches that looks at n drafted tokens of every sequence at
+    once, and what keeps the accepted ones: per layer ripple_paged_append (the draft's keys
+    rotated into their pages, its queries rotated) and ripple_paged_tree_attn; then, when the
+    caller has compared the outputs with the guesses, ripple_paged_keep_rows for all layers.
+
+    caches, lens, active, rope, before, after, scale: as for PagedDecodeLoop (caches in 8 bits
+        too), with tokens: q [B][n][Hq][d], k and v [B][n][Hkv][d], out [B][n][Hq][d] in the
+        queries' dtype. lens counts the draft from the step on, and only the accepted tokens
+        once keep has run.
+    positions: device int32 [B][n], the drafted tokens' positions (a tree's siblings have the
+        same); read when a step runs, written by the caller.
+    masks: device int64 [B][n], bit j of a token's mask: it sees token j of its sequence's draft
+        (its ancestors and itself), or None for chains; read when a step runs.
+    kept: device int32 [B][m], the accepted tokens of every draft, ascending, ended by a negative
+        entry; read when keep runs, written by the caller.
+
+    Pages are the caller's: before a step, every active sequence's table has entries for its
+    next n rows, in pages that no other sequence has. status holds RIPPLE_EFULL or
+    RIPPLE_EBOUNDS where it had not.
+    """
+
+    def __init__(self, caches, lens, positions, active, n_q_heads, rope, before, after, kept,
+                 masks=None, scale=0.0):
+        B, n = positions.shape
+        if tuple(lens.shape) != (len(caches), B):
+            raise ValueError("lens must be [layers][sequences]")
+        self.caches, self.before, self.after = list(caches), before, after
+        self.lens, self.positions, self.active = lens, positions, active
+        self.masks, self.kept, self.rope, self.scale, self.n = masks, kept, rope, scale, n
+        self.tables = R.KeepTables(self.caches)
+        k, dtype = caches[0]._keep[0], caches[0].dtype
+        # calls are ordered on one stream, so every layer shares the scratch buffers
+        ws = max(R.ripple_paged_tree_workspace_bytes(c, n_q_heads, n) for c in caches)
+        self.ws = torch.empty(ws, dtype=torch.uint8, device=k.device)
+        self.q = torch.empty(B, n, n_q_heads, k.shape[-1], dtype=dtype, device=k.device)
+        self.out = [torch.empty_like(self.q) for _ in caches]
+        self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self.graph = self.keep_graph = None
+
+    def issue_step(self):
+        """Enqueue the step of every layer on the current stream."""
+        self.lens.add_(self.active, alpha=self.n)  # the draft counts from here on
+        for l, cache in enumerate(self.caches):
+            q, k, v = self.before(l)
+            R.ripple_paged_append(cache, self.lens[l], k, v, rope=self.rope,
+                                  positions=self.positions, q=q, q_out=self.q,
+                                  dev_status=self.status)
+            R.ripple_paged_tree_attn(cache, self.q, self.lens[l], self.out[l], self.ws,
+                                     masks=self.masks, scale=self.scale, dev_status=self.status)
+            self.after(l, self.out[l])
+
+    def issue_keep(self):
+        """Enqueue the move of the accepted tokens' rows in every layer, and the new lengths."""
+        R.ripple_paged_keep_rows(self.tables, self.lens, self.kept, n_tokens=self.n,
+                                 dev_status=self.status)
+
+    def capture(self):
+        """Capture a step and a keep in a CUDA graph each. Run issue_step() and issue_keep() once
+        outside the capture first; they count like any other."""
+        self.graph, self.keep_graph = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(self.graph):
+            self.issue_step()
+        with torch.cuda.graph(self.keep_graph):
+            self.issue_keep()
+        return self.graph, self.keep_graph
+
+    def replay(self):
+        self.graph.replay()
+
+    def replay_keep(self):
+        self.keep_graph.replay()
