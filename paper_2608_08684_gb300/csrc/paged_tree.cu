@@ -20,6 +20,7 @@ constexpr int kMaxDevices = 64;
 constexpr int kThreads = 128;
 constexpr int R = kTreeSimtRows, KB = kTreeSimtKeys;
 constexpr float kSlack = 8.f;
+constexpr int kGroupCost = 1;  // blocks that a group's queries and outputs take as long as
 
 // 16 bytes of a page's row: 4 fp32 values, or 16 codes.
 template <typename T>
@@ -69,7 +70,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
     tree_simt_kernel(const __grid_constant__ TreeParams p) {
   using P = Piece<T>;
-  using W = TreeWalk<KB>;
+  using W = TreeWalk<KB, kGroupCost>;
   constexpr int kPieces = D / P::N;                        // of a row
   constexpr int kMine = KB * kPieces / kThreads;           // of a block's keys, a thread
   constexpr bool kCodes = sizeof(T) == 1;
@@ -83,15 +84,12 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
   if (blockIdx.x == 0)
     for (int b = tid; b < p.g.B; b += kThreads) TreeSeq::check(p, b);
   W w;
-  const long long total = w.start(p, run, lane);
   int2 rec = make_int2(0, 0);
-  long long t = 0;
-  const int runs = (int)min((long long)p.n_runs, total);
-  if (total > 0) t = run_start(total, runs, run);
-  for (bool more = total > 0; more; t += w.count(), more = w.next(p)) {
+  for (bool more = w.start(p, run, lane); more; more = w.next(p)) {
+    if (w.count == 0) continue;
     const TreeSeq seq(p, w.b);
-    const bool here = w.block == 0, ends = w.block + w.count() == w.blocks();
-    if (here && !ends) rec = make_int2(w.b * p.g.Hkv + w.h, run_of(total, runs, t + w.blocks() - 1) - run + 1);
+    const bool here = w.block == 0, whole = w.whole();
+    if (here && !whole) rec = make_int2(w.b * p.g.Hkv + w.h, w.runs_of_group(run));
     const int n_rows = min(seq.tokens * p.G - tile * R, R);
     if (n_rows <= 0) continue;
     // this tile's queries (scaled) and masks; row r is token r / G, head r % G
@@ -266,7 +264,6 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
         add(false);
     }
     __syncthreads();
-    const bool whole = here && ends;
     const long long slot = ((2LL * run + (here ? 1 : 0)) * p.tiles + tile) * p.tile_rows;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -448,7 +445,7 @@ size_t plan(TreeParams *p, int tile, int block, int places, void *ws) {
 }
 size_t plan(TreeParams *p, int dtype, int sms, void *ws) {
   if (dtype == RIPPLE_BF16)
-    return plan(p, kTreeTcRows, kTreeTcKeys, kTreeTcCtas * sms, ws);
+    return plan(p, kTreeTcRows, kTreeTcKeys, kTreeTcTeams * sms, ws);
   return plan(p, kTreeSimtRows, kTreeSimtKeys, kTreeSimtCtas * sms, ws);
 }
 
@@ -526,7 +523,7 @@ extern "C" ripple_status ripple_paged_tree_attn(
   cudaStream_t st = (cudaStream_t)stream;
   const bool d128 = desc->head_dim == 128;
   if (desc->dtype == RIPPLE_BF16) {
-    RIPPLE_CUDA_TRY(launch_tree_tc(p, scales != nullptr, dev, st));
+    RIPPLE_CUDA_TRY(launch_tree_tc(p, scales != nullptr, dev, sm_count(dev), st));
     RIPPLE_CUDA_TRY((d128 ? launch_join<__nv_bfloat16, 128>(p, st)
                           : launch_join<__nv_bfloat16, 64>(p, st)));
     return RIPPLE_OK;

@@ -2,7 +2,8 @@
 // runs, and the join of a group's partials.
 //
 // Work: the cache rows of every (sequence, KV head) group are cut into blocks, and the
-// blocks of all groups, in order, into equal runs. The queries of a group, n_b tokens times
+// blocks of all groups, in order, into runs of equal cost: a group's first block costs kGroupCost
+// more (its queries, its outputs), in units of a block that begin the group. The queries of a group, n_b tokens times
 // G heads, are rows of tiles; a CTA takes a run for one row tile, and the CTAs of a run's
 // tiles are neighbours, so that they read the same rows from L2 at about the same time.
 // Lengths are read on the device; every CTA finds its run by a sum over the sequences. A
@@ -81,74 +82,85 @@ struct TreeSeq {
   }
 };
 
-// Where a run of `total` blocks begins.
+// Where a run of `total` units begins.
 __device__ __forceinline__ long long run_start(long long total, int runs, int run) {
   return total * run / runs;
 }
-// The run that has block t.
+// The run that has unit t.
 __device__ __forceinline__ int run_of(long long total, int runs, long long t) {
   return (int)(((t + 1) * runs - 1) / total);
 }
 
-// A walk over the parts of groups in a run. KB: rows of a block.
-template <int KB>
+// A walk over the parts of groups in a run. KB: rows of a block; COST: units of a group besides
+// its blocks.
+template <int KB, int COST>
 struct TreeWalk {
   int b, h, len;
   int block;           // the part's first in its group
+  int count;           // blocks of the part
   int begin, end;      // the part's rows
-  long long left;      // blocks of the run, the part's included
+  long long at, stop;  // the group's first unit, the run's end
+  long long total;
+  int runs;
   static __device__ __forceinline__ int blocks_of(const TreeSeq &s) {
     return s.tokens > 0 ? s.len / KB + (s.len % KB != 0) : 0;
   }
+  static __device__ __forceinline__ long long units_of(const TreeSeq &s) {
+    const int n = blocks_of(s);
+    return n > 0 ? n + COST : 0;
+  }
   __device__ __forceinline__ int blocks() const { return len / KB + (len % KB != 0); }
-  __device__ __forceinline__ int count() const {
-    return (int)min((long long)(blocks() - block), left);
-  }
-  __device__ __forceinline__ void set() {
+  __device__ __forceinline__ void set(int first) {
+    block = first;
+    count = (int)min((long long)blocks(), max(stop - at - COST, (long long)first)) - first;
     begin = block * KB;
-    end = (int)min((long long)len, (long long)(block + count()) * KB);
+    end = (int)min((long long)len, (long long)(block + count) * KB);
   }
-  // To the next part; false at the end of the run.
+  // The part begins its group; the runs from this one on that have the group's blocks.
+  __device__ __forceinline__ bool whole() const { return block == 0 && count == blocks(); }
+  __device__ __forceinline__ int runs_of_group(int run) const {
+    return run_of(total, runs, at + COST + blocks() - 1) - run + 1;
+  }
+  // To the next part; false at the end of the run. (A part may have no blocks: the units that
+  // begin its group are all that the run has of it.)
   __device__ __forceinline__ bool next(const TreeParams &p) {
-    left -= count();
-    if (left <= 0) return false;
-    block = 0;
+    at += blocks() + COST;
+    if (at >= stop) return false;
     if (++h >= p.g.Hkv) {
       h = 0;
-      for (;;) {  // left > 0: there are more
+      for (;;) {  // at < stop: there are more
         const TreeSeq s(p, ++b);
         len = s.len;
         if (blocks_of(s) > 0) break;
       }
     }
-    set();
+    set(0);
     return true;
   }
-  // The run's first part, by one warp; returns the number of all blocks, 0 where the run is
-  // empty (or nothing is to do).
-  __device__ __forceinline__ long long start(const TreeParams &p, int run, int lane) {
+  // To the run's first part, by one warp; false where the run is empty.
+  __device__ __forceinline__ bool start(const TreeParams &p, int run, int lane) {
     constexpr unsigned kAll = 0xffffffffu;
     const int per = (p.g.B + 31) / 32;
     const int b0 = min(lane * per, p.g.B), b1 = min(b0 + per, p.g.B);
     long long mine = 0;
-    for (int i = b0; i < b1; ++i) mine += (long long)blocks_of(TreeSeq(p, i)) * p.g.Hkv;
+    for (int i = b0; i < b1; ++i) mine += units_of(TreeSeq(p, i)) * p.g.Hkv;
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long y = __shfl_up_sync(kAll, incl, o);
       if (lane >= o) incl += y;
     }
-    const long long total = __shfl_sync(kAll, incl, 31);
-    const int runs = (int)min((long long)p.n_runs, total);
-    if (run >= runs) return 0;
+    total = __shfl_sync(kAll, incl, 31);
+    runs = (int)min((long long)p.n_runs, total);
+    if (run >= runs) return false;
     const long long t0 = run_start(total, runs, run);
-    left = run_start(total, runs, run + 1) - t0;
+    stop = run_start(total, runs, run + 1);
     const int owner = __ffs(__ballot_sync(kAll, incl > t0)) - 1;
     int seq = 0;
     long long rest = t0 - (incl - mine);
     if (lane == owner) {
       for (seq = b0;; ++seq) {
-        const long long k = (long long)blocks_of(TreeSeq(p, seq)) * p.g.Hkv;
+        const long long k = units_of(TreeSeq(p, seq)) * p.g.Hkv;
         if (rest < k) break;
         rest -= k;
       }
@@ -156,10 +168,12 @@ struct TreeWalk {
     b = __shfl_sync(kAll, seq, owner);
     rest = __shfl_sync(kAll, rest, owner);
     len = TreeSeq(p, b).len;
-    h = (int)(rest / blocks());
-    block = (int)(rest % blocks());
-    set();
-    return total;
+    const int units = blocks() + COST;
+    h = (int)(rest / units);
+    const int in = (int)(rest % units);
+    at = t0 - in;
+    set(max(0, in - COST));
+    return true;
   }
 };
 
@@ -175,10 +189,10 @@ __device__ __forceinline__ void put4(__nv_bfloat16 *p, const float4 &x) {
                                              *reinterpret_cast<const uint32_t *>(&b));
 }
 
-// bf16 queries: on the tensor cores (paged_tree_tc.cu). Rows of a tile, keys of a block, CTAs
-// of an SM.
-constexpr int kTreeTcRows = 128, kTreeTcKeys = 64, kTreeTcCtas = 2;
-cudaError_t launch_tree_tc(const TreeParams &p, bool codes, int dev, cudaStream_t st);
+// bf16 queries: on the tensor cores (paged_tree_tc.cu). Rows of a tile, keys of a block, teams
+// (which take the place of CTAs) of an SM.
+constexpr int kTreeTcRows = 128, kTreeTcKeys = 64, kTreeTcTeams = 2;
+cudaError_t launch_tree_tc(const TreeParams &p, bool codes, int dev, int sms, cudaStream_t st);
 // fp32 queries: on the CUDA cores (paged_tree.cu).
 constexpr int kTreeSimtRows = 32, kTreeSimtKeys = 32, kTreeSimtCtas = 3;
 

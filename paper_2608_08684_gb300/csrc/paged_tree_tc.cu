@@ -1,21 +1,34 @@
 // ripple_paged_tree_attn for bf16 queries, on the 5th-generation tensor cores.
 //
-// A CTA (288 threads, two on an SM) has up to 128 query rows of a KV head and takes its run's
-// blocks of 64 keys: S = Q . K^T (128 x 64) into TMEM, softmax by a thread a row, P as bf16
-// back into TMEM over S, O += P . V (128 x d) in TMEM. A draft of n tokens with G heads a KV
-// head has n G rows; up to 128 the padding costs nothing that the cache's bytes do not: a
-// block is 32 KB, 1400 cycles of an SM's share of HBM, and 512 of its tensor cores.
+// A team of 7 warps (two in a CTA, one CTA an SM) has the 128 rows of a matrix product for up to
+// 128 query rows of a KV head and takes its run's blocks of 64 keys: S = Q . K^T (128 x 64) into
+// TMEM, softmax by a thread a row, P back into TMEM over S, O += P . V (128 x d) in TMEM. A
+// draft of n tokens with G heads a KV head has n G query rows. With 32 of them or fewer the
+// product's rows hold four copies, with 64 two, and every copy takes its share of a block's keys
+// (the others' probabilities are 0), so that the four softmax warps share the work however few
+// rows there are; the copies are joined when a group is done. The products' rows cost nothing
+// that the cache's bytes do not: a block is 32 KB, 1400 cycles of an SM's share of HBM, and 512 of
+// its tensor cores.
 //
-// Warps 0-3: softmax and outputs; warp 4: issues the MMAs; warps 5, 6 fetch keys (and a
-// group's queries), 7, 8 values: a block by TMA (a box a page, with the 128-byte swizzle that
-// the MMAs read), or, where rows of it are missing or pages have fewer than 8, by 16-byte copies to
-// the same places. 8-bit pages come into a ring of their own, two blocks ahead, and these
-// warps make them the bf16 values that they stand for, exactly, so that all else is the same.
-// Scores of the next block are on their way while a block's softmax runs; S and P of two
-// blocks and O fill half of the TMEM, the other CTA's the other half.
+// Of a team, 4 warps: queries, softmax and outputs; one issues the MMAs; one fetches keys, one
+// values: a block by TMA (a box a page, with the 128-byte swizzle that the MMAs read), or,
+// where rows of it are missing or pages have fewer than 8, by 16-byte copies to the same
+// places. Scores of the next block are on their way while a block's softmax runs; S and P of
+// two blocks and O fill half of the TMEM. The teams share nothing: one's softmax runs while the
+// other's blocks are on their way. (Two CTAs of one team each do not find a place on an SM at
+// the same time, though registers, shared memory and TMEM have room.)
 //
 // P in one bf16 part: the output is rounded to bf16 as well, and a probability's rounding
 // (2^-9) enters the output as part of a mean. The sum is of the unrounded ones, in fp32.
+//
+// 8-bit pages come into a ring of their own, two blocks ahead, and warps 5 and 6 make them fp16
+// values: a code (exact in fp16) times its row's scale over the largest scale of the block (keys;
+// the block's scores are multiplied by that) or of the run's blocks so far (values; the outputs
+// are brought to a larger one as they are to a larger maximum). A row whose scale is 2^-15
+// of that or more stays exact; others are off by 2^-25 of the largest at most, less than
+// fp32 sums lose. A query row is multiplied by the power of two that brings its largest element
+// to [2^14, 2^15). P has 2^7 more than for bf16, so that what it loses at the lower end (2^-32 a
+// key) is nothing.
 #include "paged_tree.cuh"
 #include "tc_ptx.cuh"
 
@@ -29,37 +42,44 @@ namespace {
 
 constexpr int KB = kTreeTcKeys;
 constexpr int kRows = kTreeTcRows;
-constexpr int kThreads = 288;
-constexpr int kFetchers = 64;  // threads that fetch keys, and values
+// Warps 0-3, 4-7: softmax of the teams; 8, 9: their MMAs; 10, 11 and 12, 13: their keys and values.
+// (A warp reaches the TMEM lanes 32 (warp % 4) on.)
+constexpr int kTeams = 2;
+constexpr int kThreads = 448;
+constexpr int kGroupCost = 4;  // blocks that a group's queries and outputs take as long as
 constexpr int kRing = 3;       // blocks of 8-bit rows on their way or being widened
-constexpr uint32_t kTmemCols = 256;  // S and P of two blocks (64 each), O (d) from 128 on
+constexpr uint32_t kTeamCols = 256;  // of TMEM: S and P of two blocks (64 each), O (d) from 128 on
 constexpr uint32_t kOCol = 128;
 constexpr float kSlack = 8.f;
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kMaxDevices = 64;
-constexpr int kSlots = 4;  // of the blocks' present rows
+constexpr int kSlots = 4;  // of what the softmax is told about blocks
 
 struct Sync {
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t ring_full[2][kRing];                         // of keys, of values
-  uint64_t s_full[2], p_full[2], pv_done[2], mma_done;  // (of even and odd blocks)
+  uint64_t s_full[2], p_full[2], pv_done[2];            // of even and odd blocks
+  uint64_t q_full, mma_done;
+  uint64_t draft_done[kSlots];         // by parts with drafted tokens (values may be parts ahead)
   unsigned long long present[kSlots];  // rows of a block that are there
-  unsigned long long bad;              // drafted tokens whose values are not all finite
+  unsigned long long bad[kSlots];      // drafted tokens whose values are not all finite, by parts
   uint32_t tmem;
   int abort;                           // a role has given up waiting
+  int top[2][kSlots];                  // 8-bit pages: the scale bytes that a block's keys, values are over
   uint8_t scale[2][kRing][KB];         // of the ring's rows
+  float inv[64];                       // of a group's query rows (with copies)
 };
 
 template <int D, bool kCodes>
 struct Smem {
-  static constexpr int STAGES = kCodes ? 1 : 2;  // of bf16 blocks of keys, and of values
+  static constexpr int STAGES = kCodes ? 1 : 2;  // of 16-bit blocks of keys, and of values
   static constexpr int Q = kRows * D * 2, TILE = KB * D * 2;
   static constexpr int RAW = KB * D;             // a block of 8-bit rows
   static constexpr int HALF_Q = kRows * 128, HALF = KB * 128;  // of 64 dims
   static constexpr int K0 = Q, V0 = Q + STAGES * TILE, RING = V0 + STAGES * TILE;
-  static constexpr int SYNC = RING + (kCodes ? 2 * kRing * RAW : 0);
-  static constexpr int BYTES = SYNC + (int)sizeof(Sync);
-  static_assert(2 * (BYTES + 1024) <= 228 * 1024, "two CTAs an SM");
+  static constexpr int TEAM = RING + (kCodes ? 2 * kRing * RAW : 0);
+  static constexpr int BYTES = kTeams * (TEAM + (int)sizeof(Sync));
+  static_assert(TEAM % 1024 == 0 && BYTES <= 227 * 1024, "shared memory per CTA");
 };
 
 // The pools as TMA sees them: boxes of 64 dims (8-bit: a row) x rows of a page.
@@ -79,9 +99,20 @@ __device__ __forceinline__ void copies_arrive(uint64_t *bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 // Bounded wait: gives up after the bound, or when another role has. A poll suspends the thread
-// for a quarter of the bound at most.
+// for a quarter of the bound at most; not at all where that is little, since the least that the
+// hardware suspends a thread for is then more.
 __device__ __forceinline__ bool try_wait_for(uint64_t *bar, uint32_t parity, uint32_t ns) {
   uint32_t ok;
+  if (ns < 1000) {
+    asm volatile(
+        "{\n .reg .pred p;\n"
+        " mbarrier.test_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+  }
   asm volatile(
       "{\n .reg .pred p;\n"
       " mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\n"
@@ -110,10 +141,7 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there
                "r"(there ? 16 : 0)
                : "memory");
 }
-__device__ __forceinline__ void copies_landed() {
-  asm volatile("cp.async.wait_all;" ::: "memory");
-  fence_proxy_async_smem();  // for the tensor cores' reads
-}
+__device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void st_shared16(uint32_t to, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(a), "r"(b), "r"(c), "r"(d)
                : "memory");
@@ -155,10 +183,50 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
+      "%11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+        "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
 __device__ __forceinline__ void tmem_wait_st() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+// N columns of the thread's lane: 16, 32 or 64.
+template <int N>
+__device__ __forceinline__ void tmem_load(uint32_t at, uint32_t (&r)[N]) {
+  if constexpr (N == 16)
+    tmem_ld16(at, r);
+  else
+#pragma unroll
+    for (int i = 0; i < N / 32; ++i) tmem_ld32(at + 32 * i, reinterpret_cast<uint32_t(&)[32]>(r[32 * i]));
+  tmem_wait_ld();
+}
+template <int N>
+__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t (&r)[N]) {
+  if constexpr (N == 8)
+    tmem_st8(at, r);
+  else if constexpr (N == 16)
+    tmem_st16(at, r);
+  else
+    tmem_st32(at, r);
+}
+// Two values as a pair of 16 bits, bf16 or (8-bit pages) fp16.
+template <bool kHalf>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+  if (kHalf) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+  }
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t *>(&h);
 }
@@ -167,86 +235,101 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t pair) {
   return ((pair & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) |
          ((pair & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
-// The value of a scale byte as a factor; 255 is NaN.
-__device__ __forceinline__ float scale_of_byte(int s) {
-  return s == 255 ? __int_as_float(0x7fffffff) : __int_as_float(s << 23);  // (7..247)
+// 2^(byte - top), twice, in fp16 (0 below its values); NaN for byte 255. byte <= top.
+__device__ __forceinline__ __half2 relative_scale(int byte, int top) {
+  const int d = byte - top;
+  uint32_t h = d >= -14 ? (uint32_t)(15 + d) << 10 : d >= -24 ? 1u << (24 + d) : 0u;
+  if (byte == 255) h = 0x7fffu;
+  h |= h << 16;
+  return *reinterpret_cast<const __half2 *>(&h);
 }
-// 16 codes times their scale as bf16, exactly.
-__device__ __forceinline__ void widen(const uint4 &u, float scale, uint32_t (&o)[8]) {
+// 16 codes times a scale as fp16.
+__device__ __forceinline__ void widen(const uint4 &u, __half2 scale, uint32_t (&o)[8]) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i / 2] >> (16 * (i & 1))), __NV_E4M3);
-    const float2 f = __half22float2(__half2(h));
-    o[i] = pack_bf16x2(f.x * scale, f.y * scale);
+    const __half2 x = __hmul2(__half2(h), scale);
+    o[i] = *reinterpret_cast<const uint32_t *>(&x);
   }
 }
+__device__ __forceinline__ float pow2(int e) {  // -126 <= e <= 127
+  return __int_as_float((e + 127) << 23);
+}
 
-// kCodes: 8-bit pages.
-template <int D, bool kCodes>
-__global__ void __launch_bounds__(kThreads, 2)
+// kCodes: 8-bit pages. C: copies of the query rows.
+template <int D, bool kCodes, int C>
+__global__ void __launch_bounds__(kThreads, 1)
     tree_tc_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ Maps maps) {
   using S = Smem<D, kCodes>;
+  using W = TreeWalk<KB, kGroupCost>;
   constexpr int ST = S::STAGES;
-  using W = TreeWalk<KB>;
-  extern __shared__ __align__(1024) uint8_t tiles[];
-  Sync *const sy = (Sync *)(tiles + S::SYNC);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int run = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
-  if (tid == 0) {
+  constexpr int RT = kRows / C;   // query rows of the tile
+  constexpr int KC = KB / C;      // keys of a block that a copy takes
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int lane = threadIdx.x & 31, cta_warp = threadIdx.x >> 5;
+  const int team = cta_warp < 8 ? cta_warp / 4 : cta_warp < 10 ? cta_warp - 8 : (cta_warp - 10) / 2;
+  // 0-3: softmax, 4: MMAs, 5: keys, 6: values
+  const int warp = cta_warp < 8 ? cta_warp % 4 : cta_warp < 10 ? 4 : 5 + cta_warp % 2;
+  const int tid = 32 * warp + lane;
+  uint8_t *const tiles = smem + team * S::TEAM;
+  Sync *const syncs = (Sync *)(smem + kTeams * S::TEAM), *const sy = syncs + team;
+  // (as many CTAs as SMs, or one for each team's work: teams beside one another in different CTAs)
+  const int work = blockIdx.x + team * gridDim.x;
+  const int run = work / p.tiles, tile = work % p.tiles;
+  if (warp == 4 && lane == 0) {
     sy->abort = 0;
     for (int i = 0; i < kRing; ++i) {
-      mbar_init(&sy->ring_full[0][i], kFetchers);
-      mbar_init(&sy->ring_full[1][i], kFetchers);
+      mbar_init(&sy->ring_full[0][i], 32);
+      mbar_init(&sy->ring_full[1][i], 32);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sy->k_full[i], kFetchers);
-      mbar_init(&sy->v_full[i], kFetchers);
+      mbar_init(&sy->k_full[i], 32);
+      mbar_init(&sy->v_full[i], 32);
       mbar_init(&sy->k_empty[i], 1);
       mbar_init(&sy->v_empty[i], 1);
       mbar_init(&sy->s_full[i], 1);
       mbar_init(&sy->p_full[i], 4);
       mbar_init(&sy->pv_done[i], 1);
     }
+    mbar_init(&sy->q_full, 4);
+    for (int i = 0; i < kSlots; ++i) mbar_init(&sy->draft_done[i], 32);
     mbar_init(&sy->mma_done, 1);
     fence_mbar_init();
     fence_proxy_async_smem();
   }
-  if (warp == 4) {
-    tmem_alloc(&sy->tmem, kTmemCols);
+  if (cta_warp == 8) {
+    tmem_alloc(&syncs->tmem, kTeams * kTeamCols);
     tmem_relinquish();
   }
   pdl_wait();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = sy->tmem;
+  const uint32_t tmem = syncs->tmem + team * kTeamCols;
   if (blockIdx.x == 0)
-    for (int b = tid; b < p.g.B; b += kThreads) TreeSeq::check(p, b);
+    for (int b = threadIdx.x; b < p.g.B; b += kThreads) TreeSeq::check(p, b);
 
   const uint32_t qs = smem_u32(tiles), ks = qs + S::K0, vs = qs + S::V0;
   W w;
-  const long long total = w.start(p, run, lane);
-  const bool any = total > 0;
+  const bool any = w.start(p, run, lane);
   int n = 0;  // blocks of this CTA so far
   bool ok = true;
-
   auto wait_for = [&](uint64_t *bar, int phase) {  // by a whole warp
     return __all_sync(kAll, wait_bar(bar, phase, p, &sy->abort));
   };
 
   if (warp >= 5) {
-    // -------------------------------------------------- keys (and queries), values
-    const bool keys = warp < 7;
-    const int th = tid - (keys ? 160 : 224), wk = th >> 5;
+    // -------------------------------------------------- keys, values
+    const bool keys = warp == 5;
     uint64_t *const full = keys ? sy->k_full : sy->v_full, *const empty = keys ? sy->k_empty : sy->v_empty;
     const uint32_t stages = keys ? ks : vs;
     const uint8_t *const pool = (const uint8_t *)(keys ? p.k_pages : p.v_pages);
     const CUtensorMap *const map = keys ? &maps.k : &maps.v;
     constexpr int kElem = kCodes ? 1 : 2;
     constexpr int kPieces = D * kElem / 16;     // of a row in its page
-    constexpr int kRowsWarp = 32 / kPieces;     // rows of a warp's copy
-    constexpr int kSteps = KB / (2 * kRowsWarp);
+    constexpr int kRowsWarp = 32 / kPieces;     // rows of a copy of the warp
+    constexpr int kSteps = KB / kRowsWarp;
     const int sub = lane / kPieces, pc = lane % kPieces;
     const int page_rows = 1 << p.g.shift, box = min(page_rows, KB);
     // entries of the block table for the rows lane and lane + 32 of the next block
@@ -274,27 +357,26 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
       const uint32_t lo = __ballot_sync(kAll, there[0]), hi = __ballot_sync(kAll, there[1]);
       present = (unsigned long long)hi << 32 | lo;
-      if (!kCodes && keys && th == 0) sy->present[n % kSlots] = present;
+      if (!kCodes && keys && lane == 0) sy->present[n % kSlots] = present;
+      __syncwarp();
       if (allowed && p.tma && present == ~0ull) {
-        if (th == 0) mbar_arrive_expect_tx(bar, KB * D * kElem);
-        if (wk == 0) {
-          __syncwarp();
-          // a lane a page: the entry of its first row
-          const int boxes = KB / box, first = lane * box;
-          const int e0 = __shfl_sync(kAll, entry[0], first & 31), e1 = __shfl_sync(kAll, entry[1], first & 31);
-          if (lane < boxes) {
-            const int page = first < 32 ? e0 : e1, slot = (row0 + first) & (page_rows - 1);
-            if constexpr (kCodes) {
-              tma_load_4d(to + first * D, map, 0, slot, w.h, page, bar);
-            } else {
+        if (lane == 0) mbar_arrive_expect_tx(bar, KB * D * kElem);
+        __syncwarp();
+        // a lane a page: the entry of its first row
+        const int boxes = KB / box, first = lane * box;
+        const int e0 = __shfl_sync(kAll, entry[0], first & 31), e1 = __shfl_sync(kAll, entry[1], first & 31);
+        if (lane < boxes) {
+          const int page = first < 32 ? e0 : e1, slot = (row0 + first) & (page_rows - 1);
+          if constexpr (kCodes) {
+            tma_load_4d(to + first * D, map, 0, slot, w.h, page, bar);
+          } else {
 #pragma unroll
-              for (int half = 0; half < D / 64; ++half)
-                tma_load_4d(to + half * S::HALF + first * 128, map, 64 * half, slot, w.h, page, bar);
-            }
+            for (int half = 0; half < D / 64; ++half)
+              tma_load_4d(to + half * S::HALF + first * 128, map, 64 * half, slot, w.h, page, bar);
           }
-          __syncwarp();
         }
-        if (th != 0) mbar_arrive(bar);
+        __syncwarp();
+        if (lane != 0) mbar_arrive(bar);
         return true;
       }
       long long place[2];
@@ -305,98 +387,105 @@ __global__ void __launch_bounds__(kThreads, 2)
                                (row & (page_rows - 1)) * p.g.row_stride) * kElem
                             : -1;
       }
-#pragma unroll
+#pragma unroll 8
       for (int i = 0; i < kSteps; ++i) {
-        const int row = (2 * i + wk) * kRowsWarp + sub;
-        const long long at = __shfl_sync(kAll, row < 32 ? place[0] : place[1], row & 31);
+        const int row = i * kRowsWarp + sub;
+        const long long at = __shfl_sync(kAll, i * kRowsWarp < 32 ? place[0] : place[1], row & 31);
         copy16(kCodes ? to + row * D + 16 * pc
                       : to + (pc >> 3) * S::HALF + row * 128 + (((pc & 7) ^ (row & 7)) << 4),
                pool + (at >= 0 ? at + 16 * pc : 0), at >= 0);
       }
       return false;
     };
-    // What both warps of keys (of values) agree on: they fetch a block, or neither does, so that
-    // what is on its way is waited for by its barrier also when a wait has given up.
-    auto both = [&](bool mine) {
-      int all;
-      asm volatile(
-          "{\n .reg .pred p, q;\n setp.ne.b32 q, %1, 0;\n"
-          " barrier.cta.red.and.pred p, %2, %3, q;\n selp.s32 %0, 1, 0, p;\n}\n"
-          : "=r"(all)
-          : "r"((int)mine), "r"(keys ? 2 : 3), "r"(kFetchers)
-          : "memory");
-      return all != 0;
+    // Values of drafted tokens that are not finite are left out of the products (a hidden one's
+    // weight is 0, and 0 times them is NaN) and added to the outputs of the rows that see them: who
+    // they are is told with the part's last block.
+    int drafts = 0;  // parts with drafted tokens
+    unsigned long long bad = 0;
+    auto tell_bad = [&]() {
+      const uint32_t lo = __reduce_or_sync(kAll, (uint32_t)bad), hi = __reduce_or_sync(kAll, (uint32_t)(bad >> 32));
+      if (lane == 0) sy->bad[drafts % kSlots] = (unsigned long long)hi << 32 | lo;
+      bad = 0;
+      mbar_arrive(&sy->draft_done[drafts % kSlots]);
+      ++drafts;
     };
     int ring_n = 0, issued = 0;  // blocks that have gone through the ring, that were put there
     for (bool more = any; more && ok; more = w.next(p)) {
       const TreeSeq seq(p, w.b);
-      const int n_rows = min(seq.tokens * p.G - tile * kRows, kRows);
-      if (n_rows <= 0) continue;
+      if (seq.tokens * p.G - tile * RT <= 0 || w.count == 0) continue;
       look_up(w.begin);
-      // the group's queries, once the scores of the group before are done
-      auto fetch_queries = [&]() {
-        if (n > 0 && !both(wait_for(&sy->k_empty[(n - 1) % ST], (n - 1) / ST))) return false;
-        constexpr int kQPieces = D / 8;
-        for (int i = th; i < kRows * kQPieces; i += kFetchers) {
-          const int r = i / kQPieces, c = i % kQPieces;
-          const bool there = r < n_rows;
-          const int row = tile * kRows + (there ? r : 0), tok = row / p.G, head = w.h * p.G + row % p.G;
-          const __nv_bfloat16 *q = (const __nv_bfloat16 *)p.q + head * p.q_head +
-                                   (p.starts == nullptr ? w.b * p.q_seq + tok * p.q_token
-                                                        : (long long)(seq.first + tok) * p.q_token);
-          copy16(qs + (c >> 3) * S::HALF_Q + r * 128 + (((c & 7) ^ (r & 7)) << 4), q + 8 * c, there);
-        }
-        return true;
-      };
       if constexpr (!kCodes) {
         for (int row0 = w.begin; row0 < w.end; row0 += KB, ++n) {
           const int stage = n % ST;
-          if (n >= ST && !(ok = both(wait_for(&empty[stage], n / ST - 1)))) break;
-          // drafted tokens' values that are not finite are left out here (a hidden one's weight is
-          // 0, and 0 times them is NaN) and added to the outputs of the rows that see them
-          const bool draft = !keys && row0 + KB > seq.prefix, queries = keys && row0 == w.begin;
+          if (n >= ST && !(ok = wait_for(&empty[stage], n / ST - 1))) break;
+          const bool draft = !keys && w.end > seq.prefix && row0 + KB > seq.prefix;
           const uint32_t to = stages + stage * S::TILE;
-          if (queries && !(ok = fetch_queries())) break;
-          // (the queries are waited for below, and this thread arrives after that)
-          const bool by_tma = fetch(row0, to, &full[stage], !draft && !queries);
+          const bool by_tma = fetch(row0, to, &full[stage], !draft);
           if (row0 + KB < w.end) look_up(row0 + KB);
           if (by_tma) continue;
-          asm volatile("cp.async.wait_all;" ::: "memory");
+          copies_landed();
           if (draft) {
-#pragma unroll 1
-            for (int i = 0; i < kSteps; ++i) {
-              const int row = (2 * i + wk) * kRowsWarp + sub;
+            const int first = (int)max(0LL, seq.prefix - row0);  // row of the block
+#pragma unroll 4
+            for (int i = first / kRowsWarp; i < kSteps; ++i) {
+              const int row = i * kRowsWarp + sub;
               const uint32_t at = to + (pc >> 3) * S::HALF + row * 128 + (((pc & 7) ^ (row & 7)) << 4);
               const uint4 u = ld_shared16(at);
               const uint32_t b[4] = {not_finite(u.x), not_finite(u.y), not_finite(u.z), not_finite(u.w)};
-              if (row0 + row >= seq.prefix && (b[0] | b[1] | b[2] | b[3]) != 0)
+              if (row >= first && (b[0] | b[1] | b[2] | b[3]) != 0) {
                 st_shared16(at, u.x & ~b[0], u.y & ~b[1], u.z & ~b[2], u.w & ~b[3]);
+                bad |= 1ull << (row0 + row - seq.prefix & 63);
+              }
             }
+            if (row0 + KB >= w.end) tell_bad();
           }
-          fence_proxy_async_smem();
+          fence_proxy_async_smem();  // for the tensor cores' reads
           mbar_arrive(&full[stage]);
         }
       } else {
-        const uint8_t *const scales = keys ? p.k_scales : p.v_scales;
         uint8_t(*const scale_ring)[KB] = sy->scale[keys ? 0 : 1];
         uint64_t *const ring_full = sy->ring_full[keys ? 0 : 1];
         const uint32_t ring = qs + S::RING + (keys ? 0 : kRing * S::RAW);
-        const int my_row = 32 * wk + lane;
-        int byte = 0, byte_slot = -1;  // of the thread's row of the block issued last
-        auto put_scale = [&]() {
-          if (byte_slot >= 0) scale_ring[byte_slot][my_row] = (uint8_t)byte;
+        // scale bytes of the rows lane and lane + 32 of the block issued last (0: not there), of
+        // keys and of values; they are put into the ring when the next one is issued, with the
+        // largest (255 is none): the block's of keys, the run's so far of values
+        int k_byte[2], v_byte[2], byte_slot = -1, v_top = 0;
+        unsigned long long ring_present[kRing];
+        int ring_top[2][kRing];
+        auto put_scales = [&]() {
+          if (byte_slot < 0) return;
+          int top[2] = {0, 0};
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            scale_ring[byte_slot][lane + 32 * i] = (uint8_t)(keys ? k_byte[i] : v_byte[i]);
+            if (keys && k_byte[i] != 255) top[0] = max(top[0], k_byte[i]);
+            if (v_byte[i] != 255) top[1] = max(top[1], v_byte[i]);
+          }
+          v_top = max(v_top, __reduce_max_sync(kAll, top[1]));
+          top[0] = keys ? __reduce_max_sync(kAll, top[0]) : 0;
+#pragma unroll
+          for (int k = 0; k < kRing; ++k)
+            if (k == byte_slot) {
+              ring_top[0][k] = top[0] > 0 ? top[0] : 127;
+              ring_top[1][k] = v_top > 0 ? v_top : 7;
+            }
           byte_slot = -1;
         };
-        // the block at row0 into the ring; its scales are put there when the next one is issued
-        unsigned long long ring_present[kRing];
         auto issue = [&](int row0, int i) {
           const int slot = i % kRing;
           issued = i + 1;
-          put_scale();
-          const int page = wk == 0 ? entry[0] : entry[1], row = row0 + my_row;
-          byte = 0;
-          if ((unsigned)page < (unsigned)p.g.n_pages)
-            byte = scales[page * p.scale_page + w.h * p.scale_head + (row & (page_rows - 1)) * p.scale_row];
+          put_scales();
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int page = entry[k], row = row0 + lane + 32 * k;
+            k_byte[k] = v_byte[k] = 0;
+            if ((unsigned)page < (unsigned)p.g.n_pages) {
+              const long long at =
+                  page * p.scale_page + w.h * p.scale_head + (row & (page_rows - 1)) * p.scale_row;
+              if (keys) k_byte[k] = p.k_scales[at];
+              v_byte[k] = p.v_scales[at];
+            }
+          }
           byte_slot = slot;
           if (!fetch(row0, ring + slot * S::RAW, &ring_full[slot], true)) copies_arrive(&ring_full[slot]);
 #pragma unroll
@@ -407,28 +496,34 @@ __global__ void __launch_bounds__(kThreads, 2)
         issue(w.begin, ring_n);
         if (w.begin + KB < w.end) issue(w.begin + KB, ring_n + 1);
         for (int row0 = w.begin; row0 < w.end; row0 += KB, ++n, ++ring_n) {
-          put_scale();
+          put_scales();
+          __syncwarp();  // (the slot that is issued to has been read, the scales are there)
           if (row0 + 2 * KB < w.end) issue(row0 + 2 * KB, ring_n + 2);
           const int slot = ring_n % kRing, stage = n % ST;
-          // (then the scales of this block are there as well)
-          ok = both(wait_for(&ring_full[slot], ring_n / kRing) &&
-                    (n < ST || wait_for(&empty[stage], n / ST - 1)));
+          ok = wait_for(&ring_full[slot], ring_n / kRing) &&
+               (n < ST || wait_for(&empty[stage], n / ST - 1));
           if (!ok) break;
-          if (keys && row0 == w.begin && !(ok = fetch_queries())) break;
-          if (keys && th == 0) {
+          int top = 0;
 #pragma unroll
-            for (int k = 0; k < kRing; ++k)
-              if (k == slot) sy->present[n % kSlots] = ring_present[k];
-          }
+          for (int k = 0; k < kRing; ++k)
+            if (k == slot) {
+              top = ring_top[keys ? 0 : 1][k];
+              if (keys && lane == 0) {
+                sy->present[n % kSlots] = ring_present[k];
+                sy->top[0][n % kSlots] = ring_top[0][k];
+                sy->top[1][n % kSlots] = ring_top[1][k];
+              }
+            }
           const uint32_t from = ring + slot * S::RAW, to = stages + stage * S::TILE;
-          const bool draft = !keys && row0 + KB > seq.prefix;
-#pragma unroll
+          const bool draft = !keys && w.end > seq.prefix && row0 + KB > seq.prefix;
+#pragma unroll 4
           for (int i = 0; i < kSteps; ++i) {
-            const int row = (2 * i + wk) * kRowsWarp + sub;
-            float f = scale_of_byte(scale_ring[slot][row]);
+            const int row = i * kRowsWarp + sub, byte = scale_ring[slot][row];
             uint4 u = ld_shared16(from + row * D + 16 * pc);
-            if (draft && f != f && row0 + row >= seq.prefix) {  // as infinite values of bf16 pages
-              f = 0.f;
+            __half2 f = relative_scale(byte, top);
+            if (draft && byte == 255 && row0 + row >= seq.prefix) {
+              bad |= 1ull << (row0 + row - seq.prefix & 63);
+              f = __half2(__ushort_as_half(0), __ushort_as_half(0));
               u = make_uint4(0, 0, 0, 0);
             }
             uint32_t o[8];
@@ -438,10 +533,9 @@ __global__ void __launch_bounds__(kThreads, 2)
             st_shared16(at + (((c & 7) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
             st_shared16(at + ((((c & 7) + 1) ^ (row & 7)) << 4), o[4], o[5], o[6], o[7]);
           }
-          if (keys && row0 == w.begin) asm volatile("cp.async.wait_all;" ::: "memory");
-          fence_proxy_async_smem();
+          if (draft && row0 + KB >= w.end) tell_bad();
+          fence_proxy_async_smem();  // for the tensor cores' reads
           mbar_arrive(&full[stage]);
-          named_bar_sync(keys ? 2 : 3, kFetchers);  // the slot has been read
         }
       }
     }
@@ -456,8 +550,9 @@ __global__ void __launch_bounds__(kThreads, 2)
     }
   } else if (warp == 4) {
     // -------------------------------------------------- MMAs (the whole warp waits, one lane issues)
-    constexpr uint32_t id_qk = idesc_bf16(kRows, KB);
-    constexpr uint32_t id_pv = idesc_bf16(kRows, D) | (1u << 16);  // V: d is the contiguous one
+    constexpr uint32_t kType = kCodes ? ~((1u << 7) | (1u << 10)) : ~0u;  // fp16 in place of bf16
+    constexpr uint32_t id_qk = idesc_bf16(kRows, KB) & kType;
+    constexpr uint32_t id_pv = (idesc_bf16(kRows, D) & kType) | (1u << 16);  // V: d is the contiguous one
     const uint64_t qd = sw128_desc(qs);
     // scores of block i: S(i). The products P . V of the blocks up to n - 1 have been issued, and
     // all of them have to be done: P of block i - 2 lies where S(i) goes, and a barrier that has
@@ -481,10 +576,12 @@ __global__ void __launch_bounds__(kThreads, 2)
       __syncwarp();
       return true;
     };
+    int part = 0;
     for (bool more = any; more && ok; more = w.next(p)) {
       const TreeSeq seq(p, w.b);
-      if (seq.tokens * p.G - tile * kRows <= 0) continue;
-      const int count = w.count();
+      if (seq.tokens * p.G - tile * RT <= 0 || w.count == 0) continue;
+      const int count = w.count;
+      if (!(ok = wait_for(&sy->q_full, part++))) break;
       ok = scores(n);
       for (int i = 0; i < count && ok; ++i, ++n) {
         if (i + 1 < count && !(ok = scores(n + 1))) break;
@@ -500,7 +597,8 @@ __global__ void __launch_bounds__(kThreads, 2)
           for (int kk = 0; kk < KB / 16; ++kk)  // 16 keys: 8 columns of P, 2 KB of V
             mma_bf16_ts(tmem + kOCol, tmem + (n & 1) * KB + kk * 8, vd + (kk * 2048 >> 4), id_pv,
                         kk > 0 || i > 0);
-          mma_commit(&sy->v_empty[st]);
+          // (the copies are joined in the last block's stage)
+          if (C == 1 || i + 1 < count) mma_commit(&sy->v_empty[st]);
           mma_commit(&sy->pv_done[n & 1]);
         }
         __syncwarp();
@@ -510,96 +608,160 @@ __global__ void __launch_bounds__(kThreads, 2)
     __syncwarp();
     mbar_wait(&sy->mma_done, 0, nullptr);
   } else {
-    // -------------------------------------------------- softmax and outputs, a thread a row
+    // ------------------------------------ queries, softmax and outputs, a thread a row of the products
     const uint32_t lanes = tmem + ((uint32_t)(32 * warp) << 16);
     int2 rec = make_int2(0, 0);
-    const int runs = (int)min((long long)p.n_runs, total);
-    long long t = any ? run_start(total, runs, run) : 0;
-    const int r = tid;  // row of the tile
-    for (bool more = any; more && ok; t += w.count(), more = w.next(p)) {
+    const int copy = tid / RT, r = tid % RT;
+    const int key0 = copy * KC;
+    // The queries of the part at `w`, once the products with the ones before are done; returns what
+    // the row's scores are multiplied by.
+    auto fetch_queries = [&](const W &w, const TreeSeq &seq) {
+      const int n_rows = min(seq.tokens * p.G - tile * RT, RT);
+      const bool live = r < n_rows;
+      const int row = tile * RT + (live ? r : 0), tok = row / p.G, head = w.h * p.G + row % p.G;
+      const __nv_bfloat16 *q = (const __nv_bfloat16 *)p.q + head * p.q_head +
+                               (p.starts == nullptr ? w.b * p.q_seq + tok * p.q_token
+                                                    : (long long)(seq.first + tok) * p.q_token);
+      const uint32_t to = qs + tid * 128;
+      float scale = p.scale2;
+      if constexpr (!kCodes) {
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c)
+          copy16(to + (c >> 3) * S::HALF_Q + (((c & 7) ^ (tid & 7)) << 4), q + 8 * c, live);
+        copies_landed();
+      } else {
+        uint4 x[D / 8];
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c)
+          x[c] = live ? reinterpret_cast<const uint4 *>(q)[c] : make_uint4(0, 0, 0, 0);
+        float most = 0.f;
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) {
+          const uint32_t u[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            most = fmaxf(most, fmaxf(fabsf(__uint_as_float(u[i] << 16)),
+                                     fabsf(__uint_as_float(u[i] & 0xffff0000u))));
+        }
+        // (infinities keep the others finite; what is below 2^-86 may be lost)
+        const int up = most == 0.f ? 0 : min(14 - ((__float_as_int(most) >> 23) - 127), 100);
+        const float f = pow2(up);
+        scale *= pow2(-up);
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) {
+          const uint32_t u[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+          uint32_t o[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            o[i] = pack16<true>(__uint_as_float(u[i] << 16) * f, __uint_as_float(u[i] & 0xffff0000u) * f);
+          st_shared16(to + (c >> 3) * S::HALF_Q + (((c & 7) ^ (tid & 7)) << 4), o[0], o[1], o[2], o[3]);
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sy->q_full);
+      return scale;
+    };
+    float row_scale = 0.f;  // of the part's queries
+    bool have_queries = false;
+    int drafts = 0;  // parts with drafted tokens
+    for (bool more = any; more && ok; more = w.next(p)) {
       const TreeSeq seq(p, w.b);
-      const bool here = w.block == 0, ends = w.block + w.count() == w.blocks();
-      if (here && !ends)
-        rec = make_int2(w.b * p.g.Hkv + w.h, run_of(total, runs, t + w.blocks() - 1) - run + 1);
-      const int n_rows = min(seq.tokens * p.G - tile * kRows, kRows);
+      if (w.count == 0) continue;
+      const bool here = w.block == 0, whole = w.whole();
+      if (here && !whole) rec = make_int2(w.b * p.g.Hkv + w.h, w.runs_of_group(run));
+      const int n_rows = min(seq.tokens * p.G - tile * RT, RT);
       if (n_rows <= 0) continue;
-      const int row = tile * kRows + r, tok = row / p.G;
-      const bool live = r < n_rows, warp_live = 32 * warp < n_rows;
+      if (!have_queries) row_scale = fetch_queries(w, seq);
+      const bool live = r < n_rows, warp_live = 32 * warp % RT < n_rows;
+      // query row r of the tile: token, output row
+      auto token_of = [&](int i) { return (tile * RT + i) / p.G; };
+      auto out_row = [&](int i) {
+        return (long long)(seq.first + token_of(i)) * p.Hq + w.h * p.G + (tile * RT + i) % p.G;
+      };
       uint64_t mask = 0;
-      if (live) mask = p.masks == nullptr ? ~0ull >> (63 - tok) : p.masks[seq.first + tok];
-      // drafted tokens of this part whose values are not finite
-      unsigned long long bad = 0;
-      if (w.end > seq.prefix) {
-        if (tid == 0) sy->bad = 0;
-        named_bar_sync(1, 128);
-        for (int j = warp; j < seq.tokens; j += 4) {
-          const long long at_row = seq.prefix + j;
-          if (at_row < w.begin || at_row >= w.end) continue;
+      if (live) mask = p.masks == nullptr ? ~0ull >> (63 - token_of(r)) : p.masks[seq.first + token_of(r)];
+      // adds what the values of the drafted tokens in `which` have that is not finite to the dims
+      // from d0 on
+      auto add_bad = [&](unsigned long long which, int d0, float *o, int dims) {
+        for (unsigned long long left = which; left != 0; left &= left - 1) {
+          const long long at_row = seq.prefix + __ffsll(left) - 1;
           const int page = p.table[guard((long long)w.b * p.g.max_pages + (at_row >> p.g.shift), 1,
                                          (long long)p.g.B * p.g.max_pages, p.status)];
-          if ((unsigned)page >= (unsigned)p.g.n_pages) continue;
-          const int slot = (int)(at_row & ((1 << p.g.shift) - 1));
-          bool found;
-          if constexpr (kCodes) {
-            found = p.v_scales[page * p.scale_page + w.h * p.scale_head + slot * p.scale_row] == 255;
-          } else {
-            const uint32_t *v = reinterpret_cast<const uint32_t *>(
-                (const __nv_bfloat16 *)p.v_pages + page * p.g.page_stride + w.h * p.g.head_stride +
-                slot * p.g.row_stride);
-            uint32_t any_bad = 0;
-#pragma unroll
-            for (int i = 0; i < D / 64; ++i) any_bad |= not_finite(v[lane + 32 * i]);
-            found = any_bad != 0;
+          const int v_slot = (int)(at_row & ((1 << p.g.shift) - 1));
+          const __nv_bfloat16 *v = (const __nv_bfloat16 *)p.v_pages + page * p.g.page_stride +
+                                   w.h * p.g.head_stride + v_slot * p.g.row_stride + d0;
+          for (int i = 0; i < dims; ++i) {
+            const float x = kCodes ? __int_as_float(0x7fffffff) : __bfloat162float(v[i]);
+            if (!(fabsf(x) < INFINITY)) o[i] += x;
           }
-          if (__any_sync(kAll, found) && lane == 0) atomicOr(&sy->bad, 1ull << j);
         }
-        named_bar_sync(1, 128);
-        bad = sy->bad & mask;
-      }
+      };
+      // For four outputs from dim d0 on, those that are NaN: the sum of the values that are not
+      // finite over the part's rows before the draft; others stay.
+      auto add_not_finite = [&](int d0, float (&o)[4]) {
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const int end = (int)min((long long)w.end, seq.prefix);
+        for (int row = w.begin; row < end; ++row) {
+          const int page = p.table[guard((long long)w.b * p.g.max_pages + (row >> p.g.shift), 1,
+                                         (long long)p.g.B * p.g.max_pages, p.status)];
+          if ((unsigned)page >= (unsigned)p.g.n_pages) continue;
+          const uint2 u = *reinterpret_cast<const uint2 *>(
+              (const __nv_bfloat16 *)p.v_pages + page * p.g.page_stride + w.h * p.g.head_stride +
+              (row & ((1 << p.g.shift) - 1)) * p.g.row_stride + d0);
+          const uint32_t bits[4] = {u.x << 16, u.x & 0xffff0000u, u.y << 16, u.y & 0xffff0000u};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if ((bits[i] & 0x7f800000u) == 0x7f800000u) sum[i] += __uint_as_float(bits[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (o[i] != o[i] && sum[i] != 0.f) o[i] = sum[i];
+      };
+      // m: what the probabilities are relative to, a maximum (8-bit pages: less 7), in log2
+      constexpr float kLow = kCodes ? 7.f : 0.f;
       float m = -INFINITY, l = 0.f;
+      int v_top = 127;     // 8-bit pages: O is over this value's scale
       bool begun = false;  // O has a block
       for (int row0 = w.begin; row0 < w.end && ok; row0 += KB, ++n, begun = true) {
         if (!(ok = wait_for(&sy->s_full[n & 1], n / 2))) break;
         if (warp_live) {
           tc_fence_after();
           const uint32_t s_at = lanes + (n & 1) * KB;
+          uint32_t u[KC];
+          tmem_load<KC>(s_at + key0, u);
           const unsigned long long present = sy->present[n % kSlots];
-          const bool masked = present != ~0ull || row0 + KB > seq.prefix;
-          unsigned long long seen = ~0ull;
-          if (masked) {
+          if (present != ~0ull || row0 + KB > seq.prefix) {
             // the draft's token j is the block's key j - j0
             const long long j0 = row0 - seq.prefix;
-            seen = present & (j0 <= -64 ? ~0ull
-                              : j0 < 0  ? mask << -j0 | ((1ull << -j0) - 1)
-                              : j0 < 64 ? mask >> j0
-                                        : 0ull);
+            const unsigned long long seen =
+                (present & (j0 <= -64 ? ~0ull
+                            : j0 < 0  ? mask << -j0 | ((1ull << -j0) - 1)
+                            : j0 < 64 ? mask >> j0
+                                      : 0ull)) >> key0;
+#pragma unroll
+            for (int i = 0; i < KC; ++i)
+              if (!(seen >> i & 1)) u[i] = 0xff800000u;  // -infinity
           }
-          // 32 scores of the row (read twice: a thread has no room for 64 beside the rest)
-          uint32_t u[32];
-          auto load_scores = [&](int half) {
-            tmem_ld32(s_at + 32 * half, u);
-            tmem_wait_ld();
-            if (masked) {
-              const uint32_t on = (uint32_t)(seen >> (32 * half));
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (!(on >> i & 1)) u[i] = 0xff800000u;  // -infinity
-            }
-          };
-          float mb = -INFINITY;
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            load_scores(half);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) mb = fmaxf(mb, __uint_as_float(u[i]));
+          float rs = row_scale, a = 1.f, a_o = 1.f;
+          bool grow = false;
+          if constexpr (kCodes) {
+            rs *= pow2(sy->top[0][n % kSlots] - 127);
+            const int top = sy->top[1][n % kSlots];
+            grow = begun && top != v_top;
+            if (grow) a_o = fast_exp2((float)(v_top - top));
+            v_top = top;
           }
-          mb *= p.scale2;  // (>= 0)
-          float a = 1.f;
-          const bool grow = mb > m + kSlack;
-          if (grow) {
-            a = fast_exp2(m - mb);
-            m = mb;
+          float mb = __uint_as_float(u[0]);
+#pragma unroll
+          for (int i = 1; i < KC; ++i) mb = fmaxf(mb, __uint_as_float(u[i]));
+          mb *= rs;  // (> 0)
+          if (mb > m + kLow + kSlack) {
+            a = fast_exp2(m - (mb - kLow));
+            m = mb - kLow;
             l *= a;
+            a_o *= a;
+            grow = true;
           }
           if (__any_sync(kAll, grow) && begun) {
             // O of the blocks before, once they are in it
@@ -608,101 +770,178 @@ __global__ void __launch_bounds__(kThreads, 2)
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
               uint32_t o[32];
-              tmem_ld32(lanes + kOCol + c, o);
-              tmem_wait_ld();
+              tmem_load<32>(lanes + kOCol + c, o);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * a);
-              tmem_st32(lanes + kOCol + c, o);
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * a_o);
+              tmem_store<32>(lanes + kOCol + c, o);
             }
           }
           // scores of -infinity alone leave no finite maximum; the fused multiply-add, which
           // leaves out the score's rounding, must not meet a maximum whose own rounding counts
           const float sub = m == -INFINITY ? 0.f : m;
-          const bool rounded = fabsf(sub) >= 65536.f;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          uint32_t pr[KC / 2];
+          if (!__any_sync(kAll, fabsf(sub) >= 65536.f)) {
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {  // (P lies over scores that have been read)
-            load_scores(half);
-            uint32_t pr[16];
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              float e[2];
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const float sc = __uint_as_float(u[i + k]);
-                const float y = rounded ? sc * p.scale2 - sub : fmaf(sc, p.scale2, -sub);
-                e[k] = fast_exp2(y);
-                sum[(i / 2) & 3] += e[k];
-              }
-              pr[i / 2] = pack_bf16x2(e[0], e[1]);
+            for (int i = 0; i < KC; i += 2) {
+              float2 y = __ffma2_rn(make_float2(__uint_as_float(u[i]), __uint_as_float(u[i + 1])),
+                                    make_float2(rs, rs), make_float2(-sub, -sub));
+              y.x = fast_exp2(y.x);
+              y.y = fast_exp2(y.y);
+              sum[i / 2 & 1] = __fadd2_rn(sum[i / 2 & 1], y);
+              pr[i / 2] = pack16<kCodes>(y.x, y.y);
             }
-            tmem_st16(s_at + 16 * half, pr);
+          } else {
+#pragma unroll
+            for (int i = 0; i < KC; i += 2) {
+              const float2 y = make_float2(fast_exp2(__uint_as_float(u[i]) * rs - sub),
+                                           fast_exp2(__uint_as_float(u[i + 1]) * rs - sub));
+              sum[i / 2 & 1] = __fadd2_rn(sum[i / 2 & 1], y);
+              pr[i / 2] = pack16<kCodes>(y.x, y.y);
+            }
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+          // the copy's own keys; the other copies' have no weight here
+#pragma unroll
+          for (int k = 0; k < C; ++k) {
+            uint32_t of[KC / 2];
+#pragma unroll
+            for (int i = 0; i < KC / 2; ++i) of[i] = C == 1 || k == copy ? pr[i] : 0u;
+            tmem_store<KC / 2>(s_at + k * (KC / 2), of);
+          }
           tmem_wait_st();
           tc_fence_before();
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sy->p_full[n & 1]);
       }
-      if (!ok || !(ok = wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2))) break;
-      if (!warp_live) continue;
-      tc_fence_after();
-      const bool whole = here && ends;
-      const long long slot = ((2LL * run + (here ? 1 : 0)) * p.tiles + tile) * p.tile_rows + r;
-      const long long at = (long long)(seq.first + tok) * p.Hq + w.h * p.G + row % p.G;
-      const float inv = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;  // 0: no row counts
-#pragma unroll 1
-      for (int c = 0; c < D; c += 32) {
-        __syncwarp();
-        uint32_t o[32];
-        tmem_ld32(lanes + kOCol + c, o);
-        tmem_wait_ld();
-        if (!live) continue;
-        if (bad != 0) {
-          for (unsigned long long left = bad; left != 0; left &= left - 1) {
-            const long long at_row = seq.prefix + __ffsll(left) - 1;
-            const int page = p.table[guard((long long)w.b * p.g.max_pages + (at_row >> p.g.shift), 1,
-                                           (long long)p.g.B * p.g.max_pages, p.status)];
-            const int v_slot = (int)(at_row & ((1 << p.g.shift) - 1));
-            const __nv_bfloat16 *v = (const __nv_bfloat16 *)p.v_pages + page * p.g.page_stride +
-                                     w.h * p.g.head_stride + v_slot * p.g.row_stride + c;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float x = kCodes ? __int_as_float(0x7fffffff) : __bfloat162float(v[i]);
-              if (!(fabsf(x) < INFINITY)) o[i] = __float_as_uint(__uint_as_float(o[i]) + x);
-            }
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 32; i += 8) {
-          float y[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[i + k]) * inv;
-          if (whole) {
-            *reinterpret_cast<uint4 *>((__nv_bfloat16 *)p.out + at * D + c + i) =
-                make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]),
-                           pack_bf16x2(y[6], y[7]));
-          } else {
-            put4(p.ws_o + slot * D + c + i, make_float4(y[0], y[1], y[2], y[3]));
-            put4(p.ws_o + slot * D + c + i + 4, make_float4(y[4], y[5], y[6], y[7]));
+      if (!ok) break;
+      // the next part's queries: its first scores are computed while this one's outputs are written
+      {
+        W next = w;
+        have_queries = false;
+        if (next.next(p)) {
+          const TreeSeq next_seq(p, next.b);
+          if (next_seq.tokens * p.G - tile * RT > 0 && next.count > 0) {
+            row_scale = fetch_queries(next, next_seq);
+            have_queries = true;
           }
         }
       }
-      if (live) {
+      if (!(ok = wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2))) break;
+      unsigned long long bad = 0;
+      if (w.end > seq.prefix) {
+        if (!(ok = wait_for(&sy->draft_done[drafts % kSlots], drafts / kSlots))) break;
+        bad = sy->bad[drafts++ % kSlots];
+      }
+      tc_fence_after();
+      const float o_scale = kCodes ? pow2(v_top - 127) : 1.f;
+      const long long slot = ((2LL * run + (here ? 1 : 0)) * p.tiles + tile) * p.tile_rows;
+      // four outputs of query row i: the output, or the partial
+      auto put = [&](int i, int d, const float4 &x) {
+        if (whole)
+          put4((__nv_bfloat16 *)p.out + out_row(i) * D + d, x);
+        else
+          put4(p.ws_o + (slot + i) * D + d, x);
+      };
+      auto put_stats = [&](int i, float m, float l) {
         if (!whole)
-          p.ws_ml[slot] = make_float2(m, l);
+          p.ws_ml[slot + i] = make_float2(m, l);
         else if (p.lse != nullptr)
-          p.lse[at] = tree_lse(m, l);
+          p.lse[out_row(i)] = tree_lse(m, l);
+      };
+      auto inverse = [&](float l) {  // 0: no row counts
+        return l != l ? l : !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;
+      };
+      if constexpr (C == 1) {
+        if (warp_live) {
+          const float inv = inverse(l) * o_scale;
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            __syncwarp();
+            uint32_t u[32];
+            tmem_load<32>(lanes + kOCol + c, u);
+            if (!live) continue;
+            float o[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(u[i]) * inv;
+            if ((bad & mask) != 0) add_bad(bad & mask, c, o, 32);
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) put(r, c + i, make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
+          }
+          if (live) put_stats(r, m, l);
+        }
+      } else {
+        // the copies, in the last block's values' stage: their statistics, then a quarter of the
+        // dims at a time, a row of the products each thread's, 16 bytes at places by the row's
+        // low bits
+        uint8_t *const stage = tiles + S::V0 + (n - 1) % ST * S::TILE;
+        constexpr int CD = D / 4, CP = CD / 4;
+        float2 *const stats = (float2 *)stage;
+        stats[tid] = make_float2(m, l);
+        named_bar_sync(1 + team, 128);
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < C; ++k) top = fmaxf(top, stats[k * RT + r].x);
+        const float sub = top == -INFINITY ? 0.f : top;
+        float den = 0.f;
+#pragma unroll
+        for (int k = 0; k < C; ++k) den += fast_exp2(stats[k * RT + r].x - sub) * stats[k * RT + r].y;
+        const float f = fast_exp2(m - sub) * o_scale;
+        if (copy == 0) {
+          sy->inv[r] = inverse(den);
+          if (live) put_stats(r, top, den);
+        }
+        named_bar_sync(1 + team, 128);
+#pragma unroll 1
+        for (int c = 0; c < D; c += CD) {
+          uint32_t u[CD];
+          tmem_load<CD>(lanes + kOCol + c, u);
+#pragma unroll
+          for (int i = 0; i < CP; ++i)
+            *reinterpret_cast<float4 *>(stage + tid * CD * 4 + ((i ^ (tid & (CP - 1))) << 4)) =
+                make_float4(__uint_as_float(u[4 * i]) * f, __uint_as_float(u[4 * i + 1]) * f,
+                            __uint_as_float(u[4 * i + 2]) * f, __uint_as_float(u[4 * i + 3]) * f);
+          named_bar_sync(1 + team, 128);
+          for (int e = tid; e < n_rows * CP; e += 128) {
+            const int i = e / CP, pc = e % CP;
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+              const int row = k * RT + i;
+              const float4 y =
+                  *reinterpret_cast<const float4 *>(stage + row * CD * 4 + ((pc ^ (row & (CP - 1))) << 4));
+              x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+            }
+            const float inv = sy->inv[i];
+            float o[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
+            // A value before the draft that is not finite makes a NaN of the copies that do not
+            // have its key (0 times it): then the outputs are the sum of what is not finite
+            // (if the probabilities are numbers)
+            if (!kCodes && inv == inv && !((x.x + x.y) + (x.z + x.w) == (x.x + x.y) + (x.z + x.w)))
+              add_not_finite(c + 4 * pc, o);
+            if (bad != 0) {
+              const int tok = token_of(i);
+              const unsigned long long sees =
+                  p.masks == nullptr ? ~0ull >> (63 - tok) : p.masks[seq.first + tok];
+              if ((bad & sees) != 0) add_bad(bad & sees, c + 4 * pc, o, 4);
+            }
+            put(i, c + 4 * pc, make_float4(o[0], o[1], o[2], o[3]));
+          }
+          named_bar_sync(1 + team, 128);
+        }
+        fence_proxy_async_smem();  // (the stage is written by TMA next)
+        named_bar_sync(1 + team, 128);
+        if (tid == 0) mbar_arrive(&sy->v_empty[(n - 1) % ST]);
       }
       tc_fence_before();  // O is read before the next group's first block is said to be ready
     }
-    if (tile == 0 && tid == 0) p.rec[run] = ok ? rec : make_int2(0, 0);
+    if (tile == 0 && tid == 0 && run < p.n_runs) p.rec[run] = ok ? rec : make_int2(0, 0);
     tc_fence_before();
   }
   __syncthreads();
   tc_fence_after();
-  if (warp == 4) tmem_dealloc(tmem, kTmemCols);
+  if (cta_warp == 8) tmem_dealloc(syncs->tmem, kTeams * kTeamCols);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
@@ -748,8 +987,8 @@ bool encode(CUtensorMap *map, const PagedGeom &g, const void *pool, bool codes) 
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool kCodes>
-cudaError_t launch(TreeParams p, int dev, cudaStream_t st) {
+template <int D, bool kCodes, int C>
+cudaError_t launch(TreeParams p, int dev, int sms, cudaStream_t st) {
   static std::atomic<bool> attr_set[kMaxDevices];
   constexpr int smem = Smem<D, kCodes>::BYTES;
   Maps maps;
@@ -759,12 +998,12 @@ cudaError_t launch(TreeParams p, int dev, cudaStream_t st) {
   p.suspend_ns = (uint32_t)std::min<long long>(p.wait_cycles / 4, 1000000);
   if (!attr_set[dev].load(std::memory_order_acquire)) {
     const cudaError_t e = cudaFuncSetAttribute(
-        tree_tc_kernel<D, kCodes>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        tree_tc_kernel<D, kCodes, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     attr_set[dev].store(true, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.n_runs * p.tiles);
+  cfg.gridDim = dim3(std::min(p.n_runs * p.tiles, std::max(sms, (p.n_runs * p.tiles + kTeams - 1) / kTeams)));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -773,16 +1012,27 @@ cudaError_t launch(TreeParams p, int dev, cudaStream_t st) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, tree_tc_kernel<D, kCodes>, p, maps);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, tree_tc_kernel<D, kCodes, C>, p, maps);
   count_launches(1);
   return e;
 }
 
+template <int D, bool kCodes>
+cudaError_t launch_copies(const TreeParams &p, int dev, int sms, cudaStream_t st) {
+  const int rows = p.max_tokens * p.G;
+  if (rows <= kRows / 4) return launch<D, kCodes, 4>(p, dev, sms, st);
+  if (rows <= kRows / 2) return launch<D, kCodes, 2>(p, dev, sms, st);
+  return launch<D, kCodes, 1>(p, dev, sms, st);
+}
+
 }  // namespace
 
-cudaError_t launch_tree_tc(const TreeParams &p, bool codes, int dev, cudaStream_t st) {
-  if (codes) return p.g.D == 128 ? launch<128, true>(p, dev, st) : launch<64, true>(p, dev, st);
-  return p.g.D == 128 ? launch<128, false>(p, dev, st) : launch<64, false>(p, dev, st);
+cudaError_t launch_tree_tc(const TreeParams &p, bool codes, int dev, int sms, cudaStream_t st) {
+  if (codes)
+    return p.g.D == 128 ? launch_copies<128, true>(p, dev, sms, st)
+                        : launch_copies<64, true>(p, dev, sms, st);
+  return p.g.D == 128 ? launch_copies<128, false>(p, dev, sms, st)
+                      : launch_copies<64, false>(p, dev, sms, st);
 }
 
 }  // namespace ripple
