@@ -9,6 +9,9 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <memory>
+#include <vector>
+
 #include "ripple.h"
 
 namespace {
@@ -320,6 +323,88 @@ PyObject *paged_tree_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+struct KeepLayers {
+  ripple_paged_desc desc;
+  std::vector<ripple_paged_scales> scales;  // of 8-bit pages
+  std::vector<void *> k, v;
+  std::vector<const int32_t *> tables;
+  int device;
+};
+
+// keep_tables(list of caches' handles): a handle of all of them
+PyObject *keep_tables(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!args_are(n, 1)) return nullptr;
+  PyObject *o = nullptr;
+  try {
+    need(PyList_Check(a[0]) && PyList_GET_SIZE(a[0]) >= 1, "expected a list of caches");
+    auto kept = std::make_unique<KeepLayers>();
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[0]); ++i) {
+      const Cache &c = cache_of(PyList_GET_ITEM(a[0], i));
+      if (i == 0) {
+        kept->desc = c.desc;
+        kept->device = c.device;
+      }
+      kept->k.push_back(c.k);
+      kept->v.push_back(c.v);
+      kept->tables.push_back(c.table);
+      if (c.codes() != nullptr) kept->scales.push_back(c.scales);
+    }
+    need(kept->scales.empty() || kept->scales.size() == kept->k.size(), "caches of one kind");
+    o = PyCapsule_New(kept.get(), "ripple_keep_tables", [](PyObject *self) {
+      delete static_cast<KeepLayers *>(PyCapsule_GetPointer(self, "ripple_keep_tables"));
+    });
+    if (o != nullptr) kept.release();
+  } catch (const Refused &r) {
+    if (r.why != nullptr) PyErr_SetString(PyExc_ValueError, r.why);
+  } catch (const std::exception &e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+  }
+  return o;
+}
+
+// paged_keep_rows(entry, tables, lens, kept, tokens per sequence or None, seq_starts, lens_out,
+// dev_status, stream)
+PyObject *paged_keep_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!args_are(n, 9)) return nullptr;
+  return guarded([&] {
+    auto *call = entry<decltype(ripple_paged_keep_rows)>(a[0]);
+    const auto *t = static_cast<const KeepLayers *>(PyCapsule_GetPointer(a[1], "ripple_keep_tables"));
+    if (t == nullptr) throw Refused{nullptr};
+    need(c10::cuda::current_device() == t->device, kDevice);
+    const int64_t L = (int64_t)t->k.size(), B = t->desc.batch;
+    const char *const lens_are = "lens and lens_out must be int32 [L][B]";
+    int32_t *lens[2];
+    for (int i = 0; i < 2; ++i) {
+      const at::Tensor &x = tensor(a[i == 0 ? 2 : 6]);
+      need(x.dim() == 2 && x.size(0) == L && x.size(1) == B, lens_are);
+      lens[i] = dense<int32_t>(a[i == 0 ? 2 : 6], t->device, at::kInt, lens_are);
+    }
+    const at::Tensor &kept = tensor(a[3]);
+    need(kept.dim() == 2 && kept.size(0) == B, "kept must be int32 [B][m]");
+    const int32_t *entries = dense<int32_t>(a[3], t->device, at::kInt, "kept must be int32 [B][m]");
+    const int64_t most = kept.size(1);
+    need(most <= 0x7fffffff, "too many kept tokens");
+    need((a[4] == Py_None) != (a[5] == Py_None), "n_tokens or seq_starts");
+    int64_t tokens = 0;
+    if (a[4] != Py_None) {
+      tokens = PyLong_AsLongLong(a[4]);
+      if (PyErr_Occurred()) throw Refused{nullptr};
+      need(tokens >= 0 && tokens <= 0x7fffffff / B, "bad number of drafted tokens");
+      tokens *= B;
+    }
+    const int32_t *starts = dense<int32_t>(a[5], t->device, at::kInt, "seq_starts must be int32 [B + 1]", B + 1);
+    int32_t *status = dense<int32_t>(a[7], t->device, at::kInt, "dev_status must be int32");
+    void *stream = stream_of(a[8]);
+    ripple_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = call(&t->desc, t->scales.empty() ? nullptr : t->scales.data(), (int32_t)L, t->k.data(),
+             t->v.data(), t->tables.data(), (int32_t)tokens, starts, (int32_t)most,
+             most > 0 ? entries : nullptr, lens[0], lens[1], status, stream);
+    Py_END_ALLOW_THREADS
+    return (long)s;
+  });
+}
+
 // token_logprobs(entry, logits, tokens, logprob_out, entropy_out, lse_out, top_idx, top_logprob,
 // scale, dev_status, stream)
 PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -375,6 +460,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
   {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {RIPPLE_METHOD(cache), RIPPLE_METHOD(paged_append),
                           RIPPLE_METHOD(paged_decode_attn), RIPPLE_METHOD(paged_tree_attn),
+                          RIPPLE_METHOD(keep_tables), RIPPLE_METHOD(paged_keep_rows),
                           RIPPLE_METHOD(token_logprobs),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods,

@@ -155,7 +155,7 @@ __device__ __forceinline__ int find_seq(const int32_t *starts, int B, int t, int
 
 // kAhead: groups whose loads are in flight at a time. kCodes: 8-bit pages.
 template <typename T, int D, bool kInter, int kAhead, bool kCodes>
-__global__ void __launch_bounds__(kAppendWarps * 32)
+__global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 6 : 1)
     append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int kLanes = D / 16;       // lanes per head row
   constexpr int kRows = 32 / kLanes;   // head rows per warp step

@@ -436,6 +436,7 @@ _paged_append = (_address(_lib.ripple_paged_append), _address(_lib.ripple_paged_
 _paged_decode_attn = (_address(_lib.ripple_paged_decode_attn),
                       _address(_lib.ripple_paged_decode_attn_q8))
 _paged_tree_attn = _address(_lib.ripple_paged_tree_attn)
+_paged_keep_rows = _address(_lib.ripple_paged_keep_rows)
 _token_logprobs = _address(_lib.ripple_token_logprobs)
 
 MAX_DRAFT = 64
@@ -579,9 +580,7 @@ class KeepTables:
                for c in caches):
             raise ValueError("the layers' caches must be of one shape, dtype and device")
         self.desc, self.device = c0.desc, c0.device
-        self.k, self.v, self.table = ((_p * L)(*[c._keep[i].data_ptr() for c in caches])
-                                      for i in range(3))
-        self.scales = (PagedScales * L)(*[c.scales for c in caches]) if c0.codes else None
+        self._handle = _binding.keep_tables([c._handle for c in caches])
         self._keep = caches
 
 
@@ -592,28 +591,11 @@ def ripple_paged_keep_rows(tables: KeepTables, lens, kept, n_tokens: int | None 
     tokens of its draft, ascending, ended by a negative entry; n_tokens: drafted tokens of every
     sequence, or seq_starts (int32 [B + 1]). lens_out (int32 [L][B], default: lens) gets the new
     lengths."""
-    lens_out = lens if lens_out is None else lens_out
-    L, B = tables.n_layers, tables.desc.batch
-    for t, shape in ((lens, (L, B)), (lens_out, (L, B)), (kept, (B, kept.shape[-1])),
-                     (seq_starts, (B + 1,))):
-        if t is None:
-            continue
-        if t.dtype is not torch.int32 or tuple(t.shape) != shape:
-            raise ValueError("lens and lens_out must be int32 [L][B], kept int32 [B][m], "
-                             "seq_starts int32 [B + 1]")
-        if t.get_device() != tables.device:
-            raise ValueError("expected CUDA tensors on one device, the current one")
-    if torch.cuda.current_device() != tables.device:
-        raise ValueError("expected CUDA tensors on one device, the current one")
-    if (n_tokens is None) == (seq_starts is None):
-        raise ValueError("n_tokens or seq_starts")
-    m = kept.shape[1]
-    _check(_lib.ripple_paged_keep_rows(ctypes.byref(tables.desc), tables.scales, L, tables.k,
-                                       tables.v, tables.table,
-                                       0 if n_tokens is None else int(n_tokens) * B,
-                                       _ptr(seq_starts), m, _ptr(kept) if m else None, _ptr(lens),
-                                       _ptr(lens_out), _ptr(dev_status), _stream(stream)),
-           "ripple_paged_keep_rows")
+    st = _binding.paged_keep_rows(_paged_keep_rows, tables._handle, lens, kept, n_tokens, seq_starts,
+                                  lens if lens_out is None else lens_out, dev_status,
+                                  None if stream is None else _stream(stream))
+    if st != OK:
+        raise RippleError(st, "ripple_paged_keep_rows")
 
 
 def ripple_token_logprobs(logits, tokens=None, logprob_out=None, entropy_out=None, lse_out=None,
