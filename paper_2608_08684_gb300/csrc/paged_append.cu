@@ -178,11 +178,10 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 
   // The rows of kAhead groups from g on, as they are.
   const int g_end = min(p.groups, (part + 1) * p.per_warp);
   Raw8<T> x[kAhead], y[kAhead];
-  auto load = [&](int g, int b, int i) {
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
+  auto load_one = [&](int g, int u, int b, int i) {
+    {
       const int r = (g + u) * kRows + sub;
-      if (g + u >= g_end || r >= n_rows) continue;
+      if (g + u >= g_end || r >= n_rows) return;
       const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.g.Hkv;
       const TokenRows &src = is_q ? p.q : is_v ? p.v : p.k;
       const int h = is_q ? r : is_v ? r - p.Hq - p.g.Hkv : r - p.Hq;
@@ -190,6 +189,10 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 
       x[u] = load_raw(from + o0);
       y[u] = load_raw(from + o1);
     }
+  };
+  auto load = [&](int g, int b, int i) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) load_one(g, u, b, i);
   };
   // where a token lies does not depend on its sequence with seq_starts (strides by t alone)
   const int src_b = b, src_i = i;
@@ -253,13 +256,13 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 
     }
   }
 
-  for (;;) {
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
+  // What becomes of group g + u.
+  auto finish = [&](int u) {
+    {
       const int r = (g + u) * kRows + sub;
-      if (g + u >= g_end || r >= n_rows) continue;
+      if (g + u >= g_end || r >= n_rows) return;
       const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.g.Hkv;
-      if (!is_q && place < 0) continue;
+      if (!is_q && place < 0) return;
       const int h = is_q ? r : is_v ? r - p.Hq - p.g.Hkv : r - p.Hq;
       float a[8], d[8];
       const bool turned = turns && !is_v;
@@ -299,7 +302,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 
         *reinterpret_cast<uint2 *>(to + o0) = codes_of(a, byte);
         *reinterpret_cast<uint2 *>(to + o1) = codes_of(d, byte);
         if (l == 0) (is_v ? p.sc.v : p.sc.k)[scale_at + h * p.sc.head_stride] = (uint8_t)byte;
-        continue;
+        return;
       }
       T *to = is_q ? (T *)p.q_out.data + src_b * p.q_out.seq + src_i * p.q_out.token +
                          h * p.q_out.head
@@ -311,9 +314,17 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 
       store_raw(to + o0, x[u]);
       store_raw(to + o1, y[u]);
     }
+  };
+  for (;;) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      finish(u);
+      // (the codes take longer to make: the other groups' rows are on their way meanwhile)
+      if (kCodes) load_one(g + kAhead, u, src_b, src_i);
+    }
     g += kAhead;
     if (g >= g_end) break;
-    load(g, src_b, src_i);
+    if (!kCodes) load(g, src_b, src_i);
   }
 }
 

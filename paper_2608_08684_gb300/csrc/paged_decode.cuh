@@ -117,6 +117,9 @@ struct Cfg {
   static constexpr int PIECES = ROW_BYTES / 16;
   static constexpr int BLOCK = sizeof(T) == 1 ? 32 * ROW_BYTES : 4096;  // bytes of K (and of V)
   static constexpr int RB = BLOCK / ROW_BYTES;  // rows of a block: 8, 16 or 32
+  // Units that a group has besides its blocks (they begin it): its queries and outputs, which
+  // count beside the short time that a block of 8-bit rows takes.
+  static constexpr int COST = sizeof(T) == 1 ? 2 : 0;
   // fp32: lanes per row (a lane's queries and outputs stay at 64 registers each), rows per
   // warp step and steps of a block
   static constexpr int S0 = G * D / 64 > G ? G * D / 64 : G;
@@ -140,7 +143,7 @@ __device__ __forceinline__ int clamp_len(const PagedDecParams &p, int b) {
   const int n = p.lens[b];
   return n <= 0 ? 0 : (int)(n < room ? n : room);
 }
-// Where the runs of `total` blocks begin.
+// Where the runs of `total` units (blocks, and what a group costs besides) begin.
 struct Runs {
   long long total;
   int places, phases;
@@ -168,34 +171,45 @@ struct Runs {
   }
 };
 
-// A walk over the parts of groups in a warp's run. RB: rows of a block.
-template <int RB>
+// A walk over the parts of groups in a warp's run. RB: rows of a block; COST: units of a group
+// besides its blocks.
+template <int RB, int COST>
 struct Walk {
   int b, h, len;
   int block;           // the part's first in its group
   int begin, end;      // the part's rows
-  long long left;      // blocks of the run, the part's included
+  long long left;      // units of the run, the part's included
+  int cost;            // units of the part before its blocks
   static __device__ __forceinline__ int blocks_of(int len) { return len / RB + (len % RB != 0); }
+  static __device__ __forceinline__ long long units_of(int len) {
+    return len > 0 ? blocks_of(len) + COST : 0;
+  }
   __device__ __forceinline__ int blocks() const { return blocks_of(len); }
+  // Blocks of the part: none where the run ends with what begins the group.
   __device__ __forceinline__ int count() const {
-    return (int)min((long long)(blocks() - block), left);
+    return (int)min((long long)(blocks() - block), COST > 0 ? max(left - cost, 0LL) : left);
   }
   __device__ __forceinline__ void set() {
     begin = block * RB;
     end = (int)min((long long)len, (long long)(block + count()) * RB);
   }
+  // The group's first part from its unit `in` on.
+  __device__ __forceinline__ void enter(int in) {
+    block = max(0, in - COST);
+    cost = max(0, COST - in);
+    set();
+  }
   // To the next part; false at the end of the run.
   __device__ __forceinline__ bool next(const PagedDecParams &p) {
-    left -= count();
+    left -= count() + cost;
     if (left <= 0) return false;
-    block = 0;
     if (++h >= p.g.Hkv) {
       h = 0;
       do len = clamp_len(p, ++b);
       while (len == 0);  // left > 0: there are more
     }
-    set();
-    return true;
+    enter(0);
+    return COST == 0 || count() > 0;
   }
 };
 
@@ -232,7 +246,7 @@ struct Stage<Codes8<Q>, D, G> {
 template <typename T, int D, int G>
 struct Fetch {
   using C = Cfg<T, D, G>;
-  Walk<C::RB> w;
+  Walk<C::RB, C::COST> w;
   int at;      // the next block's first row
   bool live;   // there is a next block
   int entry;   // block-table entry of the block, or of row at + lane % RB where it has several
@@ -363,7 +377,7 @@ struct Rows {
   float2 acc[NB][H];
   float m[H], l[H];
 
-  __device__ __forceinline__ void start(const PagedDecParams &p, const Walk<C::RB> &w, int lane) {
+  __device__ __forceinline__ void start(const PagedDecParams &p, const Walk<C::RB, C::COST> &w, int lane) {
     const int g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int i = 0; i < H; ++i) {
@@ -561,7 +575,7 @@ struct Rows<float, D, G> {
   float2 acc[G][2 * PPL];
   float m[1], l[1];                 // of head hq over this row group's rows
 
-  __device__ __forceinline__ void start(const PagedDecParams &p, const Walk<C::RB> &w, int lane) {
+  __device__ __forceinline__ void start(const PagedDecParams &p, const Walk<C::RB, C::COST> &w, int lane) {
     const int sl = lane % S, hq = sl / HL;
 #pragma unroll
     for (int j = 0; j < G; ++j) {
@@ -706,7 +720,7 @@ template <typename T, int D, int G>
 __global__ void __launch_bounds__(32, kWarpsPerSm)
     paged_decode_kernel(const __grid_constant__ PagedDecParams p) {
   using C = Cfg<T, D, G>;
-  using W = Walk<C::RB>;
+  using W = Walk<C::RB, C::COST>;
   __shared__ __align__(128) Stage<T, D, G> ring[kStages];
   const int lane = threadIdx.x, run = blockIdx.x;
   pdl_wait();
@@ -716,7 +730,7 @@ __global__ void __launch_bounds__(32, kWarpsPerSm)
   const int b0 = min(lane * per, p.g.B), b1 = min(b0 + per, p.g.B);
   long long mine = 0;
   for (int b = b0; b < b1; ++b) {
-    mine += (long long)W::blocks_of(clamp_len(p, b)) * p.g.Hkv;
+    mine += W::units_of(clamp_len(p, b)) * p.g.Hkv;
     if (run == 0 && (long long)p.lens[b] > (long long)p.g.max_pages << p.g.shift)
       report(p.status, RIPPLE_EFULL);
   }
@@ -738,7 +752,7 @@ __global__ void __launch_bounds__(32, kWarpsPerSm)
   long long rest = t0 - (incl - mine);
   if (lane == owner) {
     for (seq = b0;; ++seq) {
-      const long long k = (long long)W::blocks_of(clamp_len(p, seq)) * p.g.Hkv;
+      const long long k = W::units_of(clamp_len(p, seq)) * p.g.Hkv;
       if (rest < k) break;
       rest -= k;
     }
@@ -750,11 +764,15 @@ __global__ void __launch_bounds__(32, kWarpsPerSm)
   w.b = __shfl_sync(kAll, seq, owner);
   rest = __shfl_sync(kAll, rest, owner);
   w.len = clamp_len(p, w.b);
-  w.h = (int)(rest / w.blocks());
-  w.block = (int)(rest % w.blocks());
+  const int units = w.blocks() + C::COST, in = (int)(rest % units);
+  w.h = (int)(rest / units);
   w.left = runs.start(run + 1) - t0;
-  w.set();
-  fetch.live = true;
+  w.enter(in);
+  fetch.live = C::COST == 0 || w.count() > 0;
+  if (!fetch.live) {  // the run ends with what begins a group
+    if (lane == 0) p.rec[rec_at] = make_int2(0, 0);
+    return;
+  }
   fetch.at = w.begin;
   fetch.look_up(p, lane);
   W at = fetch.w;
@@ -767,7 +785,7 @@ __global__ void __launch_bounds__(32, kWarpsPerSm)
   const long long n_rows = (long long)p.g.B * p.Hq;
   int2 rec = make_int2(0, 0);
   int stage = 0;
-  long long t = t0;  // the part's first block
+  long long t = t0 + at.cost;  // the unit of the part's first block
   for (bool more = true; more;) {
     Rows<T, D, G> rows;
     rows.start(p, at, lane);
@@ -807,6 +825,7 @@ __global__ void __launch_bounds__(32, kWarpsPerSm)
     }
     t += at.count();
     more = at.next(p);
+    t += at.cost;
   }
   copy_wait<0>();
   if (lane == 0) p.rec[rec_at] = rec;
@@ -878,7 +897,7 @@ template <typename T, int D, int G>
 __global__ void __launch_bounds__(kShortThreads)
     paged_short_kernel(const __grid_constant__ PagedDecParams p) {
   using C = Cfg<T, D, G>;
-  using W = Walk<C::RB>;
+  using W = Walk<C::RB, C::COST>;
   extern __shared__ __align__(128) uint8_t smem_raw[];
   ShortSmem<T, D, G> &s = *reinterpret_cast<ShortSmem<T, D, G> *>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -902,6 +921,7 @@ __global__ void __launch_bounds__(kShortThreads)
     fetch.w.len = len;
     fetch.w.block = first;
     fetch.w.left = last - first;
+    fetch.w.cost = 0;
     fetch.w.set();
     fetch.live = true;
     fetch.at = fetch.w.begin;

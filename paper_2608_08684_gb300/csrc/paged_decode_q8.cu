@@ -88,7 +88,7 @@ struct Rows<Codes8<Q>, D, G> {
   int ew[NT][2];    // the outputs' reference is m + ew
   float acc[PC][NT][4];
 
-  __device__ __forceinline__ void start(const PagedDecParams &p, const Walk<C::RB> &w, int lane) {
+  __device__ __forceinline__ void start(const PagedDecParams &p, const Walk<C::RB, C::COST> &w, int lane) {
     const int g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {

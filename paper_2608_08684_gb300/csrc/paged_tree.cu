@@ -172,9 +172,10 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
       __syncthreads();
       const uint32_t present = row_there;
       if (row0 + KB < w.end) load(row0 + KB);
-      // scores
+      // scores (warps of rows that are none have nothing to do)
+      const bool busy = rg - rg % 8 < n_rows;
       float x[4][2];
-      {
+      if (busy) {
         float2 d[4][2];
 #pragma unroll
         for (int i = 0; i < 4; ++i) d[i][0] = d[i][1] = make_float2(0.f, 0.f);
@@ -201,6 +202,7 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
       // the 16 threads of a row are half a warp
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
+        if (!busy) break;
         const int r = rg + i;
         const uint64_t mask = s.mask[r];
         bool on[2];
@@ -258,7 +260,9 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
           }
         }
       };
-      if (present != 0xffffffffu || row0 + KB > seq.prefix)
+      if (!busy)
+        continue;
+      else if (present != 0xffffffffu || row0 + KB > seq.prefix)
         add(true);
       else
         add(false);

@@ -53,7 +53,7 @@ constexpr uint32_t kOCol = 128;
 constexpr float kSlack = 8.f;
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kMaxDevices = 64;
-constexpr int kSlots = 4;  // of what the softmax is told about blocks
+constexpr int kSlots = 8;  // of what the softmax is told about blocks (fetched up to two ahead)
 
 struct Sync {
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
@@ -66,6 +66,7 @@ struct Sync {
   uint32_t tmem;
   int abort;                           // a role has given up waiting
   int top[2][kSlots];                  // 8-bit pages: the scale bytes that a block's keys, values are over
+  int v_top[kRing];                    // the same of values, by the warp that widens them
   uint8_t scale[2][kRing][KB];         // of the ring's rows
   float inv[64];                       // of a group's query rows (with copies)
 };
@@ -449,29 +450,29 @@ __global__ void __launch_bounds__(kThreads, 1)
         // scale bytes of the rows lane and lane + 32 of the block issued last (0: not there), of
         // keys and of values; they are put into the ring when the next one is issued, with the
         // largest (255 is none): the block's of keys, the run's so far of values
-        int k_byte[2], v_byte[2], byte_slot = -1, v_top = 0;
-        unsigned long long ring_present[kRing];
-        int ring_top[2][kRing];
+        int k_byte[2], v_byte[2], byte_slot = -1, byte_block = 0, v_top = 0;
         auto put_scales = [&]() {
           if (byte_slot < 0) return;
-          int top[2] = {0, 0};
+          int k_top = 0, top = 0;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             scale_ring[byte_slot][lane + 32 * i] = (uint8_t)(keys ? k_byte[i] : v_byte[i]);
-            if (keys && k_byte[i] != 255) top[0] = max(top[0], k_byte[i]);
-            if (v_byte[i] != 255) top[1] = max(top[1], v_byte[i]);
+            if (keys && k_byte[i] != 255) k_top = max(k_top, k_byte[i]);
+            if (v_byte[i] != 255) top = max(top, v_byte[i]);
           }
-          v_top = max(v_top, __reduce_max_sync(kAll, top[1]));
-          top[0] = keys ? __reduce_max_sync(kAll, top[0]) : 0;
-#pragma unroll
-          for (int k = 0; k < kRing; ++k)
-            if (k == byte_slot) {
-              ring_top[0][k] = top[0] > 0 ? top[0] : 127;
-              ring_top[1][k] = v_top > 0 ? v_top : 7;
+          v_top = max(v_top, __reduce_max_sync(kAll, top));
+          if (keys) {
+            k_top = __reduce_max_sync(kAll, k_top);
+            if (lane == 0) {
+              sy->top[0][byte_block % kSlots] = k_top > 0 ? k_top : 127;
+              sy->top[1][byte_block % kSlots] = v_top > 0 ? v_top : 7;
             }
+          } else if (lane == 0) {
+            sy->v_top[byte_slot] = v_top > 0 ? v_top : 7;
+          }
           byte_slot = -1;
         };
-        auto issue = [&](int row0, int i) {
+        auto issue = [&](int row0, int i) {  // block i of the ring, n + i - ring_n of the team
           const int slot = i % kRing;
           issued = i + 1;
           put_scales();
@@ -487,10 +488,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           byte_slot = slot;
+          byte_block = n + i - ring_n;
           if (!fetch(row0, ring + slot * S::RAW, &ring_full[slot], true)) copies_arrive(&ring_full[slot]);
-#pragma unroll
-          for (int k = 0; k < kRing; ++k)
-            if (k == slot) ring_present[k] = present;
+          if (keys && lane == 0) sy->present[byte_block % kSlots] = present;
           if (row0 + KB < w.end) look_up(row0 + KB);
         };
         issue(w.begin, ring_n);
@@ -503,20 +503,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = wait_for(&ring_full[slot], ring_n / kRing) &&
                (n < ST || wait_for(&empty[stage], n / ST - 1));
           if (!ok) break;
-          int top = 0;
-#pragma unroll
-          for (int k = 0; k < kRing; ++k)
-            if (k == slot) {
-              top = ring_top[keys ? 0 : 1][k];
-              if (keys && lane == 0) {
-                sy->present[n % kSlots] = ring_present[k];
-                sy->top[0][n % kSlots] = ring_top[0][k];
-                sy->top[1][n % kSlots] = ring_top[1][k];
-              }
-            }
+          const int top = keys ? sy->top[0][n % kSlots] : sy->v_top[slot];
           const uint32_t from = ring + slot * S::RAW, to = stages + stage * S::TILE;
           const bool draft = !keys && w.end > seq.prefix && row0 + KB > seq.prefix;
-#pragma unroll 4
+#pragma unroll 8
           for (int i = 0; i < kSteps; ++i) {
             const int row = i * kRowsWarp + sub, byte = scale_ring[slot][row];
             uint4 u = ld_shared16(from + row * D + 16 * pc);
@@ -630,14 +620,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           copy16(to + (c >> 3) * S::HALF_Q + (((c & 7) ^ (tid & 7)) << 4), q + 8 * c, live);
         copies_landed();
       } else {
-        uint4 x[D / 8];
-#pragma unroll
-        for (int c = 0; c < D / 8; ++c)
-          x[c] = live ? reinterpret_cast<const uint4 *>(q)[c] : make_uint4(0, 0, 0, 0);
+        // (read twice: there is no room for the whole row)
+        auto load = [&](int c) {
+          return live ? __ldg(reinterpret_cast<const uint4 *>(q) + c) : make_uint4(0, 0, 0, 0);
+        };
         float most = 0.f;
-#pragma unroll
+#pragma unroll 4
         for (int c = 0; c < D / 8; ++c) {
-          const uint32_t u[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+          const uint4 x = load(c);
+          const uint32_t u[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             most = fmaxf(most, fmaxf(fabsf(__uint_as_float(u[i] << 16)),
@@ -647,9 +638,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int up = most == 0.f ? 0 : min(14 - ((__float_as_int(most) >> 23) - 127), 100);
         const float f = pow2(up);
         scale *= pow2(-up);
-#pragma unroll
+#pragma unroll 4
         for (int c = 0; c < D / 8; ++c) {
-          const uint32_t u[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+          const uint4 x = load(c);
+          const uint32_t u[4] = {x.x, x.y, x.z, x.w};
           uint32_t o[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i)
