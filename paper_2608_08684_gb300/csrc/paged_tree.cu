@@ -302,7 +302,7 @@ template <typename O, int D>
 __global__ void __launch_bounds__(kJoinThreads)
     tree_join_kernel(const __grid_constant__ TreeParams p) {
   constexpr int kCols = D / 4, kRows = kJoinThreads / kCols;
-  constexpr int kAt = 4;  // partials loaded at a time
+  constexpr int kAt = 8;  // partials loaded at a time
   const int tid = threadIdx.x, col = tid % kCols, sub = tid / kCols;
   pdl_wait();
   const int run = blockIdx.x;

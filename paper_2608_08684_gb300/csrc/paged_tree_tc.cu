@@ -42,12 +42,13 @@ namespace {
 
 constexpr int KB = kTreeTcKeys;
 constexpr int kRows = kTreeTcRows;
-// Warps 0-3, 4-7: softmax of the teams; 8, 9: their MMAs; 10, 11 and 12, 13: their keys and values.
-// (A warp reaches the TMEM lanes 32 (warp % 4) on.)
+// Warps 0-3, 4-7: softmax of the teams; 8, 9: their MMAs; from 10 on: keys and values of one team,
+// then of the other, a warp each, two for 8-bit pages. (A warp reaches the TMEM lanes 32 (warp
+// % 4) on.)
 constexpr int kTeams = 2;
-constexpr int kThreads = 448;
+__host__ __device__ constexpr int threads(bool codes) { return 32 * (10 + kTeams * (codes ? 4 : 2)); }
 constexpr int kGroupCost = 4;  // blocks that a group's queries and outputs take as long as
-constexpr int kRing = 3;       // blocks of 8-bit rows on their way or being widened
+constexpr int kRing = 2;       // blocks of 8-bit rows on their way or being widened
 constexpr uint32_t kTeamCols = 256;  // of TMEM: S and P of two blocks (64 each), O (d) from 128 on
 constexpr uint32_t kOCol = 128;
 constexpr float kSlack = 8.f;
@@ -62,7 +63,7 @@ struct Sync {
   uint64_t q_full, mma_done;
   uint64_t draft_done[kSlots];         // by parts with drafted tokens (values may be parts ahead)
   unsigned long long present[kSlots];  // rows of a block that are there
-  unsigned long long bad[kSlots];      // drafted tokens whose values are not all finite, by parts
+  unsigned long long bad[2][kSlots];   // drafted tokens whose values are not all finite, by parts
   uint32_t tmem;
   int abort;                           // a role has given up waiting
   int top[2][kSlots];                  // 8-bit pages: the scale bytes that a block's keys, values are over
@@ -73,11 +74,11 @@ struct Sync {
 
 template <int D, bool kCodes>
 struct Smem {
-  static constexpr int STAGES = kCodes ? 1 : 2;  // of 16-bit blocks of keys, and of values
+  static constexpr int SK = kCodes ? 1 : 2, SV = 2;  // stages of 16-bit blocks of keys, of values
   static constexpr int Q = kRows * D * 2, TILE = KB * D * 2;
   static constexpr int RAW = KB * D;             // a block of 8-bit rows
   static constexpr int HALF_Q = kRows * 128, HALF = KB * 128;  // of 64 dims
-  static constexpr int K0 = Q, V0 = Q + STAGES * TILE, RING = V0 + STAGES * TILE;
+  static constexpr int K0 = Q, V0 = Q + SK * TILE, RING = V0 + SV * TILE;
   static constexpr int TEAM = RING + (kCodes ? 2 * kRing * RAW : 0);
   static constexpr int BYTES = kTeams * (TEAM + (int)sizeof(Sync));
   static_assert(TEAM % 1024 == 0 && BYTES <= 227 * 1024, "shared memory per CTA");
@@ -260,18 +261,22 @@ __device__ __forceinline__ float pow2(int e) {  // -126 <= e <= 127
 
 // kCodes: 8-bit pages. C: copies of the query rows.
 template <int D, bool kCodes, int C>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(threads(kCodes), 1)
     tree_tc_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ Maps maps) {
   using S = Smem<D, kCodes>;
   using W = TreeWalk<KB, kGroupCost>;
-  constexpr int ST = S::STAGES;
+  constexpr int SK = S::SK, SV = S::SV;
   constexpr int RT = kRows / C;   // query rows of the tile
   constexpr int KC = KB / C;      // keys of a block that a copy takes
   extern __shared__ __align__(1024) uint8_t smem[];
   const int lane = threadIdx.x & 31, cta_warp = threadIdx.x >> 5;
-  const int team = cta_warp < 8 ? cta_warp / 4 : cta_warp < 10 ? cta_warp - 8 : (cta_warp - 10) / 2;
+  constexpr int kFetch = kCodes ? 4 : 2;  // warps of a team that fetch
+  const int team = cta_warp < 8 ? cta_warp / 4 : cta_warp < 10 ? cta_warp - 8 : (cta_warp - 10) / kFetch;
   // 0-3: softmax, 4: MMAs, 5: keys, 6: values
-  const int warp = cta_warp < 8 ? cta_warp % 4 : cta_warp < 10 ? 4 : 5 + cta_warp % 2;
+  const int warp = cta_warp < 8    ? cta_warp % 4
+                   : cta_warp < 10 ? 4
+                                   : 5 + (cta_warp - 10) % kFetch / (kFetch / 2);
+  const bool second = kCodes && cta_warp >= 10 && (cta_warp - 10) % 2 == 1;  // of two that fetch
   const int tid = 32 * warp + lane;
   uint8_t *const tiles = smem + team * S::TEAM;
   Sync *const syncs = (Sync *)(smem + kTeams * S::TEAM), *const sy = syncs + team;
@@ -285,8 +290,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&sy->ring_full[1][i], 32);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sy->k_full[i], 32);
-      mbar_init(&sy->v_full[i], 32);
+      mbar_init(&sy->k_full[i], 16 * kFetch);
+      mbar_init(&sy->v_full[i], 16 * kFetch);
       mbar_init(&sy->k_empty[i], 1);
       mbar_init(&sy->v_empty[i], 1);
       mbar_init(&sy->s_full[i], 1);
@@ -294,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&sy->pv_done[i], 1);
     }
     mbar_init(&sy->q_full, 4);
-    for (int i = 0; i < kSlots; ++i) mbar_init(&sy->draft_done[i], 32);
+    for (int i = 0; i < kSlots; ++i) mbar_init(&sy->draft_done[i], 16 * kFetch);
     mbar_init(&sy->mma_done, 1);
     fence_mbar_init();
     fence_proxy_async_smem();
@@ -309,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = syncs->tmem + team * kTeamCols;
   if (blockIdx.x == 0)
-    for (int b = threadIdx.x; b < p.g.B; b += kThreads) TreeSeq::check(p, b);
+    for (int b = threadIdx.x; b < p.g.B; b += threads(kCodes)) TreeSeq::check(p, b);
 
   const uint32_t qs = smem_u32(tiles), ks = qs + S::K0, vs = qs + S::V0;
   W w;
@@ -323,6 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp >= 5) {
     // -------------------------------------------------- keys, values
     const bool keys = warp == 5;
+    const int ST = keys ? SK : SV;
     uint64_t *const full = keys ? sy->k_full : sy->v_full, *const empty = keys ? sy->k_empty : sy->v_empty;
     const uint32_t stages = keys ? ks : vs;
     const uint8_t *const pool = (const uint8_t *)(keys ? p.k_pages : p.v_pages);
@@ -405,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     unsigned long long bad = 0;
     auto tell_bad = [&]() {
       const uint32_t lo = __reduce_or_sync(kAll, (uint32_t)bad), hi = __reduce_or_sync(kAll, (uint32_t)(bad >> 32));
-      if (lane == 0) sy->bad[drafts % kSlots] = (unsigned long long)hi << 32 | lo;
+      if (lane == 0) sy->bad[second][drafts % kSlots] = (unsigned long long)hi << 32 | lo;
       bad = 0;
       mbar_arrive(&sy->draft_done[drafts % kSlots]);
       ++drafts;
@@ -447,35 +453,31 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint8_t(*const scale_ring)[KB] = sy->scale[keys ? 0 : 1];
         uint64_t *const ring_full = sy->ring_full[keys ? 0 : 1];
         const uint32_t ring = qs + S::RING + (keys ? 0 : kRing * S::RAW);
-        // scale bytes of the rows lane and lane + 32 of the block issued last (0: not there), of
-        // keys and of values; they are put into the ring when the next one is issued, with the
-        // largest (255 is none): the block's of keys, the run's so far of values
-        int k_byte[2], v_byte[2], byte_slot = -1, byte_block = 0, v_top = 0;
-        auto put_scales = [&]() {
-          if (byte_slot < 0) return;
-          int k_top = 0, top = 0;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            scale_ring[byte_slot][lane + 32 * i] = (uint8_t)(keys ? k_byte[i] : v_byte[i]);
-            if (keys && k_byte[i] != 255) k_top = max(k_top, k_byte[i]);
-            if (v_byte[i] != 255) top = max(top, v_byte[i]);
-          }
-          v_top = max(v_top, __reduce_max_sync(kAll, top));
-          if (keys) {
-            k_top = __reduce_max_sync(kAll, k_top);
-            if (lane == 0) {
-              sy->top[0][byte_block % kSlots] = k_top > 0 ? k_top : 127;
-              sy->top[1][byte_block % kSlots] = v_top > 0 ? v_top : 7;
-            }
-          } else if (lane == 0) {
-            sy->v_top[byte_slot] = v_top > 0 ? v_top : 7;
-          }
-          byte_slot = -1;
+        // What both warps agree on: they go on to a block, or neither does.
+        const int pair_bar = 3 + 2 * team + (keys ? 0 : 1);
+        auto both = [&](bool mine) {
+          int all;
+          asm volatile(
+              "{\n .reg .pred p, q;\n setp.ne.b32 q, %1, 0;\n"
+              " barrier.cta.red.and.pred p, %2, 64, q;\n selp.s32 %0, 1, 0, p;\n}\n"
+              : "=r"(all)
+              : "r"((int)mine), "r"(pair_bar)
+              : "memory");
+          return all != 0;
         };
-        auto issue = [&](int row0, int i) {  // block i of the ring, n + i - ring_n of the team
+        // The first warp fetches blocks into the ring, block i of it being n + i - ring_n of the team.
+        auto issue = [&](int row0, int i) {
           const int slot = i % kRing;
           issued = i + 1;
-          put_scales();
+          if (!fetch(row0, ring + slot * S::RAW, &ring_full[slot], true)) copies_arrive(&ring_full[slot]);
+          if (keys && lane == 0) sy->present[(n + i - ring_n) % kSlots] = present;
+          if (row0 + KB < w.end) look_up(row0 + KB);
+        };
+        // The second brings their scales: bytes of the rows lane and lane + 32 (0: not there), of
+        // keys and of values, loaded a block before they are put into the ring, with the largest
+        // (255 is none): the block's of keys, the run's so far of values.
+        int k_byte[2], v_byte[2], v_top = 0;
+        auto load_scales = [&](int row0) {
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const int page = entry[k], row = row0 + lane + 32 * k;
@@ -487,37 +489,72 @@ __global__ void __launch_bounds__(kThreads, 1)
               v_byte[k] = p.v_scales[at];
             }
           }
-          byte_slot = slot;
-          byte_block = n + i - ring_n;
-          if (!fetch(row0, ring + slot * S::RAW, &ring_full[slot], true)) copies_arrive(&ring_full[slot]);
-          if (keys && lane == 0) sy->present[byte_block % kSlots] = present;
           if (row0 + KB < w.end) look_up(row0 + KB);
         };
-        issue(w.begin, ring_n);
-        if (w.begin + KB < w.end) issue(w.begin + KB, ring_n + 1);
+        auto put_scales = [&](int i) {
+          int k_top = 0, top = 0;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            scale_ring[i % kRing][lane + 32 * k] = (uint8_t)(keys ? k_byte[k] : v_byte[k]);
+            if (keys && k_byte[k] != 255) k_top = max(k_top, k_byte[k]);
+            if (v_byte[k] != 255) top = max(top, v_byte[k]);
+          }
+          v_top = max(v_top, __reduce_max_sync(kAll, top));
+          if (keys) {
+            k_top = __reduce_max_sync(kAll, k_top);
+            if (lane == 0) {
+              sy->top[0][(n + i - ring_n) % kSlots] = k_top > 0 ? k_top : 127;
+              sy->top[1][(n + i - ring_n) % kSlots] = v_top > 0 ? v_top : 7;
+            }
+          } else if (lane == 0) {
+            sy->v_top[i % kRing] = v_top > 0 ? v_top : 7;
+          }
+        };
+        const bool more_than_one = w.begin + KB < w.end;
+        if (!second) {
+          issue(w.begin, ring_n);
+          if (more_than_one) issue(w.begin + KB, ring_n + 1);
+        } else {
+          load_scales(w.begin);
+          put_scales(ring_n);
+          if (more_than_one) load_scales(w.begin + KB);
+        }
         for (int row0 = w.begin; row0 < w.end; row0 += KB, ++n, ++ring_n) {
-          put_scales();
-          __syncwarp();  // (the slot that is issued to has been read, the scales are there)
-          if (row0 + 2 * KB < w.end) issue(row0 + 2 * KB, ring_n + 2);
           const int slot = ring_n % kRing, stage = n % ST;
-          ok = wait_for(&ring_full[slot], ring_n / kRing) &&
-               (n < ST || wait_for(&empty[stage], n / ST - 1));
+          ok = both(wait_for(&ring_full[slot], ring_n / kRing) &&
+                    (n < ST || wait_for(&empty[stage], n / ST - 1)));
           if (!ok) break;
           const int top = keys ? sy->top[0][n % kSlots] : sy->v_top[slot];
           const uint32_t from = ring + slot * S::RAW, to = stages + stage * S::TILE;
           const bool draft = !keys && w.end > seq.prefix && row0 + KB > seq.prefix;
-#pragma unroll 8
-          for (int i = 0; i < kSteps; ++i) {
-            const int row = i * kRowsWarp + sub, byte = scale_ring[slot][row];
-            uint4 u = ld_shared16(from + row * D + 16 * pc);
-            __half2 f = relative_scale(byte, top);
-            if (draft && byte == 255 && row0 + row >= seq.prefix) {
-              bad |= 1ull << (row0 + row - seq.prefix & 63);
-              f = __half2(__ushort_as_half(0), __ushort_as_half(0));
-              u = make_uint4(0, 0, 0, 0);
+          // the steps of one warp, kAt at a time: their loads together, then the rest
+          constexpr int kAt = kSteps / 2 < 8 ? kSteps / 2 : 8;
+          static_assert(kSteps / 2 == kAt, "a warp's steps at once");
+          const int first = second ? kAt : 0;
+          uint4 u[kAt];
+          int byte[kAt];
+#pragma unroll
+          for (int i = 0; i < kAt; ++i) {
+            const int row = (first + i) * kRowsWarp + sub;
+            byte[i] = scale_ring[slot][row];
+            u[i] = ld_shared16(from + row * D + 16 * pc);
+          }
+          if (draft) {
+#pragma unroll
+            for (int i = 0; i < kAt; ++i) {
+              const int row = row0 + (first + i) * kRowsWarp + sub;
+              if (byte[i] == 255 && row >= seq.prefix) {
+                bad |= 1ull << (row - seq.prefix & 63);
+                byte[i] = 0;
+                u[i] = make_uint4(0, 0, 0, 0);
+              }
             }
+          }
+#pragma unroll
+          for (int i = 0; i < kAt; ++i) {
+            const int row = (first + i) * kRowsWarp + sub;
             uint32_t o[8];
-            widen(u, f, o);
+            widen(u[i], relative_scale(byte[i], top), o);
             const int c = 2 * pc;  // of 16-byte pieces in the stage
             const uint32_t at = to + (c >> 3) * S::HALF + row * 128;
             st_shared16(at + (((c & 7) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
@@ -526,6 +563,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (draft && row0 + KB >= w.end) tell_bad();
           fence_proxy_async_smem();  // for the tensor cores' reads
           mbar_arrive(&full[stage]);
+          named_bar_sync(pair_bar, 64);  // the ring's place has been read
+          if (!second) {
+            if (row0 + 2 * KB < w.end) issue(row0 + 2 * KB, ring_n + 2);
+          } else {
+            if (row0 + KB < w.end) put_scales(ring_n + 1);
+            if (row0 + 2 * KB < w.end) load_scales(row0 + 2 * KB);
+          }
         }
       }
     }
@@ -533,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!ok) {  // what TMA still has on its way lands before the CTA leaves
       if (!kCodes) {
         for (int i = max(0, n - ST); i < n; ++i) mbar_wait(&full[i % ST], i / ST & 1, nullptr);
-      } else {
+      } else {  // (the second warp has issued none)
         for (int i = max(0, issued - kRing); i < issued; ++i)
           mbar_wait(&sy->ring_full[keys ? 0 : 1][i % kRing], i / kRing & 1, nullptr);
       }
@@ -548,8 +592,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     // all of them have to be done: P of block i - 2 lies where S(i) goes, and a barrier that has
     // gone on by two phases cannot be waited for.
     auto scores = [&](int i) {
-      const int st = i % ST;
-      if (!wait_for(&sy->k_full[st], i / ST)) return false;
+      const int st = i % SK;
+      if (!wait_for(&sy->k_full[st], i / SK)) return false;
       if (n > 0 && !wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2)) return false;
       tc_fence_after();
       if (elect_one()) {
@@ -575,8 +619,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = scores(n);
       for (int i = 0; i < count && ok; ++i, ++n) {
         if (i + 1 < count && !(ok = scores(n + 1))) break;
-        const int st = n % ST;
-        if (!wait_for(&sy->p_full[n & 1], n / 2) || !wait_for(&sy->v_full[st], n / ST)) {
+        const int st = n % SV;
+        if (!wait_for(&sy->p_full[n & 1], n / 2) || !wait_for(&sy->v_full[st], n / SV)) {
           ok = false;
           break;
         }
@@ -720,21 +764,37 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (warp_live) {
           tc_fence_after();
           const uint32_t s_at = lanes + (n & 1) * KB;
-          uint32_t u[KC];
-          tmem_load<KC>(s_at + key0, u);
+          // (8-bit pages without copies: a thread has no room for 64 scores, and reads them twice)
+          constexpr int NH = kCodes && C == 1 ? 2 : 1, HK = KC / NH;
+          uint32_t u[HK];
           const unsigned long long present = sy->present[n % kSlots];
-          if (present != ~0ull || row0 + KB > seq.prefix) {
+          const bool masked = present != ~0ull || row0 + KB > seq.prefix;
+          unsigned long long seen = ~0ull;
+          if (masked) {
             // the draft's token j is the block's key j - j0
             const long long j0 = row0 - seq.prefix;
-            const unsigned long long seen =
-                (present & (j0 <= -64 ? ~0ull
-                            : j0 < 0  ? mask << -j0 | ((1ull << -j0) - 1)
-                            : j0 < 64 ? mask >> j0
-                                      : 0ull)) >> key0;
-#pragma unroll
-            for (int i = 0; i < KC; ++i)
-              if (!(seen >> i & 1)) u[i] = 0xff800000u;  // -infinity
+            seen = (present & (j0 <= -64 ? ~0ull
+                               : j0 < 0  ? mask << -j0 | ((1ull << -j0) - 1)
+                               : j0 < 64 ? mask >> j0
+                                         : 0ull)) >> key0;
           }
+          auto load_scores = [&](int half) {
+            tmem_load<HK>(s_at + key0 + half * HK, u);
+            if (masked) {
+              const unsigned long long on = seen >> (half * HK);
+#pragma unroll
+              for (int i = 0; i < HK; ++i)
+                if (!(on >> i & 1)) u[i] = 0xff800000u;  // -infinity
+            }
+          };
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int half = 0; half < NH; ++half) {
+            load_scores(half);
+#pragma unroll
+            for (int i = 0; i < HK; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(u[i]));
+          }
+          float mb = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
           float rs = row_scale, a = 1.f, a_o = 1.f;
           bool grow = false;
           if constexpr (kCodes) {
@@ -744,9 +804,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (grow) a_o = fast_exp2((float)(v_top - top));
             v_top = top;
           }
-          float mb = __uint_as_float(u[0]);
-#pragma unroll
-          for (int i = 1; i < KC; ++i) mb = fmaxf(mb, __uint_as_float(u[i]));
           mb *= rs;  // (> 0)
           if (mb > m + kLow + kSlack) {
             a = fast_exp2(m - (mb - kLow));
@@ -772,35 +829,40 @@ __global__ void __launch_bounds__(kThreads, 1)
           // leaves out the score's rounding, must not meet a maximum whose own rounding counts
           const float sub = m == -INFINITY ? 0.f : m;
           float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          uint32_t pr[KC / 2];
-          if (!__any_sync(kAll, fabsf(sub) >= 65536.f)) {
+          const bool far = __any_sync(kAll, fabsf(sub) >= 65536.f);
 #pragma unroll
-            for (int i = 0; i < KC; i += 2) {
-              float2 y = __ffma2_rn(make_float2(__uint_as_float(u[i]), __uint_as_float(u[i + 1])),
-                                    make_float2(rs, rs), make_float2(-sub, -sub));
-              y.x = fast_exp2(y.x);
-              y.y = fast_exp2(y.y);
-              sum[i / 2 & 1] = __fadd2_rn(sum[i / 2 & 1], y);
-              pr[i / 2] = pack16<kCodes>(y.x, y.y);
+          for (int half = 0; half < NH; ++half) {
+            if (NH > 1) load_scores(half);  // (P lies over scores that have been read)
+            uint32_t pr[HK / 2];
+            if (!far) {
+#pragma unroll
+              for (int i = 0; i < HK; i += 2) {
+                float2 y = __ffma2_rn(make_float2(__uint_as_float(u[i]), __uint_as_float(u[i + 1])),
+                                      make_float2(rs, rs), make_float2(-sub, -sub));
+                y.x = fast_exp2(y.x);
+                y.y = fast_exp2(y.y);
+                sum[i / 2 & 1] = __fadd2_rn(sum[i / 2 & 1], y);
+                pr[i / 2] = pack16<kCodes>(y.x, y.y);
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < HK; i += 2) {
+                const float2 y = make_float2(fast_exp2(__uint_as_float(u[i]) * rs - sub),
+                                             fast_exp2(__uint_as_float(u[i + 1]) * rs - sub));
+                sum[i / 2 & 1] = __fadd2_rn(sum[i / 2 & 1], y);
+                pr[i / 2] = pack16<kCodes>(y.x, y.y);
+              }
             }
-          } else {
+            // the copy's own keys; the other copies' have no weight here
 #pragma unroll
-            for (int i = 0; i < KC; i += 2) {
-              const float2 y = make_float2(fast_exp2(__uint_as_float(u[i]) * rs - sub),
-                                           fast_exp2(__uint_as_float(u[i + 1]) * rs - sub));
-              sum[i / 2 & 1] = __fadd2_rn(sum[i / 2 & 1], y);
-              pr[i / 2] = pack16<kCodes>(y.x, y.y);
+            for (int k = 0; k < C; ++k) {
+              uint32_t of[HK / 2];
+#pragma unroll
+              for (int i = 0; i < HK / 2; ++i) of[i] = C == 1 || k == copy ? pr[i] : 0u;
+              tmem_store<HK / 2>(s_at + (C == 1 ? half : k) * (HK / 2), of);
             }
           }
           l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-          // the copy's own keys; the other copies' have no weight here
-#pragma unroll
-          for (int k = 0; k < C; ++k) {
-            uint32_t of[KC / 2];
-#pragma unroll
-            for (int i = 0; i < KC / 2; ++i) of[i] = C == 1 || k == copy ? pr[i] : 0u;
-            tmem_store<KC / 2>(s_at + k * (KC / 2), of);
-          }
           tmem_wait_st();
           tc_fence_before();
         }
@@ -824,7 +886,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       unsigned long long bad = 0;
       if (w.end > seq.prefix) {
         if (!(ok = wait_for(&sy->draft_done[drafts % kSlots], drafts / kSlots))) break;
-        bad = sy->bad[drafts++ % kSlots];
+        bad = sy->bad[0][drafts % kSlots] | (kCodes ? sy->bad[1][drafts % kSlots] : 0ull);
+        ++drafts;
       }
       tc_fence_after();
       const float o_scale = kCodes ? pow2(v_top - 127) : 1.f;
@@ -867,7 +930,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // the copies, in the last block's values' stage: their statistics, then a quarter of the
         // dims at a time, a row of the products each thread's, 16 bytes at places by the row's
         // low bits
-        uint8_t *const stage = tiles + S::V0 + (n - 1) % ST * S::TILE;
+        uint8_t *const stage = tiles + S::V0 + (n - 1) % SV * S::TILE;
         constexpr int CD = D / 4, CP = CD / 4;
         float2 *const stats = (float2 *)stage;
         stats[tid] = make_float2(m, l);
@@ -924,7 +987,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         fence_proxy_async_smem();  // (the stage is written by TMA next)
         named_bar_sync(1 + team, 128);
-        if (tid == 0) mbar_arrive(&sy->v_empty[(n - 1) % ST]);
+        if (tid == 0) mbar_arrive(&sy->v_empty[(n - 1) % SV]);
       }
       tc_fence_before();  // O is read before the next group's first block is said to be ready
     }
@@ -996,7 +1059,7 @@ cudaError_t launch(TreeParams p, int dev, int sms, cudaStream_t st) {
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(std::min(p.n_runs * p.tiles, std::max(sms, (p.n_runs * p.tiles + kTeams - 1) / kTeams)));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads(kCodes));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
