@@ -453,6 +453,21 @@ size_t plan(TreeParams *p, int dtype, int sms, void *ws) {
   return plan(p, kTreeSimtRows, kTreeSimtKeys, kTreeSimtCtas * sms, ws);
 }
 
+// Shares of a group on the tensor cores where the table's room is short, 0 where it is not: as
+// many teams as find a place at once, at most one a block, with few blocks each; their partials
+// fit where the runs' would.
+constexpr int kMostTeams = 16;  // (a cluster of 8)
+constexpr int kShortBlocks = 8;
+int short_teams(const TreeParams &p, int sms) {
+  if (p.tiles > 1) return 0;
+  const long long groups = (long long)p.g.B * p.g.Hkv, places = (long long)kTreeTcTeams * sms;
+  const long long blocks = (((long long)p.g.max_pages << p.g.shift) + kTreeTcKeys - 1) / kTreeTcKeys;
+  if (groups > places) return 0;
+  int teams = 1;
+  while (teams < kMostTeams && 2 * teams <= blocks && groups * 2 * teams <= places) teams *= 2;
+  return blocks <= (long long)teams * kShortBlocks ? teams : 0;
+}
+
 }  // namespace
 
 }  // namespace ripple
@@ -527,6 +542,11 @@ extern "C" ripple_status ripple_paged_tree_attn(
   cudaStream_t st = (cudaStream_t)stream;
   const bool d128 = desc->head_dim == 128;
   if (desc->dtype == RIPPLE_BF16) {
+    p.teams = short_teams(p, sm_count(dev));
+    if (p.teams > 0) {
+      RIPPLE_CUDA_TRY(launch_tree_tc(p, scales != nullptr, dev, sm_count(dev), st));
+      return RIPPLE_OK;
+    }
     RIPPLE_CUDA_TRY(launch_tree_tc(p, scales != nullptr, dev, sm_count(dev), st));
     RIPPLE_CUDA_TRY((d128 ? launch_join<__nv_bfloat16, 128>(p, st)
                           : launch_join<__nv_bfloat16, 64>(p, st)));

@@ -40,6 +40,7 @@ struct TreeParams {
   int n_tokens, per_seq, max_tokens;     // per_seq: tokens of every sequence, without starts
   int tiles, tile_rows;                  // row tiles of a group at most, rows of a partial
   int n_runs;
+  int teams;                             // on the tensor cores, short caches: shares of a group (0: runs)
   long long wait_cycles;
   uint32_t suspend_ns;                   // of a poll of an mbarrier, at most
   bool tma;                              // whole blocks by TMA
@@ -136,6 +137,22 @@ struct TreeWalk {
     }
     set(0);
     return true;
+  }
+  // The share `of` in `shares` equal ones of a group, the only part; false where it has no blocks.
+  __device__ __forceinline__ bool share(const TreeParams &p, int group, int of, int shares) {
+    if (group >= p.g.B * p.g.Hkv) return false;
+    b = group / p.g.Hkv;
+    h = group % p.g.Hkv;
+    const TreeSeq s(p, b);
+    len = s.len;
+    const long long n = blocks_of(s);
+    block = (int)(n * of / shares);
+    count = (int)(n * (of + 1) / shares) - block;
+    begin = block * KB;
+    end = (int)min((long long)len, (long long)(block + count) * KB);
+    at = stop = total = 0;
+    runs = 0;
+    return count > 0;
   }
   // To the run's first part, by one warp; false where the run is empty.
   __device__ __forceinline__ bool start(const TreeParams &p, int run, int lane) {

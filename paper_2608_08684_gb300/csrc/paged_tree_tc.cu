@@ -67,8 +67,7 @@ struct Sync {
   uint32_t tmem;
   int abort;                           // a role has given up waiting
   int top[2][kSlots];                  // 8-bit pages: the scale bytes that a block's keys, values are over
-  int v_top[kRing];                    // the same of values, by the warp that widens them
-  uint8_t scale[2][kRing][KB];         // of the ring's rows
+  uint16_t scale[2][kRing][KB];        // of the ring's rows, over that, in fp16
   float inv[64];                       // of a group's query rows (with copies)
 };
 
@@ -237,16 +236,15 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t pair) {
   return ((pair & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) |
          ((pair & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
-// 2^(byte - top), twice, in fp16 (0 below its values); NaN for byte 255. byte <= top.
-__device__ __forceinline__ __half2 relative_scale(int byte, int top) {
+// 2^(byte - top) in fp16 (0 below its values); NaN for byte 255. byte <= top.
+constexpr uint16_t kNanScale = 0x7fff;
+__device__ __forceinline__ uint16_t relative_scale(int byte, int top) {
   const int d = byte - top;
-  uint32_t h = d >= -14 ? (uint32_t)(15 + d) << 10 : d >= -24 ? 1u << (24 + d) : 0u;
-  if (byte == 255) h = 0x7fffu;
-  h |= h << 16;
-  return *reinterpret_cast<const __half2 *>(&h);
+  return byte == 255 ? kNanScale : d >= -14 ? (15 + d) << 10 : d >= -24 ? 1 << (24 + d) : 0;
 }
 // 16 codes times a scale as fp16.
-__device__ __forceinline__ void widen(const uint4 &u, __half2 scale, uint32_t (&o)[8]) {
+__device__ __forceinline__ void widen(const uint4 &u, uint16_t factor, uint32_t (&o)[8]) {
+  const __half2 scale = __half2half2(__ushort_as_half(factor));
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -281,8 +279,10 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
   uint8_t *const tiles = smem + team * S::TEAM;
   Sync *const syncs = (Sync *)(smem + kTeams * S::TEAM), *const sy = syncs + team;
   // (as many CTAs as SMs, or one for each team's work: teams beside one another in different CTAs)
-  const int work = blockIdx.x + team * gridDim.x;
-  const int run = work / p.tiles, tile = work % p.tiles;
+  // Short caches: p.teams teams of a cluster (or one) have equal shares of a group.
+  const int teams = p.teams;
+  const int work = teams > 1 ? kTeams * (int)blockIdx.x + team : (int)(blockIdx.x + team * gridDim.x);
+  const int run = teams > 0 ? work : work / p.tiles, tile = teams > 0 ? 0 : work % p.tiles;
   if (warp == 4 && lane == 0) {
     sy->abort = 0;
     for (int i = 0; i < kRing; ++i) {
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
 
   const uint32_t qs = smem_u32(tiles), ks = qs + S::K0, vs = qs + S::V0;
   W w;
-  const bool any = w.start(p, run, lane);
+  const bool any = teams > 0 ? w.share(p, work / teams, work % teams, teams) : w.start(p, run, lane);
   int n = 0;  // blocks of this CTA so far
   bool ok = true;
   auto wait_for = [&](uint64_t *bar, int phase) {  // by a whole warp
@@ -450,7 +450,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           mbar_arrive(&full[stage]);
         }
       } else {
-        uint8_t(*const scale_ring)[KB] = sy->scale[keys ? 0 : 1];
+        uint16_t(*const scale_ring)[KB] = sy->scale[keys ? 0 : 1];
         uint64_t *const ring_full = sy->ring_full[keys ? 0 : 1];
         const uint32_t ring = qs + S::RING + (keys ? 0 : kRing * S::RAW);
         // What both warps agree on: they go on to a block, or neither does.
@@ -495,20 +495,23 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           int k_top = 0, top = 0;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            scale_ring[i % kRing][lane + 32 * k] = (uint8_t)(keys ? k_byte[k] : v_byte[k]);
             if (keys && k_byte[k] != 255) k_top = max(k_top, k_byte[k]);
             if (v_byte[k] != 255) top = max(top, v_byte[k]);
           }
           v_top = max(v_top, __reduce_max_sync(kAll, top));
+          top = v_top > 0 ? v_top : 7;
           if (keys) {
             k_top = __reduce_max_sync(kAll, k_top);
+            if (k_top == 0) k_top = 127;
             if (lane == 0) {
-              sy->top[0][(n + i - ring_n) % kSlots] = k_top > 0 ? k_top : 127;
-              sy->top[1][(n + i - ring_n) % kSlots] = v_top > 0 ? v_top : 7;
+              sy->top[0][(n + i - ring_n) % kSlots] = k_top;
+              sy->top[1][(n + i - ring_n) % kSlots] = top;
             }
-          } else if (lane == 0) {
-            sy->v_top[i % kRing] = v_top > 0 ? v_top : 7;
           }
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            scale_ring[i % kRing][lane + 32 * k] =
+                keys ? relative_scale(k_byte[k], k_top) : relative_scale(v_byte[k], top);
         };
         const bool more_than_one = w.begin + KB < w.end;
         if (!second) {
@@ -524,7 +527,6 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           ok = both(wait_for(&ring_full[slot], ring_n / kRing) &&
                     (n < ST || wait_for(&empty[stage], n / ST - 1)));
           if (!ok) break;
-          const int top = keys ? sy->top[0][n % kSlots] : sy->v_top[slot];
           const uint32_t from = ring + slot * S::RAW, to = stages + stage * S::TILE;
           const bool draft = !keys && w.end > seq.prefix && row0 + KB > seq.prefix;
           // the steps of one warp, kAt at a time: their loads together, then the rest
@@ -532,20 +534,20 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           static_assert(kSteps / 2 == kAt, "a warp's steps at once");
           const int first = second ? kAt : 0;
           uint4 u[kAt];
-          int byte[kAt];
+          uint16_t f[kAt];
 #pragma unroll
           for (int i = 0; i < kAt; ++i) {
             const int row = (first + i) * kRowsWarp + sub;
-            byte[i] = scale_ring[slot][row];
+            f[i] = scale_ring[slot][row];
             u[i] = ld_shared16(from + row * D + 16 * pc);
           }
           if (draft) {
 #pragma unroll
             for (int i = 0; i < kAt; ++i) {
               const int row = row0 + (first + i) * kRowsWarp + sub;
-              if (byte[i] == 255 && row >= seq.prefix) {
+              if (f[i] == kNanScale && row >= seq.prefix) {
                 bad |= 1ull << (row - seq.prefix & 63);
-                byte[i] = 0;
+                f[i] = 0;
                 u[i] = make_uint4(0, 0, 0, 0);
               }
             }
@@ -554,7 +556,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           for (int i = 0; i < kAt; ++i) {
             const int row = (first + i) * kRowsWarp + sub;
             uint32_t o[8];
-            widen(u[i], relative_scale(byte[i], top), o);
+            widen(u[i], f[i], o);
             const int c = 2 * pc;  // of 16-byte pieces in the stage
             const uint32_t at = to + (c >> 3) * S::HALF + row * 128;
             st_shared16(at + (((c & 7) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
@@ -705,7 +707,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       const TreeSeq seq(p, w.b);
       if (w.count == 0) continue;
       const bool here = w.block == 0, whole = w.whole();
-      if (here && !whole) rec = make_int2(w.b * p.g.Hkv + w.h, w.runs_of_group(run));
+      if (teams == 0 && here && !whole) rec = make_int2(w.b * p.g.Hkv + w.h, w.runs_of_group(run));
       const int n_rows = min(seq.tokens * p.G - tile * RT, RT);
       if (n_rows <= 0) continue;
       if (!have_queries) row_scale = fetch_queries(w, seq);
@@ -891,7 +893,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       }
       tc_fence_after();
       const float o_scale = kCodes ? pow2(v_top - 127) : 1.f;
-      const long long slot = ((2LL * run + (here ? 1 : 0)) * p.tiles + tile) * p.tile_rows;
+      const long long slot =
+          (teams > 0 ? (long long)work : (2LL * run + (here ? 1 : 0)) * p.tiles + tile) * p.tile_rows;
       // four outputs of query row i: the output, or the partial
       auto put = [&](int i, int d, const float4 &x) {
         if (whole)
@@ -991,12 +994,74 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       }
       tc_fence_before();  // O is read before the next group's first block is said to be ready
     }
-    if (tile == 0 && tid == 0 && run < p.n_runs) p.rec[run] = ok ? rec : make_int2(0, 0);
+    if (teams == 0 && tile == 0 && tid == 0 && run < p.n_runs) p.rec[run] = ok ? rec : make_int2(0, 0);
     tc_fence_before();
   }
   __syncthreads();
   tc_fence_after();
   if (cta_warp == 8) tmem_dealloc(syncs->tmem, kTeams * kTeamCols);
+  if (teams == 0) return;
+
+  // the shares' partials joined in order, a row of 16 bytes of outputs a thread; and the outputs of
+  // idle sequences
+  if (teams > 1) {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  }
+  const int members = teams > 1 ? teams / kTeams * threads(kCodes) : threads(kCodes);
+  const int me = teams > 1 ? (int)blockIdx.x % (teams / kTeams) * threads(kCodes) + threadIdx.x : threadIdx.x;
+  for (int g = 0; g < (teams > 1 ? 1 : kTeams); ++g) {
+    const int group = teams > 1 ? work / teams : (int)(blockIdx.x + g * gridDim.x);
+    if (group >= p.g.B * p.g.Hkv) break;
+    const int b = group / p.g.Hkv, h = group % p.g.Hkv;
+    const TreeSeq seq(p, b);
+    const int blocks = W::blocks_of(seq), rows = seq.tokens * p.G;
+    const bool idle = seq.len == 0;
+    if (!idle && (teams == 1 || blocks == 1)) continue;  // (whole shares have been written)
+    constexpr int kCols = D / 4;
+    for (int e = me; e < rows * kCols; e += members) {
+      const int i = e / kCols, col = e % kCols;
+      float m = -INFINITY, den = 0.f;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k0 = 0; k0 < (idle ? 0 : teams); k0 += 8) {
+        float2 ml[8];
+        float4 o[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int of = k0 + k;
+          ml[k] = make_float2(-INFINITY, 0.f);
+          o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (of < teams && (long long)blocks * of / teams < (long long)blocks * (of + 1) / teams) {
+            const long long at = ((long long)group * teams + of) * p.tile_rows + i;
+            ml[k] = __ldcg(&p.ws_ml[at]);
+            o[k] = __ldcg(reinterpret_cast<const float4 *>(p.ws_o + at * D) + col);
+          }
+        }
+        float mn = m;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) mn = fmaxf(mn, ml[k].x);
+        const float subm = mn == -INFINITY ? 0.f : mn, a = fast_exp2(m - subm);
+        sum = make_float4(sum.x * a, sum.y * a, sum.z * a, sum.w * a);
+        den *= a;
+        m = mn;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float f = fast_exp2(ml[k].x - subm);
+          if (ml[k].y == 0.f) continue;  // (no row counts; a share without blocks)
+          sum.x += f * o[k].x;
+          sum.y += f * o[k].y;
+          sum.z += f * o[k].z;
+          sum.w += f * o[k].w;
+          den += f * ml[k].y;
+        }
+      }
+      const long long at = (long long)(seq.first + i / p.G) * p.Hq + h * p.G + i % p.G;
+      const float inv = den != 0.f ? 1.f / den : 0.f;  // 0: no row counts
+      put4((__nv_bfloat16 *)p.out + at * D + 4 * col,
+           make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+      if (p.lse != nullptr && col == 0) p.lse[at] = tree_lse(m, den);
+    }
+  }
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
@@ -1058,15 +1123,21 @@ cudaError_t launch(TreeParams p, int dev, int sms, cudaStream_t st) {
     attr_set[dev].store(true, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(std::min(p.n_runs * p.tiles, std::max(sms, (p.n_runs * p.tiles + kTeams - 1) / kTeams)));
+  const int works = p.teams > 0 ? p.g.B * p.g.Hkv * p.teams : p.n_runs * p.tiles;
+  cfg.gridDim = dim3(p.teams > 1 ? works / kTeams
+                                 : std::min(works, std::max(sms, (works + kTeams - 1) / kTeams)));
   cfg.blockDim = dim3(threads(kCodes));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = p.teams > 1 ? p.teams / kTeams : 1;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = p.teams > kTeams ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, tree_tc_kernel<D, kCodes, C>, p, maps);
   count_launches(1);
   return e;
