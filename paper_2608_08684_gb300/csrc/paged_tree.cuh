@@ -145,7 +145,7 @@ struct TreeWalk {
     h = group % p.g.Hkv;
     const TreeSeq s(p, b);
     len = s.len;
-    const long long n = blocks_of(s);
+    const unsigned n = blocks_of(s);  // (fewer than 2^25)
     block = (int)(n * of / shares);
     count = (int)(n * (of + 1) / shares) - block;
     begin = block * KB;

@@ -54,6 +54,7 @@ constexpr uint32_t kOCol = 128;
 constexpr float kSlack = 8.f;
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kMaxDevices = 64;
+constexpr int kDrafts = 4; // parts with drafted tokens that the values may be ahead
 constexpr int kSlots = 8;  // of what the softmax is told about blocks (fetched up to two ahead)
 
 struct Sync {
@@ -61,14 +62,15 @@ struct Sync {
   uint64_t ring_full[2][kRing];                         // of keys, of values
   uint64_t s_full[2], p_full[2], pv_done[2];            // of even and odd blocks
   uint64_t q_full, mma_done;
-  uint64_t draft_done[kSlots];         // by parts with drafted tokens (values may be parts ahead)
+  uint64_t draft_done[kDrafts];        // by parts with drafted tokens (values may be parts ahead)
   unsigned long long present[kSlots];  // rows of a block that are there
-  unsigned long long bad[2][kSlots];   // drafted tokens whose values are not all finite, by parts
+  unsigned long long bad[2][kDrafts];  // drafted tokens whose values are not all finite, by parts
   uint32_t tmem;
   int abort;                           // a role has given up waiting
   int top[2][kSlots];                  // 8-bit pages: the scale bytes that a block's keys, values are over
   uint16_t scale[2][kRing][KB];        // of the ring's rows, over that, in fp16
-  float inv[64];                       // of a group's query rows (with copies)
+  float inv[64];                       // of a group's query rows (with copies), and where they go
+  int out_row[64];
 };
 
 template <int D, bool kCodes>
@@ -299,7 +301,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       mbar_init(&sy->pv_done[i], 1);
     }
     mbar_init(&sy->q_full, 4);
-    for (int i = 0; i < kSlots; ++i) mbar_init(&sy->draft_done[i], 16 * kFetch);
+    for (int i = 0; i < kDrafts; ++i) mbar_init(&sy->draft_done[i], 16 * kFetch);
     mbar_init(&sy->mma_done, 1);
     fence_mbar_init();
     fence_proxy_async_smem();
@@ -411,9 +413,9 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
     unsigned long long bad = 0;
     auto tell_bad = [&]() {
       const uint32_t lo = __reduce_or_sync(kAll, (uint32_t)bad), hi = __reduce_or_sync(kAll, (uint32_t)(bad >> 32));
-      if (lane == 0) sy->bad[second][drafts % kSlots] = (unsigned long long)hi << 32 | lo;
+      if (lane == 0) sy->bad[second][drafts % kDrafts] = (unsigned long long)hi << 32 | lo;
       bad = 0;
-      mbar_arrive(&sy->draft_done[drafts % kSlots]);
+      mbar_arrive(&sy->draft_done[drafts % kDrafts]);
       ++drafts;
     };
     int ring_n = 0, issued = 0;  // blocks that have gone through the ring, that were put there
@@ -651,49 +653,65 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
     const int key0 = copy * KC;
     // The queries of the part at `w`, once the products with the ones before are done; returns what
     // the row's scores are multiplied by.
+    // A warp has 32 rows of the products, a row's 16-byte pieces on neighbouring lanes.
     auto fetch_queries = [&](const W &w, const TreeSeq &seq) {
+      constexpr int kQPieces = D / 8, kAtOnce = 32 / kQPieces, kSteps = 32 / kAtOnce;
       const int n_rows = min(seq.tokens * p.G - tile * RT, RT);
-      const bool live = r < n_rows;
-      const int row = tile * RT + (live ? r : 0), tok = row / p.G, head = w.h * p.G + row % p.G;
-      const __nv_bfloat16 *q = (const __nv_bfloat16 *)p.q + head * p.q_head +
-                               (p.starts == nullptr ? w.b * p.q_seq + tok * p.q_token
-                                                    : (long long)(seq.first + tok) * p.q_token);
-      const uint32_t to = qs + tid * 128;
+      const int mine = tile * RT + (r < n_rows ? r : 0), tok = mine / p.G, head = w.h * p.G + mine - tok * p.G;
+      // where the thread's own row lies (-1: it is none)
+      const long long at = r < n_rows ? head * p.q_head + (p.starts == nullptr
+                                                               ? w.b * p.q_seq + tok * p.q_token
+                                                               : (long long)(seq.first + tok) * p.q_token)
+                                      : -1;
+      const int pc = lane % kQPieces, sub = lane / kQPieces;
       float scale = p.scale2;
+      auto place = [&](int row) {  // of the piece of a row of the warp
+        return qs + (pc >> 3) * S::HALF_Q + (32 * warp + row) * 128 + (((pc & 7) ^ (row & 7)) << 4);
+      };
       if constexpr (!kCodes) {
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c)
-          copy16(to + (c >> 3) * S::HALF_Q + (((c & 7) ^ (tid & 7)) << 4), q + 8 * c, live);
+        for (int i = 0; i < kSteps; ++i) {
+          const int row = i * kAtOnce + sub;
+          const long long from = __shfl_sync(kAll, at, row);
+          copy16(place(row), (const __nv_bfloat16 *)p.q + (from >= 0 ? from + 8 * pc : 0), from >= 0);
+        }
         copies_landed();
       } else {
-        // (read twice: there is no room for the whole row)
-        auto load = [&](int c) {
-          return live ? __ldg(reinterpret_cast<const uint4 *>(q) + c) : make_uint4(0, 0, 0, 0);
-        };
-        float most = 0.f;
-#pragma unroll 4
-        for (int c = 0; c < D / 8; ++c) {
-          const uint4 x = load(c);
-          const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+        constexpr int kAt = kSteps < 8 ? kSteps : 8;  // loaded at a time
+        int up = 0;                                   // of the thread's own row
+#pragma unroll 1
+        for (int i0 = 0; i0 < kSteps; i0 += kAt) {
+          uint4 x[kAt];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            most = fmaxf(most, fmaxf(fabsf(__uint_as_float(u[i] << 16)),
-                                     fabsf(__uint_as_float(u[i] & 0xffff0000u))));
+          for (int i = 0; i < kAt; ++i) {
+            const long long from = __shfl_sync(kAll, at, (i0 + i) * kAtOnce + sub);
+            x[i] = make_uint4(0, 0, 0, 0);
+            if (from >= 0) x[i] = __ldg(reinterpret_cast<const uint4 *>((const __nv_bfloat16 *)p.q + from) + pc);
+          }
+#pragma unroll
+          for (int i = 0; i < kAt; ++i) {
+            const int row = (i0 + i) * kAtOnce + sub;
+            const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            float most = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              most = fmaxf(most, fmaxf(fabsf(__uint_as_float(u[k] << 16)),
+                                       fabsf(__uint_as_float(u[k] & 0xffff0000u))));
+#pragma unroll
+            for (int o = 1; o < kQPieces; o <<= 1) most = fmaxf(most, __shfl_xor_sync(kAll, most, o));
+            // (infinities keep the others finite; what is below 2^-86 may be lost)
+            const int e = most == 0.f ? 0 : min(14 - ((__float_as_int(most) >> 23) - 127), 100);
+            const float f = pow2(e);
+            uint32_t o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              o[k] = pack16<true>(__uint_as_float(u[k] << 16) * f, __uint_as_float(u[k] & 0xffff0000u) * f);
+            st_shared16(place(row), o[0], o[1], o[2], o[3]);
+            const int of_row = __shfl_sync(kAll, e, lane % kAtOnce * kQPieces);
+            if (lane / kAtOnce == i0 + i) up = of_row;
+          }
         }
-        // (infinities keep the others finite; what is below 2^-86 may be lost)
-        const int up = most == 0.f ? 0 : min(14 - ((__float_as_int(most) >> 23) - 127), 100);
-        const float f = pow2(up);
         scale *= pow2(-up);
-#pragma unroll 4
-        for (int c = 0; c < D / 8; ++c) {
-          const uint4 x = load(c);
-          const uint32_t u[4] = {x.x, x.y, x.z, x.w};
-          uint32_t o[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            o[i] = pack16<true>(__uint_as_float(u[i] << 16) * f, __uint_as_float(u[i] & 0xffff0000u) * f);
-          st_shared16(to + (c >> 3) * S::HALF_Q + (((c & 7) ^ (tid & 7)) << 4), o[0], o[1], o[2], o[3]);
-        }
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -887,18 +905,18 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       if (!(ok = wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2))) break;
       unsigned long long bad = 0;
       if (w.end > seq.prefix) {
-        if (!(ok = wait_for(&sy->draft_done[drafts % kSlots], drafts / kSlots))) break;
-        bad = sy->bad[0][drafts % kSlots] | (kCodes ? sy->bad[1][drafts % kSlots] : 0ull);
+        if (!(ok = wait_for(&sy->draft_done[drafts % kDrafts], drafts / kDrafts))) break;
+        bad = sy->bad[0][drafts % kDrafts] | (kCodes ? sy->bad[1][drafts % kDrafts] : 0ull);
         ++drafts;
       }
       tc_fence_after();
       const float o_scale = kCodes ? pow2(v_top - 127) : 1.f;
       const long long slot =
           (teams > 0 ? (long long)work : (2LL * run + (here ? 1 : 0)) * p.tiles + tile) * p.tile_rows;
-      // four outputs of query row i: the output, or the partial
-      auto put = [&](int i, int d, const float4 &x) {
+      // four outputs of query row i, whose output row is `at`: the output, or the partial
+      auto put = [&](int i, long long at, int d, const float4 &x) {
         if (whole)
-          put4((__nv_bfloat16 *)p.out + out_row(i) * D + d, x);
+          put4((__nv_bfloat16 *)p.out + at * D + d, x);
         else
           put4(p.ws_o + (slot + i) * D + d, x);
       };
@@ -914,6 +932,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       if constexpr (C == 1) {
         if (warp_live) {
           const float inv = inverse(l) * o_scale;
+          const long long at = live ? out_row(r) : 0;
 #pragma unroll 1
           for (int c = 0; c < D; c += 32) {
             __syncwarp();
@@ -925,7 +944,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
             for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(u[i]) * inv;
             if ((bad & mask) != 0) add_bad(bad & mask, c, o, 32);
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) put(r, c + i, make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
+            for (int i = 0; i < 32; i += 4) put(r, at, c + i, make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
           }
           if (live) put_stats(r, m, l);
         }
@@ -948,6 +967,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
         const float f = fast_exp2(m - sub) * o_scale;
         if (copy == 0) {
           sy->inv[r] = inverse(den);
+          sy->out_row[r] = live ? (int)(out_row(r) - (long long)seq.first * p.Hq) : 0;
           if (live) put_stats(r, top, den);
         }
         named_bar_sync(1 + team, 128);
@@ -984,7 +1004,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
                   p.masks == nullptr ? ~0ull >> (63 - tok) : p.masks[seq.first + tok];
               if ((bad & sees) != 0) add_bad(bad & sees, c + 4 * pc, o, 4);
             }
-            put(i, c + 4 * pc, make_float4(o[0], o[1], o[2], o[3]));
+            put(i, sy->out_row[i] + (long long)seq.first * p.Hq, c + 4 * pc, make_float4(o[0], o[1], o[2], o[3]));
           }
           named_bar_sync(1 + team, 128);
         }
