@@ -110,8 +110,14 @@ struct IsCodes<Codes8<Q>> {
   static constexpr bool v = true;
 };
 
+// Warps an SM over 8-bit pages: blocks of 64 dims are half as long.
+__host__ __device__ constexpr int codes_warps(int d, int group) {
+  return d == 64 && group <= 8 ? 12 : kWarpsPerSm;
+}
+
 template <typename T, int D, int G>
 struct Cfg {
+  static constexpr int WARPS = sizeof(T) == 1 ? codes_warps(D, G) : kWarpsPerSm;
   static constexpr bool kMma = sizeof(T) == 2;
   static constexpr int ROW_BYTES = D * (int)sizeof(T);
   static constexpr int PIECES = ROW_BYTES / 16;
@@ -717,7 +723,7 @@ __device__ __forceinline__ float lse_of(float m, float l) {  // of log2 units; n
 }
 
 template <typename T, int D, int G>
-__global__ void __launch_bounds__(32, kWarpsPerSm)
+__global__ void __launch_bounds__(32, Cfg<T, D, G>::WARPS)
     paged_decode_kernel(const __grid_constant__ PagedDecParams p) {
   using C = Cfg<T, D, G>;
   using W = Walk<C::RB, C::COST>;
@@ -1175,11 +1181,11 @@ bool query_strides(const ripple_paged_desc *d, int n_q_heads, const ripple_token
 // Runs of a call and the workspace: records, (max, sum), outputs of the partials. The runs are
 // bounded by the blocks that the table has room for, so that small caches take few CTAs;
 // everything grows with the call. Returns the bytes; fills p's pointers if given a base.
-size_t plan(PagedDecParams *p, int block_rows, int sms, void *ws) {
+size_t plan(PagedDecParams *p, int block_rows, int warps_per_sm, int sms, void *ws) {
   const int rows = block_rows;
   const long long room =
       (((long long)p->g.max_pages << p->g.shift) + rows - 1) / rows * p->g.B * p->g.Hkv;
-  p->places = sms * kWarpsPerSm;
+  p->places = sms * warps_per_sm;
   const int phases = (long long)p->g.B * p->g.Hkv <= kFewGroups ? 1 : kPhases;
   p->n_runs = (int)std::min<long long>(phases * p->places, room);
   const size_t slots = 2 * (size_t)p->n_runs;

@@ -94,16 +94,25 @@ struct Rows<Codes8<Q>, D, G> {
     for (int nt = 0; nt < NT; ++nt) {
       const int head = (kTwice ? g & 3 : g) + 8 * nt;
       const Q *q = (const Q *)p.q + w.b * p.q_seq + (w.h * p.G + min(head, p.G - 1)) * p.q_head;
+      // (as it lies: the loads of a lane are in flight together)
+      constexpr int kRaw = 2 * sizeof(Q);  // 16-byte pieces of 16 elements
+      uint4 raw[D / 64][kRaw];
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+        for (int j = 0; j < kRaw; ++j)
+          raw[i][j] = *(reinterpret_cast<const uint4 *>(q + 16 * (t + 4 * i)) + j);
+      auto element = [&](int i, int e) {  // of the 16 of piece i
+        const uint4 &u = raw[i][e * sizeof(Q) / 16];
+        const int word = e * sizeof(Q) % 16 / 4;
+        const uint32_t w = word == 0 ? u.x : word == 1 ? u.y : word == 2 ? u.z : u.w;
+        return __uint_as_float(sizeof(Q) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16);
+      };
       float most = 0.f;
 #pragma unroll
       for (int i = 0; i < D / 64; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float x[8];
-          load8(q + 16 * (t + 4 * i) + 8 * j, x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
-        }
+        for (int e = 0; e < 16; ++e) most = fmaxf(most, fabsf(element(i, e)));
       most = fmaxf(most, __shfl_xor_sync(kAll, most, 1));
       most = fmaxf(most, __shfl_xor_sync(kAll, most, 2));
       // (infinities keep the others finite; what is below 2^-86 may be lost)
@@ -112,16 +121,12 @@ struct Rows<Codes8<Q>, D, G> {
 #pragma unroll
       for (int i = 0; i < D / 64; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float x[8];
-          load8(q + 16 * (t + 4 * i) + 8 * j, x);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {  // step 4 i + 2 j + e / 2
-            const float lo = head < p.G ? x[2 * e] * f : 0.f, hi = head < p.G ? x[2 * e + 1] * f : 0.f;
-            const uint32_t h = pack_f16x2(lo, hi);
-            qb[0][nt][4 * i + 2 * j + e / 2][e & 1] = h;
-            if constexpr (QP == 2) qb[1][nt][4 * i + 2 * j + e / 2][e & 1] = rest_f16x2(lo, hi, h);
-          }
+        for (int e = 0; e < 8; ++e) {  // step 4 i + e / 2
+          const float lo = head < p.G ? element(i, 2 * e) * f : 0.f;
+          const float hi = head < p.G ? element(i, 2 * e + 1) * f : 0.f;
+          const uint32_t h = pack_f16x2(lo, hi);
+          qb[0][nt][4 * i + e / 2][e & 1] = h;
+          if constexpr (QP == 2) qb[1][nt][4 * i + e / 2][e & 1] = rest_f16x2(lo, hi, h);
         }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -348,6 +353,11 @@ cudaError_t launch_q8(const PagedDecParams &p, int dev, cudaStream_t st) {
 }
 
 constexpr int kBlockRows = 32;
+// Bytes of a call's workspace; those of the most warps that any group size has, so that more
+// query heads never need fewer.
+size_t workspace_need(PagedDecParams p, int sms) {
+  return plan(&p, kBlockRows, codes_warps(p.g.D, 1), sms, nullptr);
+}
 
 }  // namespace
 }  // namespace ripple
@@ -361,7 +371,7 @@ extern "C" ripple_status ripple_paged_decode_q8_workspace_bytes(const ripple_pag
   if (!decode_args(desc, n_q_heads, &p, true) || bytes_host == nullptr) return RIPPLE_EINVAL;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
-  *bytes_host = plan(&p, kBlockRows, sm_count(dev), nullptr);
+  *bytes_host = workspace_need(p, sm_count(dev));
   return RIPPLE_OK;
 }
 
@@ -385,7 +395,8 @@ extern "C" ripple_status ripple_paged_decode_attn_q8(
   int dev = 0;
   const cudaError_t got = cudaGetDevice(&dev);
   if (got != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
-  if (workspace_bytes < plan(&p, kBlockRows, sm_count(dev), workspace)) return RIPPLE_EWORKSPACE;
+  if (workspace_bytes < workspace_need(p, sm_count(dev))) return RIPPLE_EWORKSPACE;
+  plan(&p, kBlockRows, codes_warps(p.g.D, p.G), sm_count(dev), workspace);
   if (got != cudaSuccess) return RIPPLE_ECUDA;
   p.scale2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)desc->head_dim)) * kLog2e;
   p.q = q;

@@ -70,7 +70,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
     tree_simt_kernel(const __grid_constant__ TreeParams p) {
   using P = Piece<T>;
-  using W = TreeWalk<KB, kGroupCost>;
+  using W = TreeWalk<KB, kGroupCost, R>;
   constexpr int kPieces = D / P::N;                        // of a row
   constexpr int kMine = KB * kPieces / kThreads;           // of a block's keys, a thread
   constexpr bool kCodes = sizeof(T) == 1;
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
   SimtSmem<D> &s = *reinterpret_cast<SimtSmem<D> *>(smem_raw);
   static_assert(KB * kPieces % kThreads == 0, "");
   const int tid = threadIdx.x, lane = tid & 31;
-  const int run = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
+  const int run = blockIdx.x;
   pdl_wait();
   if (blockIdx.x == 0)
     for (int b = tid; b < p.g.B; b += kThreads) TreeSeq::check(p, b);
@@ -88,10 +88,11 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
   for (bool more = w.start(p, run, lane); more; more = w.next(p)) {
     if (w.count == 0) continue;
     const TreeSeq seq(p, w.b);
+    const int tile = w.tile;
     const bool here = w.block == 0, whole = w.whole();
-    if (here && !whole) rec = make_int2(w.b * p.g.Hkv + w.h, w.runs_of_group(run));
+    if (here && !whole)
+      rec = make_int2((w.b * p.g.Hkv + w.h) * p.tiles + tile, w.runs_of_group(run));
     const int n_rows = min(seq.tokens * p.G - tile * R, R);
-    if (n_rows <= 0) continue;
     // this tile's queries (scaled) and masks; row r is token r / G, head r % G
     for (int i = tid; i < R * (D / 4); i += kThreads) {
       const int r = i / (D / 4), c = i % (D / 4) * 4;
@@ -268,7 +269,7 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
         add(false);
     }
     __syncthreads();
-    const long long slot = ((2LL * run + (here ? 1 : 0)) * p.tiles + tile) * p.tile_rows;
+    const long long slot = (2LL * run + (here ? 1 : 0)) * p.tile_rows;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = rg + i;
@@ -291,14 +292,15 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
     }
     __syncthreads();
   }
-  if (tile == 0 && tid == 0) p.rec[run] = rec;
+  if (tid == 0) p.rec[run] = rec;
 }
 
 // Joins the partials of the group that begins in run blockIdx.x and goes on, kJoinRows of its
 // query rows per blockIdx.y; and writes the outputs of idle sequences.
 constexpr int kJoinThreads = 256;
 
-template <typename O, int D>
+// kTiles: every tile is a group of its own.
+template <typename O, int D, bool kTiles>
 __global__ void __launch_bounds__(kJoinThreads)
     tree_join_kernel(const __grid_constant__ TreeParams p) {
   constexpr int kCols = D / 4, kRows = kJoinThreads / kCols;
@@ -308,11 +310,12 @@ __global__ void __launch_bounds__(kJoinThreads)
   const int run = blockIdx.x;
   const int2 rec = __ldcg(&p.rec[run]);
   if (rec.y > 0) {
-    const int b = rec.x / p.g.Hkv, h = rec.x % p.g.Hkv;
+    const int group = kTiles ? rec.x / p.tiles : rec.x, b = group / p.g.Hkv, h = group % p.g.Hkv;
     const TreeSeq seq(p, b);
-    const int row = blockIdx.y * kRows + sub;
-    if (row < seq.tokens * p.G) {
-      const int tile = row / p.tile_rows, r = row % p.tile_rows;
+    const int in = blockIdx.y * kRows + sub;
+    const int tile = kTiles ? rec.x % p.tiles : in / p.tile_rows, r = kTiles ? in : in % p.tile_rows;
+    const int row = kTiles ? tile * p.tile_rows + in : in;
+    if (row < seq.tokens * p.G && r < p.tile_rows) {
       float m = -INFINITY, den = 0.f;
       float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int k0 = 0; k0 < rec.y; k0 += kAt) {
@@ -321,8 +324,8 @@ __global__ void __launch_bounds__(kJoinThreads)
 #pragma unroll
         for (int i = 0; i < kAt; ++i) {
           const int k = min(k0 + i, rec.y - 1);
-          const long long slot =
-              ((2LL * (run + k) + (k == 0 ? 1 : 0)) * p.tiles + tile) * p.tile_rows + r;
+          const long long part = 2LL * (run + k) + (k == 0 ? 1 : 0);
+          const long long slot = (kTiles ? part : part * p.tiles + tile) * p.tile_rows + r;
           ml[i] = __ldcg(&p.ws_ml[slot]);
           o[i] = __ldcg(reinterpret_cast<const float4 *>(p.ws_o + slot * D) + col);
         }
@@ -390,13 +393,13 @@ cudaError_t launch_simt(const TreeParams &p, int dev, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     attr_set[dev].store(true, std::memory_order_release);
   }
-  return launch_pdl(tree_simt_kernel<T, D>, dim3(p.n_runs * p.tiles), kThreads, p, st, smem);
+  return launch_pdl(tree_simt_kernel<T, D>, dim3(p.n_runs), kThreads, p, st, smem);
 }
 
-template <typename O, int D>
+template <typename O, int D, bool kTiles>
 cudaError_t launch_join(const TreeParams &p, cudaStream_t st) {
-  const int rows = kJoinThreads / (D / 4);
-  return launch_pdl(tree_join_kernel<O, D>, dim3(p.n_runs, (p.max_tokens * p.G + rows - 1) / rows),
+  const int rows = kJoinThreads / (D / 4), most = kTiles ? p.tile_rows : p.max_tokens * p.G;
+  return launch_pdl(tree_join_kernel<O, D, kTiles>, dim3(p.n_runs, (most + rows - 1) / rows),
                     kJoinThreads, p, st);
 }
 
@@ -428,18 +431,27 @@ bool tree_args(const ripple_paged_desc *d, const ripple_paged_scales *scales, in
 
 // Tiles and runs of a call and the workspace: records, (max, sum), outputs of the partials. The
 // runs are bounded by the blocks that the table has room for; everything grows with the call.
-// Returns the bytes; fills p's pointers if given a base.
-size_t plan(TreeParams *p, int tile, int block, int places, void *ws) {
+// together: the CTAs of a run's tiles go over the same rows (tensor cores: the reads are shared
+// through L2), otherwise every tile is a group of its own (the CUDA cores: bound by the FMAs, and
+// sequences of few tokens have fewer tiles). Returns the bytes; fills p's pointers if given a base.
+size_t plan(TreeParams *p, int tile, int block, int places, bool together, void *ws) {
   const int rows = p->max_tokens * p->G;
   p->tiles = (rows + tile - 1) / tile;
   p->tile_rows = rows < tile ? rows : tile;
   const long long room = (((long long)p->g.max_pages << p->g.shift) + block - 1) / block *
                          p->g.B * p->g.Hkv;
-  // (as many for one tile as for several, so that the workspace of more tokens is no smaller)
-  p->n_runs = (int)std::min<long long>(std::max(1, places / p->tiles), room);
-  const long long most = std::min<long long>(places, room);
-  const size_t slots = 2 * (size_t)std::max<long long>((long long)p->n_runs * p->tiles, most) * p->tile_rows;
-  const size_t rec = round_up((size_t)std::min<long long>(places, room) * sizeof(int2));
+  size_t parts, runs;  // partials' tiles over two, records
+  if (together) {
+    // (as many for one tile as for several, so that the workspace of more tokens is no smaller)
+    p->n_runs = (int)std::min<long long>(std::max(1, places / p->tiles), room);
+    runs = (size_t)std::min<long long>(places, room);
+    parts = std::max((size_t)p->n_runs * p->tiles, runs);
+  } else {
+    p->n_runs = (int)std::min<long long>(places, room * p->tiles);
+    parts = runs = (size_t)p->n_runs;
+  }
+  const size_t slots = 2 * parts * p->tile_rows;
+  const size_t rec = round_up(runs * sizeof(int2));
   const size_t ml = round_up(slots * sizeof(float2));
   uint8_t *base = (uint8_t *)ws;
   p->rec = (int2 *)base;
@@ -449,8 +461,8 @@ size_t plan(TreeParams *p, int tile, int block, int places, void *ws) {
 }
 size_t plan(TreeParams *p, int dtype, int sms, void *ws) {
   if (dtype == RIPPLE_BF16)
-    return plan(p, kTreeTcRows, kTreeTcKeys, kTreeTcTeams * sms, ws);
-  return plan(p, kTreeSimtRows, kTreeSimtKeys, kTreeSimtCtas * sms, ws);
+    return plan(p, kTreeTcRows, kTreeTcKeys, kTreeTcTeams * sms, true, ws);
+  return plan(p, kTreeSimtRows, kTreeSimtKeys, kTreeSimtCtas * sms, false, ws);
 }
 
 // Shares of a group on the tensor cores where the table's room is short, 0 where it is not: as
@@ -548,14 +560,14 @@ extern "C" ripple_status ripple_paged_tree_attn(
       return RIPPLE_OK;
     }
     RIPPLE_CUDA_TRY(launch_tree_tc(p, scales != nullptr, dev, sm_count(dev), st));
-    RIPPLE_CUDA_TRY((d128 ? launch_join<__nv_bfloat16, 128>(p, st)
-                          : launch_join<__nv_bfloat16, 64>(p, st)));
+    RIPPLE_CUDA_TRY((d128 ? launch_join<__nv_bfloat16, 128, false>(p, st)
+                          : launch_join<__nv_bfloat16, 64, false>(p, st)));
     return RIPPLE_OK;
   }
   RIPPLE_CUDA_TRY((scales != nullptr ? (d128 ? launch_simt<uint8_t, 128>(p, dev, st)
                                              : launch_simt<uint8_t, 64>(p, dev, st))
                                      : (d128 ? launch_simt<float, 128>(p, dev, st)
                                              : launch_simt<float, 64>(p, dev, st))));
-  RIPPLE_CUDA_TRY((d128 ? launch_join<float, 128>(p, st) : launch_join<float, 64>(p, st)));
+  RIPPLE_CUDA_TRY((d128 ? launch_join<float, 128, true>(p, st) : launch_join<float, 64, true>(p, st)));
   return RIPPLE_OK;
 }

@@ -44,7 +44,8 @@ struct TreeParams {
   long long wait_cycles;
   uint32_t suspend_ns;                   // of a poll of an mbarrier, at most
   bool tma;                              // whole blocks by TMA
-  int2 *rec;      // [n_runs] the group that begins in the run and goes on, and its runs (0: none)
+  int2 *rec;      // [n_runs] the group that begins in the run and goes on (with tiles of its own:
+                  // times tiles, plus the tile), and its runs (0: none)
   float *ws_o;    // [2 * n_runs][tiles][tile_rows][D] partials: of the group begun before, begun here
   float2 *ws_ml;  // [2 * n_runs][tiles][tile_rows] their maximum (log2) and sum
 };
@@ -93,10 +94,12 @@ __device__ __forceinline__ int run_of(long long total, int runs, long long t) {
 }
 
 // A walk over the parts of groups in a run. KB: rows of a block; COST: units of a group besides
-// its blocks.
-template <int KB, int COST>
+// its blocks; TR: query rows of a tile where every tile is a group of its own (0: a tile each
+// for other CTAs).
+template <int KB, int COST, int TR>
 struct TreeWalk {
   int b, h, len;
+  int tiles, tile;     // of the sequence, with TR; the group's
   int block;           // the part's first in its group
   int count;           // blocks of the part
   int begin, end;      // the part's rows
@@ -106,9 +109,13 @@ struct TreeWalk {
   static __device__ __forceinline__ int blocks_of(const TreeSeq &s) {
     return s.tokens > 0 ? s.len / KB + (s.len % KB != 0) : 0;
   }
-  static __device__ __forceinline__ long long units_of(const TreeSeq &s) {
+  static __device__ __forceinline__ int tiles_of(const TreeParams &p, const TreeSeq &s) {
+    return TR > 0 ? (s.tokens * p.G + TR - 1) / (TR > 0 ? TR : 1) : 1;
+  }
+  // Units of a sequence's groups of one KV head.
+  static __device__ __forceinline__ long long units_of(const TreeParams &p, const TreeSeq &s) {
     const int n = blocks_of(s);
-    return n > 0 ? n + COST : 0;
+    return n > 0 ? (long long)(n + COST) * tiles_of(p, s) : 0;
   }
   __device__ __forceinline__ int blocks() const { return len / KB + (len % KB != 0); }
   __device__ __forceinline__ void set(int first) {
@@ -127,11 +134,17 @@ struct TreeWalk {
   __device__ __forceinline__ bool next(const TreeParams &p) {
     at += blocks() + COST;
     if (at >= stop) return false;
+    if (++tile < tiles) {
+      set(0);
+      return true;
+    }
+    tile = 0;
     if (++h >= p.g.Hkv) {
       h = 0;
       for (;;) {  // at < stop: there are more
         const TreeSeq s(p, ++b);
         len = s.len;
+        tiles = tiles_of(p, s);
         if (blocks_of(s) > 0) break;
       }
     }
@@ -151,7 +164,8 @@ struct TreeWalk {
     begin = block * KB;
     end = (int)min((long long)len, (long long)(block + count) * KB);
     at = stop = total = 0;
-    runs = 0;
+    runs = tile = 0;
+    tiles = 1;
     return count > 0;
   }
   // To the run's first part, by one warp; false where the run is empty.
@@ -160,7 +174,7 @@ struct TreeWalk {
     const int per = (p.g.B + 31) / 32;
     const int b0 = min(lane * per, p.g.B), b1 = min(b0 + per, p.g.B);
     long long mine = 0;
-    for (int i = b0; i < b1; ++i) mine += units_of(TreeSeq(p, i)) * p.g.Hkv;
+    for (int i = b0; i < b1; ++i) mine += units_of(p, TreeSeq(p, i)) * p.g.Hkv;
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -177,17 +191,20 @@ struct TreeWalk {
     long long rest = t0 - (incl - mine);
     if (lane == owner) {
       for (seq = b0;; ++seq) {
-        const long long k = units_of(TreeSeq(p, seq)) * p.g.Hkv;
+        const long long k = units_of(p, TreeSeq(p, seq)) * p.g.Hkv;
         if (rest < k) break;
         rest -= k;
       }
     }
     b = __shfl_sync(kAll, seq, owner);
     rest = __shfl_sync(kAll, rest, owner);
-    len = TreeSeq(p, b).len;
+    const TreeSeq s(p, b);
+    len = s.len;
+    tiles = tiles_of(p, s);
     const int units = blocks() + COST;
-    h = (int)(rest / units);
-    const int in = (int)(rest % units);
+    const int group = (int)(rest / units), in = (int)(rest % units);
+    h = group / tiles;
+    tile = group % tiles;
     at = t0 - in;
     set(max(0, in - COST));
     return true;

@@ -264,7 +264,7 @@ template <int D, bool kCodes, int C>
 __global__ void __launch_bounds__(threads(kCodes), 1)
     tree_tc_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ Maps maps) {
   using S = Smem<D, kCodes>;
-  using W = TreeWalk<KB, kGroupCost>;
+  using W = TreeWalk<KB, kGroupCost, 0>;
   constexpr int SK = S::SK, SV = S::SV;
   constexpr int RT = kRows / C;   // query rows of the tile
   constexpr int KC = KB / C;      // keys of a block that a copy takes

@@ -107,6 +107,21 @@ def test_decode_refuses_bad_arguments(lib):
     assert lib._lib.ripple_paged_decode_q8_workspace_bytes(ctypes.byref(_desc(lib)), 8, None) == E
 
 
+def test_decode_workspace_grows_with_the_call(lib):
+    def need(hq=8, **over):
+        n = ctypes.c_size_t()
+        assert lib._lib.ripple_paged_decode_q8_workspace_bytes(ctypes.byref(_desc(lib, **over)), hq,
+                                                               ctypes.byref(n)) == lib.OK
+        return n.value
+
+    for d in (64, 128):
+        for sizes in ([need(batch=b, head_dim=d) for b in range(1, 400)],
+                      [need(max_pages=m, head_dim=d) for m in range(1, 3000, 7)],
+                      [need(hq=2 * g, head_dim=d, max_pages=3000) for g in range(1, 17)],
+                      [need(hq=8 * h, n_kv_heads=h, head_dim=d) for h in range(1, 40)]):
+            assert sizes == sorted(sizes)
+
+
 def _tree(lib, desc=None, scales=None, n=12, starts=None, most=4, masks=FAKE, hq=8, scale=0.0, q=FAKE,
           qs=(4096, 1024, 128), kp=FAKE, vp=FAKE, table=FAKE, lens=FAKE, out=FAKE, lse=None, ws=FAKE,
           wsb=1 << 40, status=None):
