@@ -57,7 +57,6 @@ struct SimtSmem {
   static constexpr int LD = D + 4;  // rows of a quarter warp start in other banks
   float q[R][LD], k[KB][LD], v[KB][D];
   float p[KB][R + 4];   // probabilities; negative: the key is hidden from the row
-  float m[R], l[R], a[R];
   uint64_t mask[R];
 };
 
@@ -113,14 +112,16 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
       if (tid < n_rows)
         mask = p.masks == nullptr ? ~0ull >> (63 - tok) : p.masks[seq.first + tok];
       s.mask[tid] = mask;
-      s.m[tid] = -INFINITY;
-      s.l[tid] = 0.f;
     }
     float o[4][DT];
+    float m[4], l[4];  // of the thread's rows, the same in the 16 threads of a row
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
 #pragma unroll
       for (int j = 0; j < DT; ++j) o[i][j] = 0.f;
+    }
     const int rg = tid / 16 * 4, cg = tid % 16;  // rows rg.., keys cg and cg + 16, dims 4 cg + 64 j..
 
     uint4 kx[kMine], vx[kMine];
@@ -157,21 +158,24 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
     load(w.begin);
     for (int row0 = w.begin; row0 < w.end; row0 += KB) {
       __syncthreads();  // the block before has been read
-      if (tid == 0) row_there = 0;
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
         const int e = tid + i * kThreads, r = e / kPieces, c = e % kPieces * P::N;
         P::put(&s.k[r][c], kx[i], kCodes ? ksc[i % (kCodes ? kMine : 1)] : 1.f);
         P::put(&s.v[r][c], vx[i], kCodes ? vsc[i % (kCodes ? kMine : 1)] : 1.f);
       }
-      __syncthreads();
+      uint32_t present = 0xffffffffu;
+      if (!__syncthreads_and(there == (1u << kMine) - 1)) {  // which rows are there
+        if (tid == 0) row_there = 0;
+        __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        const int e = tid + i * kThreads;
-        if (e % kPieces == 0 && (there >> i & 1)) atomicOr(&row_there, 1u << (e / kPieces));
+        for (int i = 0; i < kMine; ++i) {
+          const int e = tid + i * kThreads;
+          if (e % kPieces == 0 && (there >> i & 1)) atomicOr(&row_there, 1u << (e / kPieces));
+        }
+        __syncthreads();
+        present = row_there;
       }
-      __syncthreads();
-      const uint32_t present = row_there;
       if (row0 + KB < w.end) load(row0 + KB);
       // scores (warps of rows that are none have nothing to do)
       const bool busy = rg - rg % 8 < n_rows;
@@ -200,45 +204,50 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
 #pragma unroll
           for (int j = 0; j < 2; ++j) x[i][j] = d[i][j].x + d[i][j].y;
       }
-      // the 16 threads of a row are half a warp
+      // the 16 threads of a row are half a warp; the four rows' steps side by side
+      if (busy) {
+        bool on[4][2];
+        float mb[4], sum[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (!busy) break;
-        const int r = rg + i;
-        const uint64_t mask = s.mask[r];
-        bool on[2];
+        for (int i = 0; i < 4; ++i) {
+          const uint64_t mask = s.mask[rg + i];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int c = cg + 16 * j;
-          const long long of_draft = row0 + c - seq.prefix;
-          on[j] = (present >> c & 1) && (of_draft < 0 || (mask >> (of_draft & 63) & 1));
-          if (!on[j]) x[i][j] = -INFINITY;
-        }
-        float mb = fmaxf(x[i][0], x[i][1]);
-#pragma unroll
-        for (int k = 1; k < 16; k <<= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, k));
-        const float was = s.m[r];
-        const float m = mb > was + kSlack ? mb : was;
-        const float sub = m == -INFINITY ? 0.f : m;
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float e = on[j] ? fast_exp2(x[i][j] - sub) : 0.f;
-          sum += e;
-          s.p[cg + 16 * j][r] = on[j] ? e : -1.f;
+          for (int j = 0; j < 2; ++j) {
+            const int c = cg + 16 * j;
+            const long long of_draft = row0 + c - seq.prefix;
+            on[i][j] = (present >> c & 1) && (of_draft < 0 || (mask >> (of_draft & 63) & 1));
+            if (!on[i][j]) x[i][j] = -INFINITY;
+          }
+          mb[i] = fmaxf(x[i][0], x[i][1]);
         }
 #pragma unroll
-        for (int k = 1; k < 16; k <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-        __syncwarp();  // s.m has been read
-        const float a = m == was ? 1.f : fast_exp2(was - m);
-        if (cg == 0) {
-          s.m[r] = m;
-          s.l[r] = s.l[r] * a + sum;
-        }
-        if (a != 1.f) {
+        for (int k = 1; k < 16; k <<= 1)
 #pragma unroll
-          for (int j = 0; j < DT; ++j) o[i][j] *= a;
+          for (int i = 0; i < 4; ++i) mb[i] = fmaxf(mb[i], __shfl_xor_sync(0xffffffffu, mb[i], k));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (mb[i] > m[i] + kSlack) {
+            const float a = fast_exp2(m[i] - mb[i]);
+            m[i] = mb[i];
+            l[i] *= a;
+#pragma unroll
+            for (int j = 0; j < DT; ++j) o[i][j] *= a;
+          }
+          const float sub = m[i] == -INFINITY ? 0.f : m[i];
+          sum[i] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float e = on[i][j] ? fast_exp2(x[i][j] - sub) : 0.f;
+            sum[i] += e;
+            s.p[cg + 16 * j][rg + i] = on[i][j] ? e : -1.f;
+          }
         }
+#pragma unroll
+        for (int k = 1; k < 16; k <<= 1)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l[i] += sum[i];
       }
       __syncthreads();
       // outputs: a negative probability's key counts for nothing, whatever its value holds
@@ -274,10 +283,9 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
     for (int i = 0; i < 4; ++i) {
       const int r = rg + i;
       if (r >= n_rows) continue;
-      const float m = s.m[r], l = s.l[r];
       const int row = tile * R + r;
       const long long at = (long long)(seq.first + row / p.G) * p.Hq + w.h * p.G + row % p.G;
-      const float inv = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;  // 0: no row counts
+      const float inv = !whole ? 1.f : l[i] != 0.f ? 1.f / l[i] : 0.f;  // 0: no row counts
       float *to = whole ? (float *)p.out + at * D : p.ws_o + (slot + r) * D;
 #pragma unroll
       for (int j = 0; j < DT; j += 4)
@@ -285,9 +293,9 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
              make_float4(o[i][j] * inv, o[i][j + 1] * inv, o[i][j + 2] * inv, o[i][j + 3] * inv));
       if (cg == 0) {
         if (!whole)
-          p.ws_ml[slot + r] = make_float2(m, l);
+          p.ws_ml[slot + r] = make_float2(m[i], l[i]);
         else if (p.lse != nullptr)
-          p.lse[at] = tree_lse(m, l);
+          p.lse[at] = tree_lse(m[i], l[i]);
       }
     }
     __syncthreads();
