@@ -155,7 +155,7 @@ __device__ __forceinline__ int find_seq(const int32_t *starts, int B, int t, int
 
 // kAhead: groups whose loads are in flight at a time. kCodes: 8-bit pages.
 template <typename T, int D, bool kInter, int kAhead, bool kCodes>
-__global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 6 : 1)
+__global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 8 : 1)
     append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int kLanes = D / 16;       // lanes per head row
   constexpr int kRows = 32 / kLanes;   // head rows per warp step
@@ -178,10 +178,11 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 
   // The rows of kAhead groups from g on, as they are.
   const int g_end = min(p.groups, (part + 1) * p.per_warp);
   Raw8<T> x[kAhead], y[kAhead];
-  auto load_one = [&](int g, int u, int b, int i) {
-    {
+  auto load = [&](int g, int b, int i) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
       const int r = (g + u) * kRows + sub;
-      if (g + u >= g_end || r >= n_rows) return;
+      if (g + u >= g_end || r >= n_rows) continue;
       const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.g.Hkv;
       const TokenRows &src = is_q ? p.q : is_v ? p.v : p.k;
       const int h = is_q ? r : is_v ? r - p.Hq - p.g.Hkv : r - p.Hq;
@@ -189,10 +190,6 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 
       x[u] = load_raw(from + o0);
       y[u] = load_raw(from + o1);
     }
-  };
-  auto load = [&](int g, int b, int i) {
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) load_one(g, u, b, i);
   };
   // where a token lies does not depend on its sequence with seq_starts (strides by t alone)
   const int src_b = b, src_i = i;
@@ -258,73 +255,67 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 
 
   // What becomes of group g + u.
   auto finish = [&](int u) {
-    {
-      const int r = (g + u) * kRows + sub;
-      if (g + u >= g_end || r >= n_rows) return;
-      const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.g.Hkv;
-      if (!is_q && place < 0) return;
-      const int h = is_q ? r : is_v ? r - p.Hq - p.g.Hkv : r - p.Hq;
-      float a[8], d[8];
-      const bool turned = turns && !is_v;
-      if (turned || (kCodes && !is_q)) {
-        unpack(x[u], a);
-        unpack(y[u], d);
-      }
-      if (turned) {
-        if (kInter) {  // pairs (0, 1), (2, 3), .. of the 16 elements a, d
+    const int r = (g + u) * kRows + sub;
+    if (g + u >= g_end || r >= n_rows) return;
+    const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.g.Hkv;
+    if (!is_q && place < 0) return;
+    const int h = is_q ? r : is_v ? r - p.Hq - p.g.Hkv : r - p.Hq;
+    float a[8], d[8];
+    const bool turned = turns && !is_v;
+    if (turned || (kCodes && !is_q)) {
+      unpack(x[u], a);
+      unpack(y[u], d);
+    }
+    if (turned) {
+      if (kInter) {  // pairs (0, 1), (2, 3), .. of the 16 elements a, d
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float a0 = a[2 * j], a1 = a[2 * j + 1], d0 = d[2 * j], d1 = d[2 * j + 1];
-            a[2 * j] = a0 * c[j] - a1 * s[j];
-            a[2 * j + 1] = a1 * c[j] + a0 * s[j];
-            d[2 * j] = d0 * c[4 + j] - d1 * s[4 + j];
-            d[2 * j + 1] = d1 * c[4 + j] + d0 * s[4 + j];
-          }
-        } else {  // pairs (a_j, d_j)
+        for (int j = 0; j < 4; ++j) {
+          const float a0 = a[2 * j], a1 = a[2 * j + 1], d0 = d[2 * j], d1 = d[2 * j + 1];
+          a[2 * j] = a0 * c[j] - a1 * s[j];
+          a[2 * j + 1] = a1 * c[j] + a0 * s[j];
+          d[2 * j] = d0 * c[4 + j] - d1 * s[4 + j];
+          d[2 * j + 1] = d1 * c[4 + j] + d0 * s[4 + j];
+        }
+      } else {  // pairs (a_j, d_j)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float a0 = a[j], d0 = d[j];
-            a[j] = a0 * c[j] - d0 * s[j];
-            d[j] = d0 * c[j] + a0 * s[j];
-          }
+        for (int j = 0; j < 8; ++j) {
+          const float a0 = a[j], d0 = d[j];
+          a[j] = a0 * c[j] - d0 * s[j];
+          d[j] = d0 * c[j] + a0 * s[j];
         }
       }
-      if (kCodes && !is_q) {
-        uint32_t most = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          most = max(most, max(__float_as_uint(a[j]) & 0x7fffffffu, __float_as_uint(d[j]) & 0x7fffffffu));
-        const uint32_t row_lanes = ((1u << kLanes) - 1) << (sub * kLanes);
-#pragma unroll
-        for (int o = 1; o < kLanes; o <<= 1) most = max(most, __shfl_xor_sync(row_lanes, most, o));
-        const int byte = scale_byte(most);
-        uint8_t *to = (uint8_t *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
-        *reinterpret_cast<uint2 *>(to + o0) = codes_of(a, byte);
-        *reinterpret_cast<uint2 *>(to + o1) = codes_of(d, byte);
-        if (l == 0) (is_v ? p.sc.v : p.sc.k)[scale_at + h * p.sc.head_stride] = (uint8_t)byte;
-        return;
-      }
-      T *to = is_q ? (T *)p.q_out.data + src_b * p.q_out.seq + src_i * p.q_out.token +
-                         h * p.q_out.head
-                   : (T *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
-      if (turned) {
-        pack(a, x[u]);
-        pack(d, y[u]);
-      }
-      store_raw(to + o0, x[u]);
-      store_raw(to + o1, y[u]);
     }
+    if (kCodes && !is_q) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        most = max(most, max(__float_as_uint(a[j]) & 0x7fffffffu, __float_as_uint(d[j]) & 0x7fffffffu));
+      const uint32_t row_lanes = ((1u << kLanes) - 1) << (sub * kLanes);
+#pragma unroll
+      for (int o = 1; o < kLanes; o <<= 1) most = max(most, __shfl_xor_sync(row_lanes, most, o));
+      const int byte = scale_byte(most);
+      uint8_t *to = (uint8_t *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
+      *reinterpret_cast<uint2 *>(to + o0) = codes_of(a, byte);
+      *reinterpret_cast<uint2 *>(to + o1) = codes_of(d, byte);
+      if (l == 0) (is_v ? p.sc.v : p.sc.k)[scale_at + h * p.sc.head_stride] = (uint8_t)byte;
+      return;
+    }
+    T *to = is_q ? (T *)p.q_out.data + src_b * p.q_out.seq + src_i * p.q_out.token +
+                       h * p.q_out.head
+                 : (T *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
+    if (turned) {
+      pack(a, x[u]);
+      pack(d, y[u]);
+    }
+    store_raw(to + o0, x[u]);
+    store_raw(to + o1, y[u]);
   };
   for (;;) {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      finish(u);
-      // (the codes take longer to make: the other groups' rows are on their way meanwhile)
-      if (kCodes) load_one(g + kAhead, u, src_b, src_i);
-    }
+    for (int u = 0; u < kAhead; ++u) finish(u);
     g += kAhead;
     if (g >= g_end) break;
-    if (!kCodes) load(g, src_b, src_i);
+    load(g, src_b, src_i);
   }
 }
 
@@ -366,8 +357,11 @@ cudaError_t launch_as(const AppendParams &p, int grid, cudaStream_t st) {
 
 template <typename T, int D, bool kCodes>
 cudaError_t launch(const AppendParams &p, bool inter, int grid, cudaStream_t st) {
-  constexpr int kMany = sizeof(T) == 2 && D == 64 ? 4 : 2;  // 4 to 8 loads of a lane in flight
-  if (p.per_warp == 1)
+  // 4 to 8 loads of a lane in flight; the codes take longer to make, and more warps with fewer loads
+  // each do better (65.6k tokens of 48 head rows: two groups at 90, 80, 72, 64 registers 300, 278,
+  // 273, 268 us, four at 128 328, one at 64 262)
+  constexpr int kMany = kCodes ? 1 : sizeof(T) == 2 && D == 64 ? 4 : 2;
+  if (kMany == 1 || p.per_warp == 1)
     return inter ? launch_as<T, D, true, 1, kCodes>(p, grid, st)
                  : launch_as<T, D, false, 1, kCodes>(p, grid, st);
   return inter ? launch_as<T, D, true, kMany, kCodes>(p, grid, st)

@@ -37,7 +37,7 @@ extern "C" ripple_status ripple_paged_decode_workspace_bytes(const ripple_paged_
   if (!decode_args(desc, n_q_heads, &p) || bytes_host == nullptr) return RIPPLE_EINVAL;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
-  *bytes_host = plan(&p, block_rows(desc), kWarpsPerSm, sm_count(dev), nullptr);
+  *bytes_host = plan(&p, block_rows(desc), kWarpsPerSm, true, sm_count(dev), nullptr);
   return RIPPLE_OK;
 }
 
@@ -59,7 +59,7 @@ extern "C" ripple_status ripple_paged_decode_attn(
   int dev = 0;
   const cudaError_t got = cudaGetDevice(&dev);
   if (got != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
-  if (workspace_bytes < plan(&p, block_rows(desc), kWarpsPerSm, sm_count(dev), workspace)) return RIPPLE_EWORKSPACE;
+  if (workspace_bytes < plan(&p, block_rows(desc), kWarpsPerSm, true, sm_count(dev), workspace)) return RIPPLE_EWORKSPACE;
   if (got != cudaSuccess) return RIPPLE_ECUDA;
   p.scale2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)desc->head_dim)) * kLog2e;
   p.q = q;

@@ -1181,12 +1181,13 @@ bool query_strides(const ripple_paged_desc *d, int n_q_heads, const ripple_token
 // Runs of a call and the workspace: records, (max, sum), outputs of the partials. The runs are
 // bounded by the blocks that the table has room for, so that small caches take few CTAs;
 // everything grows with the call. Returns the bytes; fills p's pointers if given a base.
-size_t plan(PagedDecParams *p, int block_rows, int warps_per_sm, int sms, void *ws) {
+// `phased`: more than one phase may be.
+size_t plan(PagedDecParams *p, int block_rows, int warps_per_sm, bool phased, int sms, void *ws) {
   const int rows = block_rows;
   const long long room =
       (((long long)p->g.max_pages << p->g.shift) + rows - 1) / rows * p->g.B * p->g.Hkv;
   p->places = sms * warps_per_sm;
-  const int phases = (long long)p->g.B * p->g.Hkv <= kFewGroups ? 1 : kPhases;
+  const int phases = !phased || (long long)p->g.B * p->g.Hkv <= kFewGroups ? 1 : kPhases;
   p->n_runs = (int)std::min<long long>(phases * p->places, room);
   const size_t slots = 2 * (size_t)p->n_runs;
   const size_t rec = round_up(p->n_runs * sizeof(int2));

@@ -47,7 +47,7 @@ constexpr int kRows = kTreeTcRows;
 // % 4) on.)
 constexpr int kTeams = 2;
 __host__ __device__ constexpr int threads(bool codes) { return 32 * (10 + kTeams * (codes ? 4 : 2)); }
-constexpr int kGroupCost = 4;  // blocks that a group's queries and outputs take as long as
+constexpr int kGroupCost = 7;  // blocks that a group's queries and outputs take as long as
 constexpr int kRing = 2;       // blocks of 8-bit rows on their way or being widened
 constexpr uint32_t kTeamCols = 256;  // of TMEM: S and P of two blocks (64 each), O (d) from 128 on
 constexpr uint32_t kOCol = 128;
