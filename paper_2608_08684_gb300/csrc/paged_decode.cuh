@@ -857,7 +857,12 @@ constexpr int kMaxCluster = 8;
 // and 9.4, of 4000 15.8 and 10.4; and where lengths are far apart: 64 of 66 to 4000 rows, 16 heads
 // on one KV head, 29.5 and 21.9; 64 of 33 to 2000, 7 on each of 4, 32.1 and 25.2; 9 of which one
 // has 5979 and the next 1792, 7 on each of 4, 15.7 and 14.0 (1437 and 897: 7.9 and 10.9).
-constexpr int kShortFew = 8, kShortMany = 32;
+// Over codes (blocks of twice the rows, made floats by the warp that multiplies them) the runs' even
+// shares win sooner: D 128, 8 KV heads, 4 heads a group, clusters and runs: 128 sequences of up to
+// 3000 rows 71.3 and 44.6, of 3000 each 162.9 and 128.9, 64 of 1000 35.8 and 31.9, of 2000 62.0 and
+// 50.5, 32 of up to 1000 14.9 and 14.0; but 32 of 500 11.7 and 15.1, 8 of 1000 8.5 and 11.6, one of
+// 470 6.1 and 10.7, of 2000 7.7 and 8.4, of 4000 (behind the bound) 10.6 and 10.8.
+constexpr int kShortFew = 8, kShortMany = 32, kShortCodes = 4;
 
 template <typename T, int D, int G>
 struct ShortSmem {
@@ -1239,7 +1244,7 @@ int short_cluster(const PagedDecParams &p, int sms) {
   // soon (a block each, clusters and runs: 400 groups 6.5 and 8.2 us, 1024 groups of d 64
   // 12.3 and 9.0, 2048 of d 128 18.6 and 10.5)
   if (rows <= Cfg<T, D, G>::RB && groups > 2 * places(1)) return 0;
-  const int most = groups * ctas >= sms ? kShortMany : kShortFew;
+  const int most = sizeof(T) == 1 ? kShortCodes : groups * ctas >= sms ? kShortMany : kShortFew;
   return rows <= (long long)ctas * kShortWarps * most * Cfg<T, D, G>::RB ? ctas : 0;
 }
 
