@@ -18,13 +18,21 @@
 // other's blocks are on their way. (Two CTAs of one team each do not find a place on an SM at
 // the same time, though registers, shared memory and TMEM have room.)
 //
-// P in one bf16 part: the output is rounded to bf16 as well, and a probability's rounding
-// (2^-9) enters the output as part of a mean. The sum is of the unrounded ones, in fp32.
+// Measured, D 128, 8 KV heads: 48 sequences of up to 32768 rows, 2 to 12 tokens of 32 heads 163 us
+// (1.01 GB, 91% of the copy rate; with one team a CTA and no copies of the query rows 285); 3 of about
+// 31000 rows with 64 tokens of 64 heads 193 us (196 GFLOP, 1.02 PFLOP/s): there the chain scores -
+// softmax - product of a block, two of them an SM, leaves the tensor pipe half idle; 8-bit pages,
+// 32 sequences of up to 32768 rows, 16 tokens 161 us (419 MB, 38%): bound by the widening warps'
+// instructions. One sequence of 900 rows and 4 tokens 14.0 us: the launch, lengths, table, queries,
+// two blocks, the join of the copies and of the shares, one after the other.
 //
-// 8-bit pages come into a ring of their own, two blocks ahead, and warps 5 and 6 make them fp16
-// values: a code (exact in fp16) times its row's scale over the largest scale of the block (keys;
-// the block's scores are multiplied by that) or of the run's blocks so far (values; the outputs
-// are brought to a larger one as they are to a larger maximum). A row whose scale is 2^-15
+// P in one bf16 part: the output is rounded to bf16 as well, and a probability's rounding
+// (2^-8) enters the output as part of a mean. The sum is of the unrounded ones, in fp32.
+//
+// 8-bit pages come into a ring of their own, two blocks ahead, and two warps each for keys and values
+// make them fp16 values: a code (exact in fp16) times its row's scale over the largest scale of the
+// block (keys; the block's scores are multiplied by that) or of the run's blocks so far (values; the
+// outputs are brought to a larger one as they are to a larger maximum). A row whose scale is 2^-15
 // of that or more stays exact; others are off by 2^-25 of the largest at most, less than
 // fp32 sums lose. A query row is multiplied by the power of two that brings its largest element
 // to [2^14, 2^15). P has 2^7 more than for bf16, so that what it loses at the lower end (2^-32 a
@@ -34,6 +42,7 @@
 
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
+#include <float.h>
 
 #include <atomic>
 
@@ -47,7 +56,10 @@ constexpr int kRows = kTreeTcRows;
 // % 4) on.)
 constexpr int kTeams = 2;
 __host__ __device__ constexpr int threads(bool codes) { return 32 * (10 + kTeams * (codes ? 4 : 2)); }
-constexpr int kGroupCost = 7;  // blocks that a group's queries and outputs take as long as
+// Blocks that a group's queries and outputs take as long as (their copies' join in the main). us for
+// 2, 4, 7, 10, 14, D 128, 4 heads a KV head: 48 sequences of up to 32768 rows and 2 to 12 tokens
+// 186.5, 163.0, 163.3, 165.6, 168.5; 8-bit pages, 32 sequences of 16 tokens 210, 188, 161, 163, 169.
+constexpr int kGroupCost = 7;
 constexpr int kRing = 2;       // blocks of 8-bit rows on their way or being widened
 constexpr uint32_t kTeamCols = 256;  // of TMEM: S and P of two blocks (64 each), O (d) from 128 on
 constexpr uint32_t kOCol = 128;
@@ -818,7 +830,9 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           float rs = row_scale, a = 1.f, a_o = 1.f;
           bool grow = false;
           if constexpr (kCodes) {
-            rs *= pow2(sy->top[0][n % kSlots] - 127);
+            // (a positive number: hidden keys' -infinity stays that; scores have 2^-95 at most
+            // where fp32 has no smaller factor)
+            rs = fminf(fmaxf(rs * pow2(sy->top[0][n % kSlots] - 127), FLT_MIN), FLT_MAX);
             const int top = sy->top[1][n % kSlots];
             grow = begun && top != v_top;
             if (grow) a_o = fast_exp2((float)(v_top - top));

@@ -95,11 +95,11 @@ class Pool8:
         return int(self.np_table[b, r // self.page]), r % self.page
 
 
-def any_pool(lib, kind, rows, heads, d, page, seed, layout="heads"):
+def any_pool(lib, kind, rows, heads, d, page, seed, layout="heads", width=0):
     """kind: bf16, f32, or the queries' type over 8-bit pages: q8-bf16, q8-f32."""
     if kind.startswith("q8"):
-        return Pool8(lib, rows, heads, d, page, kind[3:], seed, layout)
-    return P.Pool(lib, rows, heads, d, page, kind, seed, layout)
+        return Pool8(lib, rows, heads, d, page, kind[3:], seed, layout, width=width)
+    return P.Pool(lib, rows, heads, d, page, kind, seed, layout, width=width)
 
 
 def type_of(kind):

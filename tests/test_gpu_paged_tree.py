@@ -85,6 +85,34 @@ def test_splits(lib, lens, counts, H, G, d, kind):
     assert torch.equal(out[:n], again[:n]) and torch.equal(lse[:n], lse2[:n])
 
 
+# (sequences, KV heads, pages of 32 rows in the table): a group's rows by one team to sixteen, of a
+# block each or of eight, with and without an even number of groups, and by runs
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("B,H,pages", [
+    (1, 1, 1), (1, 1, 2), (1, 1, 4), (1, 1, 9), (1, 1, 31), (1, 1, 256), (1, 1, 257), (3, 1, 40),
+    (19, 1, 33), (20, 1, 130), (19, 2, 16), (13, 3, 64), (38, 2, 7), (7, 11, 33), (76, 2, 4),
+    (77, 2, 16), (51, 3, 17), (152, 2, 3), (61, 5, 3), (2, 8, 1024)])
+def test_room_of_the_table(lib, B, H, pages, kind):
+    rng = np.random.default_rng(B * 1000 + pages)
+    G, d, rows = 2, 64, min(pages * 32, 5000)
+    counts = [int(n) for n in rng.integers(1, min(rows, 9) + 1, B)]
+    lens = [int(n) for n in rng.integers(0, rows + 1, B)]
+    lens = [rows if i == 0 else max(n, c) for i, (n, c) in enumerate(zip(lens, counts))]
+    if B > 4:
+        lens[3] = 0
+        counts[3] = 2
+    pool = P8.any_pool(lib, kind, lens, H, d, 32, 350 + B, width=pages)
+    assert pool.np_table.shape[1] == pages
+    q = P.randn((sum(counts), H * G, d), P8.type_of(kind), 351)
+    bits = P8.random_masks(counts, 352)
+    starts = P.i32([0] + np.cumsum(counts).tolist())
+    out, lse, st = P8.run_tree(lib, pool, q, P.i32(lens), P8.to_i64(bits), starts, max(counts))
+    assert int(st.item()) == 0
+    _check(pool, kind, q, lens, counts, bits, out, lse)
+    again, lse2, _ = P8.run_tree(lib, pool, q, P.i32(lens), P8.to_i64(bits), starts, max(counts))
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_uniform_chains_and_strides(lib, kind):
     B, n, H, G, d = 5, 6, 2, 4, 128
@@ -179,6 +207,22 @@ def test_values_before_the_draft_that_are_not_finite(lib, kind):
     assert (out[0, :, :, 5] == float("inf")).all()
     cols = [c for c in range(d) if c != 5]
     assert torch.equal(out[..., cols], base[..., cols])
+
+
+@pytest.mark.parametrize("kind", ["q8-bf16", "q8-f32"])
+@pytest.mark.parametrize("G,before", [(2, 0), (4, 300), (16, 61)])
+def test_scores_below_the_range(lib, G, before, kind):
+    # keys of 2^-118 and queries of 2^-80 (and of 0): every score is 0 to fp32, hidden rows stay hidden
+    n, H, d = 10, 1, 128
+    pool = P8.any_pool(lib, kind, [before + n], H, d, 16, 630)
+    pool.ks.fill_(7)
+    q = P.randn((1, n, G, d), "f32", 631) * 2.0 ** -80
+    q[0, 3] = 0
+    q = q.to(P.DT[P8.type_of(kind)])
+    bits = P8.random_masks([n], 8)
+    out, lse, st = P8.run_tree(lib, pool, q, P.i32([before + n]), P8.to_i64(bits).view(1, n))
+    assert int(st.item()) == 0
+    _check(pool, kind, q, [before + n], [n], bits, out, lse)
 
 
 @pytest.mark.parametrize("kind", KINDS)
