@@ -5,9 +5,10 @@
 // has 4 rows x 2 keys, outputs: 4 rows x D / 16 dims, both from shared memory by 16 bytes; the
 // next block's rows are loaded into registers meanwhile. A row's 16 threads are half a warp, so its
 // maximum and sum are shuffles. The cache's bytes are 8 d a row and the FMAs 2 n G d: above a few rows
-// a KV head the instructions bound it, 1640 a warp and block of 64 dims, of which 640 are FMAs. Every
-// row tile is a group of its own (sequences of few tokens have fewer tiles, and CTAs of all tiles would
-// idle beside them). 7 sequences of up to 6000 rows, 1 to 9 tokens of 28 heads on 4, d 64: 44 us.
+// a KV head the instructions bound it, about 1400 a warp and block of 64 dims, of which 512 are FMAs, two
+// of them in each. Every row tile is a group of its own (sequences of few tokens have fewer tiles, and CTAs
+// of all tiles would idle beside them). 7 sequences of up to 6000 rows, 1 to 9 tokens of 28 heads on 4,
+// d 64: 40.5 us (four and five CTAs an SM at 128 and 96 registers: 41.2 and 45.4).
 #include "paged_tree.cuh"
 
 #include <cuda_fp16.h>
@@ -115,14 +116,14 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
         mask = p.masks == nullptr ? ~0ull >> (63 - tok) : p.masks[seq.first + tok];
       s.mask[tid] = mask;
     }
-    float o[4][DT];
+    float2 o[4][DT / 2];
     float m[4], l[4];  // of the thread's rows, the same in the 16 threads of a row
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       m[i] = -INFINITY;
       l[i] = 0.f;
 #pragma unroll
-      for (int j = 0; j < DT; ++j) o[i][j] = 0.f;
+      for (int j = 0; j < DT / 2; ++j) o[i][j] = make_float2(0.f, 0.f);
     }
     const int rg = tid / 16 * 4, cg = tid % 16;  // rows rg.., keys cg and cg + 16, dims 4 cg + 64 j..
 
@@ -233,7 +234,7 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
             m[i] = mb[i];
             l[i] *= a;
 #pragma unroll
-            for (int j = 0; j < DT; ++j) o[i][j] *= a;
+            for (int j = 0; j < DT / 2; ++j) o[i][j] = __fmul2_rn(o[i][j], make_float2(a, a));
           }
           const float sub = m[i] == -INFINITY ? 0.f : m[i];
           sum[i] = 0.f;
@@ -264,10 +265,9 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               if (hidden && pp[i] < 0.f) continue;
-              o[i][j] = fmaf(pp[i], vv.x, o[i][j]);
-              o[i][j + 1] = fmaf(pp[i], vv.y, o[i][j + 1]);
-              o[i][j + 2] = fmaf(pp[i], vv.z, o[i][j + 2]);
-              o[i][j + 3] = fmaf(pp[i], vv.w, o[i][j + 3]);
+              const float2 both = make_float2(pp[i], pp[i]);
+              o[i][j / 2] = __ffma2_rn(both, make_float2(vv.x, vv.y), o[i][j / 2]);
+              o[i][j / 2 + 1] = __ffma2_rn(both, make_float2(vv.z, vv.w), o[i][j / 2 + 1]);
             }
           }
         }
@@ -292,7 +292,8 @@ __global__ void __launch_bounds__(kThreads, kTreeSimtCtas)
 #pragma unroll
       for (int j = 0; j < DT; j += 4)
         put4(to + 4 * cg + 16 * j,
-             make_float4(o[i][j] * inv, o[i][j + 1] * inv, o[i][j + 2] * inv, o[i][j + 3] * inv));
+             make_float4(o[i][j / 2].x * inv, o[i][j / 2].y * inv, o[i][j / 2 + 1].x * inv,
+                         o[i][j / 2 + 1].y * inv));
       if (cg == 0) {
         if (!whole)
           p.ws_ml[slot + r] = make_float2(m[i], l[i]);
