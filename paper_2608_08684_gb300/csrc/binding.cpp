@@ -9,6 +9,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <memory>
 #include <vector>
 
@@ -303,7 +304,7 @@ PyObject *paged_tree_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
       if (PyErr_Occurred()) throw Refused{nullptr};
       need(most >= 0 && most <= RIPPLE_MAX_DRAFT, "too many tokens of a sequence");
     } else if (!ragged) {
-      most = q.lead[1];
+      most = std::max<int64_t>(1, q.lead[1]);
       need(most <= RIPPLE_MAX_DRAFT, "too many tokens of a sequence");
     }
     float *lse = nullptr;

@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(kThreads) keep_kernel(const __grid_constant__ 
     const int len = p.lens[at];
     const int n_b = p.per_seq > 0 || p.starts == nullptr ? p.per_seq : p.starts[b + 1] - p.starts[b];
     const long long first = (long long)len - n_b;
-    const bool idle = len <= 0, short_of = !idle && first < 0;
+    const bool idle = len <= 0, short_of = !idle && (first < 0 || n_b < 0);  // no such draft
     // how many entries count: up to the first that is negative, no token or does not ascend
     int n = 0;
     bool bad = short_of;

@@ -480,6 +480,8 @@ class PagedCache:
                     not k_scales.dtype is v_scales.dtype is torch.float8_e8m0fnu:
                 raise ValueError("k_scales and v_scales must be float8_e8m0fnu "
                                  "[n_pages][Hkv][page_size], alike")
+            if k_scales.numel() > 1 and not any(k_scales.stride()):
+                raise ValueError("k_scales and v_scales must have a place for every row")
             if k_scales.get_device() != self.device or v_scales.get_device() != self.device:
                 raise ValueError("expected CUDA tensors on one device")
             self.scales = PagedScales(k_scales.data_ptr(), v_scales.data_ptr(), *k_scales.stride())
@@ -512,7 +514,8 @@ def ripple_paged_append(cache: PagedCache, lens, k, v, rope: Rope | None = None,
     their queries q into q_out (which may be q). k, v: [B][Hkv][d] (one token per sequence),
     [B][n][Hkv][d], or with seq_starts (int32 [B + 1]) [tokens][Hkv][d]; q, q_out likewise
     with the query heads; any strides with the dims consecutive. lens (int32 [B]) counts the
-    new tokens (8-bit pages: ripple_paged_append_q8); positions: int32, k's leading sizes, or None (a token's cache row)."""
+    new tokens; positions: int32, k's leading sizes, or None (a token's cache row). 8-bit pages:
+    ripple_paged_append_q8."""
     st = _binding.paged_append(_paged_append[cache.codes], cache._handle, None if rope is None else rope._addr,
                                lens, k, v, positions, seq_starts, q, q_out, dev_status,
                                None if stream is None else _stream(stream))
@@ -579,6 +582,8 @@ class KeepTables:
         if any(bytes(c.desc) != bytes(c0.desc) or c.codes != c0.codes or c.device != c0.device
                for c in caches):
             raise ValueError("the layers' caches must be of one shape, dtype and device")
+        if len({t.data_ptr() for c in caches for t in c._keep[:2]}) != 2 * L:
+            raise ValueError("the layers' pools must be apart")
         self.desc, self.device = c0.desc, c0.device
         self._handle = _binding.keep_tables([c._handle for c in caches])
         self._keep = caches

@@ -123,6 +123,19 @@ def test_entries_that_are_none(lib, kind):
     assert all(torch.equal(a, b) for a, b in zip(_tensors(pool), was))
 
 
+def test_drafts_of_descending_starts_change_nothing(lib):
+    pool = P8.any_pool(lib, "bf16", [40, 40, 40], 2, 64, 16, 55)
+    tables = lib.KeepTables([pool.cache])
+    was = [t.clone() for t in _tensors(pool)]
+    for kept in ([[0, -1], [-1, -1], [-1, -1]], [[0, 1], [0, 1], [0, 1]]):
+        st, lens_t = torch.zeros(1, dtype=torch.int32, device=DEV), P.i32([[40, 40, 40]])
+        lib.ripple_paged_keep_rows(tables, lens_t, P.i32(kept), seq_starts=P.i32([0, 4, 1, 3]),
+                                   dev_status=st)
+        n = [len([e for e in k if e >= 0]) for k in kept]
+        assert lens_t.tolist() == [[36 + n[0], 40, 38 + n[2]]] and int(st.item()) == lib.EBOUNDS
+        assert all(torch.equal(a, b) for a, b in zip(_tensors(pool), was))
+
+
 def test_a_captured_call_reads_what_is_accepted_at_its_time(lib):
     L, n = 2, 6
     lens = [[50, 20], [33, 48]]
@@ -150,6 +163,8 @@ def test_binding_refuses_wrong_shapes(lib):
         lib.KeepTables([pools[0].cache, other.cache])
     with pytest.raises(ValueError):
         lib.KeepTables([])
+    with pytest.raises(ValueError):  # a layer twice: its rows would be moved twice at a time
+        lib.KeepTables([pools[0].cache, pools[1].cache, pools[0].cache])
     t = lib.KeepTables([p.cache for p in pools])
     lens, kept = P.i32([[20, 20]] * 2), P.i32([[0, 1]] * 2)
     before = lib.ripple_kernel_launches()

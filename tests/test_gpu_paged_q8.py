@@ -370,3 +370,11 @@ def test_streams_and_graphs_that_share_a_workspace(lib):
     torch.cuda.synchronize()
     ref, _ = P.decode_ref(pools[1], qs[1], [3, 4999])
     C.assert_decode_close(outs[1].cpu().numpy(), ref)
+
+
+def test_scales_without_a_place_for_every_row_are_refused(lib):
+    pool = P8.Pool8(lib, [20, 20], 2, 64, 8, "bf16", 990)
+    f8, e8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    one = torch.full((1, 1, 1), 127, dtype=torch.uint8, device=DEV).expand(pool.ks.shape).view(e8)
+    with pytest.raises(ValueError):  # (strides of 0 alone mean dense ones to the C call)
+        lib.PagedCache(pool.k.view(f8), pool.v.view(f8), pool.table, k_scales=one, v_scales=one)

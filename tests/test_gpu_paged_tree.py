@@ -365,6 +365,18 @@ def test_streams_and_graphs_that_share_a_workspace(lib, kind):
         assert torch.equal(o, w)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_no_tokens(lib, kind):
+    pool = P8.any_pool(lib, kind, [8, 8], 2, 64, 8, 1290)
+    ws = torch.empty(lib.ripple_paged_tree_workspace_bytes(pool.cache, 4, 3), dtype=torch.uint8, device=DEV)
+    before = lib.ripple_kernel_launches()
+    for shape, starts in (((2, 0, 4, 64), None), ((0, 4, 64), P.i32([0, 0, 0]))):
+        q = torch.zeros(shape, dtype=P.DT[P8.type_of(kind)], device=DEV)
+        lib.ripple_paged_tree_attn(pool.cache, q, P.i32([8, 8]), torch.empty_like(q), ws, seq_starts=starts,
+                                   max_tokens=None if starts is None else 3)
+    assert lib.ripple_kernel_launches() == before
+
+
 def test_binding_refuses_wrong_shapes(lib):
     pool = P.Pool(lib, [8, 8], 2, 64, 8, "f32", 1300)
     q, out = torch.zeros(2, 3, 4, 64, device=DEV), torch.zeros(2, 3, 4, 64, device=DEV)
