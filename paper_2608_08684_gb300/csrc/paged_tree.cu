@@ -23,7 +23,9 @@ constexpr int kMaxDevices = 64;
 constexpr int kThreads = 128;
 constexpr int R = kTreeSimtRows, KB = kTreeSimtKeys;
 constexpr float kSlack = 8.f;
-constexpr int kGroupCost = 1;  // blocks that a group's queries and outputs take as long as
+// Blocks that a group's queries and outputs take as long as (0, 1, 2, 4: 41.6, 40.2, 40.1, 40.4 us for the
+// batch above, 29.4, 26.5, 29.7, 28.9 for 54 sequences of up to 148 rows and 43 tokens).
+constexpr int kGroupCost = 1;
 
 // 16 bytes of a page's row: 4 fp32 values, or 16 codes.
 template <typename T>
