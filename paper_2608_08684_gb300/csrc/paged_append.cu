@@ -155,7 +155,7 @@ __device__ __forceinline__ int find_seq(const int32_t *starts, int B, int t, int
 
 // kAhead: groups whose loads are in flight at a time. kCodes: 8-bit pages.
 template <typename T, int D, bool kInter, int kAhead, bool kCodes>
-__global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 8 : 1)
+__global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 8 : 0)
     append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int kLanes = D / 16;       // lanes per head row
   constexpr int kRows = 32 / kLanes;   // head rows per warp step
@@ -253,66 +253,68 @@ __global__ void __launch_bounds__(kAppendWarps * 32, kCodes && sizeof(T) == 2 ? 
     }
   }
 
-  // What becomes of group g + u.
-  auto finish = [&](int u) {
-    const int r = (g + u) * kRows + sub;
-    if (g + u >= g_end || r >= n_rows) return;
-    const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.g.Hkv;
-    if (!is_q && place < 0) return;
-    const int h = is_q ? r : is_v ? r - p.Hq - p.g.Hkv : r - p.Hq;
-    float a[8], d[8];
-    const bool turned = turns && !is_v;
-    if (turned || (kCodes && !is_q)) {
-      unpack(x[u], a);
-      unpack(y[u], d);
-    }
-    if (turned) {
-      if (kInter) {  // pairs (0, 1), (2, 3), .. of the 16 elements a, d
+  auto turn = [&](float (&a)[8], float (&d)[8]) {
+    if (kInter) {  // pairs (0, 1), (2, 3), .. of the 16 elements a, d
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float a0 = a[2 * j], a1 = a[2 * j + 1], d0 = d[2 * j], d1 = d[2 * j + 1];
-          a[2 * j] = a0 * c[j] - a1 * s[j];
-          a[2 * j + 1] = a1 * c[j] + a0 * s[j];
-          d[2 * j] = d0 * c[4 + j] - d1 * s[4 + j];
-          d[2 * j + 1] = d1 * c[4 + j] + d0 * s[4 + j];
-        }
-      } else {  // pairs (a_j, d_j)
+      for (int j = 0; j < 4; ++j) {
+        const float a0 = a[2 * j], a1 = a[2 * j + 1], d0 = d[2 * j], d1 = d[2 * j + 1];
+        a[2 * j] = a0 * c[j] - a1 * s[j];
+        a[2 * j + 1] = a1 * c[j] + a0 * s[j];
+        d[2 * j] = d0 * c[4 + j] - d1 * s[4 + j];
+        d[2 * j + 1] = d1 * c[4 + j] + d0 * s[4 + j];
+      }
+    } else {  // pairs (a_j, d_j)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float a0 = a[j], d0 = d[j];
-          a[j] = a0 * c[j] - d0 * s[j];
-          d[j] = d0 * c[j] + a0 * s[j];
-        }
+      for (int j = 0; j < 8; ++j) {
+        const float a0 = a[j], d0 = d[j];
+        a[j] = a0 * c[j] - d0 * s[j];
+        d[j] = d0 * c[j] + a0 * s[j];
       }
     }
-    if (kCodes && !is_q) {
-      uint32_t most = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        most = max(most, max(__float_as_uint(a[j]) & 0x7fffffffu, __float_as_uint(d[j]) & 0x7fffffffu));
-      const uint32_t row_lanes = ((1u << kLanes) - 1) << (sub * kLanes);
-#pragma unroll
-      for (int o = 1; o < kLanes; o <<= 1) most = max(most, __shfl_xor_sync(row_lanes, most, o));
-      const int byte = scale_byte(most);
-      uint8_t *to = (uint8_t *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
-      *reinterpret_cast<uint2 *>(to + o0) = codes_of(a, byte);
-      *reinterpret_cast<uint2 *>(to + o1) = codes_of(d, byte);
-      if (l == 0) (is_v ? p.sc.v : p.sc.k)[scale_at + h * p.sc.head_stride] = (uint8_t)byte;
-      return;
-    }
-    T *to = is_q ? (T *)p.q_out.data + src_b * p.q_out.seq + src_i * p.q_out.token +
-                       h * p.q_out.head
-                 : (T *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
-    if (turned) {
-      pack(a, x[u]);
-      pack(d, y[u]);
-    }
-    store_raw(to + o0, x[u]);
-    store_raw(to + o1, y[u]);
   };
   for (;;) {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) finish(u);
+    for (int u = 0; u < kAhead; ++u) {
+      const int r = (g + u) * kRows + sub;
+      if (g + u >= g_end || r >= n_rows) continue;
+      const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.g.Hkv;
+      if (!is_q && place < 0) continue;
+      const int h = is_q ? r : is_v ? r - p.Hq - p.g.Hkv : r - p.Hq;
+      if constexpr (kCodes) {
+        if (!is_q) {
+          float a[8], d[8];
+          unpack(x[u], a);
+          unpack(y[u], d);
+          if (turns && !is_v) turn(a, d);
+          uint32_t most = 0;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            most = max(most, max(__float_as_uint(a[j]) & 0x7fffffffu, __float_as_uint(d[j]) & 0x7fffffffu));
+          const uint32_t row_lanes = ((1u << kLanes) - 1) << (sub * kLanes);
+#pragma unroll
+          for (int o = 1; o < kLanes; o <<= 1) most = max(most, __shfl_xor_sync(row_lanes, most, o));
+          const int byte = scale_byte(most);
+          uint8_t *to = (uint8_t *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
+          *reinterpret_cast<uint2 *>(to + o0) = codes_of(a, byte);
+          *reinterpret_cast<uint2 *>(to + o1) = codes_of(d, byte);
+          if (l == 0) (is_v ? p.sc.v : p.sc.k)[scale_at + h * p.sc.head_stride] = (uint8_t)byte;
+          continue;
+        }
+      }
+      T *to = is_q ? (T *)p.q_out.data + src_b * p.q_out.seq + src_i * p.q_out.token +
+                         h * p.q_out.head
+                   : (T *)(is_v ? p.v_pages : p.k_pages) + place + h * p.g.head_stride;
+      if (turns && !is_v) {
+        float a[8], d[8];
+        unpack(x[u], a);
+        unpack(y[u], d);
+        turn(a, d);
+        pack(a, x[u]);
+        pack(d, y[u]);
+      }
+      store_raw(to + o0, x[u]);
+      store_raw(to + o1, y[u]);
+    }
     g += kAhead;
     if (g >= g_end) break;
     load(g, src_b, src_i);
@@ -357,9 +359,9 @@ cudaError_t launch_as(const AppendParams &p, int grid, cudaStream_t st) {
 
 template <typename T, int D, bool kCodes>
 cudaError_t launch(const AppendParams &p, bool inter, int grid, cudaStream_t st) {
-  // 4 to 8 loads of a lane in flight; the codes take longer to make, and more warps with fewer loads
-  // each do better (65.6k tokens of 48 head rows: two groups at 90, 80, 72, 64 registers 300, 278,
-  // 273, 268 us, four at 128 328, one at 64 262, 81% of the copy rate)
+  // 4 to 8 loads of a lane in flight. Over 8-bit pages more warps with fewer loads each do better
+  // (65.6k tokens of 48 head rows: one group at 64 registers 246 us, 86% of the copy rate, at 72 255; two
+  // at 64 252, at 72 267).
   constexpr int kMany = kCodes ? 1 : sizeof(T) == 2 && D == 64 ? 4 : 2;
   if (kMany == 1 || p.per_warp == 1)
     return inter ? launch_as<T, D, true, 1, kCodes>(p, grid, st)
