@@ -136,7 +136,7 @@ struct Rows<Codes8<Q>, D, G> {
         qs[nt][e] = p.scale2 * pow2(-__shfl_sync(kAll, up, (2 * t + e) * 4));
         m[nt][e] = -INFINITY;
         l[nt][e] = 0.f;
-        ew[nt][e] = -400;
+        ew[nt][e] = 0;
       }
 #pragma unroll
       for (int i = 0; i < PC; ++i)
@@ -206,25 +206,29 @@ struct Rows<Codes8<Q>, D, G> {
         const float a1 = sc[nt][2 + e] * s1.x, b1 = s1.y * qs[nt][e];
         const float x0 = on0 ? a0 * b0 : -INFINITY, x1 = on1 ? a1 * b1 : -INFINITY;
         const float mb = fmaxf(x0, x1);
-        const float yb = fmaxf(on0 ? x0 + s0.z : -INFINITY, on1 ? x1 + s1.z : -INFINITY);
         float sub = m[nt][e] == -INFINITY ? 0.f : m[nt][e];
-        if (__any_sync(kAll, mb > m[nt][e] + kSlack || yb > sub + (float)ew[nt][e] + kSlackW)) {
-          float mr = mb, yr = yb;
+        auto top_weight = [&] {  // of the lane's two, log2, over the scores' maximum
+          return fmaxf(on0 ? (x0 - sub) + s0.z : -INFINITY, on1 ? (x1 - sub) + s1.z : -INFINITY);
+        };
+        if (__any_sync(kAll, mb > m[nt][e] + kSlack || top_weight() > (float)ew[nt][e] + kSlackW)) {
+          // (both references move together where one has to; the outputs' never falls, and is none
+          // before the first score)
+          float mr = mb;
 #pragma unroll
-          for (int o = 4; o < 32; o <<= 1) {
-            mr = fmaxf(mr, __shfl_xor_sync(kAll, mr, o));
-            yr = fmaxf(yr, __shfl_xor_sync(kAll, yr, o));
-          }
-          // (both references move together where one has to; the outputs' never falls)
-          const float was = sub + (float)ew[nt][e];
+          for (int o = 4; o < 32; o <<= 1) mr = fmaxf(mr, __shfl_xor_sync(kAll, mr, o));
+          float was = m[nt][e] == -INFINITY ? -INFINITY : (float)ew[nt][e];
           if (mr > m[nt][e]) {
-            l[nt][e] *= fast_exp2(m[nt][e] - mr);
+            const float fall = m[nt][e] - mr;
+            l[nt][e] *= fast_exp2(fall);
+            was += fall;
             m[nt][e] = mr;
             sub = mr;
           }
-          const float to = fmaxf(was, yr) - sub;
-          ew[nt][e] = (int)fminf(fmaxf(ceilf(to), -400.f), 400.f);
-          const float a = fast_exp2(was - (sub + (float)ew[nt][e]));
+          float yr = top_weight();
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) yr = fmaxf(yr, __shfl_xor_sync(kAll, yr, o));
+          ew[nt][e] = (int)fminf(fmaxf(ceilf(fmaxf(was, yr)), -400.f), 400.f);
+          const float a = fast_exp2(was - (float)ew[nt][e]);
 #pragma unroll
           for (int i = 0; i < PC; ++i) {
             acc[i][nt][e] *= a;
