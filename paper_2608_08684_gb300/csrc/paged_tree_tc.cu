@@ -590,13 +590,13 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       }
     }
     copies_landed();
-    if (!ok) {  // what TMA still has on its way lands before the CTA leaves
-      if (!kCodes) {
-        for (int i = max(0, n - ST); i < n; ++i) mbar_wait(&full[i % ST], i / ST & 1, nullptr);
-      } else {  // (the second warp has issued none)
-        for (int i = max(0, issued - kRing); i < issued; ++i)
-          mbar_wait(&sy->ring_full[keys ? 0 : 1][i % kRing], i / kRing & 1, nullptr);
-      }
+    // What TMA still has on its way lands before the CTA leaves: this warp may be done where
+    // another role has given up on it.
+    if (!kCodes) {
+      for (int i = max(0, n - ST); i < n; ++i) mbar_wait(&full[i % ST], i / ST & 1, nullptr);
+    } else if (!ok) {  // (else every block has been waited for; the second warp has issued none)
+      for (int i = max(0, issued - kRing); i < issued; ++i)
+        mbar_wait(&sy->ring_full[keys ? 0 : 1][i % kRing], i / kRing & 1, nullptr);
     }
   } else if (warp == 4) {
     // -------------------------------------------------- MMAs (the whole warp waits, one lane issues)

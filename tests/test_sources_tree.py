@@ -1,0 +1,20 @@
+"""How the trees' tensor-core kernel leaves when a wait is out of time: what no run can show, since
+the runs that would go wrong are the ones that must not be made."""
+import re
+
+from tests.test_sources import _code
+
+
+def _loaders(code):
+    """The fetching warps' part."""
+    return code[code.index("if (warp >= 5) {"):code.index("} else if (warp == 4) {")]
+
+
+def test_every_load_of_16_bit_pages_has_landed_when_a_cta_leaves():
+    # a warp that has fetched its last blocks waits for them whether or not its own waits ended
+    # well: the role that gave up may be another
+    part = re.sub(r"\s+", " ", _loaders(_code("paged_tree_tc.cu")))
+    assert part.rstrip(" }").endswith("nullptr);")
+    end = part[part.rindex("copies_landed();"):]
+    assert end.startswith("copies_landed(); if (!kCodes) { for (int i = max(0, n - ST); i < n; ++i) "
+                          "mbar_wait(&full[i % ST], i / ST & 1, nullptr); } else if (!ok) {")
