@@ -730,6 +730,17 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       if (lane == 0) mbar_arrive(&sy->q_full);
       return scale;
     };
+    // Whether no warp of the four has given up: before barriers that all of them have to reach.
+    auto none_gave_up = [&](bool mine) {
+      int all;
+      asm volatile(
+          "{\n .reg .pred p, q;\n setp.ne.b32 q, %1, 0;\n"
+          " barrier.cta.red.and.pred p, %2, 128, q;\n selp.s32 %0, 1, 0, p;\n}\n"
+          : "=r"(all)
+          : "r"((int)mine), "r"(1 + team)
+          : "memory");
+      return all != 0;
+    };
     float row_scale = 0.f;  // of the part's queries
     bool have_queries = false;
     int drafts = 0;  // parts with drafted tokens
@@ -903,9 +914,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&sy->p_full[n & 1]);
       }
-      if (!ok) break;
       // the next part's queries: its first scores are computed while this one's outputs are written
-      {
+      if (ok) {
         W next = w;
         have_queries = false;
         if (next.next(p)) {
@@ -916,13 +926,16 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           }
         }
       }
-      if (!(ok = wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2))) break;
+      ok = ok && wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2);
       unsigned long long bad = 0;
-      if (w.end > seq.prefix) {
-        if (!(ok = wait_for(&sy->draft_done[drafts % kDrafts], drafts / kDrafts))) break;
+      if (ok && w.end > seq.prefix) {
+        ok = wait_for(&sy->draft_done[drafts % kDrafts], drafts / kDrafts);
         bad = sy->bad[0][drafts % kDrafts] | (kCodes ? sy->bad[1][drafts % kDrafts] : 0ull);
         ++drafts;
       }
+      // (a wait can end well for one warp and badly for another)
+      if constexpr (C > 1) ok = none_gave_up(ok);
+      if (!ok) break;
       tc_fence_after();
       const float o_scale = kCodes ? pow2(v_top - 127) : 1.f;
       const long long slot =

@@ -18,3 +18,15 @@ def test_every_load_of_16_bit_pages_has_landed_when_a_cta_leaves():
     end = part[part.rindex("copies_landed();"):]
     assert end.startswith("copies_landed(); if (!kCodes) { for (int i = max(0, n - ST); i < n; ++i) "
                           "mbar_wait(&full[i % ST], i / ST & 1, nullptr); } else if (!ok) {")
+
+
+def test_softmax_warps_agree_before_the_copies_join():
+    # each decides for itself whether a wait ended well: they do so together before barriers that
+    # all four have to reach, and no wait stands between those
+    code = _code("paged_tree_tc.cu")
+    part = code[code.index("} else if (warp == 4) {"):]
+    agree = part.index("if constexpr (C > 1) ok = none_gave_up(ok);")
+    assert part[agree:].split("\n", 2)[1].strip() == "if (!ok) break;"
+    join = part[agree:part.index("cta_warp == 8) tmem_dealloc")]
+    assert "named_bar_sync(1 + team, 128)" in join and "wait_for(" not in join
+    assert "named_bar_sync(1 + team" not in part[:agree]
