@@ -892,8 +892,9 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
             } else {
 #pragma unroll
               for (int i = 0; i < HK; i += 2) {
-                const float2 y = make_float2(fast_exp2(__uint_as_float(u[i]) * rs - sub),
-                                             fast_exp2(__uint_as_float(u[i + 1]) * rs - sub));
+                // (rounded apart, as the maximum was: fused they may be far above it)
+                const float2 y = make_float2(fast_exp2(__fsub_rn(__fmul_rn(__uint_as_float(u[i]), rs), sub)),
+                                             fast_exp2(__fsub_rn(__fmul_rn(__uint_as_float(u[i + 1]), rs), sub)));
                 sum[i / 2 & 1] = __fadd2_rn(sum[i / 2 & 1], y);
                 pr[i / 2] = pack16<kCodes>(y.x, y.y);
               }
