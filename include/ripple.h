@@ -626,12 +626,13 @@ ripple_status ripple_paged_tree_workspace_bytes(const ripple_paged_desc *desc,
  *             Calls that share a workspace must be ordered on the GPU.
  * Rows whose page entry is out of range, drafted tokens whose row is negative while
  * lens[b] > 0 (both RIPPLE_EBOUNDS) and rows behind max_pages * page_size (RIPPLE_EFULL)
- * are left out of the attention. Softmax statistics and sums are fp32. With dtype bf16
- * the probabilities are rounded to bf16 (8-bit pages: fp16) for the matrix instructions (as the
- * output is; of 8-bit pages, keys are taken to 2^-24 of their block of 64 rows' largest scale,
- * values to 2^-24 of the largest scale so far, an element of a query to 2^-39 of the head's
- * largest, and a query below 2^-86 may count as 0). Results do not depend on the run. The call may
- * be captured in a CUDA graph: lengths, starts, masks and the table are read on the device.
+ * are left out of the attention. Softmax statistics and sums are fp32. With dtype bf16 the
+ * probabilities are rounded to bf16 for the matrix instructions (as the output is). Over 8-bit pages
+ * it is their products with the values' scales that are rounded, to fp16: to 2^-11 of themselves or
+ * 2^-32 of the largest so far (2^-21 where their rows' scales are 2^11 apart); an element of a query
+ * counts to 2^-39 of the head's largest, and a query below 2^-86 may count as 0. Results do not
+ * depend on the run. The call may be captured in a CUDA graph: lengths, starts, masks and the table
+ * are read on the device.
  * Errors: RIPPLE_EINVAL, RIPPLE_EWORKSPACE, RIPPLE_ECUDA. Device status: also RIPPLE_ETIMEOUT.
  */
 ripple_status ripple_paged_tree_attn(const ripple_paged_desc *desc,

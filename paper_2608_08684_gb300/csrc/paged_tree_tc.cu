@@ -22,21 +22,28 @@
 // (1.01 GB, 91% of the copy rate; with one team a CTA and no copies of the query rows 285); 3 of about
 // 31000 rows with 64 tokens of 64 heads 193 us (196 GFLOP, 1.02 PFLOP/s): there the chain scores -
 // softmax - product of a block, two of them an SM, leaves the tensor pipe half idle; 8-bit pages,
-// 32 sequences of up to 32768 rows, 16 tokens 161 us (419 MB, 38%): bound by the widening warps'
-// instructions. One sequence of 900 rows and 4 tokens 14.0 us: the launch, lengths, table, queries,
+// 32 sequences of up to 32768 rows, 16 tokens 172 us (419 MB, 36%): bound by the fetching warps'
+// instructions (of a block's 3500 cycles their loads, scales and tables take 1250, the widening 950;
+// 96 registers a thread, of which the instances spill 200 bytes). One sequence of 900 rows and 4 tokens 14.0 us: the launch, lengths, table, queries,
 // two blocks, the join of the copies and of the shares, one after the other.
 //
 // P in one bf16 part: the output is rounded to bf16 as well, and a probability's rounding
 // (2^-8) enters the output as part of a mean. The sum is of the unrounded ones, in fp32.
 //
-// 8-bit pages come into a ring of their own, two blocks ahead, and two warps each for keys and values
-// make them fp16 values: a code (exact in fp16) times its row's scale over the largest scale of the
-// block (keys; the block's scores are multiplied by that) or of the run's blocks so far (values; the
-// outputs are brought to a larger one as they are to a larger maximum). A row whose scale is 2^-15
-// of that or more stays exact; others are off by 2^-25 of the largest at most, less than
-// fp32 sums lose. A query row is multiplied by the power of two that brings its largest element
-// to [2^14, 2^15). P has 2^7 more than for bf16, so that what it loses at the lower end (2^-32 a
-// key) is nothing.
+// 8-bit pages come into a ring of their own, two blocks ahead, and two warps each for keys and
+// values make them fp16 values: a code times its row's scale over a reference of the block's, the
+// largest scale of its rows before the draft. That is exact for rows up to 2^kBelow below it and
+// 2^kAbove above. Rows beyond (hardly ever there) are left for further passes over the block, with
+// references in steps of that, and count for nothing in this one. So no row takes anything from
+// another, whatever a hidden one holds, or one without weight. The keys' reference multiplies the
+// scores; the values' counts with the probability, 2^(x + e), relative to the largest such weight
+// that the query row has seen, which is held as 2^7 to 2^15 in fp16: a weight loses 2^-32 of that
+// one at most at the lower end (times 2^11 where their rows' scales are as far apart). The sum of
+// the probabilities has the scores' own maximum, in fp32. A query row is multiplied by the power of
+// two that brings its largest element to [2^14, 2^15).
+// (Scales relative to the largest of any row of the block and, of values, so far: 161 us for the
+// batch above, 172 now, but a hidden row could cost the others all their bits. Scales by rows in the
+// softmax: 182 to 243, the block's scores then wait for them in a thread that has no registers left.)
 #include "paged_tree.cuh"
 #include "tc_ptx.cuh"
 
@@ -58,7 +65,7 @@ constexpr int kTeams = 2;
 __host__ __device__ constexpr int threads(bool codes) { return 32 * (10 + kTeams * (codes ? 4 : 2)); }
 // Blocks that a group's queries and outputs take as long as (their copies' join in the main). us for
 // 2, 4, 7, 10, 14, D 128, 4 heads a KV head: 48 sequences of up to 32768 rows and 2 to 12 tokens
-// 186.5, 163.0, 163.3, 165.6, 168.5; 8-bit pages, 32 sequences of 16 tokens 210, 188, 161, 163, 169.
+// 188, 164, 163.5, 165, 168; 8-bit pages, 32 sequences of 16 tokens 210, 185, 172, 176, 181.
 constexpr int kGroupCost = 7;
 constexpr int kRing = 2;       // blocks of 8-bit rows on their way or being widened
 constexpr uint32_t kTeamCols = 256;  // of TMEM: S and P of two blocks (64 each), O (d) from 128 on
@@ -67,20 +74,37 @@ constexpr float kSlack = 8.f;
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kMaxDevices = 64;
 constexpr int kDrafts = 4; // parts with drafted tokens that the values may be ahead
-constexpr int kSlots = 8;  // of what the softmax is told about blocks (fetched up to two ahead)
+constexpr int kSlots = 8;  // of the rows that are there (known up to two blocks ahead)
+constexpr int kScaled = 3; // of passes over 8-bit blocks (widened at most two ahead of the softmax)
+// log2 of how far a row's scale may be from the reference to be put into fp16 values: codes reach
+// from 2^-9 (of 4 bits) to 448, fp16 from 2^-24 to 65504.
+constexpr int kBelow = 8, kAbove = 3, kWindow = kBelow + kAbove + 1;
 
-struct Sync {
+// What the fetching warps tell one another and the softmax about blocks.
+template <bool kCodes>
+struct Told {
+  uint64_t draft_done[kDrafts];        // by parts with drafted tokens (values may be parts ahead)
+  unsigned long long bad[kDrafts];     // drafted tokens whose values are not all finite, by parts
+  unsigned long long present[kSlots];  // rows of a block that are there
+};
+template <>
+struct Told<true> {
+  uint16_t factor[2][kRing][KB];       // what the ring's keys, values are multiplied by, fp16
+  bool more[2][kRing];                 // another pass over the same rows follows
+  unsigned long long present[kScaled]; // rows that count in the pass
+  unsigned long long nan[kScaled];     // those of them whose values are NaN
+  float key[kScaled], value[kScaled];  // the references: the keys', log2 of the values'
+  int again[kScaled];                  // 1: another pass over the same rows follows; 2: see nan
+};
+template <bool kCodes>
+struct alignas(16) Sync {
+  Told<kCodes> told;
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t ring_full[2][kRing];                         // of keys, of values
   uint64_t s_full[2], p_full[2], pv_done[2];            // of even and odd blocks
   uint64_t q_full, mma_done;
-  uint64_t draft_done[kDrafts];        // by parts with drafted tokens (values may be parts ahead)
-  unsigned long long present[kSlots];  // rows of a block that are there
-  unsigned long long bad[2][kDrafts];  // drafted tokens whose values are not all finite, by parts
   uint32_t tmem;
   int abort;                           // a role has given up waiting
-  int top[2][kSlots];                  // 8-bit pages: the scale bytes that a block's keys, values are over
-  uint16_t scale[2][kRing][KB];        // of the ring's rows, over that, in fp16
   float inv[64];                       // of a group's query rows (with copies), and where they go
   int out_row[64];
 };
@@ -93,7 +117,7 @@ struct Smem {
   static constexpr int HALF_Q = kRows * 128, HALF = KB * 128;  // of 64 dims
   static constexpr int K0 = Q, V0 = Q + SK * TILE, RING = V0 + SV * TILE;
   static constexpr int TEAM = RING + (kCodes ? 2 * kRing * RAW : 0);
-  static constexpr int BYTES = kTeams * (TEAM + (int)sizeof(Sync));
+  static constexpr int BYTES = kTeams * (TEAM + (int)sizeof(Sync<kCodes>));
   static_assert(TEAM % 1024 == 0 && BYTES <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -250,13 +274,8 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t pair) {
   return ((pair & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) |
          ((pair & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
-// 2^(byte - top) in fp16 (0 below its values); NaN for byte 255. byte <= top.
-constexpr uint16_t kNanScale = 0x7fff;
-__device__ __forceinline__ uint16_t relative_scale(int byte, int top) {
-  const int d = byte - top;
-  return byte == 255 ? kNanScale : d >= -14 ? (15 + d) << 10 : d >= -24 ? 1 << (24 + d) : 0;
-}
-// 16 codes times a scale as fp16.
+constexpr uint16_t kNanFactor = 0x7fff;
+// 16 codes times a factor as fp16.
 __device__ __forceinline__ void widen(const uint4 &u, uint16_t factor, uint32_t (&o)[8]) {
   const __half2 scale = __half2half2(__ushort_as_half(factor));
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -291,7 +310,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
   const bool second = kCodes && cta_warp >= 10 && (cta_warp - 10) % 2 == 1;  // of two that fetch
   const int tid = 32 * warp + lane;
   uint8_t *const tiles = smem + team * S::TEAM;
-  Sync *const syncs = (Sync *)(smem + kTeams * S::TEAM), *const sy = syncs + team;
+  Sync<kCodes> *const syncs = (Sync<kCodes> *)(smem + kTeams * S::TEAM), *const sy = syncs + team;
   // (as many CTAs as SMs, or one for each team's work: teams beside one another in different CTAs)
   // Short caches: p.teams teams of a cluster (or one) have equal shares of a group.
   const int teams = p.teams;
@@ -313,7 +332,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       mbar_init(&sy->pv_done[i], 1);
     }
     mbar_init(&sy->q_full, 4);
-    for (int i = 0; i < kDrafts; ++i) mbar_init(&sy->draft_done[i], 16 * kFetch);
+    if constexpr (!kCodes)
+      for (int i = 0; i < kDrafts; ++i) mbar_init(&sy->told.draft_done[i], 32);
     mbar_init(&sy->mma_done, 1);
     fence_mbar_init();
     fence_proxy_async_smem();
@@ -378,7 +398,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       }
       const uint32_t lo = __ballot_sync(kAll, there[0]), hi = __ballot_sync(kAll, there[1]);
       present = (unsigned long long)hi << 32 | lo;
-      if (!kCodes && keys && lane == 0) sy->present[n % kSlots] = present;
+      if constexpr (!kCodes)
+        if (keys && lane == 0) sy->told.present[n % kSlots] = present;
       __syncwarp();
       if (allowed && p.tma && present == ~0ull) {
         if (lane == 0) mbar_arrive_expect_tx(bar, KB * D * kElem);
@@ -423,12 +444,15 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
     // they are is told with the part's last block.
     int drafts = 0;  // parts with drafted tokens
     unsigned long long bad = 0;
+    // (8-bit pages have their own way: Told<true>::nan)
     auto tell_bad = [&]() {
-      const uint32_t lo = __reduce_or_sync(kAll, (uint32_t)bad), hi = __reduce_or_sync(kAll, (uint32_t)(bad >> 32));
-      if (lane == 0) sy->bad[second][drafts % kDrafts] = (unsigned long long)hi << 32 | lo;
-      bad = 0;
-      mbar_arrive(&sy->draft_done[drafts % kDrafts]);
-      ++drafts;
+      if constexpr (!kCodes) {
+        const uint32_t lo = __reduce_or_sync(kAll, (uint32_t)bad), hi = __reduce_or_sync(kAll, (uint32_t)(bad >> 32));
+        if (lane == 0) sy->told.bad[drafts % kDrafts] = (unsigned long long)hi << 32 | lo;
+        bad = 0;
+        mbar_arrive(&sy->told.draft_done[drafts % kDrafts]);
+        ++drafts;
+      }
     };
     int ring_n = 0, issued = 0;  // blocks that have gone through the ring, that were put there
     for (bool more = any; more && ok; more = w.next(p)) {
@@ -464,7 +488,6 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           mbar_arrive(&full[stage]);
         }
       } else {
-        uint16_t(*const scale_ring)[KB] = sy->scale[keys ? 0 : 1];
         uint64_t *const ring_full = sy->ring_full[keys ? 0 : 1];
         const uint32_t ring = qs + S::RING + (keys ? 0 : kRing * S::RAW);
         // What both warps agree on: they go on to a block, or neither does.
@@ -484,108 +507,181 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           const int slot = i % kRing;
           issued = i + 1;
           if (!fetch(row0, ring + slot * S::RAW, &ring_full[slot], true)) copies_arrive(&ring_full[slot]);
-          if (keys && lane == 0) sy->present[(n + i - ring_n) % kSlots] = present;
           if (row0 + KB < w.end) look_up(row0 + KB);
         };
-        // The second brings their scales: bytes of the rows lane and lane + 32 (0: not there), of
-        // keys and of values, loaded a block before they are put into the ring, with the largest
-        // (255 is none): the block's of keys, the run's so far of values.
-        int k_byte[2], v_byte[2], v_top = 0;
+        // The second brings the scales of keys and values, bytes of the rows lane and lane + 32,
+        // loaded a block before they are put beside the ring (and not looked at until then: what
+        // does waits for them, 243 us for the batch above).
+        int coming[2][2] = {{0, 0}, {0, 0}}, there = 0;  // which of the two rows are in the cache
+        uint32_t bytes = 0;                     // of this block: keys from bit 0, values from 16 on
+        int id[2] = {0, 0};                     // the pass that a row belongs to (0: none any more)
+        int ref[2] = {127, 127}, now = 0;       // bytes of the first pass's references; this pass
+        uint32_t rows[2] = {0, 0};              // of the pass
+        bool several = false, follows = false;  // passes over the block; another after this one
+        constexpr int kFirst = 32 << 8 | 32;    // windows up or down, and 32, of keys and values
+        auto byte_of = [&](int kind, int k) { return (int)(bytes >> (16 * kind + 8 * k) & 0xffu); };
         auto load_scales = [&](int row0) {
+          there = 0;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const int page = entry[k], row = row0 + lane + 32 * k;
-            k_byte[k] = v_byte[k] = 0;
             if ((unsigned)page < (unsigned)p.g.n_pages) {
               const long long at =
                   page * p.scale_page + w.h * p.scale_head + (row & (page_rows - 1)) * p.scale_row;
-              if (keys) k_byte[k] = p.k_scales[at];
-              v_byte[k] = p.v_scales[at];
+              coming[0][k] = p.k_scales[at];
+              coming[1][k] = p.v_scales[at];
+              there |= 1 << k;
             }
           }
           if (row0 + KB < w.end) look_up(row0 + KB);
         };
-        auto put_scales = [&](int i) {
-          int k_top = 0, top = 0;
+        // Passes over the block at row0: rows by how many windows their scales lie from the
+        // references. (Neither these nor the passes' order hang on drafted rows; NaN is of the
+        // first.)
+        auto sort_rows = [&](int row0) {
+          bytes = coming[0][0] | coming[0][1] << 8 | coming[1][0] << 16 | coming[1][1] << 24;
+          const int before = (int)(seq.prefix - row0) - lane;  // rows before the draft from the lane's on
+#pragma unroll
+          for (int kind = 0; kind < 2; ++kind) {
+            int top = 0;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              if (byte_of(kind, k) != 255 && before > 32 * k) top = max(top, byte_of(kind, k));
+            top = __reduce_max_sync(kAll, top);
+            ref[kind] = top > 0 ? top : 127;
+          }
+          bool apart = false;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            if (keys && k_byte[k] != 255) k_top = max(k_top, k_byte[k]);
-            if (v_byte[k] != 255) top = max(top, v_byte[k]);
+            id[k] = there >> k & 1 ? kFirst : 0;
+#pragma unroll
+            for (int kind = 0; kind < 2; ++kind)
+              apart |= id[k] != 0 &&
+                       (unsigned)(byte_of(kind, k) - ref[kind] + kBelow) >= (unsigned)kWindow;
           }
-          v_top = max(v_top, __reduce_max_sync(kAll, top));
-          top = v_top > 0 ? v_top : 7;
-          if (keys) {
-            k_top = __reduce_max_sync(kAll, k_top);
-            if (k_top == 0) k_top = 127;
-            if (lane == 0) {
-              sy->top[0][(n + i - ring_n) % kSlots] = k_top;
-              sy->top[1][(n + i - ring_n) % kSlots] = top;
+          several = __any_sync(kAll, apart);
+          if (several) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              int at[2];
+#pragma unroll
+              for (int kind = 0; kind < 2; ++kind) {
+                const int byte = byte_of(kind, k);  // (32 windows are more than a byte has)
+                at[kind] = byte == 255 ? 32 : (byte - ref[kind] + kBelow + 32 * kWindow) / kWindow;
+              }
+              if (id[k] != 0) id[k] = at[0] << 8 | at[1];
             }
           }
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-            scale_ring[i % kRing][lane + 32 * k] =
-                keys ? relative_scale(k_byte[k], k_top) : relative_scale(v_byte[k], top);
         };
-        const bool more_than_one = w.begin + KB < w.end;
+        // The next pass, beside the ring's block i.
+        auto put_scales = [&](int i) {
+          if constexpr (kCodes) {
+            now = kFirst;
+            follows = false;
+            if (several) {
+              constexpr unsigned kNone = ~0u;
+              const unsigned a = id[0] == 0 ? kNone : id[0], b = id[1] == 0 ? kNone : id[1];
+              now = (int)__reduce_min_sync(kAll, min(a, b));
+              follows = __any_sync(kAll, (id[0] != 0 && id[0] != now) ||
+                                             (id[1] != 0 && id[1] != now));
+            }
+            const int kind = keys ? 0 : 1;
+            const int centre = ref[kind] + ((keys ? now >> 8 : now & 0xff) - 32) * kWindow;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int byte = byte_of(kind, k);
+              sy->told.factor[kind][i % kRing][lane + 32 * k] =
+                  id[k] != now ? 0
+                  : byte == 255  ? (keys ? kNanFactor : 0)
+                                 : (15 + byte - centre) << 10;
+              rows[k] = __ballot_sync(kAll, id[k] == now);
+            }
+            if (lane == 0) sy->told.more[kind][i % kRing] = follows;
+          }
+        };
+        // What the softmax gets, once the pass three before it has been read.
+        auto tell_scales = [&]() {
+          if constexpr (kCodes) {
+            const int slot = n % kScaled;
+            const bool nan[2] = {id[0] == now && byte_of(1, 0) == 255,
+                                 id[1] == now && byte_of(1, 1) == 255};
+            const bool any_nan = __any_sync(kAll, nan[0] || nan[1]);
+            if (any_nan) {
+              const uint32_t lo = __ballot_sync(kAll, nan[0]), hi = __ballot_sync(kAll, nan[1]);
+              if (lane == 0) sy->told.nan[slot] = (unsigned long long)hi << 32 | lo;
+            }
+            if (lane == 0) {
+              const int key = ref[0] + ((now >> 8) - 32) * kWindow;
+              sy->told.present[slot] = (unsigned long long)rows[1] << 32 | rows[0];
+              sy->told.key[slot] = key >= 255 ? FLT_MAX : pow2(key - 127);
+              sy->told.value[slot] = (float)(ref[1] + ((now & 0xff) - 32) * kWindow - 127);
+              sy->told.again[slot] = (int)follows | (any_nan ? 2 : 0);
+            }
+          }
+        };
         if (!second) {
           issue(w.begin, ring_n);
-          if (more_than_one) issue(w.begin + KB, ring_n + 1);
+          if (w.begin + KB < w.end) issue(w.begin + KB, ring_n + 1);
         } else {
           load_scales(w.begin);
+          sort_rows(w.begin);
           put_scales(ring_n);
-          if (more_than_one) load_scales(w.begin + KB);
+          if (w.begin + KB < w.end) load_scales(w.begin + KB);
         }
-        for (int row0 = w.begin; row0 < w.end; row0 += KB, ++n, ++ring_n) {
+        for (int row0 = w.begin; row0 < w.end; ++n) {
           const int slot = ring_n % kRing, stage = n % ST;
           ok = both(wait_for(&ring_full[slot], ring_n / kRing) &&
                     (n < ST || wait_for(&empty[stage], n / ST - 1)));
           if (!ok) break;
+          bool more = false;
+          if constexpr (kCodes) more = sy->told.more[keys ? 0 : 1][slot];
+          if (keys && second) tell_scales();
           const uint32_t from = ring + slot * S::RAW, to = stages + stage * S::TILE;
-          const bool draft = !keys && w.end > seq.prefix && row0 + KB > seq.prefix;
           // the steps of one warp, kAt at a time: their loads together, then the rest
-          constexpr int kAt = kSteps / 2 < 8 ? kSteps / 2 : 8;
-          static_assert(kSteps / 2 == kAt, "a warp's steps at once");
-          const int first = second ? kAt : 0;
-          uint4 u[kAt];
-          uint16_t f[kAt];
-#pragma unroll
-          for (int i = 0; i < kAt; ++i) {
-            const int row = (first + i) * kRowsWarp + sub;
-            f[i] = scale_ring[slot][row];
-            u[i] = ld_shared16(from + row * D + 16 * pc);
-          }
-          if (draft) {
+          constexpr int kMine = kSteps / 2, kAt = 4;
+          static_assert(kMine % kAt == 0, "");
+#pragma unroll 1
+          for (int i0 = 0; i0 < kMine; i0 += kAt) {
+            const int first = (second ? kMine : 0) + i0;
+            uint4 u[kAt];
+            uint16_t by[kAt];
 #pragma unroll
             for (int i = 0; i < kAt; ++i) {
-              const int row = row0 + (first + i) * kRowsWarp + sub;
-              if (f[i] == kNanScale && row >= seq.prefix) {
-                bad |= 1ull << (row - seq.prefix & 63);
-                f[i] = 0;
-                u[i] = make_uint4(0, 0, 0, 0);
-              }
+              const int row = (first + i) * kRowsWarp + sub;
+              if constexpr (kCodes) by[i] = sy->told.factor[keys ? 0 : 1][slot][row];
+              u[i] = ld_shared16(from + row * D + 16 * pc);
+            }
+#pragma unroll
+            for (int i = 0; i < kAt; ++i) {
+              const int row = (first + i) * kRowsWarp + sub;
+              uint32_t o[8];
+              widen(u[i], by[i], o);
+              const int c = 2 * pc;  // of 16-byte pieces in the stage
+              const uint32_t at = to + (c >> 3) * S::HALF + row * 128;
+              st_shared16(at + (((c & 7) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
+              st_shared16(at + ((((c & 7) + 1) ^ (row & 7)) << 4), o[4], o[5], o[6], o[7]);
             }
           }
-#pragma unroll
-          for (int i = 0; i < kAt; ++i) {
-            const int row = (first + i) * kRowsWarp + sub;
-            uint32_t o[8];
-            widen(u[i], f[i], o);
-            const int c = 2 * pc;  // of 16-byte pieces in the stage
-            const uint32_t at = to + (c >> 3) * S::HALF + row * 128;
-            st_shared16(at + (((c & 7) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
-            st_shared16(at + ((((c & 7) + 1) ^ (row & 7)) << 4), o[4], o[5], o[6], o[7]);
-          }
-          if (draft && row0 + KB >= w.end) tell_bad();
           fence_proxy_async_smem();  // for the tensor cores' reads
           mbar_arrive(&full[stage]);
           named_bar_sync(pair_bar, 64);  // the ring's place has been read
+          if (more) {
+            if (second) {
+#pragma unroll
+              for (int k = 0; k < 2; ++k) id[k] = id[k] == now ? 0 : id[k];
+              put_scales(ring_n);
+            }
+            continue;
+          }
           if (!second) {
             if (row0 + 2 * KB < w.end) issue(row0 + 2 * KB, ring_n + 2);
-          } else {
-            if (row0 + KB < w.end) put_scales(ring_n + 1);
+          } else if (row0 + KB < w.end) {
+            sort_rows(row0 + KB);
+            put_scales(ring_n + 1);
             if (row0 + 2 * KB < w.end) load_scales(row0 + 2 * KB);
           }
+          row0 += KB;
+          ++ring_n;
         }
       }
     }
@@ -626,6 +722,11 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       __syncwarp();
       return true;
     };
+    // (8-bit pages: another pass over the rows of block n follows; known once its keys are there)
+    auto again = [&]() {
+      if constexpr (kCodes) return (sy->told.again[n % kScaled] & 1) != 0;
+      else return false;
+    };
     int part = 0;
     for (bool more = any; more && ok; more = w.next(p)) {
       const TreeSeq seq(p, w.b);
@@ -633,8 +734,10 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       const int count = w.count;
       if (!(ok = wait_for(&sy->q_full, part++))) break;
       ok = scores(n);
-      for (int i = 0; i < count && ok; ++i, ++n) {
-        if (i + 1 < count && !(ok = scores(n + 1))) break;
+      bool begun = false;  // O has a block
+      for (int i = 0; i < count && ok; ++n, begun = true) {
+        if (!again()) ++i;
+        if (i < count && !(ok = scores(n + 1))) break;
         const int st = n % SV;
         if (!wait_for(&sy->p_full[n & 1], n / 2) || !wait_for(&sy->v_full[st], n / SV)) {
           ok = false;
@@ -646,9 +749,9 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
 #pragma unroll
           for (int kk = 0; kk < KB / 16; ++kk)  // 16 keys: 8 columns of P, 2 KB of V
             mma_bf16_ts(tmem + kOCol, tmem + (n & 1) * KB + kk * 8, vd + (kk * 2048 >> 4), id_pv,
-                        kk > 0 || i > 0);
+                        kk > 0 || begun);
           // (the copies are joined in the last block's stage)
-          if (C == 1 || i + 1 < count) mma_commit(&sy->v_empty[st]);
+          if (C == 1 || i < count) mma_commit(&sy->v_empty[st]);
           mma_commit(&sy->pv_done[n & 1]);
         }
         __syncwarp();
@@ -663,8 +766,9 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
     int2 rec = make_int2(0, 0);
     const int copy = tid / RT, r = tid % RT;
     const int key0 = copy * KC;
-    // The queries of the part at `w`, once the products with the ones before are done; returns what
-    // the row's scores are multiplied by.
+    // The queries of the part at `w`, once the products with the ones before are done. The row's
+    // products are multiplied by row_scale.
+    float row_scale = 0.f;
     // A warp has 32 rows of the products, a row's 16-byte pieces on neighbouring lanes.
     auto fetch_queries = [&](const W &w, const TreeSeq &seq) {
       constexpr int kQPieces = D / 8, kAtOnce = 32 / kQPieces, kSteps = 32 / kAtOnce;
@@ -728,7 +832,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sy->q_full);
-      return scale;
+      row_scale = scale;
     };
     // Whether no warp of the four has given up: before barriers that all of them have to reach.
     auto none_gave_up = [&](bool mine) {
@@ -741,7 +845,6 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           : "memory");
       return all != 0;
     };
-    float row_scale = 0.f;  // of the part's queries
     bool have_queries = false;
     int drafts = 0;  // parts with drafted tokens
     for (bool more = any; more && ok; more = w.next(p)) {
@@ -751,7 +854,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       if (teams == 0 && here && !whole) rec = make_int2(w.b * p.g.Hkv + w.h, w.runs_of_group(run));
       const int n_rows = min(seq.tokens * p.G - tile * RT, RT);
       if (n_rows <= 0) continue;
-      if (!have_queries) row_scale = fetch_queries(w, seq);
+      if (!have_queries) fetch_queries(w, seq);
       const bool live = r < n_rows, warp_live = 32 * warp % RT < n_rows;
       // query row r of the tile: token, output row
       auto token_of = [&](int i) { return (tile * RT + i) / p.G; };
@@ -771,7 +874,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           const __nv_bfloat16 *v = (const __nv_bfloat16 *)p.v_pages + page * p.g.page_stride +
                                    w.h * p.g.head_stride + v_slot * p.g.row_stride + d0;
           for (int i = 0; i < dims; ++i) {
-            const float x = kCodes ? __int_as_float(0x7fffffff) : __bfloat162float(v[i]);
+            const float x = __bfloat162float(v[i]);
             if (!(fabsf(x) < INFINITY)) o[i] += x;
           }
         }
@@ -797,20 +900,23 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
         for (int i = 0; i < 4; ++i)
           if (o[i] != o[i] && sum[i] != 0.f) o[i] = sum[i];
       };
-      // m: what the probabilities are relative to, a maximum (8-bit pages: less 7), in log2
-      constexpr float kLow = kCodes ? 7.f : 0.f;
-      float m = -INFINITY, l = 0.f;
-      int v_top = 127;     // 8-bit pages: O is over this value's scale
-      bool begun = false;  // O has a block
-      for (int row0 = w.begin; row0 < w.end && ok; row0 += KB, ++n, begun = true) {
+      // m: what the probabilities are relative to, a maximum, in log2. ew (8-bit pages): of their
+      // products with the values' scales, over m; the largest is held as 2^kTop or up to 2^kSlack more
+      constexpr float kTop = 7.f;
+      float m = -INFINITY, l = 0.f, ew = 0.f;
+      bool begun = false;     // O has a block
+      bool poisoned = false;  // 8-bit pages: a value that the row sees is NaN
+      for (int row0 = w.begin; row0 < w.end && ok; ++n, begun = true) {
         if (!(ok = wait_for(&sy->s_full[n & 1], n / 2))) break;
+        bool more = false;  // 8-bit pages: another pass over the same rows follows
         if (warp_live) {
           tc_fence_after();
           const uint32_t s_at = lanes + (n & 1) * KB;
-          // (8-bit pages without copies: a thread has no room for 64 scores, and reads them twice)
+          // (8-bit pages without copies: a thread has no room for 64 scores, and reads them again)
           constexpr int NH = kCodes && C == 1 ? 2 : 1, HK = KC / NH;
           uint32_t u[HK];
-          const unsigned long long present = sy->present[n % kSlots];
+          const int slot = n % (kCodes ? kScaled : kSlots);
+          const unsigned long long present = sy->told.present[slot];
           const bool masked = present != ~0ull || row0 + KB > seq.prefix;
           unsigned long long seen = ~0ull;
           if (masked) {
@@ -830,6 +936,50 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
                 if (!(on >> i & 1)) u[i] = 0xff800000u;  // -infinity
             }
           };
+          // O of the blocks before times a, once they are in it; false: the wait ran out
+          auto rescale = [&](bool grow, float a) {
+            if (!__any_sync(kAll, grow) || !begun) return true;
+            if (!wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2)) return false;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              uint32_t o[32];
+              tmem_load<32>(lanes + kOCol + c, o);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * a);
+              tmem_store<32>(lanes + kOCol + c, o);
+            }
+            return true;
+          };
+          // 8-bit pages: both references, where the largest score or weight (`most`, log2, over the
+          // maximum `over` so far) may be beyond what they allow; they move together
+          bool grow = false;
+          float a_o = 1.f;
+          auto raise = [&](float mb, auto most) {
+            float was = m == -INFINITY ? -INFINITY : ew;  // (none before the first score)
+            float over = m == -INFINITY ? 0.f : m;
+            if (mb > m + kSlack) {
+              const float fall = m - mb;
+              l *= fast_exp2(fall);
+              was += fall;
+              m = over = mb;
+              grow = true;
+            }
+            const float y = most(over);
+            if (grow || y > ew + kSlack) {
+              // (above 2^-120, the least scale, so that the outputs' factor is an fp32 value)
+              ew = fminf(fmaxf(ceilf(fmaxf(was, y)), -112.f), 128.f);
+              a_o = fast_exp2(was - ew);
+              grow = true;
+            }
+          };
+          float key_scale = 1.f, value = 0.f;
+          if constexpr (kCodes) {
+            key_scale = sy->told.key[slot];
+            value = sy->told.value[slot];
+            if ((sy->told.again[slot] & 2) != 0)
+              poisoned |= (seen & sy->told.nan[slot] >> key0 & (~0ull >> (64 - KC))) != 0;
+          }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
           for (int half = 0; half < NH; ++half) {
@@ -838,52 +988,41 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
             for (int i = 0; i < HK; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(u[i]));
           }
           float mb = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-          float rs = row_scale, a = 1.f, a_o = 1.f;
-          bool grow = false;
-          if constexpr (kCodes) {
-            // (a positive number: hidden keys' -infinity stays that; scores have 2^-95 at most
-            // where fp32 has no smaller factor)
-            rs = fminf(fmaxf(rs * pow2(sy->top[0][n % kSlots] - 127), FLT_MIN), FLT_MAX);
-            const int top = sy->top[1][n % kSlots];
-            grow = begun && top != v_top;
-            if (grow) a_o = fast_exp2((float)(v_top - top));
-            v_top = top;
-          }
+          float rs = row_scale;
+          // (a positive number; scores have 2^-95 at most where fp32 has no smaller factor)
+          if (kCodes) rs = fminf(fmaxf(rs * key_scale, FLT_MIN), FLT_MAX);
           mb *= rs;  // (> 0)
-          if (mb > m + kLow + kSlack) {
-            a = fast_exp2(m - (mb - kLow));
-            m = mb - kLow;
-            l *= a;
-            a_o *= a;
-            grow = true;
-          }
-          if (__any_sync(kAll, grow) && begun) {
-            // O of the blocks before, once they are in it
-            if (!(ok = wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2))) break;
-            tc_fence_after();
-#pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-              uint32_t o[32];
-              tmem_load<32>(lanes + kOCol + c, o);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * a_o);
-              tmem_store<32>(lanes + kOCol + c, o);
+          if constexpr (!kCodes) {
+            if (mb > m + kSlack) {
+              a_o = fast_exp2(m - mb);
+              m = mb;
+              l *= a_o;
+              grow = true;
             }
+          } else {
+            if (mb > m + kSlack || (mb - (m == -INFINITY ? 0.f : m)) + value > ew + kSlack)
+              raise(mb, [&](float over) { return (mb - over) + value; });
           }
-          // scores of -infinity alone leave no finite maximum; the fused multiply-add, which
-          // leaves out the score's rounding, must not meet a maximum whose own rounding counts
+          if (!(ok = rescale(grow, a_o))) break;
+          // scores of -infinity alone leave no finite maximum; the fused multiply-add, which leaves
+          // out the score's rounding, must not meet a maximum whose own rounding counts
+          // (8-bit pages: by threads, so that no row's scores hang on another's)
           const float sub = m == -INFINITY ? 0.f : m;
           float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          const bool far = __any_sync(kAll, fabsf(sub) >= 65536.f);
+          const bool far = kCodes ? fabsf(sub) >= 65536.f : __any_sync(kAll, fabsf(sub) >= 65536.f);
+          // 8-bit pages: the weights over the probabilities, log2. The sum is of the weights, brought
+          // back, but where that is so much that either may be no fp32 value.
+          const float up = kCodes ? value + (kTop - ew) : 0.f;
+          const bool apart = kCodes && fabsf(up) > 90.f;
 #pragma unroll
           for (int half = 0; half < NH; ++half) {
             if (NH > 1) load_scores(half);  // (P lies over scores that have been read)
             uint32_t pr[HK / 2];
-            if (!far) {
+            if (!far && !apart) {
 #pragma unroll
               for (int i = 0; i < HK; i += 2) {
                 float2 y = __ffma2_rn(make_float2(__uint_as_float(u[i]), __uint_as_float(u[i + 1])),
-                                      make_float2(rs, rs), make_float2(-sub, -sub));
+                                      make_float2(rs, rs), make_float2(up - sub, up - sub));
                 y.x = fast_exp2(y.x);
                 y.y = fast_exp2(y.y);
                 sum[i / 2 & 1] = __fadd2_rn(sum[i / 2 & 1], y);
@@ -893,12 +1032,15 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
 #pragma unroll
               for (int i = 0; i < HK; i += 2) {
                 // (rounded apart, as the maximum was: fused they may be far above it)
-                const float2 y = make_float2(fast_exp2(__fsub_rn(__fmul_rn(__uint_as_float(u[i]), rs), sub)),
-                                             fast_exp2(__fsub_rn(__fmul_rn(__uint_as_float(u[i + 1]), rs), sub)));
-                sum[i / 2 & 1] = __fadd2_rn(sum[i / 2 & 1], y);
-                pr[i / 2] = pack16<kCodes>(y.x, y.y);
+                const float2 y = make_float2(__fsub_rn(__fmul_rn(__uint_as_float(u[i]), rs), sub),
+                                             __fsub_rn(__fmul_rn(__uint_as_float(u[i + 1]), rs), sub));
+                float2 z = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+                sum[i / 2 & 1] = __fadd2_rn(sum[i / 2 & 1], z);
+                if (kCodes) z = make_float2(fast_exp2(y.x + up), fast_exp2(y.y + up));
+                pr[i / 2] = pack16<kCodes>(z.x, z.y);
               }
             }
+            if (kCodes) __syncwarp();
             // the copy's own keys; the other copies' have no weight here
 #pragma unroll
             for (int k = 0; k < C; ++k) {
@@ -908,10 +1050,13 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
               tmem_store<HK / 2>(s_at + (C == 1 ? half : k) * (HK / 2), of);
             }
           }
-          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+          const float all = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+          l += kCodes && !far && !apart ? all * fast_exp2(-up) : all;
           tmem_wait_st();
           tc_fence_before();
         }
+        if constexpr (kCodes) more = (sy->told.again[n % kScaled] & 1) != 0;
+        if (!more) row0 += KB;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sy->p_full[n & 1]);
       }
@@ -922,23 +1067,25 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
         if (next.next(p)) {
           const TreeSeq next_seq(p, next.b);
           if (next_seq.tokens * p.G - tile * RT > 0 && next.count > 0) {
-            row_scale = fetch_queries(next, next_seq);
+            fetch_queries(next, next_seq);
             have_queries = true;
           }
         }
       }
       ok = ok && wait_for(&sy->pv_done[(n - 1) & 1], (n - 1) / 2);
       unsigned long long bad = 0;
-      if (ok && w.end > seq.prefix) {
-        ok = wait_for(&sy->draft_done[drafts % kDrafts], drafts / kDrafts);
-        bad = sy->bad[0][drafts % kDrafts] | (kCodes ? sy->bad[1][drafts % kDrafts] : 0ull);
-        ++drafts;
+      if constexpr (!kCodes) {
+        if (ok && w.end > seq.prefix) {
+          ok = wait_for(&sy->told.draft_done[drafts % kDrafts], drafts / kDrafts);
+          bad = sy->told.bad[drafts % kDrafts];
+          ++drafts;
+        }
       }
       // (a wait can end well for one warp and badly for another)
       if constexpr (C > 1) ok = none_gave_up(ok);
       if (!ok) break;
       tc_fence_after();
-      const float o_scale = kCodes ? pow2(v_top - 127) : 1.f;
+      const float o_scale = kCodes ? pow2((int)(ew - kTop)) : 1.f;
       const long long slot =
           (teams > 0 ? (long long)work : (2LL * run + (here ? 1 : 0)) * p.tiles + tile) * p.tile_rows;
       // four outputs of query row i, whose output row is `at`: the output, or the partial
@@ -959,7 +1106,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       };
       if constexpr (C == 1) {
         if (warp_live) {
-          const float inv = inverse(l) * o_scale;
+          const float inv = poisoned ? __int_as_float(0x7fffffff) : inverse(l) * o_scale;
           const long long at = live ? out_row(r) : 0;
 #pragma unroll 1
           for (int c = 0; c < D; c += 32) {
@@ -970,7 +1117,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
             float o[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(u[i]) * inv;
-            if ((bad & mask) != 0) add_bad(bad & mask, c, o, 32);
+            if (!kCodes && (bad & mask) != 0) add_bad(bad & mask, c, o, 32);
 #pragma unroll
             for (int i = 0; i < 32; i += 4) put(r, at, c + i, make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
           }
@@ -992,7 +1139,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
         float den = 0.f;
 #pragma unroll
         for (int k = 0; k < C; ++k) den += fast_exp2(stats[k * RT + r].x - sub) * stats[k * RT + r].y;
-        const float f = fast_exp2(m - sub) * o_scale;
+        const float f = poisoned ? __int_as_float(0x7fffffff) : fast_exp2(m - sub) * o_scale;
         if (copy == 0) {
           sy->inv[r] = inverse(den);
           sy->out_row[r] = live ? (int)(out_row(r) - (long long)seq.first * p.Hq) : 0;
@@ -1026,7 +1173,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
             // (if the probabilities are numbers)
             if (!kCodes && inv == inv && !((x.x + x.y) + (x.z + x.w) == (x.x + x.y) + (x.z + x.w)))
               add_not_finite(c + 4 * pc, o);
-            if (bad != 0) {
+            if (!kCodes && bad != 0) {
               const int tok = token_of(i);
               const unsigned long long sees =
                   p.masks == nullptr ? ~0ull >> (63 - tok) : p.masks[seq.first + tok];
