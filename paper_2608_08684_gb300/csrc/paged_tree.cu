@@ -455,10 +455,12 @@ size_t plan(TreeParams *p, int tile, int block, int places, bool together, void 
                          p->g.B * p->g.Hkv;
   size_t parts, runs;  // partials' tiles over two, records
   if (together) {
-    // (as many for one tile as for several, so that the workspace of more tokens is no smaller)
+    // (as many records and partials as the places allow, whether or not the tiles divide them, so
+    // that the workspace of more tokens is no smaller)
     p->n_runs = (int)std::min<long long>(std::max(1, places / p->tiles), room);
     runs = (size_t)std::min<long long>(places, room);
-    parts = std::max((size_t)p->n_runs * p->tiles, runs);
+    parts = std::max((size_t)p->n_runs * p->tiles,
+                     (size_t)std::min<long long>(places, room * p->tiles));
   } else {
     p->n_runs = (int)std::min<long long>(places, room * p->tiles);
     parts = runs = (size_t)p->n_runs;
