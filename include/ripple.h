@@ -658,8 +658,8 @@ ripple_status ripple_paged_tree_attn(const ripple_paged_desc *desc,
  * scales_host    host [n_layers], strides all alike, or NULL: pages in desc->dtype
  * n_layers       1..RIPPLE_MAX_LAYERS
  * k_pages_host, v_pages_host, block_tables_host  host arrays of n_layers device pointers.
- *                No two layers' pools have a place in common; a page that holds drafted
- *                rows belongs to one sequence only.
+ *                No two layers' pools or scales have a place in common (a layer's own are
+ *                checked); a page that holds drafted rows belongs to one sequence only.
  * n_tokens, seq_starts  the drafted tokens, as in ripple_paged_append
  * max_kept       0..RIPPLE_MAX_DRAFT
  * kept           device int32 [B][max_kept] (NULL where max_kept is 0): the accepted tokens

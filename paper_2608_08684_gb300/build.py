@@ -85,7 +85,8 @@ def build_binding(force: bool = False, verbose: bool = False) -> str:
     """Build the extension module if it is missing or older than its sources; return its
     path."""
     binding = binding_path()
-    if not force and not _stale(binding, [BINDING_SRC, os.path.join(INCLUDE, "ripple.h")]):
+    if not force and not _stale(binding, [BINDING_SRC, os.path.join(CSRC, "paged.cuh"),
+                                          os.path.join(INCLUDE, "ripple.h")]):
         return binding
     import sysconfig
 

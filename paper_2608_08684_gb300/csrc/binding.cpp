@@ -13,6 +13,7 @@
 #include <memory>
 #include <vector>
 
+#include "paged.cuh"
 #include "ripple.h"
 
 namespace {
@@ -332,13 +333,34 @@ struct KeepLayers {
   int device;
 };
 
-// keep_tables(list of caches' handles): a handle of all of them
+// A cache's pools (and scales), in bytes.
+struct Places {
+  ripple::RowSet rows;
+  long long inner;
+};
+void add_places(const Cache &c, std::vector<Places> *to) {
+  const ripple_paged_desc &d = c.desc;
+  const long long elem = c.codes() != nullptr ? 1 : c.type == at::kBFloat16 ? 2 : 4;
+  const auto add = [&](const void *at, long long row, long long head, long long page, long long inner) {
+    to->push_back({{(long long)(uintptr_t)at, {row, head, page}, {d.page_size, d.n_kv_heads, d.n_pages}},
+                   inner});
+  };
+  for (const void *at : {c.k, c.v})
+    add(at, d.row_stride * elem, d.head_stride * elem, d.page_stride * elem, d.head_dim * elem);
+  if (c.codes() != nullptr)
+    for (const void *at : {c.scales.k_scales, c.scales.v_scales})
+      add(at, c.scales.row_stride, c.scales.head_stride, c.scales.page_stride, 1);
+}
+
+// keep_tables(list of caches' handles): a handle of all of them. Every layer's rows are moved at the
+// same time, so that no two layers may have a place in common, nor a layer's keys, values and scales.
 PyObject *keep_tables(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!args_are(n, 1)) return nullptr;
   PyObject *o = nullptr;
   try {
     need(PyList_Check(a[0]) && PyList_GET_SIZE(a[0]) >= 1, "expected a list of caches");
     auto kept = std::make_unique<KeepLayers>();
+    std::vector<Places> places;
     for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[0]); ++i) {
       const Cache &c = cache_of(PyList_GET_ITEM(a[0], i));
       if (i == 0) {
@@ -349,7 +371,12 @@ PyObject *keep_tables(PyObject *, PyObject *const *a, Py_ssize_t n) {
       kept->v.push_back(c.v);
       kept->tables.push_back(c.table);
       if (c.codes() != nullptr) kept->scales.push_back(c.scales);
+      add_places(c, &places);
     }
+    for (size_t i = 0; i < places.size(); ++i)
+      for (size_t j = 0; j < i; ++j)
+        need(!ripple::overlap(places[i].rows, places[j].rows, places[i].inner, places[j].inner),
+             "the layers' pools and scales must be apart");
     need(kept->scales.empty() || kept->scales.size() == kept->k.size(), "caches of one kind");
     o = PyCapsule_New(kept.get(), "ripple_keep_tables", [](PyObject *self) {
       delete static_cast<KeepLayers *>(PyCapsule_GetPointer(self, "ripple_keep_tables"));

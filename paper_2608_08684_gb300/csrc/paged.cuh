@@ -44,12 +44,21 @@ inline bool disjoint(int n, const long long *stride, const long long *count, lon
   return true;
 }
 
-// Whether an element lies in a row of `a` (inner elements) and in one of `b` (inner_b, or as many). Dimensions that both have with
-// the same stride are looked at row by row (by the difference of the indices), the others as
-// the span that they reach over: what is said to be apart is, and two views of one buffer
-// that interleave (heads side by side in a token's row) are told from ones that overlap.
+// Whether an element lies in a row of `a` (inner elements) and in one of `b` (inner_b, or as
+// many). Dimensions that both have with the same stride are looked at row by row (by the
+// difference of the indices), the others as the span that they reach over: what is said to be
+// apart is, and two views of one buffer that interleave (heads side by side in a token's row)
+// are told from ones that overlap.
 inline bool overlap(const RowSet &a, const RowSet &b, long long inner, long long inner_b = -1) {
   long long span_a = inner, span_b = inner_b < 0 ? inner : inner_b;
+  {  // nearly always: one ends before the other begins
+    long long end_a = a.at + span_a, end_b = b.at + span_b;
+    for (int i = 0; i < 3; ++i) {
+      end_a += a.stride[i] * (a.count[i] - 1);
+      end_b += b.stride[i] * (b.count[i] - 1);
+    }
+    if (end_a <= b.at || end_b <= a.at) return false;
+  }
   long long stride[3], most[3], least[3];  // of the shared dimensions, and the index differences
   int n = 0;
   for (int i = 0; i < 3; ++i) {

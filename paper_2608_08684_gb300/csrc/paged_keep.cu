@@ -181,6 +181,12 @@ extern "C" ripple_status ripple_paged_keep_rows(
       if (l > 0 && (s.page_stride != p.scale_page || s.head_stride != p.scale_head ||
                     s.row_stride != p.scale_row))
         return RIPPLE_EINVAL;
+      // what one thread moves no other may: the scales lie apart from each other and from the rows
+      const RowSet rows[2] = {p.g.rows(x.k, 1), p.g.rows(x.v, 1)};
+      const RowSet places[2] = {s.rows(s.k, p.g), s.rows(s.v, p.g)};
+      if (overlap(places[0], places[1], 1)) return RIPPLE_EINVAL;
+      for (int i = 0; i < 4; ++i)
+        if (overlap(rows[i / 2], places[i % 2], desc->head_dim, 1)) return RIPPLE_EINVAL;
       p.scale_page = s.page_stride;
       p.scale_head = s.head_stride;
       p.scale_row = s.row_stride;

@@ -571,7 +571,7 @@ def ripple_paged_tree_attn(cache: PagedCache, q, lens, out, workspace, masks=Non
 
 class KeepTables:
     """Host arrays (pools, tables) of ripple_paged_keep_rows, built once from a PagedCache
-    per layer, all of one shape."""
+    per layer, all of one shape, whose pools and scales have no place in common."""
 
     def __init__(self, caches):
         caches = list(caches)
@@ -582,8 +582,6 @@ class KeepTables:
         if any(bytes(c.desc) != bytes(c0.desc) or c.codes != c0.codes or c.device != c0.device
                for c in caches):
             raise ValueError("the layers' caches must be of one shape, dtype and device")
-        if len({t.data_ptr() for c in caches for t in c._keep[:2]}) != 2 * L:
-            raise ValueError("the layers' pools must be apart")
         self.desc, self.device = c0.desc, c0.device
         self._handle = _binding.keep_tables([c._handle for c in caches])
         self._keep = caches
