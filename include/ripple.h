@@ -668,7 +668,8 @@ ripple_status ripple_paged_tree_attn(const ripple_paged_desc *desc,
  *                RIPPLE_EBOUNDS and ends it too.
  * lens           device int32 [n_layers][B], the drafted tokens included; a sequence with
  *                lens <= 0 is idle: nothing is moved, lens_out is lens
- * lens_out       device int32 [n_layers][B]; may be lens, else apart from it
+ * lens_out       device int32 [n_layers][B]; may be lens, else apart from it, and from kept and
+ *                seq_starts
  * Rows whose page entry is out of range, and a draft with more tokens than rows or with
  * descending seq_starts (lens_out is then lens), are reported as RIPPLE_EBOUNDS and not
  * moved, rows behind max_pages * page_size as RIPPLE_EFULL. One launch; no workspace. The call may be captured

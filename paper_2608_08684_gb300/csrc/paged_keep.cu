@@ -194,6 +194,16 @@ extern "C" ripple_status ripple_paged_keep_rows(
       x.v_scales = s.v;
     }
   }
+  // what one thread block reads no other may write
+  const long long entries = (long long)n_layers * desc->batch;
+  const auto over_lens_out = [&](const int32_t *at, long long n) {
+    return at != nullptr && (uintptr_t)at < (uintptr_t)(lens_out + entries) &&
+           (uintptr_t)lens_out < (uintptr_t)(at + n);
+  };
+  if ((lens != lens_out && over_lens_out(lens, entries)) ||
+      over_lens_out(kept, (long long)max_kept * desc->batch) ||
+      over_lens_out(seq_starts, desc->batch + 1LL))
+    return RIPPLE_EINVAL;
   p.g.page_stride *= bytes;
   p.g.head_stride *= bytes;
   p.g.row_stride *= bytes;
