@@ -458,6 +458,8 @@ class PagedCache:
             raise ValueError("k_pages and v_pages must be [n_pages][Hkv][page_size][d], alike")
         if k_pages.stride(3) != 1:
             raise ValueError("the dims of a cache row must be consecutive")
+        if k_pages[..., 0].numel() > 1 and not any(k_pages.stride()[:3]):
+            raise ValueError("k_pages and v_pages must have a place for every row")
         if block_table.dim() != 2 or block_table.dtype != torch.int32:
             raise ValueError("block_table must be int32 [B][max_pages]")
         n_pages, H, ps, d = k_pages.shape
