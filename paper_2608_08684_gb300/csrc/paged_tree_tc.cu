@@ -86,6 +86,9 @@ struct Told {
   uint64_t draft_done[kDrafts];        // by parts with drafted tokens (values may be parts ahead)
   unsigned long long bad[kDrafts];     // drafted tokens whose values are not all finite, by parts
   unsigned long long present[kSlots];  // rows of a block that are there
+  // (among the softmax's warps) what the values of a part have in a quarter of the dims that is not
+  // finite: 1: infinity, 2: -infinity, 4: NaN
+  uint32_t not_finite[32];
 };
 template <>
 struct Told<true> {
@@ -834,8 +837,9 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
       if (lane == 0) mbar_arrive(&sy->q_full);
       row_scale = scale;
     };
-    // Whether no warp of the four has given up: before barriers that all of them have to reach.
-    auto none_gave_up = [&](bool mine) {
+    // A barrier of the team's four warps, and whether all of their threads say so. (That none has given
+    // up, before barriers that all of them have to reach.)
+    auto all_say = [&](bool mine) {
       int all;
       asm volatile(
           "{\n .reg .pred p, q;\n setp.ne.b32 q, %1, 0;\n"
@@ -879,26 +883,45 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           }
         }
       };
-      // For four outputs from dim d0 on, those that are NaN: the sum of the values that are not
-      // finite over the part's rows before the draft; others stay.
-      auto add_not_finite = [&](int d0, float (&o)[4]) {
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        const int end = (int)min((long long)w.end, seq.prefix);
-        for (int row = w.begin; row < end; ++row) {
-          const int page = p.table[guard((long long)w.b * p.g.max_pages + (row >> p.g.shift), 1,
-                                         (long long)p.g.B * p.g.max_pages, p.status)];
-          if ((unsigned)page >= (unsigned)p.g.n_pages) continue;
-          const uint2 u = *reinterpret_cast<const uint2 *>(
-              (const __nv_bfloat16 *)p.v_pages + page * p.g.page_stride + w.h * p.g.head_stride +
-              (row & ((1 << p.g.shift) - 1)) * p.g.row_stride + d0);
-          const uint32_t bits[4] = {u.x << 16, u.x & 0xffff0000u, u.y << 16, u.y & 0xffff0000u};
+      // told.not_finite for the dims from d0 on, by the team's 128 threads: over the part's rows before
+      // the draft, 16 bytes' quarter (four dims) of every 128 / pieces-th row a thread.
+      auto find_not_finite = [&](int d0, int pieces) {
+        if constexpr (!kCodes) {
+          if (tid < 4 * pieces) sy->told.not_finite[tid] = 0;
+          named_bar_sync(1 + team, 128);
+          const int pc = tid % pieces, step = 128 / pieces;
+          const int end = (int)min((long long)w.end, seq.prefix);
+          uint32_t found[4] = {0, 0, 0, 0};
+#pragma unroll 1
+          for (int row = w.begin + tid / pieces; row < end; row += step) {
+            const int page = p.table[guard((long long)w.b * p.g.max_pages + (row >> p.g.shift), 1,
+                                           (long long)p.g.B * p.g.max_pages, p.status)];
+            if ((unsigned)page >= (unsigned)p.g.n_pages) continue;
+            const uint2 u = *reinterpret_cast<const uint2 *>(
+                (const __nv_bfloat16 *)p.v_pages + page * p.g.page_stride + w.h * p.g.head_stride +
+                (row & ((1 << p.g.shift) - 1)) * p.g.row_stride + d0 + 4 * pc);
+            const uint32_t bits[4] = {u.x << 16, u.x & 0xffff0000u, u.y << 16, u.y & 0xffff0000u};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if ((bits[i] & 0x7f800000u) == 0x7f800000u)
+                found[i] |= (bits[i] & 0x7fffffu) != 0 ? 4 : bits[i] >> 31 ? 2 : 1;
+          }
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if ((bits[i] & 0x7f800000u) == 0x7f800000u) sum[i] += __uint_as_float(bits[i]);
+            if (found[i] != 0) atomicOr(&sy->told.not_finite[4 * pc + i], found[i]);
+          named_bar_sync(1 + team, 128);
         }
+      };
+      // Of four outputs of that quarter, from its dim d on, those that are NaN: the sum of what the
+      // values have that is not finite; others stay.
+      auto put_not_finite = [&](int d, float (&o)[4]) {
+        if constexpr (!kCodes) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (o[i] != o[i] && sum[i] != 0.f) o[i] = sum[i];
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t has = sy->told.not_finite[d + i];
+            if (o[i] != o[i] && (has == 1 || has == 2)) o[i] = has == 1 ? INFINITY : -INFINITY;
+          }
+        }
       };
       // m: what the probabilities are relative to, a maximum, in log2. ew (8-bit pages): of their
       // products with the values' scales, over m; the largest is held as 2^kTop or up to 2^kSlack more
@@ -1082,7 +1105,7 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
         }
       }
       // (a wait can end well for one warp and badly for another)
-      if constexpr (C > 1) ok = none_gave_up(ok);
+      if constexpr (C > 1) ok = all_say(ok);
       if (!ok) break;
       tc_fence_after();
       const float o_scale = kCodes ? pow2((int)(ew - kTop)) : 1.f;
@@ -1156,32 +1179,41 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
                 make_float4(__uint_as_float(u[4 * i]) * f, __uint_as_float(u[4 * i + 1]) * f,
                             __uint_as_float(u[4 * i + 2]) * f, __uint_as_float(u[4 * i + 3]) * f);
           named_bar_sync(1 + team, 128);
-          for (int e = tid; e < n_rows * CP; e += 128) {
-            const int i = e / CP, pc = e % CP;
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+          // A value before the draft that is not finite makes a NaN of the copies that do not have
+          // its key (0 times it): then the outputs are the sum of what is not finite (if the
+          // probabilities are numbers). What that is takes a look at all of the part's values, once
+          // for all rows, and a second time over the outputs.
+#pragma unroll 1
+          for (int look = 0; look < 2; ++look) {
+            bool nan = false;
+            for (int e = tid; e < n_rows * CP; e += 128) {
+              const int i = e / CP, pc = e % CP;
+              float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int k = 0; k < C; ++k) {
-              const int row = k * RT + i;
-              const float4 y =
-                  *reinterpret_cast<const float4 *>(stage + row * CD * 4 + ((pc ^ (row & (CP - 1))) << 4));
-              x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+              for (int k = 0; k < C; ++k) {
+                const int row = k * RT + i;
+                const float4 y =
+                    *reinterpret_cast<const float4 *>(stage + row * CD * 4 + ((pc ^ (row & (CP - 1))) << 4));
+                x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+              }
+              const float inv = sy->inv[i];
+              float o[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
+              if (!kCodes && inv == inv && !((x.x + x.y) + (x.z + x.w) == (x.x + x.y) + (x.z + x.w))) {
+                nan = true;
+                if (look > 0) put_not_finite(4 * pc, o);
+              }
+              if (!kCodes && bad != 0) {
+                const int tok = token_of(i);
+                const unsigned long long sees =
+                    p.masks == nullptr ? ~0ull >> (63 - tok) : p.masks[seq.first + tok];
+                if ((bad & sees) != 0) add_bad(bad & sees, c + 4 * pc, o, 4);
+              }
+              put(i, sy->out_row[i] + (long long)seq.first * p.Hq, c + 4 * pc, make_float4(o[0], o[1], o[2], o[3]));
             }
-            const float inv = sy->inv[i];
-            float o[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
-            // A value before the draft that is not finite makes a NaN of the copies that do not
-            // have its key (0 times it): then the outputs are the sum of what is not finite
-            // (if the probabilities are numbers)
-            if (!kCodes && inv == inv && !((x.x + x.y) + (x.z + x.w) == (x.x + x.y) + (x.z + x.w)))
-              add_not_finite(c + 4 * pc, o);
-            if (!kCodes && bad != 0) {
-              const int tok = token_of(i);
-              const unsigned long long sees =
-                  p.masks == nullptr ? ~0ull >> (63 - tok) : p.masks[seq.first + tok];
-              if ((bad & sees) != 0) add_bad(bad & sees, c + 4 * pc, o, 4);
-            }
-            put(i, sy->out_row[i] + (long long)seq.first * p.Hq, c + 4 * pc, make_float4(o[0], o[1], o[2], o[3]));
+            // (a barrier too: the stage has been read)
+            if (all_say(!nan) || look > 0) break;
+            find_not_finite(c, CP);
           }
-          named_bar_sync(1 + team, 128);
         }
         fence_proxy_async_smem();  // (the stage is written by TMA next)
         named_bar_sync(1 + team, 128);

@@ -25,8 +25,12 @@ def test_softmax_warps_agree_before_the_copies_join():
     # all four have to reach, and no wait stands between those
     code = _code("paged_tree_tc.cu")
     part = code[code.index("} else if (warp == 4) {"):]
-    agree = part.index("if constexpr (C > 1) ok = none_gave_up(ok);")
+    agree = part.index("if constexpr (C > 1) ok = all_say(ok);")
     assert part[agree:].split("\n", 2)[1].strip() == "if (!ok) break;"
     join = part[agree:part.index("cta_warp == 8) tmem_dealloc")]
     assert "named_bar_sync(1 + team, 128)" in join and "wait_for(" not in join
-    assert "named_bar_sync(1 + team" not in part[:agree]
+    # (what looks for values that are not finite is called from the join)
+    helper = part.index("auto find_not_finite")
+    before = part[:helper] + part[part.index("auto put_not_finite"):agree]
+    assert "named_bar_sync(1 + team" not in before and "find_not_finite(" not in before
+    assert "find_not_finite(c, CP);" in join
