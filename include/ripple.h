@@ -672,8 +672,8 @@ ripple_status ripple_paged_tree_attn(const ripple_paged_desc *desc,
  *                seq_starts
  * Rows whose page entry is out of range, and a draft with more tokens than rows or with
  * descending seq_starts (lens_out is then lens), are reported as RIPPLE_EBOUNDS and not
- * moved, rows behind max_pages * page_size as RIPPLE_EFULL. One launch; no workspace. The call may be captured
- * in a CUDA graph.
+ * moved, rows behind max_pages * page_size as RIPPLE_EFULL. One launch; no workspace. The call may
+ * be captured in a CUDA graph.
  * Errors: RIPPLE_EINVAL, RIPPLE_ECUDA.
  */
 ripple_status ripple_paged_keep_rows(const ripple_paged_desc *desc,

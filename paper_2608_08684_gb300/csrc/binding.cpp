@@ -158,8 +158,8 @@ PyObject *cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return o;
 }
 
-// paged_append(entry (of the cache's kind: 8-bit pages have one of their own), cache, rope address or None, lens, k, v, positions, seq_starts, q, q_out,
-// dev_status, stream)
+// paged_append(entry (of the cache's kind: 8-bit pages have one of their own), cache, rope address or
+// None, lens, k, v, positions, seq_starts, q, q_out, dev_status, stream)
 PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!args_are(n, 12)) return nullptr;
   return guarded([&] {
@@ -420,7 +420,8 @@ PyObject *paged_keep_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
       need(tokens >= 0 && tokens <= 0x7fffffff / B, "bad number of drafted tokens");
       tokens *= B;
     }
-    const int32_t *starts = dense<int32_t>(a[5], t->device, at::kInt, "seq_starts must be int32 [B + 1]", B + 1);
+    const int32_t *starts = dense<int32_t>(a[5], t->device, at::kInt,
+                                           "seq_starts must be int32 [B + 1]", B + 1);
     int32_t *status = dense<int32_t>(a[7], t->device, at::kInt, "dev_status must be int32");
     void *stream = stream_of(a[8]);
     ripple_status s;

@@ -401,7 +401,8 @@ bool row_set(const TokenRows &t, const AppendParams &p, int heads, int elem, Row
 
 // scales: NULL for pages in desc->dtype.
 ripple_status append(
-    const ripple_paged_desc *desc, const ripple_paged_scales *scales, const ripple_rope *rope, int32_t n_tokens,
+    const ripple_paged_desc *desc, const ripple_paged_scales *scales, const ripple_rope *rope,
+    int32_t n_tokens,
     const int32_t *seq_starts, int32_t n_q_heads, const void *q,
     const ripple_token_strides *q_strides, void *q_out, const ripple_token_strides *q_out_strides,
     const void *k, const ripple_token_strides *k_strides, const void *v,
@@ -410,7 +411,8 @@ ripple_status append(
   AppendParams p;
   const bool codes = scales != nullptr;
   p.sc = ScaleGeom{};
-  if (!paged_geom(desc, &p.g, codes) || (codes && !scale_geom(desc, scales, &p.sc)) || n_tokens < 0) return RIPPLE_EINVAL;
+  if (!paged_geom(desc, &p.g, codes) || (codes && !scale_geom(desc, scales, &p.sc)) || n_tokens < 0)
+    return RIPPLE_EINVAL;
   if (seq_starts == nullptr && n_tokens % desc->batch != 0) return RIPPLE_EINVAL;
   if ((q == nullptr) != (q_out == nullptr)) return RIPPLE_EINVAL;
   p.rot = 0;
@@ -509,7 +511,8 @@ extern "C" ripple_status ripple_paged_append(
 }
 
 extern "C" ripple_status ripple_paged_append_q8(
-    const ripple_paged_desc *desc, const ripple_paged_scales *scales, const ripple_rope *rope, int32_t n_tokens,
+    const ripple_paged_desc *desc, const ripple_paged_scales *scales, const ripple_rope *rope,
+    int32_t n_tokens,
     const int32_t *seq_starts, int32_t n_q_heads, const void *q,
     const ripple_token_strides *q_strides, void *q_out, const ripple_token_strides *q_out_strides,
     const void *k, const ripple_token_strides *k_strides, const void *v,

@@ -12,10 +12,12 @@
 //  - probability and value scale together, 2^(x_r + e_r), are taken relative to their own
 //    running maximum, not the scores', times 2^14, in two fp16 parts: 22 bits, and at most
 //    2^-39 of the largest lost where they are tiny.
-// The sum of the probabilities has the scores' maximum, in fp32.
-// Measured, D 128, 8 KV heads, 4 heads each: 64 sequences of 64 to 32768 rows (622 MB) 104.5 us, 5.95 TB/s
-// (88% of the copy rate; bf16 pages 151); one of 470 rows 5.4 us. fp32 queries, 7 on each of 4 KV
-// heads of 64, 9 sequences of up to 60000 rows 33 us, the chain of a block's two products and softmax.
+// The sum of the probabilities has the scores' maximum, in fp32, and the products' reference is
+// relative to that: there is none before the first score.
+// Measured, D 128, 8 KV heads, 4 heads each: 64 sequences of 64 to 32768 rows (622 MB) 105 us,
+// 5.9 TB/s (87% of the copy rate; bf16 pages 151); one of 470 rows 5.5 us. fp32 queries, 7 on each
+// of 4 KV heads of 64, 9 sequences of up to 60000 rows 33 us, the chain of a block's two products
+// and softmax.
 #include <cuda_fp16.h>
 
 #include "paged_decode.cuh"

@@ -47,7 +47,8 @@ struct Piece<uint8_t> {
       float x[4];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i] >> (16 * j)), __NV_E4M3);
+        const __half2_raw h =
+            __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i] >> (16 * j)), __NV_E4M3);
         const float2 f = __half22float2(__half2(h));
         x[2 * j] = f.x * scale;
         x[2 * j + 1] = f.y * scale;
@@ -482,11 +483,13 @@ size_t plan(TreeParams *p, int dtype, int sms, void *ws) {
 
 // Shares of a group on the tensor cores where the table's room is short, 0 where it is not: as
 // many teams as find a place at once, at most one a block, with few blocks each; their partials
-// fit where the runs' would. Shares and runs (us, D 128, 8 KV heads, 4 heads each, 4 tokens; runs have
-// a second launch and sums over the sequences): 16 sequences of 100 to 1000 rows 20.2 and 19.0, 32 of 60
-// to 200 15.5 and 21.1, one of 900 15.6 and 14.9, of 4000 19.8 and 21.5, of 8000 25.0 and 25.2, 4 of 2000
-// 19.2 and 20.1; 8-bit pages, 16 tokens: one of 900 21.6 and 18.6, of 8000 33.8 and 30.0, 32 of 64 rows
-// 21.4 and 33.8.
+// fit where the runs' would. Shares and runs (us, D 128, 8 KV heads, 4 heads each, 4 tokens; runs
+// have a second launch and sums over the sequences): 16 sequences of 100 to 1000 rows 19.4 and 19.3,
+// 32 of 60 to 200 14.1 and 18.2, one of 900 14.4 and 14.3, of 4000 19.1 and 19.0, of 8000 24.5 and
+// 23.0, 4 of 2000 17.6 and 20.1. 8-bit pages, 16 tokens: 16 of 100 to 1000 rows 28.0 and 27.8, 4 of
+// 2000 22.4 and 26.9, 32 of 64 15.5 and 21.7, but one of 900 18.8 and 16.8, of 8000 32.0 and 27.5.
+// (Shares gain with several sequences, up to a third; one long sequence alone loses by a tenth, most
+// over 8-bit pages.)
 constexpr int kMostTeams = 16;  // (a cluster of 8)
 constexpr int kShortBlocks = 8;
 int short_teams(const TreeParams &p, int sms) {
@@ -574,11 +577,8 @@ extern "C" ripple_status ripple_paged_tree_attn(
   const bool d128 = desc->head_dim == 128;
   if (desc->dtype == RIPPLE_BF16) {
     p.teams = short_teams(p, sm_count(dev));
-    if (p.teams > 0) {
-      RIPPLE_CUDA_TRY(launch_tree_tc(p, scales != nullptr, dev, sm_count(dev), st));
-      return RIPPLE_OK;
-    }
     RIPPLE_CUDA_TRY(launch_tree_tc(p, scales != nullptr, dev, sm_count(dev), st));
+    if (p.teams > 0) return RIPPLE_OK;
     RIPPLE_CUDA_TRY((d128 ? launch_join<__nv_bfloat16, 128, false>(p, st)
                           : launch_join<__nv_bfloat16, 64, false>(p, st)));
     return RIPPLE_OK;

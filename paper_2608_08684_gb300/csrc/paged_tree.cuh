@@ -3,9 +3,10 @@
 //
 // Work: the cache rows of every (sequence, KV head) group are cut into blocks, and the
 // blocks of all groups, in order, into runs of equal cost: a group's first block costs kGroupCost
-// more (its queries, its outputs), in units of a block that begin the group. The queries of a group, n_b tokens times
-// G heads, are rows of tiles; a CTA takes a run for one row tile, and the CTAs of a run's
-// tiles are neighbours, so that they read the same rows from L2 at about the same time.
+// more (its queries, its outputs), in units of a block that begin the group. The queries of a
+// group, n_b tokens times G heads, are rows of tiles; a CTA takes a run for one row tile, and the
+// CTAs of a run's tiles are neighbours, so that they read the same rows from L2 at about the same
+// time.
 // Lengths are read on the device; every CTA finds its run by a sum over the sequences. A
 // group that lies in one run is written there; of the others every run leaves a partial
 // (a run has two at most: of the group it begins within and of the one it ends within),

@@ -1,31 +1,35 @@
 // ripple_paged_tree_attn for bf16 queries, on the 5th-generation tensor cores.
 //
-// A team of 7 warps (two in a CTA, one CTA an SM) has the 128 rows of a matrix product for up to
-// 128 query rows of a KV head and takes its run's blocks of 64 keys: S = Q . K^T (128 x 64) into
-// TMEM, softmax by a thread a row, P back into TMEM over S, O += P . V (128 x d) in TMEM. A
-// draft of n tokens with G heads a KV head has n G query rows. With 32 of them or fewer the
-// product's rows hold four copies, with 64 two, and every copy takes its share of a block's keys
-// (the others' probabilities are 0), so that the four softmax warps share the work however few
-// rows there are; the copies are joined when a group is done. The products' rows cost nothing
-// that the cache's bytes do not: a block is 32 KB, 1400 cycles of an SM's share of HBM, and 512 of
-// its tensor cores.
+// A team of 7 warps (9 over 8-bit pages; two teams a CTA, one CTA an SM) has the 128 rows of a
+// matrix product for up to 128 query rows of a KV head and takes its run's blocks of 64 keys:
+// S = Q . K^T (128 x 64) into TMEM, softmax by a thread a row, P back into TMEM over S, O += P . V
+// (128 x d) in TMEM. A draft of n tokens with G heads a KV head has n G query rows. With 32 of them
+// or fewer the product's rows hold four copies, with 64 two, and every copy takes its share of a
+// block's keys (the others' probabilities are 0), so that the four softmax warps share the work
+// however few rows there are; the copies are joined when a group is done. The products' rows cost
+// nothing that the cache's bytes do not: a block is 32 KB, 1400 cycles of an SM's share of HBM, and
+// 512 of its tensor cores.
 //
 // Of a team, 4 warps: queries, softmax and outputs; one issues the MMAs; one fetches keys, one
-// values: a block by TMA (a box a page, with the 128-byte swizzle that the MMAs read), or,
-// where rows of it are missing or pages have fewer than 8, by 16-byte copies to the same
-// places. Scores of the next block are on their way while a block's softmax runs; S and P of
+// values (8-bit pages: two each): a block by TMA (a box a page, with the 128-byte swizzle that the
+// MMAs read), or, where rows of it are missing or pages have fewer than 8, by 16-byte copies to the
+// same places. Scores of the next block are on their way while a block's softmax runs; S and P of
 // two blocks and O fill half of the TMEM. The teams share nothing: one's softmax runs while the
 // other's blocks are on their way. (Two CTAs of one team each do not find a place on an SM at
 // the same time, though registers, shared memory and TMEM have room.)
 //
+// A wait that runs out ends the call: its role and then the others leave, the softmax warps of a
+// team together, each fetching warp once what it issued has landed.
+//
 // Measured, D 128, 8 KV heads: 48 sequences of up to 32768 rows, 2 to 12 tokens of 32 heads 163 us
-// (1.01 GB, 91% of the copy rate; with one team a CTA and no copies of the query rows 285); 3 of about
-// 31000 rows with 64 tokens of 64 heads 193 us (196 GFLOP, 1.02 PFLOP/s): there the chain scores -
-// softmax - product of a block, two of them an SM, leaves the tensor pipe half idle; 8-bit pages,
-// 32 sequences of up to 32768 rows, 16 tokens 172 us (419 MB, 36%): bound by the fetching warps'
-// instructions (of a block's 3500 cycles their loads, scales and tables take 1250, the widening 950;
-// 96 registers a thread, of which the instances spill 200 bytes). One sequence of 900 rows and 4 tokens 14.0 us: the launch, lengths, table, queries,
-// two blocks, the join of the copies and of the shares, one after the other.
+// (1.01 GB, 91% of the copy rate; with one team a CTA and no copies of the query rows 285); 3 of
+// about 31000 rows with 64 tokens of 64 heads 191 us (196 GFLOP, 1.03 PFLOP/s): there the chain
+// scores - softmax - product of a block, two of them an SM, leaves the tensor pipe half idle (and
+// 128 registers a thread are not enough: 180 bytes spilt); 8-bit pages, 32 sequences of up to 32768
+// rows, 16 tokens 172 us (419 MB, 36%): bound by the fetching warps' instructions (of a block's 3500
+// cycles their loads, scales and tables take 1250, the widening 950; 18 warps leave 96 registers a
+// thread, 110 to 240 bytes spilt). One sequence of 900 rows and 4 tokens 14.4 us: the launch,
+// lengths, table, queries, two blocks, the join of the copies and of the shares, one after the other.
 //
 // P in one bf16 part: the output is rounded to bf16 as well, and a probability's rounding
 // (2^-8) enters the output as part of a mean. The sum is of the unrounded ones, in fp32.
@@ -284,7 +288,8 @@ __device__ __forceinline__ void widen(const uint4 &u, uint16_t factor, uint32_t 
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i / 2] >> (16 * (i & 1))), __NV_E4M3);
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(
+        (__nv_fp8x2_storage_t)(w[i / 2] >> (16 * (i & 1))), __NV_E4M3);
     const __half2 x = __hmul2(__half2(h), scale);
     o[i] = *reinterpret_cast<const uint32_t *>(&x);
   }
@@ -409,7 +414,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
         __syncwarp();
         // a lane a page: the entry of its first row
         const int boxes = KB / box, first = lane * box;
-        const int e0 = __shfl_sync(kAll, entry[0], first & 31), e1 = __shfl_sync(kAll, entry[1], first & 31);
+        const int e0 = __shfl_sync(kAll, entry[0], first & 31);
+        const int e1 = __shfl_sync(kAll, entry[1], first & 31);
         if (lane < boxes) {
           const int page = first < 32 ? e0 : e1, slot = (row0 + first) & (page_rows - 1);
           if constexpr (kCodes) {
@@ -450,7 +456,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
     // (8-bit pages have their own way: Told<true>::nan)
     auto tell_bad = [&]() {
       if constexpr (!kCodes) {
-        const uint32_t lo = __reduce_or_sync(kAll, (uint32_t)bad), hi = __reduce_or_sync(kAll, (uint32_t)(bad >> 32));
+        const uint32_t lo = __reduce_or_sync(kAll, (uint32_t)bad);
+        const uint32_t hi = __reduce_or_sync(kAll, (uint32_t)(bad >> 32));
         if (lane == 0) sy->told.bad[drafts % kDrafts] = (unsigned long long)hi << 32 | lo;
         bad = 0;
         mbar_arrive(&sy->told.draft_done[drafts % kDrafts]);
@@ -776,7 +783,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
     auto fetch_queries = [&](const W &w, const TreeSeq &seq) {
       constexpr int kQPieces = D / 8, kAtOnce = 32 / kQPieces, kSteps = 32 / kAtOnce;
       const int n_rows = min(seq.tokens * p.G - tile * RT, RT);
-      const int mine = tile * RT + (r < n_rows ? r : 0), tok = mine / p.G, head = w.h * p.G + mine - tok * p.G;
+      const int mine = tile * RT + (r < n_rows ? r : 0), tok = mine / p.G;
+      const int head = w.h * p.G + mine - tok * p.G;
       // where the thread's own row lies (-1: it is none)
       const long long at = r < n_rows ? head * p.q_head + (p.starts == nullptr
                                                                ? w.b * p.q_seq + tok * p.q_token
@@ -805,7 +813,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
           for (int i = 0; i < kAt; ++i) {
             const long long from = __shfl_sync(kAll, at, (i0 + i) * kAtOnce + sub);
             x[i] = make_uint4(0, 0, 0, 0);
-            if (from >= 0) x[i] = __ldg(reinterpret_cast<const uint4 *>((const __nv_bfloat16 *)p.q + from) + pc);
+            if (from >= 0)
+              x[i] = __ldg(reinterpret_cast<const uint4 *>((const __nv_bfloat16 *)p.q + from) + pc);
           }
 #pragma unroll
           for (int i = 0; i < kAt; ++i) {
@@ -1142,7 +1151,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
             for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(u[i]) * inv;
             if (!kCodes && (bad & mask) != 0) add_bad(bad & mask, c, o, 32);
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) put(r, at, c + i, make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
+            for (int i = 0; i < 32; i += 4)
+              put(r, at, c + i, make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
           }
           if (live) put_stats(r, m, l);
         }
@@ -1192,8 +1202,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
 #pragma unroll
               for (int k = 0; k < C; ++k) {
                 const int row = k * RT + i;
-                const float4 y =
-                    *reinterpret_cast<const float4 *>(stage + row * CD * 4 + ((pc ^ (row & (CP - 1))) << 4));
+                const float4 y = *reinterpret_cast<const float4 *>(
+                    stage + row * CD * 4 + ((pc ^ (row & (CP - 1))) << 4));
                 x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
               }
               const float inv = sy->inv[i];
@@ -1208,7 +1218,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
                     p.masks == nullptr ? ~0ull >> (63 - tok) : p.masks[seq.first + tok];
                 if ((bad & sees) != 0) add_bad(bad & sees, c + 4 * pc, o, 4);
               }
-              put(i, sy->out_row[i] + (long long)seq.first * p.Hq, c + 4 * pc, make_float4(o[0], o[1], o[2], o[3]));
+              put(i, sy->out_row[i] + (long long)seq.first * p.Hq, c + 4 * pc,
+                  make_float4(o[0], o[1], o[2], o[3]));
             }
             // (a barrier too: the stage has been read)
             if (all_say(!nan) || look > 0) break;
@@ -1236,7 +1247,8 @@ __global__ void __launch_bounds__(threads(kCodes), 1)
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
   }
   const int members = teams > 1 ? teams / kTeams * threads(kCodes) : threads(kCodes);
-  const int me = teams > 1 ? (int)blockIdx.x % (teams / kTeams) * threads(kCodes) + threadIdx.x : threadIdx.x;
+  const int me =
+      threadIdx.x + (teams > 1 ? (int)blockIdx.x % (teams / kTeams) * threads(kCodes) : 0);
   for (int g = 0; g < (teams > 1 ? 1 : kTeams); ++g) {
     const int group = teams > 1 ? work / teams : (int)(blockIdx.x + g * gridDim.x);
     if (group >= p.g.B * p.g.Hkv) break;

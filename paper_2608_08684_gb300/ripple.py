@@ -518,8 +518,9 @@ def ripple_paged_append(cache: PagedCache, lens, k, v, rope: Rope | None = None,
     with the query heads; any strides with the dims consecutive. lens (int32 [B]) counts the
     new tokens; positions: int32, k's leading sizes, or None (a token's cache row). 8-bit pages:
     ripple_paged_append_q8."""
-    st = _binding.paged_append(_paged_append[cache.codes], cache._handle, None if rope is None else rope._addr,
-                               lens, k, v, positions, seq_starts, q, q_out, dev_status,
+    st = _binding.paged_append(_paged_append[cache.codes], cache._handle,
+                               None if rope is None else rope._addr, lens, k, v, positions,
+                               seq_starts, q, q_out, dev_status,
                                None if stream is None else _stream(stream))
     if st != OK:
         raise RippleError(st, "ripple_paged_append")
