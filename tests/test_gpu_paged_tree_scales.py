@@ -142,3 +142,48 @@ def test_keys_of_far_scales_beside_others(lib, n, G, kind):
         want, want_lse, size64 = P8.tree_ref(pool, q.reshape(n, G, d), [rows], [n], None)
         assert (np.abs(out[0].double().cpu().numpy() - want) <= F.bound(kind, 64.0, size64, want)).all()
         assert np.abs(lse[0].double().cpu().numpy() - want_lse).max() <= 1e-4 + 2.0 ** -21 * 64
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page,layout", [(1, "rows"), (8, "heads"), (64, "rows"), (1024, "heads")])
+@pytest.mark.parametrize("G,most", [(2, 16), (4, 16), (7, 64)])
+def test_scales_far_apart_among_rows_that_are_none(lib, G, most, page, layout, d, kind):
+    # rows of any scale beside hidden rows held as NaN, entries that are no page, rows behind the
+    # length; over tables with room for little and for much
+    H, rng = 3, np.random.default_rng(page + d)
+    counts = [int(n) for n in rng.integers(1, most + 1, 12)]
+    rows = [n + int(rng.integers(0, 900)) for n in counts]
+    bits = P8.random_masks(counts, 91)
+    for width in (0, 8192 // page):
+        pool = P8.any_pool(lib, kind, rows, H, d, page, 90, layout, width=width)
+        shape = tuple(pool.vs.shape)
+        pool.vs.copy_(torch.from_numpy(rng.integers(87, 168, shape)).to(DEV))
+        pool.ks.copy_(torch.from_numpy(118 + rng.integers(-30, 2, shape)).to(DEV))
+        missing, hide, t0 = set(), [], 0
+        masks = list(bits)
+        for b, (n, m) in enumerate(zip(rows, counts)):
+            if b % 3 == 0 and n - m > 2 * page:  # an entry before the draft
+                at = int(rng.integers(0, (n - m) // page - 1))
+                pool.table[b, at] = -1
+                missing |= {(b, r) for r in range(at * page, min((at + 1) * page, n - m))}
+            if m > 2:  # a drafted token that no other sees
+                j = int(rng.integers(1, m))
+                p, s = pool.place(b, n - m + j)
+                (pool.vs if b % 2 else pool.ks)[p, :, s] = 255
+                hide.append(t0 + j)
+                for i in range(m):
+                    masks[t0 + i] &= ~(1 << j)
+                masks[t0 + j] |= 1 << j
+            t0 += m
+        q = P.randn((sum(counts), H * G, d), P8.type_of(kind), 93)
+        starts = P.i32([0] + np.cumsum(counts).tolist())
+        out, lse, st = P8.run_tree(lib, pool, q, P.i32(rows), P8.to_i64(masks), starts, most)
+        assert int(st.item()) == (lib.EBOUNDS if missing else 0)
+        want, want_lse, size = P8.tree_ref(pool, q, rows, counts, masks, missing=missing)
+        got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+        rest = [i for i in range(sum(counts)) if i not in hide]
+        assert np.isfinite(want[rest]).all()
+        assert (np.abs(got - want) <= F.bound(kind, 64.0, size, want))[rest].all()
+        assert (np.abs(got_lse - want_lse)[rest] <= 1e-4 + 2.0 ** -21 * 64).all()
+        assert np.isnan(got[hide]).all() and (np.isnan(got_lse) == np.isnan(want_lse)).all()
